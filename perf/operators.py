@@ -1,0 +1,332 @@
+"""Performance cases of the key/value cache operators: what one step of an inference engine asks of them.
+
+The knobs that this framework tunes (block size, most requests and most tokens per step, chunked prefill) decide three
+operations of the engine's step, and these are measured here:
+
+  assign  blocks, block tables, positions and cache slots of a step's tokens, from the requests' lengths
+  write   the step's keys and values into the paged cache, as they are or in 8 bits
+  attend  attention of the step's tokens (whole prompts, chunks of prompts, single tokens) over the paged cache
+
+Block sizes and step sizes are those of the engine space in workloads/synth.py (blocks of 8, 16 and 32 tokens, 64 to 8192
+requests and tokens per step, a model length of 4096) and beyond it what long prompts bring.  Lengths are a function of the
+case; values and the order of the blocks are a function of the seed.
+"""
+import math
+import random
+
+import torch
+
+own = False
+
+DEV = "cuda:0"
+TYPES = {"f16": torch.float16, "bf16": torch.bfloat16, "f8": torch.float8_e4m3fn}
+BYTES = {"f16": 2, "bf16": 2, "f8": 1}
+F8_MAX = 448.0  # largest finite value of the 8-bit type
+
+
+def _case(name, kind, dtype="bf16", cache="", hq=32, hkv=8, d=128, block=16, decodes=0, chunks=0, chunk=0, ctx=0, window=0,
+          short=False):
+    """``decodes`` requests with one new token, ``chunks`` with up to ``chunk`` new ones; contexts of up to ``ctx`` tokens."""
+    return dict(name=name, kind=kind, dtype=dtype, cache=cache or dtype, hq=hq, hkv=hkv, d=d, block=block, decodes=decodes,
+                chunks=chunks, chunk=chunk, ctx=ctx, window=window, short=short)
+
+
+def listed():
+    return [
+        # The step of a lightly loaded engine: 64 requests (the space's lower bound), a token each.
+        _case("assign_decode", "assign", decodes=64, ctx=4095),
+        # A full step of chunked prefill: prompt chunks beside decoding requests, short of free blocks at its end.
+        _case("assign_mixed", "assign", block=8, decodes=1019, chunks=23, chunk=512, ctx=4095, short=True),
+        # The most requests of the space, each with a chunk.
+        _case("assign_large", "assign", block=32, chunks=8192, chunk=24, ctx=4000),
+        # A decoding step's keys and values: single tokens, each to a place of its own.
+        _case("write_decode", "write", decodes=256, ctx=4095),
+        # A full step of 8192 prompt tokens, keys and values still inside the fused projection's rows.
+        _case("write_chunk", "write", block=32, chunks=3, chunk=3000, ctx=1000),
+        # A long prompt into an 8-bit cache; odd numbers of tokens and heads.
+        _case("write_f8", "write", dtype="f16", cache="f8", hq=15, hkv=5, d=64, block=8, decodes=77, chunks=2, chunk=32768, ctx=501),
+        # One user waits for the next token: the smallest call, latency alone.
+        _case("attend_one", "attend", decodes=1, ctx=1000),
+        # A decoding step of a loaded engine, ragged contexts up to the model length.
+        _case("attend_decode", "attend", decodes=256, ctx=4095),
+        # Decoding with long contexts out of an 8-bit cache.
+        _case("attend_decode_f8", "attend", cache="f8", hq=64, decodes=48, ctx=32767, block=32),
+        # A step of chunked prefill: prompt chunks beside decoding requests, seven query heads to a key head.
+        _case("attend_mixed", "attend", dtype="f16", hq=28, hkv=4, block=8, decodes=61, chunks=3, chunk=700, ctx=3395),
+        # Whole prompts of the model length.
+        _case("attend_prefill", "attend", chunks=4, chunk=4096),
+        # A late chunk of a long prompt.
+        _case("attend_long", "attend", d=64, chunks=1, chunk=1024, ctx=65536 - 1024),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return min(hi, max(lo, round(math.exp(rng.uniform(math.log(lo), math.log(hi))))))
+
+
+def draw(rng):
+    kind = rng.choice(["assign", "write", "attend", "attend", "attend"])
+    hq, hkv, d = rng.choice([(32, 8, 128), (28, 4, 128), (16, 16, 64), (15, 5, 64), (8, 1, 256), (64, 8, 128), (12, 4, 192),
+                             (8, 8, 128)])
+    dtype = rng.choice(["bf16", "f16"])
+    cache = rng.choice([dtype, dtype, "f8"])
+    block = rng.choice([8, 16, 32])
+    more = dict(kind=kind, dtype=dtype, cache=cache, hq=hq, hkv=hkv, d=d, block=block)
+    if kind == "assign":
+        c = _case(None, decodes=_log_int(rng, 1, 4096), chunks=_log_int(rng, 1, 4096), chunk=_log_int(rng, 2, 24),
+                  ctx=_log_int(rng, 1, 4000), short=rng.random() < 0.25, **more)
+    elif kind == "write":
+        c = _case(None, decodes=rng.choice([0, _log_int(rng, 1, 2000)]), chunks=rng.randint(1, 3),
+                  chunk=_log_int(rng, 1, 8192), ctx=_log_int(rng, 1, 2000), **more)
+    else:
+        form = rng.choice(["decode", "chunk", "mixed"])
+        ctx = _log_int(rng, 1, 32767)
+        fit = max(1, min(256, 2 ** 20 // (ctx + 1)))
+        decodes = 0 if form == "chunk" else _log_int(rng, 1, fit)
+        chunks = 0 if form == "decode" else rng.randint(1, 3)
+        chunk = _log_int(rng, 2, min(2048, max(2, 2 ** 25 // (ctx + 2048)))) if chunks else 0
+        c = _case(None, decodes=decodes, chunks=chunks, chunk=chunk, ctx=ctx,
+                  window=rng.choice([0, 0, 0, _log_int(rng, 1, 4096)]), **more)
+    del c["name"]
+    return c
+
+
+def _lengths(c):
+    """(context, new) of every request: the first of a kind has the full size, the others up to it; kinds are shuffled."""
+    r = random.Random("%(decodes)d %(chunks)d %(chunk)d %(ctx)d" % c)
+    some = lambda most, first: most if first else r.randint(most // 4, most)  # noqa: E731
+    got = [(some(c["ctx"], not i), some(c["chunk"], not i) if c["ctx"] or not i else r.randint(c["chunk"] // 2, c["chunk"]))
+           for i in range(c["chunks"])]
+    got += [(some(c["ctx"], not i), 1) for i in range(c["decodes"])]
+    r.shuffle(got)
+    return got
+
+
+def _blocks(c, lens):
+    """Blocks of the contexts, and new ones that the step needs."""
+    used = sum(-(-a // c["block"]) for a, _ in lens)
+    return used, sum(-(-(a + n) // c["block"]) for a, n in lens) - used
+
+
+def prepare(case, seed):
+    c = dict(case)
+    lens = _lengths(c)
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    bs, most = c["block"], max(-(-(a + n) // c["block"]) for a, n in lens)
+    tokens = sum(n for _, n in lens)
+    used, need = _blocks(c, lens)
+    spare = -(-need // 8) + 8
+    total = used + need + spare
+    order = torch.randperm(total, generator=g, device=DEV).to(torch.int32)  # the pool after much use: any block anywhere
+    ctx = torch.tensor([a for a, _ in lens], dtype=torch.int32)
+    new = torch.tensor([n for _, n in lens], dtype=torch.int32)
+    held = (ctx + bs - 1) // bs if c["kind"] != "attend" else (ctx + new + bs - 1) // bs
+    at = torch.arange(most)[None, :] < held[:, None]
+    table = torch.full((len(lens), most), -1, dtype=torch.int32)
+    n_held = int(held.sum())
+    table[at] = order[:n_held].cpu()
+    start = torch.zeros(len(lens) + 1, dtype=torch.int32)
+    start[1:] = torch.cumsum(new, 0)
+    s = dict(case=c, tokens=tokens, context_len=ctx.to(DEV), new_len=new.to(DEV), block_table=table.to(DEV),
+             max_new=int(new.max()), max_seq=int((ctx + new).max()))
+    if c["kind"] == "assign":
+        free = order[n_held:].contiguous()
+        s["free_blocks"] = free[:max(1, need - need // 16)] if c["short"] else free
+        return s
+    dtype, kv = TYPES[c["dtype"]], TYPES[c["cache"]]
+    hq, hkv, d = c["hq"], c["hkv"], c["d"]
+    # Queries, keys and values as the fused projection leaves them; keys and values with a mean per channel.
+    qkv = torch.randn(tokens, (hq + 2 * hkv) * d, generator=g, device=DEV)
+    mean = torch.randn((hq + 2 * hkv) * d, generator=g, device=DEV)
+    mean[:hq * d] = 0
+    qkv = qkv.add_(mean, alpha=0.5).to(dtype)
+    s["q"] = qkv[:, :hq * d].view(tokens, hq, d)
+    s["k"] = qkv[:, hq * d:(hq + hkv) * d].view(tokens, hkv, d)
+    s["v"] = qkv[:, (hq + hkv) * d:].view(tokens, hkv, d)
+    s["k_scale"], s["v_scale"] = (0.03, 0.05) if c["cache"] == "f8" else (1.0, 1.0)
+    if c["kind"] == "write":
+        pos = torch.cat([torch.arange(a, a + n) for a, n in lens])
+        req = torch.repeat_interleave(torch.arange(len(lens)), new.long())
+        fresh = (pos // bs) - held[req].long()  # new blocks come from the pool in the requests' order
+        got = (ctx + new + bs - 1) // bs - held
+        base = torch.cumsum(got, 0) - got
+        own_block = table[req, (pos // bs).clamp(max=most - 1)].long()
+        new_block = order.cpu()[(n_held + base[req] + fresh.clamp(min=0)).long()].long()
+        block = torch.where(fresh < 0, own_block, new_block)
+        s["slots"] = (block * bs + pos % bs).to(DEV)
+        s["k_cache"] = torch.zeros(total, hkv, bs, d, dtype=kv, device=DEV)
+        s["v_cache"] = torch.zeros(total, hkv, bs, d, dtype=kv, device=DEV)
+        return s
+    s["query_start"] = start.to(DEV)
+    s["seq_len"] = (ctx + new).to(DEV)
+    for name, at in (("k_cache", hq * d), ("v_cache", (hq + hkv) * d)):
+        x = torch.empty(total, hkv, bs, d, dtype=kv, device=DEV)
+        some = max(1, 2 ** 27 // (hkv * bs * d))
+        for i in range(0, total, some):
+            part = torch.randn(min(some, total - i), hkv, bs, d, generator=g, device=DEV)
+            part.add_(mean[at:at + hkv * d].view(hkv, 1, d), alpha=0.5)
+            x[i:i + some] = part.div_(s[name[0] + "_scale"]).clamp_(-F8_MAX, F8_MAX).to(kv)
+        s[name] = x
+    plain = [i for i, (_, n) in enumerate(lens) if n == 1]
+    longer = [i for i, (_, n) in enumerate(lens) if n > 1]
+    # The plain form takes the requests with one new token and the others as two padded batches.
+    s["groups"] = [(torch.tensor(i, device=DEV), max(lens[j][1] for j in i), max(sum(lens[j]) for j in i))
+                   for i in (plain, longer) if i]
+    return s
+
+
+def _plain_assign(s):
+    c, bs = s["case"], s["case"]["block"]
+    ctx, new, table, free = s["context_len"].long(), s["new_len"].long(), s["block_table"], s["free_blocks"]
+    used = (ctx + bs - 1) // bs
+    need = (ctx + new + bs - 1) // bs - used
+    end = torch.cumsum(new, 0)
+    fits = (end <= s["tokens"]) & (used + need <= table.shape[1])
+    need = torch.where(fits, need, 0)
+    taken = torch.cumsum(need, 0)
+    ok = fits & ((need == 0) | (taken <= free.shape[0]))
+    col = torch.arange(table.shape[1], device=DEV)[None, :]
+    mine = ok[:, None] & (col >= used[:, None]) & (col < (used + need)[:, None])
+    pick = ((taken - need)[:, None] + col - used[:, None]).clamp(0, free.shape[0] - 1)
+    table.copy_(torch.where(mine, free[pick], table))
+    t = torch.arange(s["tokens"], device=DEV)
+    req = torch.searchsorted(end, t, right=True).clamp(max=ctx.shape[0] - 1)
+    here = ok[req] & (t < end[-1])
+    pos = torch.where(here, ctx[req] + t - (end - new)[req], -1)
+    block = table[req, (pos.clamp(min=0) // bs).clamp(max=table.shape[1] - 1)].long()
+    slots = torch.where(here & (block >= 0), block * bs + pos % bs, -1)
+    start = torch.cat([torch.zeros(1, dtype=torch.int64, device=DEV), end]).to(torch.int32)
+    counts = torch.stack([end[-1], ok.sum(), torch.where(ok, taken, 0).amax(), taken[-1]]).to(torch.int32)
+    return table, start, torch.where(ok, ctx + new, 0).to(torch.int32), pos.to(torch.int32), slots, counts
+
+
+def _plain_store(x, scale, cache):
+    if cache.dtype != torch.float8_e4m3fn:
+        return x.to(cache.dtype)
+    return x.float().div(scale).clamp(-F8_MAX, F8_MAX).to(cache.dtype)
+
+
+def _bytes(x):
+    """8-bit floats as bytes, which indexing takes."""
+    return x.view(torch.uint8) if x.dtype == torch.float8_e4m3fn else x
+
+
+def _plain_write(s):
+    bs = s["case"]["block"]
+    block, at = s["slots"] // bs, s["slots"] % bs
+    _bytes(s["k_cache"])[block, :, at] = _bytes(_plain_store(s["k"], s["k_scale"], s["k_cache"]))
+    _bytes(s["v_cache"])[block, :, at] = _bytes(_plain_store(s["v"], s["v_scale"], s["v_cache"]))
+    return s["k_cache"], s["v_cache"]
+
+
+def _plain_gather(cache, rows, scale):
+    b, n = rows.shape
+    x = _bytes(cache)[rows.reshape(-1).clamp(min=0)].view(cache.dtype).float().mul_(scale)
+    return x.view(b, n, *x.shape[1:]).transpose(1, 2).reshape(b, x.shape[1], -1, x.shape[-1])
+
+
+def _plain_group(s, out, group):
+    c, (reqs, most_new, most_len) = s["case"], group
+    hq, hkv, d, bs = c["hq"], c["hkv"], c["d"], c["block"]
+    seq, start, new = s["seq_len"][reqs].long(), s["query_start"][reqs].long(), s["new_len"][reqs].long()
+    j = torch.arange(most_new, device=DEV)[None, :]
+    rows, real = (start[:, None] + j).clamp(max=s["tokens"] - 1), j < new[:, None]
+    table = s["block_table"][reqs][:, :-(-most_len // bs)].long()
+    b, g = reqs.shape[0], hq // hkv
+    q = s["q"][rows].float().view(b, most_new, hkv, g, d).transpose(1, 2).reshape(b, hkv, most_new * g, d)
+    p = torch.matmul(q, _plain_gather(s["k_cache"], table, s["k_scale"]).transpose(-1, -2)).mul_(d ** -0.5)
+    last = ((seq - new)[:, None] + j).repeat_interleave(g, 1)[:, None, :, None]  # a row's own position
+    at = torch.arange(p.shape[-1], device=DEV)
+    hide = at > last
+    if c["window"]:
+        hide |= at <= last - c["window"]
+    p.masked_fill_(hide, -math.inf)
+    p.sub_(p.amax(-1, keepdim=True)).exp_()
+    o = torch.matmul(p, _plain_gather(s["v_cache"], table, s["v_scale"])).div_(p.sum(-1, keepdim=True))
+    o = o.view(b, hkv, most_new, g, d).transpose(1, 2).reshape(b, most_new, hq, d)
+    out[rows[real]] = o[real].to(out.dtype)
+
+
+def _plain_attend(s):
+    out = torch.empty(s["q"].shape, dtype=s["q"].dtype, device=DEV)
+    _plain_group(s, out, s["groups"][0])
+    if len(s["groups"]) > 1:
+        _plain_group(s, out, s["groups"][1])
+    return out
+
+
+def run(s):
+    kind = s["case"]["kind"]
+    if not own:
+        return {"assign": _plain_assign, "write": _plain_write, "attend": _plain_attend}[kind](s)
+    import paper_2408_04323_amd as S
+    if kind == "assign":
+        b = S.kv_assign(s["context_len"], s["new_len"], s["block_table"], s["free_blocks"], s["case"]["block"], s["tokens"])
+        return s["block_table"], b.query_start, b.seq_len, b.positions, b.slots, b.counts
+    if kind == "write":
+        S.kv_write(s["k"], s["v"], s["slots"], s["k_cache"], s["v_cache"], k_scale=s["k_scale"], v_scale=s["v_scale"])
+        return s["k_cache"], s["v_cache"]
+    return S.kv_attention(s["q"], s["k_cache"], s["v_cache"], s["block_table"], s["query_start"], s["seq_len"],
+                          max_new_len=s["max_new"], max_seq_len=s["max_seq"], window=s["case"]["window"],
+                          k_scale=s["k_scale"], v_scale=s["v_scale"])
+
+
+def _pairs(a, n, window):
+    """(query, key) pairs of one head, and keys that any of the queries sees."""
+    if not window:
+        return n * a + n * (n + 1) // 2, a + n
+    full = max(0, min(n, window - a))  # queries that see everything before them
+    return full * a + full * (full + 1) // 2 + (n - full) * window, min(a + n, window + n - 1)
+
+
+def work(case):
+    c, lens = case, _lengths(case)
+    tokens = sum(n for _, n in lens)
+    used, need = _blocks(c, lens)
+    if c["kind"] == "assign":
+        # Lengths and free blocks in; the table's new entries, offsets, lengths, positions and slots out.
+        return {"bytes": 4 * (len(lens) * 4 + 2 * need) + 12 * tokens, "flops": 0}
+    one, kv = BYTES[c["dtype"]], BYTES[c["cache"]]
+    if c["kind"] == "write":
+        return {"bytes": tokens * (2 * c["hkv"] * c["d"] * (one + kv) + 8), "flops": 0}
+    seen = [_pairs(a, n, c["window"]) for a, n in lens]
+    table = 4 * sum(-(-k // c["block"]) for _, k in seen)
+    return {"bytes": 2 * tokens * c["hq"] * c["d"] * one + 2 * c["hkv"] * c["d"] * kv * sum(k for _, k in seen) + table,
+            "flops": 4 * c["d"] * c["hq"] * sum(p for p, _ in seen)}
+
+
+def exact(case, seed):
+    """In 64 bits, request by request and key head by key head."""
+    if case["kind"] == "assign":
+        return None  # whole numbers
+    s, c, f64 = prepare(case, seed), case, torch.float64
+    if case["kind"] == "write":
+        got = []
+        for x, cache, scale in ((s["k"], s["k_cache"], s["k_scale"]), (s["v"], s["v_cache"], s["v_scale"])):
+            to = torch.zeros(cache.shape, dtype=f64, device=DEV).transpose(1, 2).reshape(-1, c["hkv"], c["d"])
+            x = x.to(f64) / scale
+            to[s["slots"]] = x.clamp(-F8_MAX, F8_MAX) if c["cache"] == "f8" else x
+            got.append(to.view(cache.shape[0], c["block"], c["hkv"], c["d"]).transpose(1, 2))
+        return tuple(got)
+    out = torch.empty(s["q"].shape, dtype=f64, device=DEV)
+    g, at = c["hq"] // c["hkv"], 0
+    for i, (a, n) in enumerate(_lengths(c)):
+        rows = s["block_table"][i, :-(-(a + n) // c["block"])].long()
+        q = s["q"][at:at + n].to(f64)
+        for h in range(c["hkv"]):
+            k = s["k_cache"][:, h].view(torch.uint8)[rows].view(s["k_cache"].dtype).to(f64).reshape(-1, c["d"])[:a + n]
+            v = s["v_cache"][:, h].view(torch.uint8)[rows].view(s["v_cache"].dtype).to(f64).reshape(-1, c["d"])[:a + n]
+            k, v = k * s["k_scale"], v * s["v_scale"]
+            for r in range(0, n, 2048):
+                e = min(n, r + 2048)
+                own_at = torch.arange(a + r, a + e, device=DEV)[:, None, None]
+                key_at = torch.arange(a + n, device=DEV)
+                see = key_at <= own_at
+                if c["window"]:
+                    see = see & (key_at > own_at - c["window"])
+                x = torch.matmul(q[r:e, h * g:(h + 1) * g].reshape(-1, c["d"]), k.t().contiguous()) / math.sqrt(c["d"])
+                x = torch.where(see, x.view(e - r, g, a + n), -math.inf)
+                p = torch.softmax(x, -1).view(-1, a + n)
+                out[at + r:at + e, h * g:(h + 1) * g] = torch.matmul(p, v).view(e - r, g, c["d"])
+        at += n
+    return out
