@@ -196,7 +196,7 @@ def _plain_assign(s):
     block = table[req, (pos.clamp(min=0) // bs).clamp(max=table.shape[1] - 1)].long()
     slots = torch.where(here & (block >= 0), block * bs + pos % bs, -1)
     start = torch.cat([torch.zeros(1, dtype=torch.int64, device=DEV), end]).to(torch.int32)
-    counts = torch.stack([end[-1], ok.sum(), torch.where(ok, taken, 0).amax(), taken[-1]]).to(torch.int32)
+    counts = torch.stack([end[-1], ok.sum(), torch.where(ok & (need > 0), taken, 0).amax(), taken[-1]]).to(torch.int32)
     return table, start, torch.where(ok, ctx + new, 0).to(torch.int32), pos.to(torch.int32), slots, counts
 
 
