@@ -613,6 +613,105 @@ int scoot_suggest(const double* X_obs, const double* Y_obs, const uint8_t* valid
                   const scoot_space* space, const scoot_suggest_opts* opts, double* x_out, int32_t* source,
                   double* theta_out, int* n_out, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * The key/value cache of an inference engine, as the engine knobs see it.
+ *
+ * The spaces that this library searches (Table 1) are dominated by the knobs
+ * of one mechanism: a cache in blocks of `block-size` tokens, filled by steps
+ * of at most `max-num-batched-tokens` new tokens of at most `max-num-seqs`
+ * requests, whole prompts or chunks of them.  These calls are that mechanism
+ * on the GPU, so that a configuration can be evaluated where it is searched:
+ * scoot_kv_assign gives every new token of a step its place, scoot_kv_write
+ * stores the tokens' keys and values there, scoot_kv_attention lets the
+ * step's queries attend to everything stored.  Every pointer below is a
+ * device pointer owned by the caller, and all of them work asynchronously on
+ * `stream`: nothing is allocated, no length comes back to the host, and a
+ * step can be captured into a HIP graph.  Lengths and tables may hold
+ * anything: no value read on the device leads outside the arrays described
+ * here.
+ *
+ * Cache: k_cache and v_cache are [num_blocks][num_kv_heads][block_size]
+ * [head_dim] each, contiguous, 16-byte aligned, elements of cache_type.
+ * block_size is a power of two, 8 .. 256.  A request's token at position p
+ * lies in block block_table[request][p / block_size] at p % block_size; a
+ * slot is block * block_size + p % block_size, 64 bits wide.  An entry that
+ * names no block (outside 0 .. num_blocks - 1) holds no tokens.
+ * cache_type is the type of the vectors, or SCOOT_KV_F8: OCP e4m3, holding
+ * value / scale rounded to nearest even, limited to +-448, NaN kept.
+ * ------------------------------------------------------------------------- */
+typedef enum scoot_kv_type { SCOOT_KV_F16 = 0, SCOOT_KV_BF16 = 1, SCOOT_KV_F8 = 2 } scoot_kv_type;
+
+/* Places for the new tokens of a step.  Request i has context_len[i] tokens in
+ * the cache, in the first ceil(context_len[i] / block_size) blocks of its row
+ * of block_table [num_seqs rows, table_stride apart, max_blocks entries], and
+ * brings new_len[i] tokens (negative lengths count as 0).  Its new tokens fill
+ * the rest of its last block, then blocks taken from free_blocks [num_free] in
+ * the requests' order.  A request is admitted if its tokens end within
+ * max_tokens (counting all requests before it), its blocks fit max_blocks, and
+ * its new blocks, counted after those of the requests before it that pass
+ * these two tests, end within num_free.  The blocks taken are the first
+ * counts[2] of free_blocks.
+ *   block_table   in/out: the admitted requests' new entries are written.
+ *   query_start   [num_seqs + 1] out: the first token of every request, and
+ *                 the number of tokens (limited to INT32_MAX).
+ *   seq_len       [num_seqs] out: context_len + new_len; 0 if not admitted.
+ *   positions     [max_tokens] out: a token's position in its request; -1 for
+ *                 requests not admitted and past the last token.
+ *   slots         [max_tokens] out: a token's slot; -1 there, too, and where
+ *                 the table's entry is negative.
+ *   counts        [4] out: tokens, admitted requests, blocks taken, blocks
+ *                 that admitting every request that passes the first two
+ *                 tests would have taken.
+ * num_seqs <= 2^20.  Errors: INVALID_ARG, DEVICE. */
+int scoot_kv_assign(const int32_t* context_len, const int32_t* new_len, int num_seqs, int block_size,
+                    int32_t* block_table, int max_blocks, int64_t table_stride, const int32_t* free_blocks,
+                    int num_free, int64_t max_tokens, int32_t* query_start, int32_t* seq_len, int32_t* positions,
+                    int64_t* slots, int32_t* counts, void* stream);
+
+/* Stores the keys and values [num_tokens][num_kv_heads][head_dim] of a step
+ * (elements of `type`, F16 or BF16; token and head strides in elements, the
+ * last dimension contiguous) at their slots.  Slots outside the cache (-1
+ * among them) are skipped; of tokens with the same slot one is stored.
+ * k_scale, v_scale > 0: the scales of an 8-bit cache, 1 otherwise.
+ * Errors: INVALID_ARG, UNSUPPORTED (head_dim not a multiple of 8), DEVICE. */
+int scoot_kv_write(const void* k, const void* v, scoot_kv_type type, int64_t num_tokens, int num_kv_heads,
+                   int head_dim, int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
+                   int64_t v_head_stride, const int64_t* slots, void* k_cache, void* v_cache,
+                   scoot_kv_type cache_type, int64_t num_blocks, int block_size, float k_scale, float v_scale,
+                   void* stream);
+
+/* Attention of the step's tokens over the cache.  Request i's queries are the
+ * rows query_start[i] .. query_start[i + 1] - 1 of q (limited to num_tokens);
+ * its cache holds seq_len[i] tokens, the new ones included, and query j of n
+ * stands at position p = seq_len[i] - n + j.  It sees the positions
+ * max(0, p - window + 1) .. p (window = 0: 0 .. p):
+ *   out = sum_t softmax_t(scale * k_scale * q . k_t) * v_scale * v_t
+ * for query head h over key head h / (num_heads / num_kv_heads).  A query
+ * that sees nothing gets zeros; what it does not see (stale or unwritten
+ * memory, infinities and NaN included) does not reach its result.  Rows of
+ * out that belong to no request are not written.  Sums and the softmax are in
+ * float; its weights are rounded to 16 bits for the product with v.
+ *   q, out        [num_tokens][num_heads][head_dim] of `type` (F16 or BF16),
+ *                 strides in elements, 16-byte aligned, the last dimension
+ *                 contiguous; head_dim 64, 128, 192 or 256.
+ *   max_new_len, max_seq_len  what the caller knows of the longest request (of
+ *                 its new tokens, and of its tokens after the step); they choose
+ *                 how the work is split.  Larger requests are computed all the
+ *                 same, more slowly.
+ *   workspace     of at least scoot_kv_attention_workspace's bytes, 16-byte
+ *                 aligned (may be NULL if that is 0); no call that may run at
+ *                 the same time shares it.
+ * Errors: INVALID_ARG (also a workspace too small), UNSUPPORTED, DEVICE. */
+int scoot_kv_attention_workspace(int64_t num_tokens, int num_heads, int num_kv_heads, int head_dim, int num_seqs,
+                                 int64_t max_new_len, int64_t max_seq_len, int window, uint64_t* bytes);
+int scoot_kv_attention(const void* q, scoot_kv_type type, int64_t num_tokens, int num_heads, int num_kv_heads,
+                       int head_dim, int64_t q_token_stride, int64_t q_head_stride, const void* k_cache,
+                       const void* v_cache, scoot_kv_type cache_type, int64_t num_blocks, int block_size,
+                       const int32_t* block_table, int max_blocks, int64_t table_stride, const int32_t* query_start,
+                       const int32_t* seq_len, int num_seqs, int64_t max_new_len, int64_t max_seq_len, float scale,
+                       int window, float k_scale, float v_scale, void* out, int64_t out_token_stride,
+                       int64_t out_head_stride, void* workspace, uint64_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

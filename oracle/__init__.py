@@ -25,6 +25,8 @@ Tuning for LLM Inference Engines) and is written for clarity, not speed:
                      constraints (Sec. 4.5.3, 4.7, Algorithm 1)
 * ``mace``        -- MACE for one objective: UCB, PI, EI (Eq. 6-8), their Pareto
                      front over the pool and a seeded random pick (Sec. 4.5.1, 4.6)
+* ``kv_cache``    -- the engine's key/value cache that the tuned knobs shape: slots
+                     of a step's tokens, 8-bit storage, attention over blocks
 * ``pipeline``    -- the whole scoring pass over a candidate pool
 * ``suggest``     -- the suggestion step of Algorithm 1 end to end: learn,
                      train, generate, score, pick, fill

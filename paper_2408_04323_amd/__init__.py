@@ -681,6 +681,164 @@ def known_constraints(Xc, A, b, out=None, stream=None):
     return known
 
 
+# ------------------------------------------- the engine's key/value cache
+KV_F16, KV_BF16, KV_F8 = 0, 1, 2
+
+
+def _kv_type(t, name, cache=False):
+    import torch
+    if t.dtype == torch.float16:
+        return KV_F16
+    if t.dtype == torch.bfloat16:
+        return KV_BF16
+    if cache and t.dtype == torch.float8_e4m3fn:
+        return KV_F8
+    raise ValueError(f"{name} must be float16 or bfloat16" + (" or float8_e4m3fn" if cache else ""))
+
+
+def _kv_ints(t, name, numel=None):
+    import torch
+    _require_device(t, name, torch.int32, numel)
+
+
+def _kv_vectors(t, name, heads=None, dim=None):
+    """(tokens, heads, dim) with the last dimension contiguous; other strides are free."""
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be a device tensor")
+    if t.dim() != 3 or (heads is not None and t.shape[1] != heads) or (dim is not None and t.shape[2] != dim):
+        raise ValueError(f"{name} must be (tokens, {heads or 'heads'}, {dim or 'head_dim'})")
+    if t.stride(2) != 1 and t.shape[2] != 1:
+        raise ValueError(f"{name} must be contiguous in its last dimension")
+
+
+def _kv_table(t, num_seqs=None):
+    import torch
+    if t.device.type != "cuda" or t.dtype != torch.int32 or t.dim() != 2:
+        raise ValueError("block_table must be an int32 (requests, blocks) device tensor")
+    if (t.stride(1) != 1 and t.shape[1] > 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError("block_table must be contiguous in its last dimension")
+    if num_seqs is not None and t.shape[0] != num_seqs:
+        raise ValueError(f"block_table must have {num_seqs} rows")
+
+
+def _kv_caches(k_cache, v_cache):
+    kind = _kv_type(k_cache, "k_cache", cache=True)
+    if k_cache.dim() != 4:
+        raise ValueError("k_cache must be (blocks, kv_heads, block_size, head_dim)")
+    _require_device(k_cache, "k_cache")
+    _require_device(v_cache, "v_cache", k_cache.dtype)
+    if v_cache.shape != k_cache.shape:
+        raise ValueError("v_cache must have k_cache's shape")
+    return kind
+
+
+class KVBatch:
+    """Caller-owned outputs of kv_assign for ``num_seqs`` requests and at most
+    ``max_tokens`` new tokens: query_start (num_seqs + 1), seq_len (num_seqs),
+    positions (max_tokens), slots (max_tokens, int64), and counts (tokens,
+    admitted requests, blocks taken, blocks asked for)."""
+
+    def __init__(self, num_seqs, max_tokens, device="cuda"):
+        import torch
+        self.num_seqs, self.max_tokens = int(num_seqs), int(max_tokens)
+        self.slots = torch.empty(max_tokens, dtype=torch.int64, device=device)
+        ints = torch.empty(2 * num_seqs + 5 + max_tokens, dtype=torch.int32, device=device)
+        self.query_start, self.seq_len, self.counts, self.positions = ints.split(
+            (num_seqs + 1, num_seqs, 4, max_tokens))
+
+
+def kv_assign(context_len, new_len, block_table, free_blocks, block_size, max_tokens, out=None, stream=None):
+    """Places of a step's new tokens in the block cache (scoot_kv_assign): from
+    the requests' cached and new lengths (int32 (requests,)) the new tokens'
+    slots and positions, and, from ``free_blocks`` in order, the new entries of
+    ``block_table`` (int32 (requests, blocks), updated in place).  Returns a
+    KVBatch (``out`` if given); nothing is read back."""
+    n = context_len.numel()
+    _kv_ints(context_len, "context_len")
+    _kv_ints(new_len, "new_len", n)
+    _kv_ints(free_blocks, "free_blocks")
+    _kv_table(block_table, n)
+    b = KVBatch(n, max_tokens, context_len.device) if out is None else out
+    if b.num_seqs != n or b.max_tokens != max_tokens:
+        raise ValueError("out was made for other sizes")
+    check(lib().scoot_kv_assign(context_len.data_ptr(), new_len.data_ptr(), n, block_size, block_table.data_ptr(),
+                                block_table.shape[1], max(block_table.stride(0), block_table.shape[1]),
+                                free_blocks.data_ptr(), free_blocks.numel(), max_tokens, b.query_start.data_ptr(),
+                                b.seq_len.data_ptr(), b.positions.data_ptr(), b.slots.data_ptr(),
+                                b.counts.data_ptr(), _stream(stream)), "kv_assign")
+    return b
+
+
+def kv_write(k, v, slots, k_cache, v_cache, k_scale=1.0, v_scale=1.0, stream=None):
+    """Stores keys and values (tokens, kv_heads, head_dim), float16 or
+    bfloat16, at their slots of the caches (blocks, kv_heads, block_size,
+    head_dim) of the same type, or float8_e4m3fn, which holds value / scale
+    (scoot_kv_write).  Slots outside the cache are skipped."""
+    import torch
+    cache_type = _kv_caches(k_cache, v_cache)
+    blocks, heads, block_size, dim = k_cache.shape
+    kind = _kv_type(k, "k")
+    _kv_vectors(k, "k", heads, dim)
+    _kv_vectors(v, "v", heads, dim)
+    if v.dtype != k.dtype or v.shape[0] != k.shape[0]:
+        raise ValueError("v must have k's type and number of tokens")
+    _require_device(slots, "slots", torch.int64, k.shape[0])
+    check(lib().scoot_kv_write(k.data_ptr(), v.data_ptr(), kind, k.shape[0], heads, dim, k.stride(0), k.stride(1),
+                               v.stride(0), v.stride(1), slots.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+                               cache_type, blocks, block_size, k_scale, v_scale, _stream(stream)), "kv_write")
+
+
+def kv_attention(q, k_cache, v_cache, block_table, query_start, seq_len, max_new_len, max_seq_len, scale=None,
+                 window=0, k_scale=1.0, v_scale=1.0, out=None, workspace=None, stream=None):
+    """Attention of a step's queries (tokens, heads, head_dim) over the block
+    cache (scoot_kv_attention): request i owns the rows query_start[i] ..
+    query_start[i + 1] - 1, the last of its seq_len[i] positions, and every
+    query sees what stands up to its own position (the last ``window`` of
+    these, if given).  ``max_new_len`` and ``max_seq_len``: the longest request
+    of the step as the caller knows it; ``scale`` defaults to head_dim ** -0.5.
+    A ``workspace`` (uint8, at least kv_attention_workspace's bytes) may be
+    kept between calls.  Returns ``out``, made if not given."""
+    import torch
+    cache_type = _kv_caches(k_cache, v_cache)
+    blocks, kv_heads, block_size, dim = k_cache.shape
+    kind = _kv_type(q, "q")
+    _kv_vectors(q, "q", None, dim)
+    tokens, heads = q.shape[0], q.shape[1]
+    n = seq_len.numel()
+    _kv_ints(seq_len, "seq_len")
+    _kv_ints(query_start, "query_start", n + 1)
+    _kv_table(block_table, n)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    else:
+        _kv_vectors(out, "out", heads, dim)
+        if out.dtype != q.dtype or out.shape[0] != tokens:
+            raise ValueError("out must have q's type and shape")
+    if workspace is None:
+        need = kv_attention_workspace(tokens, heads, kv_heads, dim, n, max_new_len, max_seq_len, window)
+        if need:
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    else:
+        _require_device(workspace, "workspace", torch.uint8)
+    check(lib().scoot_kv_attention(q.data_ptr(), kind, tokens, heads, kv_heads, dim, q.stride(0), q.stride(1),
+                                   k_cache.data_ptr(), v_cache.data_ptr(), cache_type, blocks, block_size,
+                                   block_table.data_ptr(), block_table.shape[1],
+                                   max(block_table.stride(0), block_table.shape[1]), query_start.data_ptr(),
+                                   seq_len.data_ptr(), n, max_new_len, max_seq_len,
+                                   dim ** -0.5 if scale is None else scale, window, k_scale, v_scale, out.data_ptr(),
+                                   out.stride(0), out.stride(1), None if workspace is None else workspace.data_ptr(),
+                                   0 if workspace is None else workspace.numel(), _stream(stream)), "kv_attention")
+    return out
+
+
+def kv_attention_workspace(tokens, heads, kv_heads, head_dim, num_seqs, max_new_len, max_seq_len, window=0):
+    """Bytes that kv_attention needs for these sizes."""
+    b = C.c_uint64(0)
+    check(lib().scoot_kv_attention_workspace(tokens, heads, kv_heads, head_dim, num_seqs, max_new_len, max_seq_len,
+                                             window, C.byref(b)), "kv_attention_workspace")
+    return b.value
+
+
 # ------------------------------------------------------ the suggestion step
 class _Space(C.Structure):
     _fields_ = [("d", C.c_int), ("levels", C.POINTER(C.c_int32)), ("sobol_poly", C.POINTER(C.c_uint32)),

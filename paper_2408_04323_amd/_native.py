@@ -72,6 +72,14 @@ SIGNATURES = {
     "scoot_known_constraints": [c_vp, c_i64, c_int, P_dbl, P_dbl, c_int, c_vp, c_vp],
     "scoot_suggest": [P_dbl, P_dbl, C.POINTER(C.c_uint8), c_int, c_int, c_vp, c_vp, P_dbl, P_i32, P_dbl, P_int,
                       c_vp],
+    "scoot_kv_assign": [c_vp, c_vp, c_int, c_int, c_vp, c_int, c_i64, c_vp, c_int, c_i64, c_vp, c_vp, c_vp, c_vp,
+                        c_vp, c_vp],
+    "scoot_kv_write": [c_vp, c_vp, c_int, c_i64, c_int, c_int, c_i64, c_i64, c_i64, c_i64, c_vp, c_vp, c_vp, c_int,
+                       c_i64, c_int, C.c_float, C.c_float, c_vp],
+    "scoot_kv_attention_workspace": [c_i64, c_int, c_int, c_int, c_int, c_i64, c_i64, c_int, C.POINTER(C.c_uint64)],
+    "scoot_kv_attention": [c_vp, c_int, c_i64, c_int, c_int, c_int, c_i64, c_i64, c_vp, c_vp, c_int, c_i64, c_int, c_vp,
+                           c_int, c_i64, c_vp, c_vp, c_int, c_i64, c_i64, C.c_float, c_int, C.c_float, C.c_float,
+                           c_vp, c_i64, c_i64, c_vp, C.c_uint64, c_vp],
 }
 RESTYPES = {"scoot_status_string": C.c_char_p, "scoot_last_error": C.c_char_p}
 

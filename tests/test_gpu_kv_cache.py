@@ -1,0 +1,411 @@
+"""Key/value cache operators on the GPU against the float64 oracle: slots and
+tables exactly, stored vectors exactly, attention within the bound that the
+oracle derives from the formats (attention_bound)."""
+import sys
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2408_04323_amd as S  # noqa: E402
+from oracle import kv_cache as kv  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"f16": torch.float16, "bf16": torch.bfloat16, "f8": torch.float8_e4m3fn}
+BITS = {"f16": 11, "bf16": 8}
+
+
+def say(*a):
+    print("[case]", *a, flush=True)
+    sys.stdout.flush()
+
+
+def dev(a, dtype):
+    return torch.as_tensor(np.asarray(a)).to(dtype).to(DEV)
+
+
+def f64(t):
+    return t.detach().float().cpu().numpy().astype(np.float64)
+
+
+# ------------------------------------------------------------------ assignment
+def _assign_inputs(rng, n, bs, most_ctx, most_new, cols, free, spread=None):
+    ctx = rng.integers(0, most_ctx + 1, n)
+    new = rng.integers(0, most_new + 1, n)
+    table = np.full((n, cols), -1, dtype=np.int64)
+    order = rng.permutation(int((-(-ctx // bs)).sum()) + free + 5)
+    at = 0
+    for r in range(n):
+        u = min(-(-int(ctx[r]) // bs), cols)
+        table[r, :u] = order[at:at + u]
+        at += u
+    return ctx, new, table, order[at:at + free]
+
+
+ASSIGN = [  # requests, block size, longest context, most new, columns, free blocks, token limit (None: exactly what comes)
+    (1, 16, 0, 1, 1, 1, None), (1, 8, 100, 300, 64, 60, None), (3, 256, 1000, 1000, 9, 20, None),
+    (64, 16, 4095, 1, 300, 64, None), (64, 16, 4095, 1, 300, 2, 64), (100, 8, 50, 40, 8, 400, 1500),
+    (1000, 32, 200, 30, 8, 300, 20000), (4096, 8, 9, 5, 3, 100000, None), (4097, 8, 20, 5, 4, 3000, 9000),
+    (9000, 16, 60, 40, 7, 9000, 200000), (2, 8, 10, 5000, 700, 650, None), (7, 16, 30, 0, 3, 0, 0),
+]
+
+
+@pytest.mark.parametrize("case", ASSIGN, ids=[f"{c[0]}x{c[1]}-{i}" for i, c in enumerate(ASSIGN)])
+def test_assign_matches_oracle(case):
+    n, bs, most_ctx, most_new, cols, free, limit = case
+    say("assign", case)
+    rng = np.random.default_rng(n * 7 + bs)
+    ctx, new, table, free_blocks = _assign_inputs(rng, n, bs, most_ctx, most_new, cols, free)
+    limit = int(new.sum()) if limit is None else limit
+    if n > 50:
+        ctx[3], new[5] = -4, -1  # count as zero
+        table[10, 0] = -1        # a block that the table lacks
+    wide = torch.full((n, cols + 3), -9, dtype=torch.int32, device=DEV)
+    wide[:, :cols] = dev(table, torch.int32)
+    t = wide[:, :cols]
+    b = S.kv_assign(dev(ctx, torch.int32), dev(new, torch.int32), t, dev(free_blocks, torch.int32), bs, limit)
+    want = kv.assign(ctx, new, table, free_blocks, bs, limit)
+    for name, got, ref in zip(("table", "query_start", "seq_len", "positions", "slots", "counts"),
+                              (t, b.query_start, b.seq_len, b.positions, b.slots, b.counts), want):
+        np.testing.assert_array_equal(got.cpu().numpy(), ref, err_msg=name)
+    assert (wide[:, cols:] == -9).all()
+
+
+def test_assign_of_no_request():
+    z = torch.empty(0, dtype=torch.int32, device=DEV)
+    b = S.kv_assign(z, z, torch.empty(0, 4, dtype=torch.int32, device=DEV), z, 16, 5)
+    assert b.query_start.tolist() == [0] and b.counts.tolist() == [0, 0, 0, 0]
+    assert b.positions.tolist() == [-1] * 5 and b.slots.tolist() == [-1] * 5
+
+
+def test_assign_of_lengths_past_32_bits():
+    """Sums that pass 32 bits are limited, and nothing past the token limit is admitted."""
+    big = 2 ** 31 - 1
+    ctx, new = dev([0, 5, 0, 0], torch.int32), dev([3, big, big, 2], torch.int32)
+    t = torch.full((4, 2), -1, dtype=torch.int32, device=DEV)
+    b = S.kv_assign(ctx, new, t, dev([3, 4, 5], torch.int32), 8, 64)
+    assert b.query_start.tolist() == [0, 3, big, big, big]
+    assert b.seq_len.tolist() == [3, 0, 0, 0] and b.counts.tolist() == [big, 1, 1, 1]
+    assert b.slots.tolist() == [24, 25, 26] + [-1] * 61
+
+
+# ---------------------------------------------------------------------- writes
+WRITE = [  # type, cache, tokens, heads, dim, block size
+    ("bf16", "bf16", 1, 1, 8, 8), ("f16", "f16", 37, 5, 64, 8), ("bf16", "bf16", 300, 8, 128, 16), ("f16", "f8", 129, 3, 80, 32),
+    ("bf16", "f8", 64, 2, 256, 256), ("f16", "f16", 33, 1, 1024, 64), ("bf16", "f8", 500, 7, 24, 128),
+]
+
+
+@pytest.mark.parametrize("strided", ["rows", "fused", "odd"])
+@pytest.mark.parametrize("case", WRITE, ids=["-".join(map(str, c)) for c in WRITE])
+def test_write_matches_oracle(case, strided):
+    kind, cache, tokens, heads, d, bs = case
+    say("write", case, strided)
+    rng = np.random.default_rng(tokens + d)
+    blocks = tokens // bs + 3
+    x = rng.standard_normal((tokens, 2 * heads * d + 24)) * np.exp(rng.uniform(-6, 6, (tokens, 1)))
+    x[0, :4] = [np.nan, np.inf, -np.inf, 0.0]
+    x = dev(x, TYPES[kind])
+    if strided == "rows":
+        k, v = x[:, :heads * d].reshape(tokens, heads, d).contiguous(), x[:, heads * d:2 * heads * d].reshape(tokens, heads, d).contiguous()
+    else:
+        o = 8 if strided == "fused" else 1  # 1: rows that start off 16 bytes
+        k = x[:, o:o + heads * d].view(tokens, heads, d)
+        v = x[:, o + heads * d:o + 2 * heads * d].view(tokens, heads, d)
+    slots = rng.permutation(blocks * bs)[:tokens]
+    if tokens > 8:
+        slots[[2, 5, 7]] = [-1, blocks * bs, 2 ** 40]
+    kc = torch.full((blocks, heads, bs, d), 3.0, device=DEV).to(TYPES[cache])
+    vc = torch.full((blocks, heads, bs, d), -2.0, device=DEV).to(TYPES[cache])
+    ks, vs = (0.03, 0.7) if cache == "f8" else (1.0, 1.0)
+    S.kv_write(k, v, dev(slots, torch.int64), kc, vc, k_scale=ks, v_scale=vs)
+    for got, src, fill, scale in ((kc, k, 3.0, ks), (vc, v, -2.0, vs)):
+        store = (lambda y: kv.round_e4m3(f64(torch.as_tensor(y, dtype=torch.float32) / np.float32(scale)))) if cache == "f8" else (lambda y: y)
+        want = kv.write(f64(src), slots, np.full((blocks, heads, bs, d), fill), store)
+        np.testing.assert_array_equal(f64(got), want)
+
+
+def test_write_to_a_cache_past_32_bits():
+    """Offsets of more than 2^31 elements."""
+    say("write far")
+    blocks = 2 ** 31 // (2 * 16 * 64) + 8
+    kc = torch.zeros(blocks, 2, 16, 64, dtype=torch.bfloat16, device=DEV)
+    vc = torch.zeros_like(kc)
+    k, v = torch.randn(2, 3, 2, 64, device=DEV).to(torch.bfloat16)
+    slots = dev([blocks * 16 - 1, 0, (blocks - 3) * 16 + 5], torch.int64)
+    S.kv_write(k, v, slots, kc, vc)
+    for c, x in ((kc, k), (vc, v)):
+        for t, s in enumerate(slots.tolist()):
+            assert torch.equal(c[s // 16, :, s % 16], x[t])
+    # ... and attention out of it: one request whose block is the last one
+    table = dev([[blocks - 1]], torch.int32)
+    kc[blocks - 1], vc[blocks - 1] = torch.randn(2, 2, 16, 64, device=DEV).to(torch.bfloat16)
+    q = torch.randn(1, 4, 64, device=DEV).to(torch.bfloat16)
+    out = S.kv_attention(q, kc, vc, table, dev([0, 1], torch.int32), dev([16], torch.int32), 1, 16)
+    want, spread, reach = kv.attention(f64(q), f64(kc[-1:]), f64(vc[-1:]), np.array([[0]]), [0, 1], [16], 64 ** -0.5)
+    assert (np.abs(f64(out) - want) <= kv.attention_bound(want, spread, reach, 16, 64, 8, 8, 4.0)).all()
+
+
+# ------------------------------------------------------------------- attention
+def _case(lens, kind="bf16", cache=None, hq=4, hkv=2, d=64, bs=16, window=0, scale=None, hints=None, stale=float("nan")):
+    return dict(lens=lens, kind=kind, cache=cache or kind, hq=hq, hkv=hkv, d=d, bs=bs, window=window, scale=scale,
+                hints=hints, stale=stale)
+
+
+ATTEND = {
+    "one_token": _case([(0, 1)]),
+    "one_of_many": _case([(1000, 1)], hq=32, hkv=8, d=128),
+    "block_edges": _case([(7, 1), (8, 1), (15, 1), (16, 1), (31, 1), (32, 1), (63, 1), (64, 1), (65, 1)], bs=8),
+    "decode_ragged": _case([(i * 37 % 300, 1) for i in range(40)], hq=8, hkv=2, d=128, kind="f16"),
+    "decode_no_groups": _case([(200, 1), (31, 1), (0, 1)], hq=5, hkv=5, d=64, bs=32),
+    "decode_group_of_7": _case([(333, 1), (64, 1)], hq=28, hkv=4, d=128, bs=8, kind="f16"),
+    "decode_group_of_33": _case([(100, 1), (5, 1)], hq=33, hkv=1, d=64),
+    "decode_group_of_130": _case([(70, 1)], hq=130, hkv=1, d=64),
+    "decode_long": _case([(9000, 1), (3, 1)], hq=8, hkv=1, d=256, bs=256),
+    "decode_wide": _case([(500, 1), (20, 1)], hq=12, hkv=4, d=192, bs=16, kind="f16"),
+    "draft_tokens": _case([(700, 4), (90, 4), (0, 4)], hq=16, hkv=2, d=128),
+    "prompt": _case([(0, 200)], hq=4, hkv=4, d=64),
+    "prompt_group": _case([(0, 150), (0, 33)], hq=8, hkv=2, d=128, kind="f16"),
+    "prompt_wide": _case([(0, 90)], hq=4, hkv=2, d=256, bs=32),
+    "prompt_192": _case([(0, 70), (3, 64)], hq=6, hkv=2, d=192, bs=8),
+    "chunk": _case([(300, 130)], hq=8, hkv=2, d=64, bs=8),
+    "chunk_long": _case([(4500, 40)], hq=4, hkv=1, d=128, bs=32),
+    "mixed": _case([(50, 1), (0, 140), (33, 1), (129, 65), (0, 1), (17, 9), (0, 0), (5, 0)], hq=8, hkv=2, d=128),
+    "mixed_many": _case([(i % 50, 1 + 40 * (i % 9 == 4)) for i in range(80)], hq=7, hkv=1, d=64, kind="f16", bs=8),
+    "window": _case([(500, 1), (100, 1), (10, 1)], window=64, hq=8, hkv=2, d=128),
+    "window_chunk": _case([(300, 150), (0, 100)], window=37, hq=4, hkv=2, d=64, kind="f16", bs=8),
+    "window_one": _case([(300, 40), (9, 1)], window=1, hq=4, hkv=2),
+    "f8_decode": _case([(900, 1), (64, 1), (0, 1)], cache="f8", hq=16, hkv=2, d=128),
+    "f8_decode_64": _case([(900, 1), (37, 1)], cache="f8", kind="f16", hq=15, hkv=5, d=64, bs=8),
+    "f8_chunk": _case([(100, 150), (40, 1)], cache="f8", hq=8, hkv=2, d=128, bs=32),
+    "f8_192": _case([(100, 50), (40, 1)], cache="f8", kind="f16", hq=6, hkv=2, d=192),
+    "f8_256": _case([(70, 140), (400, 1)], cache="f8", hq=4, hkv=1, d=256),
+    "f8_window": _case([(300, 140)], cache="f8", hq=4, hkv=2, d=64, window=100, bs=8),
+    "stale_inf": _case([(70, 3), (9, 1)], stale=float("inf"), hq=4, hkv=2, d=128, kind="f16"),
+    "scale_zero": _case([(30, 20)], scale=0.0),
+    "scale_sharp": _case([(200, 150)], scale=3.0, hq=4, hkv=2, d=128, stale=0.0),
+    "hints_small": _case([(1500, 90), (20, 1), (0, 300)], hints=(1, 1), hq=8, hkv=2, d=64),
+    "hints_large": _case([(40, 2), (20, 1)], hints=(5000, 100000), hq=8, hkv=2, d=64),
+}
+
+
+def _attend_inputs(c, seed=0):
+    """A cache of blocks in random order, `stale` wherever no token of a request lies."""
+    rng = np.random.default_rng(seed)
+    lens, bs, d = c["lens"], c["bs"], c["d"]
+    need = [-(-(a + n) // bs) for a, n in lens]
+    blocks = sum(need) + 3
+    order = rng.permutation(blocks)
+    cols = max(need) + 2
+    table = np.full((len(lens), cols), -1, dtype=np.int64)
+    tokens = sum(n for _, n in lens)
+    q = rng.standard_normal((tokens, c["hq"], d))
+    kc = np.full((blocks, c["hkv"], bs, d), c["stale"])
+    vc = np.full((blocks, c["hkv"], bs, d), c["stale"])
+    at = 0
+    for r, (a, n) in enumerate(lens):
+        table[r, :need[r]] = order[at:at + need[r]]
+        table[r, need[r]:] = [order[-1], blocks + 7][:cols - need[r]] + [-1] * max(0, cols - need[r] - 2)
+        at += need[r]
+        for b in range(need[r]):
+            m = min(bs, a + n - b * bs)
+            kc[table[r, b], :, :m] = rng.standard_normal((c["hkv"], m, d)) + 0.3
+            vc[table[r, b], :, :m] = rng.standard_normal((c["hkv"], m, d)) + 0.2
+    t, ct = TYPES[c["kind"]], TYPES[c["cache"]]
+    ks, vs = (0.02, 0.03) if c["cache"] == "f8" else (1.0, 1.0)
+    if c["cache"] == "f8":
+        kc, vc = np.clip(kc / ks, -448, 448), np.clip(vc / vs, -448, 448)
+    start = np.concatenate([[0], np.cumsum([n for _, n in lens])])
+    return dict(q=dev(q, t), k=dev(kc, torch.float32).to(ct), v=dev(vc, torch.float32).to(ct), table=table, start=start,
+                seq=np.array([a + n for a, n in lens]), ks=ks, vs=vs)
+
+
+def _bound(c, s, ref, vmax=None):
+    out, spread, reach = ref
+    v = f64(s["v"]) * s["vs"]
+    vmax = np.abs(v[np.isfinite(v)]).max() if vmax is None else vmax
+    bits = 11 if c["cache"] == "f8" else BITS[c["kind"]]
+    return kv.attention_bound(out, spread, reach, max(a + n for a, n in c["lens"]), c["d"], BITS[c["kind"]], bits, vmax)
+
+
+def _reference(c, s):
+    return kv.attention(f64(s["q"]), f64(s["k"]) * s["ks"], f64(s["v"]) * s["vs"], s["table"], s["start"], s["seq"],
+                        c["d"] ** -0.5 if c["scale"] is None else c["scale"], c["window"])
+
+
+def _call(c, s, **more):
+    hints = c["hints"] or (max(n for _, n in c["lens"]), max(a + n for a, n in c["lens"]))
+    args = dict(max_new_len=hints[0], max_seq_len=hints[1], scale=c["scale"], window=c["window"], k_scale=s["ks"], v_scale=s["vs"])
+    args.update(more)
+    return S.kv_attention(s["q"], s["k"], s["v"], dev(s["table"], torch.int32), dev(s["start"], torch.int32),
+                          dev(s["seq"], torch.int32), **args)
+
+
+@pytest.mark.parametrize("name", list(ATTEND))
+def test_attention_matches_oracle(name):
+    c = ATTEND[name]
+    say("attend", name)
+    s = _attend_inputs(c, seed=len(name))
+    got = f64(_call(c, s))
+    ref = _reference(c, s)
+    off = np.abs(got - ref[0])
+    assert np.isfinite(ref[0]).all()
+    assert (off <= _bound(c, s, ref)).all(), float(np.nanmax(off / _bound(c, s, ref)))
+
+
+def test_attention_twice_is_the_same_bits():
+    for name in ("decode_long", "mixed", "chunk_long"):
+        c = ATTEND[name]
+        s = _attend_inputs(c)
+        a, b = _call(c, s), _call(c, s)
+        assert torch.equal(a.view(torch.int16), b.view(torch.int16)), name
+
+
+def test_attention_rows_without_keys_are_zero():
+    """Requests that were not admitted (no cached tokens), that hold fewer tokens than they ask for, or whose blocks are missing."""
+    c = _case([(20, 3), (40, 2), (0, 40), (9, 1)], hq=8, hkv=2, d=128)
+    s = _attend_inputs(c)
+    s["seq"] = np.array([0, 1, 25, 10])
+    s["table"][3] = [-1] * s["table"].shape[1]
+    got, ref = f64(_call(c, s)), _reference(c, s)
+    assert (ref[0][:3] == 0).all() and (ref[0][3] == 0).all() and (ref[0][5:20] == 0).all() and (ref[0][45] == 0).all()
+    assert (got[:4] == 0).all() and (got[5:20] == 0).all() and (got[45] == 0).all()
+    assert (np.abs(got - ref[0]) <= _bound(c, s, ref)).all()
+
+
+def test_attention_skips_missing_blocks():
+    c = _case([(200, 30), (130, 1)], hq=8, hkv=2, d=64, bs=8)
+    s = _attend_inputs(c)
+    s["table"][0, [0, 7, 20]] = [-1, s["k"].shape[0], 2 ** 31 - 1]
+    s["table"][1, [3, 4, 5, 6, 7, 16]] = -5
+    got, ref = f64(_call(c, s)), _reference(c, s)
+    assert (np.abs(got - ref[0]) <= _bound(c, s, ref)).all()
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("cache", ["bf16", "f8"])
+def test_later_tokens_do_not_reach_earlier_rows(bad, cache):
+    """A token whose key or value is not finite changes the rows that see it and no other."""
+    if cache == "f8" and bad != bad:
+        fill = float("nan")
+    elif cache == "f8":
+        pytest.skip("the 8-bit type has no infinities")
+    else:
+        fill = bad
+    c = _case([(40, 100), (10, 3)], hq=8, hkv=2, d=128, cache=cache, stale=0.0)
+    s = _attend_inputs(c)
+    clean = _call(c, s)
+    at = 90  # position of the bad token in request 0: query 50 and later see it
+    b, o = int(s["table"][0, at // 16]), at % 16
+    for which in ("k", "v"):
+        x = s[which].float()
+        x[b, :, o, 5] = fill
+        t = dict(s)
+        t[which] = x.to(s[which].dtype)
+        got = _call(c, t)
+        assert torch.equal(got[:50], clean[:50]), which
+        assert torch.equal(got[100:], clean[100:]), which
+        ref = _reference(c, t)[0][50:100] if which == "v" else None
+        if which == "v":
+            g = f64(got[50:100])
+            assert np.array_equal(np.isnan(g), np.isnan(ref)) and np.array_equal(np.isinf(g), np.isinf(ref))
+            assert np.array_equal(g[np.isinf(g)], ref[np.isinf(ref)])
+        elif bad != bad:
+            assert torch.isnan(got[50:100]).all()
+
+
+def test_attention_strides_and_kept_buffers():
+    """Queries inside a fused projection, results into one, a wide table, a kept workspace, rows of no request."""
+    c = _case([(300, 30), (2000, 1), (20, 1)], hq=8, hkv=2, d=64)
+    s = _attend_inputs(c)
+    tokens = s["q"].shape[0]
+    fused = torch.zeros(tokens + 5, 12 * 64 + 32, dtype=torch.bfloat16, device=DEV)
+    fused[3:3 + tokens, 64:64 + 512] = s["q"].reshape(tokens, 512)
+    q = fused[:, 64:64 + 512].view(tokens + 5, 8, 64)
+    res = torch.full((tokens + 5, 9, 72), 7.0, dtype=torch.bfloat16, device=DEV)
+    out = res[:, 1:, 8:]
+    table = torch.full((3, s["table"].shape[1] + 9), 2 ** 30, dtype=torch.int32, device=DEV)
+    table[:, :s["table"].shape[1]] = dev(s["table"], torch.int32)
+    start = dev(s["start"] + 3, torch.int32)
+    need = S.kv_attention_workspace(tokens + 5, 8, 2, 64, 3, 30, 2001)
+    ws = torch.empty(need + 64, dtype=torch.uint8, device=DEV)
+    got = S.kv_attention(q, s["k"], s["v"], table[:, :s["table"].shape[1]], start, dev(s["seq"], torch.int32), 30, 2001,
+                         out=out, workspace=ws)
+    assert got is out
+    ref = _reference(c, s)
+    assert (np.abs(f64(out[3:3 + tokens]) - ref[0]) <= _bound(c, s, ref)).all()
+    res[3:3 + tokens, 1:, 8:] = 7.0
+    assert (res == 7.0).all()
+
+
+def test_attention_shares_blocks_between_requests():
+    """Two requests on the same prefix blocks (prefix caching)."""
+    c = _case([(160, 5), (160, 40)], hq=8, hkv=2, d=128)
+    s = _attend_inputs(c)
+    s["table"][1, :10] = s["table"][0, :10]
+    got, ref = f64(_call(c, s)), _reference(c, s)
+    assert (np.abs(got - ref[0]) <= _bound(c, s, ref)).all()
+
+
+def test_a_step_end_to_end_and_in_a_graph():
+    """Assign, write and attend on a stream of their own, eagerly and captured; every replay equals the eager result."""
+    rng = np.random.default_rng(11)
+    bs, hq, hkv, d = 16, 8, 2, 128
+    lens = [(40, 1), (0, 70), (13, 20), (200, 1)]
+    ctx, new = np.array([a for a, _ in lens]), np.array([n for _, n in lens])
+    used = -(-ctx // bs)
+    order = rng.permutation(60)
+    table = np.full((4, 20), -1)
+    at = 0
+    for r in range(4):
+        table[r, :used[r]] = order[at:at + used[r]]
+        at += used[r]
+    tokens, limit = int(new.sum()), int(new.sum()) + 8
+    kc0 = dev(rng.standard_normal((60, hkv, bs, d)), torch.bfloat16)
+    vc0 = dev(rng.standard_normal((60, hkv, bs, d)), torch.bfloat16)
+    qkv = dev(rng.standard_normal((limit, hq + 2 * hkv, d)), torch.bfloat16)
+    kc, vc, tab = kc0.clone(), vc0.clone(), dev(table, torch.int32)
+    args = dev(ctx, torch.int32), dev(new, torch.int32)
+    free = dev(order[at:], torch.int32)
+    batch = S.KVBatch(4, limit, DEV)
+    out = torch.zeros(limit, hq, d, dtype=torch.bfloat16, device=DEV)
+    need = S.kv_attention_workspace(limit, hq, hkv, d, 4, 70, 201)
+    ws = torch.empty(max(1, need), dtype=torch.uint8, device=DEV)
+
+    def step():
+        S.kv_assign(*args, tab, free, bs, limit, out=batch)
+        S.kv_write(qkv[:, hq:hq + hkv], qkv[:, hq + hkv:], batch.slots, kc, vc)
+        S.kv_attention(qkv[:, :hq], kc, vc, tab, batch.query_start, batch.seq_len, 70, 201, out=out, workspace=ws)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    want = kv.assign(ctx, new, table, order[at:], bs, limit)
+    np.testing.assert_array_equal(batch.slots.cpu().numpy(), want[4])
+    full_k = kv.write(f64(qkv[:, hq:hq + hkv]), want[4], f64(kc0), lambda y: y)
+    full_v = kv.write(f64(qkv[:, hq + hkv:]), want[4], f64(vc0), lambda y: y)
+    np.testing.assert_array_equal(f64(kc), full_k)
+    ref = kv.attention(f64(qkv[:, :hq]), full_k, full_v, want[0], want[1], want[2], d ** -0.5)
+    eager = out.clone()
+    b = kv.attention_bound(ref[0][:tokens], ref[1][:tokens], ref[2][:tokens], 201, d, 8, 8, 5.0)
+    assert (np.abs(f64(eager[:tokens]) - ref[0][:tokens]) <= b).all()
+    assert (eager[tokens:] == 0).all()  # rows of no request
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=side):
+        step()
+    for i in range(4):
+        kc.copy_(kc0)
+        vc.copy_(vc0)
+        tab.copy_(dev(table, torch.int32))
+        out.zero_()
+        batch.slots.fill_(-3)
+        if i == 2:
+            torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager), i
+        np.testing.assert_array_equal(f64(kc), full_k)
