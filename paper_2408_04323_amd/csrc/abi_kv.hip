@@ -190,7 +190,8 @@ int scoot_kv_attention(const void* q, scoot_kv_type type, int64_t num_tokens, in
   a.max_blocks = num_blocks > 0 ? max_blocks : 0;  // a cache without blocks holds no tokens
   a.block_shift = shift_of(block_size);
   a.window = window;
-  a.score_scale = scale * k_scale * 1.44269504088896340736f;
+  // The smallest positive float in the place of 0: it leaves nothing of a score, and -inf stays -inf.
+  a.score_scale = std::max(scale * k_scale * 1.44269504088896340736f, 1.4e-45f);
   a.v_scale = v_scale;
   a.workspace = workspace;
   return launch_kv_attention(a, type, cache_type, stream);

@@ -230,6 +230,12 @@ def _bound(c, s, ref, vmax=None):
     return kv.attention_bound(out, spread, reach, max(a + n for a, n in c["lens"]), c["d"], BITS[c["kind"]], bits, vmax)
 
 
+def _check(got, ref, bound):
+    off = np.abs(got - ref)
+    bad = ~(off <= bound)
+    assert not bad.any(), f"{bad.sum()} of {bad.size} values off, first at {np.argwhere(bad)[0].tolist()}, most {np.nanmax(off / bound):.3g} bounds"
+
+
 def _reference(c, s):
     return kv.attention(f64(s["q"]), f64(s["k"]) * s["ks"], f64(s["v"]) * s["vs"], s["table"], s["start"], s["seq"],
                         c["d"] ** -0.5 if c["scale"] is None else c["scale"], c["window"])
@@ -250,9 +256,8 @@ def test_attention_matches_oracle(name):
     s = _attend_inputs(c, seed=len(name))
     got = f64(_call(c, s))
     ref = _reference(c, s)
-    off = np.abs(got - ref[0])
     assert np.isfinite(ref[0]).all()
-    assert (off <= _bound(c, s, ref)).all(), float(np.nanmax(off / _bound(c, s, ref)))
+    _check(got, ref[0], _bound(c, s, ref))
 
 
 def test_attention_twice_is_the_same_bits():
@@ -272,7 +277,7 @@ def test_attention_rows_without_keys_are_zero():
     got, ref = f64(_call(c, s)), _reference(c, s)
     assert (ref[0][:3] == 0).all() and (ref[0][3] == 0).all() and (ref[0][5:20] == 0).all() and (ref[0][45] == 0).all()
     assert (got[:4] == 0).all() and (got[5:20] == 0).all() and (got[45] == 0).all()
-    assert (np.abs(got - ref[0]) <= _bound(c, s, ref)).all()
+    _check(got, ref[0], _bound(c, s, ref))
 
 
 def test_attention_skips_missing_blocks():
@@ -281,7 +286,7 @@ def test_attention_skips_missing_blocks():
     s["table"][0, [0, 7, 20]] = [-1, s["k"].shape[0], 2 ** 31 - 1]
     s["table"][1, [3, 4, 5, 6, 7, 16]] = -5
     got, ref = f64(_call(c, s)), _reference(c, s)
-    assert (np.abs(got - ref[0]) <= _bound(c, s, ref)).all()
+    _check(got, ref[0], _bound(c, s, ref))
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
@@ -335,7 +340,7 @@ def test_attention_strides_and_kept_buffers():
                          out=out, workspace=ws)
     assert got is out
     ref = _reference(c, s)
-    assert (np.abs(f64(out[3:3 + tokens]) - ref[0]) <= _bound(c, s, ref)).all()
+    _check(f64(out[3:3 + tokens]), ref[0], _bound(c, s, ref))
     res[3:3 + tokens, 1:, 8:] = 7.0
     assert (res == 7.0).all()
 
@@ -346,7 +351,7 @@ def test_attention_shares_blocks_between_requests():
     s = _attend_inputs(c)
     s["table"][1, :10] = s["table"][0, :10]
     got, ref = f64(_call(c, s)), _reference(c, s)
-    assert (np.abs(got - ref[0]) <= _bound(c, s, ref)).all()
+    _check(got, ref[0], _bound(c, s, ref))
 
 
 def test_a_step_end_to_end_and_in_a_graph():
@@ -392,7 +397,7 @@ def test_a_step_end_to_end_and_in_a_graph():
     ref = kv.attention(f64(qkv[:, :hq]), full_k, full_v, want[0], want[1], want[2], d ** -0.5)
     eager = out.clone()
     b = kv.attention_bound(ref[0][:tokens], ref[1][:tokens], ref[2][:tokens], 201, d, 8, 8, 5.0)
-    assert (np.abs(f64(eager[:tokens]) - ref[0][:tokens]) <= b).all()
+    _check(f64(eager[:tokens]), ref[0][:tokens], b)
     assert (eager[tokens:] == 0).all()  # rows of no request
     g = torch.cuda.CUDAGraph()
     with torch.cuda.graph(g, stream=side):
