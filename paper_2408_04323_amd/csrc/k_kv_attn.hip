@@ -20,7 +20,7 @@ using namespace kvattn;
 constexpr int64_t kSlots = 512;
 constexpr int kMinPart = 128;    // keys: a strip of 32 for each wave
 
-// Requests of at most 32 rows (new tokens x heads per key head) are items of
+// Requests of at most 16 rows (new tokens x heads per key head) are items of
 // their own; once some have more, tiles of 128 rows are.  Where the items do
 // not fill the chip four times over, their keys are split into parts, so many
 // that they do, of at least kMinPart keys.
@@ -28,7 +28,7 @@ Plan plan(int64_t num_tokens, int num_heads, int num_kv_heads, int num_seqs, int
   Plan p{};
   const int64_t G = num_heads / num_kv_heads;
   const int64_t longest = std::min<int64_t>(max_new_len, num_tokens);
-  p.mixed = longest * G > kRows;
+  p.mixed = longest * G > kFew;
   p.items = p.mixed ? num_tokens * G / kTileRows + num_seqs : num_seqs;
   int64_t keys = max_seq_len;
   if (window > 0) keys = std::min<int64_t>(keys, (int64_t)window + (p.mixed ? kTileRows / G : longest) + 32);
@@ -43,7 +43,7 @@ Plan plan(int64_t num_tokens, int num_heads, int num_kv_heads, int num_seqs, int
 }
 
 int64_t slots(const Plan& p, int num_kv_heads) {
-  return p.splits > 1 ? p.items * p.splits * num_kv_heads * (p.mixed ? kTileRows : kRows) : 0;
+  return p.splits > 1 ? p.items * p.splits * num_kv_heads * (p.mixed ? kTileRows : kFew) : 0;
 }
 }  // namespace
 

@@ -47,15 +47,15 @@ typedef short s4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
-constexpr int kRows = 32;                    // rows (queries) of a wave
-constexpr int kTileRows = kRows * kWaves;    // rows of a workgroup whose waves share the keys
+constexpr int kFew = 16;                     // rows of a request that one workgroup's waves handle together
+constexpr int kRows = 32;                    // rows of a wave otherwise,
+constexpr int kTileRows = kRows * kWaves;    // and of its workgroup
 constexpr float kNoScore = -3.0e38f;         // m before any key was seen; finite, so that m - m is 0
 constexpr float kSlack = 8.0f;               // m follows a larger score only past this
 
 constexpr int gcd256(int x) { return x % 256 == 0 ? 256 : x % 128 == 0 ? 128 : 64; }
 
-// Sizes of a cache row and of the permutations of its pieces.  Rows g apart
-// start on the same bank (256 bytes of LDS per cycle).
+// Sizes of a cache row in LDS.
 template <typename T_, bool F8_, int D_>
 struct Shape {
   typedef T_ T;
@@ -64,21 +64,39 @@ struct Shape {
   static constexpr int EB = F8 ? 1 : 2;
   static constexpr int RB = D * EB;                 // bytes of a row
   static constexpr int PC = RB / 16;                // 16-byte pieces of a row
-  static constexpr int g = 256 / gcd256(RB);
-  static constexpr int KM = 16 / g;                 // K: piece ^ (row / g % KM)
-  static constexpr int VU = 2 * EB;                 // V: pieces of 32 elements, permuted together:
-  static constexpr int VM = (8 / EB) / g;           //    32-element unit ^ (row / g % VM)
-  static constexpr int DT = D / 32;                 // tiles of O^T
-  static constexpr int KS = D / 16;                 // steps of the first product
+  static constexpr int g = 256 / gcd256(RB);        // rows this far apart start on the same bank
   static constexpr int NJ = RB / 64;                // loads of 1 KiB for 16 rows
   static constexpr int ST = D <= 128 ? 64 : 32;     // keys per strip of a shared tile
   static constexpr int SUB = ST / 32;
   static constexpr int kShared = 4 * ST * RB;       // two buffers of K and V
   static constexpr int kPrivate = kWaves * 64 * RB; // per wave one strip of 32 keys of K and V
-  static constexpr int kJoin = 2 * kRows * (D + 4) * 4;
+  static constexpr int kJoin = kWaves * kFew * (D + 4) * 4;
   // The second product runs in the cache's 16-bit type; 8-bit values are exact in half precision, which rounds the
   // weights eight times finer than bfloat16.
   typedef typename std::conditional<F8, _Float16, T>::type W;
+};
+
+// How the pieces of a row are permuted on the way into LDS.  A read instruction
+// takes one piece of 16 keys (K) or U pieces of 8 or 16 keys (V) per 256 bytes
+// that LDS delivers in a cycle; these keys, counted by kid() and vid(), must
+// hit different banks.  Keys g apart start on the same bank, so there the
+// piece (the unit of U pieces) is exchanged by XOR with the count.
+template <typename S>
+struct Tile32Order {  // 32 x 32 x 16 products
+  static constexpr int KM = 16 / S::g;
+  static constexpr int U = 2 * S::EB, VM = (8 / S::EB) / S::g;
+  static __device__ __forceinline__ constexpr int k(int key) { return key / S::g % KM; }
+  static __device__ __forceinline__ constexpr int v(int key) { return key / S::g % VM; }
+};
+template <typename S>
+struct Tile16Order {  // 16 x 16 x 32 products
+  static constexpr int KM = 16 / S::g;
+  static constexpr int U = S::EB, VM = (16 / S::EB) / S::g;
+  static constexpr uint32_t kNext = 128 / S::g;  // what the order of the next 16 keys differs by, in bytes
+  static __device__ __forceinline__ constexpr int k(int key) { return ((key & 3) | (key >> 1 & 12)) / S::g % KM; }
+  static __device__ __forceinline__ constexpr int v(int key) {
+    return (S::F8 ? key & 15 : (key & 3) | (key >> 1 & 4)) / S::g % VM;
+  }
 };
 
 template <typename T>
@@ -92,6 +110,8 @@ struct Vec<__bf16> {
 
 __device__ __forceinline__ f16v mfma(h8 a, h8 b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f16v mfma(b8 a, b8 b, f16v c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f4 mfma(h8 a, h8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f4 mfma(b8 a, b8 b, f4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
 // The key, of a strip's 32, that row r of the first product's left operand
 // holds: rows 4h .. 4h + 3 and 8 + 4h .. (the scores of the wave's half h) are
@@ -102,6 +122,9 @@ template <int N>
 __device__ __forceinline__ void wait_vm() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
+// All vector loads, in a form that the compiler takes note of: it then waits for none of them later, in a loop where
+// that would be a wait for the loads to LDS, too.
+__device__ __forceinline__ void settle() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // 64 lanes x 16 bytes from base + off to LDS at `to`, lane after lane; counted
@@ -115,7 +138,7 @@ __device__ __forceinline__ void load_lds(uint32_t to, uint64_t addr) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(addr) : "memory");
 }
 
-// What a workgroup works on: rows r0 .. r0 + 127 (or 31) of a request, one key
+// What a workgroup works on: rows row0 .. row0 + 127 (or 15) of a request, one key
 // head, keys [k0, k1) of the tile's, as split `split` of `splits`.
 struct Item {
   int64_t q0;       // token of the request's row 0
@@ -127,7 +150,7 @@ struct Item {
   int splits;       // parts that the tile's keys are in
   int split;
   int seq;
-  bool shared;      // the waves share the keys (more than kRows rows), else each wave takes strips of its own
+  bool shared;      // the waves share the keys (more than kFew rows), else each wave takes strips of its own
 };
 
 struct Plan {
@@ -184,7 +207,7 @@ __device__ __forceinline__ bool find_item(const KvAttnArgs& a, const Plan& p, in
   it.rows = rows > 0x7fffffff ? 0x7fffffff : (int)rows;
   it.seq = seq;
   it.len = (int)clamp64(len, 0, (int64_t)a.max_blocks << a.block_shift);
-  it.shared = p.mixed && rows > kRows;
+  it.shared = p.mixed && rows > kFew;
   int last_row = it.rows - 1;
   int splits = p.splits;
   if (it.shared) {
@@ -196,7 +219,7 @@ __device__ __forceinline__ bool find_item(const KvAttnArgs& a, const Plan& p, in
   } else {
     if (p.mixed && index != first) return false;
     it.row0 = 0;
-    if (it.rows > kRows) splits = 1;  // more rows than the caller announced: one workgroup, tile after tile
+    if (it.rows > kFew) splits = 1;  // more rows than the caller announced: one workgroup, tile after tile
   }
   // The tile's keys, and this split's part of them.
   const int64_t top = it.pos0 + last_row / G;
@@ -211,269 +234,6 @@ __device__ __forceinline__ bool find_item(const KvAttnArgs& a, const Plan& p, in
   it.k1 = split == it.splits - 1 ? end : it.k0 + p.part;
   return true;
 }
-
-// One wave's rows and what it knows of the keys.
-template <typename S>
-struct Wave {
-  typedef typename S::T T;
-  typedef typename S::W W;
-  typedef typename Vec<T>::v8 T8;
-  typedef typename Vec<W>::v8 W8;
-
-  int lane, half;
-  int hi, lo;              // this lane's row sees keys lo < k <= hi
-  int hi_min, hi_max, lo_max;  // over the wave's rows
-  T8 q[S::KS];
-  f16v o[S::DT];
-  float m, l;
-  int koff[S::KM / 2];     // LDS offsets of this lane's reads
-  int voff[S::VM];
-  uint32_t kdma[S::NJ], vdma[S::NJ];  // memory offsets of its loads
-
-  __device__ __forceinline__ void setup() {
-    lane = threadIdx.x & 63;
-    half = lane >> 5;
-    const int key = key_of_row(lane & 31);
-#pragma unroll
-    for (int n = 0; n < S::KM / 2; ++n) koff[n] = key * S::RB + (((2 * n + half) ^ (key / S::g % S::KM)) * 16);
-    const int n16 = lane & 15, dhalf = (lane >> 4) & 1;
-    const int row = 8 * half + (S::F8 ? n16 >> 1 : n16 >> 2);
-    const int in = S::F8 ? dhalf * 16 + (n16 & 1) * 8 : dhalf * 32 + (n16 & 3) * 8;
-#pragma unroll
-    for (int n = 0; n < S::VM; ++n) voff[n] = row * S::RB + (n ^ (row / S::g % S::VM)) * (16 * S::VU) + in;
-#pragma unroll
-    for (int j = 0; j < S::NJ; ++j) {
-      const int at = 64 * j + lane, r = at / S::PC, p = at % S::PC;
-      kdma[j] = (r & 7) * S::RB + (p ^ (r / S::g % S::KM)) * 16;
-      vdma[j] = (r & 7) * S::RB + (((p / S::VU) ^ (r / S::g % S::VM)) * S::VU + p % S::VU) * 16;
-    }
-  }
-
-  // Rows row0 .. row0 + 31 of the request (those past its last row repeat it; nothing of them is stored).
-  __device__ __forceinline__ void start(const KvAttnArgs& a, const Item& it, int row0, int head) {
-    const int G = a.num_heads / a.num_kv_heads;
-    int row = row0 + (lane & 31);
-    row = row < it.rows ? row : it.rows - 1;
-    const int tok = row / G, g = row - tok * G;
-    const int64_t pos = it.pos0 + tok;
-    hi = (int)clamp64(pos, -1, it.len - 1);
-    lo = a.window > 0 ? (int)clamp64(pos - a.window, -1, 0x7fffffff) : -1;
-    hi_min = hi_max = hi;
-    lo_max = lo;
-#pragma unroll
-    for (int x = 1; x < 32; x <<= 1) {
-      hi_min = min(hi_min, __shfl_xor(hi_min, x));
-      hi_max = max(hi_max, __shfl_xor(hi_max, x));
-      lo_max = max(lo_max, __shfl_xor(lo_max, x));
-    }
-    hi_min = uniform(hi_min);
-    hi_max = uniform(hi_max);
-    lo_max = uniform(lo_max);
-    const T* p = (const T*)a.q + (it.q0 + tok) * a.q_token_stride + (int64_t)(head * G + g) * a.q_head_stride;
-#pragma unroll
-    for (int s = 0; s < S::KS; ++s) {
-      const int d = S::F8 ? (2 * (s / 2) + half) * 16 + 8 * (s & 1) : (2 * s + half) * 8;
-      q[s] = *(const T8*)(p + d);
-    }
-#pragma unroll
-    for (int d = 0; d < S::DT; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
-    m = kNoScore;
-    l = 0.0f;
-  }
-
-  // The loads of 16 keys (two groups of eight, each inside a block) to LDS.
-  static __device__ __forceinline__ void load16(const uint32_t (&off)[S::NJ], uint32_t to, uint64_t b0, uint64_t b1) {
-#pragma unroll
-    for (int j = 0; j < S::NJ; ++j) {
-      constexpr int kHalf = 8 * S::PC;  // pieces of eight keys
-      if (64 * j + 63 < kHalf)
-        load_lds(to + 1024 * j, b0, off[j]);
-      else if (64 * j >= kHalf)
-        load_lds(to + 1024 * j, b1, off[j]);
-      else
-        load_lds(to + 1024 * j, (64 * j + (int)(threadIdx.x & 63) < kHalf ? b0 : b1) + off[j]);
-    }
-  }
-
-  // S^T of 32 keys.
-  __device__ __forceinline__ f16v scores(uint32_t lds) const {
-    f16v s;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
-    constexpr int N = S::KM / 2;
-    if constexpr (S::F8) {
-#pragma unroll
-      for (int u = 0; u < S::KS / 2; ++u) {
-        const i4 k = *(const SCOOT_LDS i4*)(lds + koff[u % N] + (u / N) * (16 * S::KM));
-#pragma unroll
-        for (int e = 0; e < 2; ++e) s = mfma(widen<T>(k[2 * e], k[2 * e + 1]), q[2 * u + e], s);
-      }
-    } else {
-#pragma unroll
-      for (int u = 0; u < S::KS; ++u) {
-        const T8 k = *(const SCOOT_LDS T8*)(lds + koff[u % N] + (u / N) * (16 * S::KM));
-        s = mfma(k, q[u], s);
-      }
-    }
-    return s;
-  }
-
-  // Eight 8-bit floats as 16-bit ones (exact).
-  template <typename R>
-  static __device__ __forceinline__ typename Vec<R>::v8 widen(int a, int b) {
-    typename Vec<R>::v8 r;
-    if constexpr (std::is_same<R, _Float16>::value) {
-      const h2 x[4] = {__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true),
-                       __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, true)};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) r[i] = x[i / 2][i % 2];
-    } else {
-      const b2 x[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true),
-                       __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true)};
-#pragma unroll
-      for (int i = 0; i < 8; ++i) r[i] = x[i / 2][i % 2];
-    }
-    return r;
-  }
-
-  // V^T: lane's element d = 32 dt + lane % 32 of the keys 16 ks + 8 half .. + 7.
-  __device__ __forceinline__ W8 values(uint32_t lds, int ks, int dt) const {
-    const uint32_t at = lds + voff[dt % S::VM] + (dt / S::VM) * (S::VM * 16 * S::VU) + ks * 16 * S::RB;
-    if constexpr (S::F8) {
-      const i2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((SCOOT_LDS i2*)at);
-      return widen<_Float16>(v[0], v[1]);
-    } else {
-      union {
-        s4 h[2];
-        W8 v;
-      } r;
-      r.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SCOOT_LDS s4*)at);
-      r.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SCOOT_LDS s4*)(at + 4 * S::RB));
-      return r.v;
-    }
-  }
-
-  // -inf for what a row does not see; `holes`: bits of the strip's groups of eight keys without a block.
-  __device__ __forceinline__ void mask(f16v& s, int key0, int holes) const {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int k = 16 * (i / 8) + 8 * half + (i & 7);
-      const int key = key0 + k;
-      if (key > hi || key <= lo || (holes >> (k / 8) & 1)) s[i] = -INFINITY;
-    }
-  }
-
-  // Weights of N strips of 32 keys, in place, rounded: m, l and o follow.
-  template <int N>
-  __device__ __forceinline__ void weights(f16v (&s)[N], float scale, W8 (&w)[2 * N]) {
-    float x = s[0][0];
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) x = fmaxf(x, s[n][i]);
-    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale;
-    if (__builtin_amdgcn_ballot_w64(x > m + kSlack)) {
-      const float up = x > m + kSlack ? x : m, f = __builtin_amdgcn_exp2f(m - up);  // no row's m depends on another row
-      m = up;
-      l *= f;
-#pragma unroll
-      for (int d = 0; d < S::DT; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] *= f;
-    }
-#pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-      for (int k = 0; k < 2; ++k) {
-        W8 r;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) r[i] = (W)__builtin_amdgcn_exp2f(fmaf(s[n][8 * k + i], scale, -m));
-        w[2 * n + k] = r;
-        // The sum takes the weights as rounded, like the product.
-#pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-          if constexpr (std::is_same<W, _Float16>::value) {
-            const h2 p = {r[i], r[i + 1]}, one = {(_Float16)1.0f, (_Float16)1.0f};
-            l = __builtin_amdgcn_fdot2(p, one, l, false);
-          } else {
-            const b2 p = {r[i], r[i + 1]}, one = {(__bf16)1.0f, (__bf16)1.0f};
-            l = __builtin_amdgcn_fdot2_f32_bf16(p, one, l, false);
-          }
-        }
-      }
-  }
-
-  template <int N>
-  __device__ __forceinline__ void product(uint32_t lds, const W8 (&w)[2 * N]) {
-#pragma unroll
-    for (int k = 0; k < 2 * N; ++k)
-#pragma unroll
-      for (int d = 0; d < S::DT; ++d) o[d] = mfma(values(lds, k, d), w[k], o[d]);
-  }
-
-  // The same where some rows do not see some keys: 0 * inf must not arise.
-  // What is not finite is taken out of the product, and rows with a weight on
-  // it get it back as what it is.
-  template <int N>
-  __device__ __forceinline__ void product_masked(uint32_t lds, const W8 (&w)[2 * N]) {
-    constexpr uint32_t kExp = std::is_same<W, _Float16>::value ? 0x7c00u : 0x7f80u;
-    constexpr uint32_t kOne = std::is_same<W, _Float16>::value ? 0x3c00u : 0x3f80u;
-#pragma unroll
-    for (int d = 0; d < S::DT; ++d) {
-#pragma unroll
-      for (int k = 0; k < 2 * N; ++k) {
-        union {
-          W8 v;
-          uint16_t u[8];
-          uint32_t w[4];
-        } x, y;
-        x.v = values(lds, k, d);
-        uint32_t bad = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          // all exponent bits set carries into the sign's place
-          const uint32_t e = x.w[i] & (kExp | kExp << 16);
-          bad |= (e + ((0x8000u - kExp) * 0x10001u)) & 0x80008000u;
-        }
-        if (__builtin_amdgcn_ballot_w64(bad != 0)) {
-#pragma unroll 1
-          for (int kind = 0; kind < 3; ++kind) {  // +inf, -inf, NaN
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const uint32_t u = x.u[i];
-              const bool is = kind == 0 ? u == kExp : kind == 1 ? u == (kExp | 0x8000u) : (u & 0x7fffu) > kExp;
-              y.u[i] = is ? kOne : 0;
-            }
-            f16v c;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) c[i] = 0.0f;
-            c = mfma(y.v, w[k], c);
-            const float add = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : __uint_as_float(0x7fc00000u);
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (!(c[i] == 0.0f)) o[d][i] += add;
-          }
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if ((x.u[i] & kExp) == kExp) x.u[i] = 0;
-        }
-        o[d] = mfma(x.v, w[k], o[d]);
-      }
-    }
-  }
-
-  // Whether the strip's keys need a mask, or are not seen at all.
-  __device__ __forceinline__ bool unseen(int key0) const { return key0 > hi_max; }
-  __device__ __forceinline__ bool partly(int key0, int n) const { return key0 + n - 1 > hi_min || key0 <= lo_max; }
-
-  __device__ __forceinline__ float row_sum() const {
-    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
-    return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-  }
-};
 
 // Blocks of the cache, as scalars.
 template <typename S>
@@ -494,14 +254,14 @@ struct Cache {
     shift = a.block_shift;
     last = a.max_blocks - 1;
   }
-  // Byte offset of eight keys from `key` on (inside one block).  An entry that names no block reads block 0, and the
-  // mask drops it.
-  __device__ __forceinline__ uint64_t at(int key) const {
-    int e = key >> shift;
-    e = e < last ? e : last;
-    uint32_t b = (uint32_t)table[e];
-    b = b < num_blocks ? b : 0;
-    return b * block_bytes + (uint64_t)(key & ((1 << shift) - 1)) * S::RB;
+  // The entry of eight keys from `key` on (inside one block), for at().
+  __device__ __forceinline__ uint32_t entry(int key) const {
+    const int e = key >> shift;
+    return (uint32_t)table[e < last ? e : last];
+  }
+  // Byte offset of these keys.  An entry that names no block reads block 0, and the mask drops it.
+  __device__ __forceinline__ uint64_t at(int key, uint32_t e) const {
+    return (e < num_blocks ? e : 0) * block_bytes + (uint64_t)(key & ((1 << shift) - 1)) * S::RB;
   }
   // Which of the four groups of eight keys from `key` on have no block.
   __device__ __forceinline__ int holes(int key) const {
@@ -513,42 +273,6 @@ struct Cache {
     return h;
   }
 };
-
-// Result rows of a wave: into `out`, or unscaled into the workspace.
-template <typename S>
-__device__ __forceinline__ void store_rows(const KvAttnArgs& a, const Wave<S>& w, const Item& it, int row0, int head, float m,
-                                           float l, int64_t slot, int slot_row, float* parts, float* stats, int tile_rows) {
-  typedef typename S::T T;
-  const int G = a.num_heads / a.num_kv_heads;
-  const int row = row0 + (w.lane & 31);
-  if (row >= it.rows) return;
-  if (it.splits > 1) {
-    const int64_t at = slot * tile_rows + slot_row + (w.lane & 31);
-    if (w.half == 0) *(float2*)(stats + at * 2) = make_float2(m, l);
-    float* p = parts + at * S::D;
-#pragma unroll
-    for (int d = 0; d < S::DT; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; i += 4) {
-        const f4 x = {w.o[d][i], w.o[d][i + 1], w.o[d][i + 2], w.o[d][i + 3]};
-        *(f4*)(p + 32 * d + 2 * i + 4 * w.half) = x;
-      }
-    return;
-  }
-  const float inv = l == 0.0f ? 0.0f : a.v_scale / l;  // a row that saw nothing has o = 0, too
-  const int tok = row / G, g = row - tok * G;
-  T* p = (T*)a.out + (it.q0 + tok) * a.out_token_stride + (int64_t)(head * G + g) * a.out_head_stride;
-  typedef T T4 __attribute__((ext_vector_type(4)));
-#pragma unroll
-  for (int d = 0; d < S::DT; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      T4 x;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] = (T)(w.o[d][i + j] * inv);
-      *(T4*)(p + 32 * d + 2 * i + 4 * w.half) = x;
-    }
-}
 
 // Whether any of the item's keys lies in an entry that names no block; `flag`:
 // a word of LDS for every wave.
@@ -563,13 +287,342 @@ __device__ __forceinline__ bool any_holes(const KvAttnArgs& a, const Item& it, i
   return uniform(flag[0] | flag[1] | flag[2] | flag[3]) != 0;
 }
 
-// More than 32 rows: the four waves take 32 rows each and share strips of keys
+
+// Eight 8-bit floats as 16-bit ones (exact).
+template <typename R>
+__device__ __forceinline__ typename Vec<R>::v8 widen(int a, int b) {
+  typename Vec<R>::v8 r;
+  if constexpr (std::is_same<R, _Float16>::value) {
+    const h2 x[4] = {__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true),
+                     __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, true)};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = x[i / 2][i % 2];
+  } else {
+    const b2 x[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true),
+                     __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true)};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = x[i / 2][i % 2];
+  }
+  return r;
+}
+
+// Eight weights 2^(scale s - m), rounded, and their sum added to l.  The sum
+// takes them as rounded, like the product.
+template <typename W, typename F>
+__device__ __forceinline__ typename Vec<W>::v8 eight_weights(F score, float scale, float m, float& l) {
+  typename Vec<W>::v8 r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = (W)__builtin_amdgcn_exp2f(fmaf(score(i), scale, -m));
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    if constexpr (std::is_same<W, _Float16>::value) {
+      const h2 p = {r[i], r[i + 1]}, one = {(_Float16)1.0f, (_Float16)1.0f};
+      l = __builtin_amdgcn_fdot2(p, one, l, false);
+    } else {
+      const b2 p = {r[i], r[i + 1]}, one = {(__bf16)1.0f, (__bf16)1.0f};
+      l = __builtin_amdgcn_fdot2_f32_bf16(p, one, l, false);
+    }
+  }
+  return r;
+}
+
+// Where some rows do not see some keys, 0 * inf must not arise: this takes out
+// of eight keys' values what is not finite, and `bad` tells if any of it lies
+// among the first `seen` keys (add_lost() then puts it back).
+template <typename W>
+__device__ __forceinline__ typename Vec<W>::v8 finite(typename Vec<W>::v8 v, int seen, uint32_t& bad) {
+  constexpr uint32_t kExp = (std::is_same<W, _Float16>::value ? 0x7c00u : 0x7f80u) * 0x10001u;
+  union {
+    typename Vec<W>::v8 v;
+    uint32_t w[4];
+  } x;
+  x.v = v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t real = (seen > 2 * i ? 0xffffu : 0u) | (seen > 2 * i + 1 ? 0xffff0000u : 0u);
+    // A full exponent carries into the sign's place; from there all over its half.
+    const uint32_t e = ((x.w[i] & kExp) + (0x80008000u - kExp)) & 0x80008000u;
+    const uint32_t full = e | (e - (e >> 15));
+    bad |= full & real;
+    x.w[i] &= ~full;
+  }
+  return x.v;
+}
+
+// Memory offsets of a lane's loads of 16 keys: its pieces, as they lie in LDS.
+template <typename S, typename Order>
+__device__ __forceinline__ void load_offsets(uint32_t (&k)[S::NJ], uint32_t (&v)[S::NJ]) {
+#pragma unroll
+  for (int j = 0; j < S::NJ; ++j) {
+    const int at = 64 * j + (int)(threadIdx.x & 63), key = at / S::PC, p = at % S::PC;
+    k[j] = (key & 7) * S::RB + (p ^ Order::k(key)) * 16;
+    v[j] = (key & 7) * S::RB + ((p / Order::U ^ Order::v(key)) * Order::U + p % Order::U) * 16;
+  }
+}
+
+// The loads of 16 keys (two groups of eight, each inside a block) to LDS.
+template <typename S, uint32_t X = 0>
+__device__ __forceinline__ void load16(const uint32_t (&off)[S::NJ], uint32_t to, uint64_t b0, uint64_t b1) {
+#pragma unroll
+  for (int j = 0; j < S::NJ; ++j) {
+    constexpr int kHalf = 8 * S::PC;  // pieces of eight keys
+    if (64 * j + 63 < kHalf)
+      load_lds(to + 1024 * j, b0, off[j] ^ X);
+    else if (64 * j >= kHalf)
+      load_lds(to + 1024 * j, b1, off[j] ^ X);
+    else
+      load_lds(to + 1024 * j, (64 * j + (int)(threadIdx.x & 63) < kHalf ? b0 : b1) + (off[j] ^ X));
+  }
+}
+
+// What `count` rows from row0 on see: a lane's row (row0 + r) keys lo < k <=
+// hi, and over the rows.  Positions grow with the rows.
+struct Sight {
+  int tok, g;  // token and head of the lane's row
+  int hi, lo, hi_min, hi_max, lo_max;
+
+  __device__ __forceinline__ void start(const KvAttnArgs& a, const Item& it, int row0, int r, int count) {
+    const int G = a.num_heads / a.num_kv_heads;
+    int row = row0 + r;  // rows past the request's last one repeat it; nothing of them is stored
+    row = row < it.rows ? row : it.rows - 1;
+    tok = row / G;
+    g = row - tok * G;
+    const int first = uniform((row0 < it.rows ? row0 : it.rows - 1) / G);
+    const int last = uniform((row0 + count < it.rows ? row0 + count - 1 : it.rows - 1) / G);
+    hi = upto(it, tok);
+    lo = after(a, it, tok);
+    hi_min = upto(it, first);
+    hi_max = upto(it, last);
+    lo_max = after(a, it, last);
+  }
+  static __device__ __forceinline__ int upto(const Item& it, int tok) { return (int)clamp64(it.pos0 + tok, -1, it.len - 1); }
+  static __device__ __forceinline__ int after(const KvAttnArgs& a, const Item& it, int tok) {
+    return a.window > 0 ? (int)clamp64(it.pos0 + tok - a.window, -1, 0x7fffffff) : -1;
+  }
+  // Strips of `keys` keys from k0 on that every row sees whole: [u0, u1).
+  __device__ __forceinline__ void whole(const Item& it, int strips, int keys, bool holes, int& u0, int& u1) const {
+    u0 = u1 = strips;
+    if (holes) return;
+    u1 = hi_min + 1 > it.k0 ? min((hi_min + 1 - it.k0) / keys, strips) : 0;
+    u0 = lo_max + 1 > it.k0 ? (lo_max + 1 - it.k0 + keys - 1) / keys : 0;
+  }
+};
+
+// Value d of the key's row as it is stored.
+template <typename S>
+__device__ __forceinline__ float stored(uint64_t row, int d) {
+  if constexpr (S::F8) return __builtin_amdgcn_cvt_f32_fp8((int)((const uint8_t*)row)[d], 0);
+  else return (float)((const typename S::W*)row)[d];
+}
+
+// ------------------------------------------------------------- shared tiles
+//
+// More than 16 rows: the four waves take 32 rows each and share strips of keys
 // through two LDS buffers.
+template <typename S>
+struct Tile32 {
+  typedef typename S::T T;
+  typedef typename S::W W;
+  typedef typename Vec<T>::v8 T8;
+  typedef typename Vec<W>::v8 W8;
+  typedef Tile32Order<S> Order;
+  static constexpr int KS = S::D / 16;  // steps of the first product
+  static constexpr int DT = S::D / 32;  // tiles of O^T
+
+  int lane, half;
+  Sight see;
+  T8 q[KS];
+  f16v o[DT];
+  float m, l;
+  int koff[Order::KM / 2];  // LDS offsets of this lane's reads
+  int voff[Order::VM];
+  uint32_t kdma[S::NJ], vdma[S::NJ];
+
+  __device__ __forceinline__ void setup() {
+    lane = threadIdx.x & 63;
+    half = lane >> 5;
+    const int key = key_of_row(lane & 31);
+#pragma unroll
+    for (int n = 0; n < Order::KM / 2; ++n) koff[n] = key * S::RB + ((2 * n + half) ^ Order::k(key)) * 16;
+    const int n16 = lane & 15, dhalf = (lane >> 4) & 1;
+    const int row = 8 * half + (S::F8 ? n16 >> 1 : n16 >> 2);
+    const int in = S::F8 ? dhalf * 16 + (n16 & 1) * 8 : dhalf * 32 + (n16 & 3) * 8;
+#pragma unroll
+    for (int n = 0; n < Order::VM; ++n) voff[n] = row * S::RB + (n ^ Order::v(row)) * (16 * Order::U) + in;
+    load_offsets<S, Order>(kdma, vdma);
+  }
+
+  __device__ __forceinline__ void start(const KvAttnArgs& a, const Item& it, int row0, int head) {
+    see.start(a, it, row0, lane & 31, kRows);
+    const int G = a.num_heads / a.num_kv_heads;
+    const T* p = (const T*)a.q + (it.q0 + see.tok) * a.q_token_stride + (int64_t)(head * G + see.g) * a.q_head_stride;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int d = S::F8 ? (2 * (s / 2) + half) * 16 + 8 * (s & 1) : (2 * s + half) * 8;
+      q[s] = *(const T8*)(p + d);
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    m = kNoScore;
+    l = 0.0f;
+  }
+
+  // S^T of 32 keys.
+  __device__ __forceinline__ f16v scores(uint32_t lds) const {
+    f16v s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+    constexpr int N = Order::KM / 2;
+    if constexpr (S::F8) {
+#pragma unroll
+      for (int u = 0; u < KS / 2; ++u) {
+        const i4 k = *(const SCOOT_LDS i4*)(lds + koff[u % N] + (u / N) * (16 * Order::KM));
+#pragma unroll
+        for (int e = 0; e < 2; ++e) s = mfma(widen<T>(k[2 * e], k[2 * e + 1]), q[2 * u + e], s);
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < KS; ++u) {
+        const T8 k = *(const SCOOT_LDS T8*)(lds + koff[u % N] + (u / N) * (16 * Order::KM));
+        s = mfma(k, q[u], s);
+      }
+    }
+    return s;
+  }
+
+  // V^T: lane's element d = 32 dt + lane % 32 of the keys 16 ks + 8 half .. + 7.
+  __device__ __forceinline__ W8 values(uint32_t lds, int ks, int dt) const {
+    const uint32_t at = lds + voff[dt % Order::VM] + (dt / Order::VM) * (Order::VM * 16 * Order::U) + ks * 16 * S::RB;
+    if constexpr (S::F8) {
+      const i2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((SCOOT_LDS i2*)at);
+      return widen<_Float16>(v[0], v[1]);
+    } else {
+      union {
+        s4 h[2];
+        W8 v;
+      } r;
+      r.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SCOOT_LDS s4*)at);
+      r.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SCOOT_LDS s4*)(at + 4 * S::RB));
+      return r.v;
+    }
+  }
+
+  // -inf for what a row does not see; `holes`: bits of the strip's groups of eight keys without a block.
+  __device__ __forceinline__ void mask(f16v& s, int key0, int holes) const {
+    const int first = key0 + 8 * half;
+    const int h = see.hi - first, l = see.lo - first;  // no underflow: hi, lo >= -1 and keys are below 2^31
+    holes >>= half;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int k = 16 * (i / 8) + (i & 7);
+      // bit operations and a select: a branch that differs between lanes here would cost copies of o in the whole loop
+      const bool hidden = (k > h) | (k <= l) | ((holes & (i < 8 ? 1 : 4)) != 0);
+      s[i] = hidden ? -INFINITY : s[i];
+    }
+  }
+
+  // Weights of a strip; m, l and o follow.
+  __device__ __forceinline__ void weights(const f16v (&s)[S::SUB], float scale, W8 (&w)[2 * S::SUB]) {
+    float x = s[0][0];
+#pragma unroll
+    for (int n = 0; n < S::SUB; ++n)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x = fmaxf(x, s[n][i]);
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale;
+    if (__builtin_amdgcn_ballot_w64(x > m + kSlack)) {
+      const float up = x > m + kSlack ? x : m, f = __builtin_amdgcn_exp2f(m - up);  // no row's m depends on another row
+      m = up;
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] *= f;
+    }
+#pragma unroll
+    for (int k = 0; k < 2 * S::SUB; ++k)
+      w[k] = eight_weights<W>([&](int i) { return s[k / 2][8 * (k & 1) + i]; }, scale, m, l);
+  }
+
+  __device__ __forceinline__ void product(uint32_t lds, const W8 (&w)[2 * S::SUB]) {
+#pragma unroll
+    for (int k = 0; k < 2 * S::SUB; ++k)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) o[d] = mfma(values(lds, k, d), w[k], o[d]);
+  }
+  __device__ __forceinline__ void product_finite(uint32_t lds, const W8 (&w)[2 * S::SUB], int key0, uint32_t& bad) {
+#pragma unroll
+    for (int k = 0; k < 2 * S::SUB; ++k)
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+        o[d] = mfma(finite<W>(values(lds, k, d), see.hi_max + 1 - (key0 + 16 * k + 8 * half), bad), w[k], o[d]);
+  }
+
+  // Adds the values that product_finite() left out, at the keys k0 .. k1 - 1,
+  // to the rows that see them: a sum with an infinity or a NaN in it.
+  __device__ __forceinline__ void add_lost(const Cache<S>& c, int k0, int k1) {
+#pragma unroll 1
+    for (int key = k0; key < k1 && key <= see.hi_max; ++key) {
+      const uint32_t e = c.entry(key);
+      if (e >= c.num_blocks) continue;
+      const bool mine = (key <= see.hi) & (key > see.lo);
+      const uint64_t row = c.v + c.at(key, e);
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float x = stored<S>(row, 32 * d + 8 * (i / 4) + 4 * half + i % 4);
+          o[d][i] += mine & !(__builtin_fabsf(x) < INFINITY) ? x : 0.0f;
+        }
+    }
+  }
+
+  __device__ __forceinline__ float row_sum() const {
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  }
+
+  // Result rows: into `out`, or unscaled into the workspace (row `at` on).
+  __device__ __forceinline__ void store(const KvAttnArgs& a, const Item& it, int row0, int head, int64_t at, float* parts,
+                                        float* stats) const {
+    const float sum = row_sum();
+    if (row0 + (lane & 31) >= it.rows) return;
+    if (it.splits > 1) {
+      at += lane & 31;
+      if (half == 0) *(float2*)(stats + at * 2) = make_float2(m, sum);
+      float* p = parts + at * S::D + 4 * half;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const f4 x = {o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
+          *(f4*)(p + 32 * d + 2 * i) = x;
+        }
+      return;
+    }
+    const float inv = sum == 0.0f ? 0.0f : a.v_scale / sum;  // a row that saw nothing has o = 0, too
+    const int G = a.num_heads / a.num_kv_heads;
+    T* p = (T*)a.out + (it.q0 + see.tok) * a.out_token_stride + (int64_t)(head * G + see.g) * a.out_head_stride + 4 * half;
+    typedef T T4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        T4 x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = (T)(o[d][i + j] * inv);
+        *(T4*)(p + 32 * d + 2 * i) = x;
+      }
+  }
+};
+
 template <typename S>
 __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it, int head, uint32_t lds, int* flag,
                                             int64_t slot, float* parts, float* stats) {
   const int wave = uniform(threadIdx.x >> 6);
-  Wave<S> w;
+  Tile32<S> w;
   Cache<S> c;
   w.setup();
   c.setup(a, it.seq, head);
@@ -577,56 +630,250 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
   const int strips = (it.k1 - it.k0 + S::ST - 1) / S::ST;
 
   // A strip's loads in groups of 16 keys of K or V; every wave takes its share.
-  auto load = [&](int strip) {
-    const uint32_t to = lds + (strip & 1) * (2 * kHalf);
-    const int key0 = it.k0 + strip * S::ST;
-    if constexpr (S::SUB == 2) {
-      const int key = key0 + 16 * wave;
-      const uint64_t b0 = c.at(key), b1 = c.at(key + 8);
-      Wave<S>::load16(w.kdma, to + wave * 16 * S::RB, c.k + b0, c.k + b1);
-      Wave<S>::load16(w.vdma, to + kHalf + wave * 16 * S::RB, c.v + b0, c.v + b1);
-    } else {
-      const int part = wave & 1;
-      const int key = key0 + 16 * part;
-      const uint64_t b0 = c.at(key), b1 = c.at(key + 8);
-      if (wave < 2) Wave<S>::load16(w.kdma, to + part * 16 * S::RB, c.k + b0, c.k + b1);
-      else Wave<S>::load16(w.vdma, to + kHalf + part * 16 * S::RB, c.v + b0, c.v + b1);
-    }
+  const int share = S::SUB == 2 ? wave : wave & 1;
+  struct Entries {
+    uint32_t e0, e1;
+  };
+  auto entries = [&](int strip) {
+    const int key = it.k0 + strip * S::ST + 16 * share;
+    return Entries{c.entry(key), c.entry(key + 8)};
+  };
+  auto load = [&](int strip, const Entries& e) {
+    const uint32_t to = lds + (strip & 1) * (2 * kHalf) + share * 16 * S::RB;
+    const int key = it.k0 + strip * S::ST + 16 * share;
+    const uint64_t b0 = c.at(key, e.e0), b1 = c.at(key + 8, e.e1);
+    if (S::SUB == 2 || wave < 2) load16<S>(w.kdma, to, c.k + b0, c.k + b1);
+    if (S::SUB == 2 || wave >= 2) load16<S>(w.vdma, to + kHalf, c.v + b0, c.v + b1);
   };
 
-  if (strips > 0) load(0);
-  w.start(a, it, it.row0 + wave * kRows, head);
+  Entries next{};
+  if (strips > 0) {
+    next = entries(0);
+    load(0, next);
+    next = entries(1);
+  }
+  const int row0 = it.row0 + wave * kRows;
+  w.start(a, it, row0, head);
   const bool holes = any_holes(a, it, flag);
-  for (int strip = 0; strip < strips; ++strip) {
+  settle();
+  int u0, u1;
+  w.see.whole(it, strips, S::ST, holes, u0, u1);
+
+  auto turn = [&](int strip) {
     // This strip has landed, for every wave, and everyone is done with the other buffer.
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (strip + 1 < strips) load(strip + 1);
-    const uint32_t at = lds + (strip & 1) * (2 * kHalf);
-    const int key0 = it.k0 + strip * S::ST;
-    if (w.unseen(key0)) continue;
-    f16v s[S::SUB];
-#pragma unroll
-    for (int n = 0; n < S::SUB; ++n) s[n] = w.scores(at + n * 32 * S::RB);
-    typename Wave<S>::W8 p[2 * S::SUB];
-    const bool masked = holes || w.partly(key0, S::ST);
-    if (masked) {
-#pragma unroll
-      for (int n = 0; n < S::SUB; ++n) w.mask(s[n], key0 + 32 * n, holes ? c.holes(key0 + 32 * n) : 0);
+    if (strip + 1 < strips) {
+      load(strip + 1, next);
+      next = entries(strip + 2);
     }
-    w.template weights<S::SUB>(s, a.score_scale, p);
-    if (masked) w.template product_masked<S::SUB>(at + kHalf, p);
-    else w.template product<S::SUB>(at + kHalf, p);
+  };
+  uint32_t bad = 0;
+  int strip = 0;
+  while (strip < strips) {
+    if (strip >= u0 && strip < u1) {
+      for (; strip < u1; ++strip) {
+        turn(strip);
+        const uint32_t at = lds + (strip & 1) * (2 * kHalf);
+        f16v s[S::SUB];
+#pragma unroll
+        for (int n = 0; n < S::SUB; ++n) s[n] = w.scores(at + n * 32 * S::RB);
+        typename Tile32<S>::W8 p[2 * S::SUB];
+        w.weights(s, a.score_scale, p);
+        w.product(at + kHalf, p);
+      }
+    } else {
+      turn(strip);
+      const uint32_t at = lds + (strip & 1) * (2 * kHalf);
+      const int key0 = it.k0 + strip * S::ST;
+      if (key0 <= w.see.hi_max) {
+        f16v s[S::SUB];
+#pragma unroll
+        for (int n = 0; n < S::SUB; ++n) {
+          s[n] = w.scores(at + n * 32 * S::RB);
+          w.mask(s[n], key0 + 32 * n, holes ? c.holes(key0 + 32 * n) : 0);
+        }
+        typename Tile32<S>::W8 p[2 * S::SUB];
+        w.weights(s, a.score_scale, p);
+        w.product_finite(at + kHalf, p, key0, bad);
+      }
+      ++strip;
+    }
   }
-  store_rows<S>(a, w, it, it.row0 + wave * kRows, head, w.m, w.row_sum(), slot, wave * kRows, parts, stats, kTileRows);
+  if (__builtin_amdgcn_ballot_w64(bad != 0)) {  // the strips that went through the mask
+    w.add_lost(c, it.k0, u0 < u1 ? it.k0 + u0 * S::ST : it.k1);
+    if (u0 < u1) w.add_lost(c, it.k0 + u1 * S::ST, it.k1);
+  }
+  w.store(a, it, row0, head, slot * kTileRows + wave * kRows, parts, stats);
 }
 
-// At most 32 rows: every wave takes strips of 32 keys of its own, through LDS
-// of its own, and the waves' results are joined at the end.
+// --------------------------------------------------------------- few rows
+//
+// At most 16 rows: bytes bound this, so the products are the smaller ones (16 x
+// 16 x 32), and no wave waits for another: each takes strips of 32 keys of its
+// own, through LDS of its own, and the results are joined at the end.
 template <typename S>
-__device__ __forceinline__ void private_rows(const KvAttnArgs& a, const Item& it, int row0, int head, uint32_t lds, char* smem, int* flag,
-                                             int64_t slot, float* parts, float* stats, int tile_rows) {
+struct Tile16 {
+  typedef typename S::T T;
+  typedef typename S::W W;
+  typedef typename Vec<T>::v8 T8;
+  typedef typename Vec<W>::v8 W8;
+  typedef Tile16Order<S> Order;
+  static constexpr int KS = S::D / 32;  // steps of the first product
+  static constexpr int DT = S::D / 16;  // tiles of O^T
+  static constexpr int KN = Order::KM / 4;
+
+  int lane, quad;  // quad: the wave's quarter, which holds the scores of eight keys
+  Sight see;
+  T8 q[KS];
+  f4 o[DT];
+  float m, l;
+  int koff[KN];
+  int voff[Order::VM];
+  uint32_t kdma[S::NJ], vdma[S::NJ];
+
+  // Row r of the first product's tile t is key 8 (r / 4) + 4 t + r % 4: quad q gets the keys 8 q .. 8 q + 7.
+  __device__ __forceinline__ void setup() {
+    lane = threadIdx.x & 63;
+    quad = lane >> 4;
+    const int n16 = lane & 15;
+    const int key = 8 * (n16 >> 2) + (n16 & 3);
+#pragma unroll
+    for (int n = 0; n < KN; ++n) koff[n] = key * S::RB + ((4 * n + quad) ^ Order::k(key)) * 16;
+    const int row = 8 * quad + (S::F8 ? n16 >> 1 : n16 >> 2);
+    const int in = S::F8 ? (n16 & 1) * 8 : (n16 & 3) * 8;
+#pragma unroll
+    for (int n = 0; n < Order::VM; ++n) voff[n] = row * S::RB + (n ^ Order::v(row)) * (16 * Order::U) + in;
+    load_offsets<S, Order>(kdma, vdma);
+  }
+
+  // A 16-byte piece holds eight or (in 8 bits) sixteen values of a key: piece 4 s + quad for step s, or for the steps
+  // 2 s and 2 s + 1.
+  __device__ __forceinline__ void start(const KvAttnArgs& a, const Item& it, int row0, int head) {
+    see.start(a, it, row0, lane & 15, kFew);
+    const int G = a.num_heads / a.num_kv_heads;
+    const T* p = (const T*)a.q + (it.q0 + see.tok) * a.q_token_stride + (int64_t)(head * G + see.g) * a.q_head_stride;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const int d = S::F8 ? (4 * (s / 2) + quad) * 16 + 8 * (s & 1) : (4 * s + quad) * 8;
+      q[s] = *(const T8*)(p + d);
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[d][i] = 0.0f;
+    m = kNoScore;
+    l = 0.0f;
+  }
+
+  // S^T of 32 keys: s[t][i] is key 8 quad + 4 t + i.
+  __device__ __forceinline__ void scores(uint32_t lds, f4 (&s)[2]) const {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[t][i] = 0.0f;
+      constexpr int N = S::F8 ? KS / 2 : KS;
+#pragma unroll
+      for (int u = 0; u < N; ++u) {
+        const uint32_t at = lds + koff[u % KN] + (u / KN) * (64 * KN) + 4 * t * S::RB;
+        if constexpr (S::F8) {
+          const i4 k = *(const SCOOT_LDS i4*)at;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) s[t] = mfma(widen<T>(k[2 * e], k[2 * e + 1]), q[2 * u + e], s[t]);
+        } else {
+          s[t] = mfma(*(const SCOOT_LDS T8*)at, q[u], s[t]);
+        }
+      }
+    }
+  }
+
+  // V^T: lane's element d = 16 dt + lane % 16 of the keys 8 quad .. + 7.
+  __device__ __forceinline__ W8 values(uint32_t lds, int dt) const {
+    const uint32_t at = lds + voff[dt % Order::VM] + (dt / Order::VM) * (Order::VM * 16 * Order::U);
+    if constexpr (S::F8) {
+      const i2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((SCOOT_LDS i2*)at);
+      return widen<_Float16>(v[0], v[1]);
+    } else {
+      union {
+        s4 h[2];
+        W8 v;
+      } r;
+      r.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SCOOT_LDS s4*)at);
+      r.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SCOOT_LDS s4*)(at + 4 * S::RB));
+      return r.v;
+    }
+  }
+
+  __device__ __forceinline__ void mask(f4 (&s)[2], int key0, int holes) const {
+    const int first = key0 + 8 * quad;
+    const int h = see.hi - first, l = see.lo - first;
+    const bool none = (holes >> quad & 1) != 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const bool hidden = (k > h) | (k <= l) | none;
+      s[k / 4][k % 4] = hidden ? -INFINITY : s[k / 4][k % 4];
+    }
+  }
+
+  __device__ __forceinline__ W8 weights(const f4 (&s)[2], float scale) {
+    float x = s[0][0];
+#pragma unroll
+    for (int k = 1; k < 8; ++k) x = fmaxf(x, s[k / 4][k % 4]);
+    auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+    sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale;
+    if (__builtin_amdgcn_ballot_w64(x > m + kSlack)) {
+      const float up = x > m + kSlack ? x : m, f = __builtin_amdgcn_exp2f(m - up);
+      m = up;
+      l *= f;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[d][i] *= f;
+    }
+    return eight_weights<W>([&](int i) { return s[i / 4][i % 4]; }, scale, m, l);
+  }
+
+  __device__ __forceinline__ void product(uint32_t lds, W8 w) {
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[d] = mfma(values(lds, d), w, o[d]);
+  }
+  __device__ __forceinline__ void product_finite(uint32_t lds, W8 w, int key0, uint32_t& bad) {
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[d] = mfma(finite<W>(values(lds, d), see.hi_max + 1 - (key0 + 8 * quad), bad), w, o[d]);
+  }
+
+  __device__ __forceinline__ void add_lost(const Cache<S>& c, int k0, int k1) {
+#pragma unroll 1
+    for (int key = k0; key < k1 && key <= see.hi_max; ++key) {
+      const uint32_t e = c.entry(key);
+      if (e >= c.num_blocks) continue;
+      const bool mine = (key <= see.hi) & (key > see.lo);
+      const uint64_t row = c.v + c.at(key, e);
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float x = stored<S>(row, 16 * d + 4 * quad + i);
+          o[d][i] += mine & !(__builtin_fabsf(x) < INFINITY) ? x : 0.0f;
+        }
+    }
+  }
+
+  __device__ __forceinline__ float row_sum() const {
+    auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(l), __float_as_uint(l), false, false);
+    const float x = __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+    sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+  }
+};
+
+template <typename S>
+__device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, int row0, int head, uint32_t lds, char* smem,
+                                         float* ml, int* flag, int64_t slot_row, float* parts, float* stats) {
+  typedef typename S::T T;
   const int wave = uniform(threadIdx.x >> 6);
-  Wave<S> w;
+  Tile16<S> w;
   Cache<S> c;
   w.setup();
   c.setup(a, it.seq, head);
@@ -634,102 +881,130 @@ __device__ __forceinline__ void private_rows(const KvAttnArgs& a, const Item& it
   const uint32_t kat = lds + wave * (2 * kHalf), vat = kat + kHalf;
   const int strips = (it.k1 - it.k0 + 31) / 32;
 
+  struct Entries {
+    uint32_t e[4];
+  };
   struct Base {
     uint64_t b[4];
   };
-  auto base = [&](int strip) {
-    Base r;
+  auto entries = [&](int strip) {
+    Entries r;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) r.b[j] = c.at(it.k0 + strip * 32 + 8 * j);
+    for (int j = 0; j < 4; ++j) r.e[j] = c.entry(it.k0 + strip * 32 + 8 * j);
     return r;
   };
-  auto load = [&](const uint32_t (&off)[S::NJ], uint32_t to, uint64_t from, const Base& b) {
-    Wave<S>::load16(off, to, from + b.b[0], from + b.b[1]);
-    Wave<S>::load16(off, to + 16 * S::RB, from + b.b[2], from + b.b[3]);
+  auto base = [&](int strip, const Entries& e) {
+    Base r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r.b[j] = c.at(it.k0 + strip * 32 + 8 * j, e.e[j]);
+    return r;
+  };
+  auto load_k = [&](const Base& b) {
+    load16<S>(w.kdma, kat, c.k + b.b[0], c.k + b.b[1]);
+    load16<S, Tile16Order<S>::kNext>(w.kdma, kat + 16 * S::RB, c.k + b.b[2], c.k + b.b[3]);
+  };
+  auto load_v = [&](const Base& b) {
+    load16<S>(w.vdma, vat, c.v + b.b[0], c.v + b.b[1]);
+    load16<S>(w.vdma, vat + 16 * S::RB, c.v + b.b[2], c.v + b.b[3]);
   };
 
   int strip = wave;
-  Base b{};
+  Entries next{};
   if (strip < strips) {
-    b = base(strip);
-    load(w.kdma, kat, c.k, b);
-    load(w.vdma, vat, c.v, b);
+    next = entries(strip);
+    const Base b = base(strip, next);
+    load_k(b);
+    load_v(b);
+    next = entries(strip + kWaves);
   }
   w.start(a, it, row0, head);
   const bool holes = any_holes(a, it, flag);
-  for (; strip < strips; strip += kWaves) {
+  settle();
+  int u0, u1;  // strips seen whole by every row
+  w.see.whole(it, strips, 32, holes, u0, u1);
+
+  uint32_t bad = 0;
+  auto step = [&](auto masked) {
+    constexpr bool kMasked = decltype(masked)::value;
     const bool more = strip + kWaves < strips;
     const int key0 = it.k0 + strip * 32;
-    b = base(strip + kWaves);
+    Base b{};
     wait_vm<2 * S::NJ>();  // the keys, not the values behind them
-    f16v s[1] = {w.scores(kat)};
+    f4 s[2];
+    w.scores(kat, s);
     wait_lds();
-    if (more) load(w.kdma, kat, c.k, b);
-    const bool masked = holes || w.partly(key0, 32);
-    if (masked) w.mask(s[0], key0, holes ? c.holes(key0) : 0);
-    typename Wave<S>::W8 p[2];
-    w.template weights<1>(s, a.score_scale, p);
+    if (more) {
+      b = base(strip + kWaves, next);
+      next = entries(strip + 2 * kWaves);
+      load_k(b);
+    }
+    if (kMasked) w.mask(s, key0, holes ? c.holes(key0) : 0);
+    const typename Tile16<S>::W8 p = w.weights(s, a.score_scale);
     if (more) wait_vm<2 * S::NJ>();
     else wait_vm<0>();
-    if (masked) w.template product_masked<1>(vat, p);
-    else w.template product<1>(vat, p);
+    if (kMasked) w.product_finite(vat, p, key0, bad);
+    else w.product(vat, p);
     wait_lds();
-    if (more) load(w.vdma, vat, c.v, b);
+    if (more) load_v(b);
+    strip += kWaves;
+  };
+  while (strip < strips) {
+    if (strip >= u0 && strip < u1) {
+      while (strip < u1) step(std::false_type{});
+    } else {
+      step(std::true_type{});
+    }
+  }
+  if (__builtin_amdgcn_ballot_w64(bad != 0)) {
+    for (strip = wave; strip < strips; strip += kWaves)
+      if (strip < u0 || strip >= u1) w.add_lost(c, it.k0 + strip * 32, min(it.k0 + strip * 32 + 32, it.k1));
   }
 
-  // Join the waves: 2, 3 into 0, 1, then 1 into 0.
-  float m = w.m, l = w.row_sum();
-  float* ml = (float*)(smem + (S::kPrivate > S::kJoin ? S::kPrivate : S::kJoin));
+  // Join the waves, in their order.
+  const float sum = w.row_sum();
   __syncthreads();
-  if (w.half == 0) {
-    ml[(wave * 32 + w.lane) * 2] = m;
-    ml[(wave * 32 + w.lane) * 2 + 1] = l;
+  if (w.quad == 0) *(float2*)(ml + (wave * kFew + w.lane) * 2) = make_float2(w.m, sum);
+  constexpr int kRow = S::D + 4;  // floats of a row, off by 16 bytes so that rows start on different banks
+  float* mine = (float*)smem + (wave * kFew + (w.lane & 15)) * kRow + 4 * w.quad;
+#pragma unroll
+  for (int d = 0; d < Tile16<S>::DT; ++d) *(f4*)(mine + 16 * d) = w.o[d];
+  __syncthreads();
+  const int G = a.num_heads / a.num_kv_heads;
+  const int rows = min(kFew, it.rows - row0);
+  for (int i = threadIdx.x; i < rows * (S::D / 4); i += kThreads) {
+    const int r = i / (S::D / 4), d = i % (S::D / 4) * 4;
+    float top = kNoScore, l = 0.0f;
+    f4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) top = fmaxf(top, ml[(v * kFew + r) * 2]);
+#pragma unroll
+    for (int v = 0; v < kWaves; ++v) {
+      const float f = __builtin_amdgcn_exp2f(ml[(v * kFew + r) * 2] - top);
+      l += f * ml[(v * kFew + r) * 2 + 1];
+      const f4 x = *(const f4*)((const float*)smem + (v * kFew + r) * kRow + d);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) o[j] += f * x[j];
+    }
+    if (it.splits > 1) {
+      if (d == 0) *(float2*)(stats + (slot_row + r) * 2) = make_float2(top, l);
+      *(f4*)(parts + (slot_row + r) * S::D + d) = o;
+    } else {
+      const float inv = l == 0.0f ? 0.0f : a.v_scale / l;
+      const int row = row0 + r, tok = row / G, g = row - tok * G;
+      typedef T T4 __attribute__((ext_vector_type(4)));
+      T4 y;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] = (T)(o[j] * inv);
+      *(T4*)((T*)a.out + (it.q0 + tok) * a.out_token_stride + (int64_t)(head * G + g) * a.out_head_stride + d) = y;
+    }
   }
   __syncthreads();
-  float top = kNoScore, sum = 0.0f;
-#pragma unroll
-  for (int v = 0; v < kWaves; ++v) top = fmaxf(top, ml[(v * 32 + (w.lane & 31)) * 2]);
-#pragma unroll
-  for (int v = 0; v < kWaves; ++v)
-    sum += ml[(v * 32 + (w.lane & 31)) * 2 + 1] * __builtin_amdgcn_exp2f(ml[(v * 32 + (w.lane & 31)) * 2] - top);
-  const float f = __builtin_amdgcn_exp2f(m - top);
-#pragma unroll
-  for (int d = 0; d < S::DT; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) w.o[d][i] *= f;
-  const bool real = row0 + (w.lane & 31) < it.rows;
-  float* mine = (float*)smem + ((wave & 1) * 32 + (w.lane & 31)) * (S::D + 4) + 4 * w.half;
-#pragma unroll
-  for (int step = 2; step > 0; step >>= 1) {
-    if (real && wave >= step && wave < 2 * step) {
-#pragma unroll
-      for (int d = 0; d < S::DT; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          const f4 x = {w.o[d][i], w.o[d][i + 1], w.o[d][i + 2], w.o[d][i + 3]};
-          *(f4*)((step == 2 ? mine : mine - 32 * (S::D + 4)) + 32 * d + 2 * i) = x;
-        }
-    }
-    __syncthreads();
-    if (real && wave < step) {
-#pragma unroll
-      for (int d = 0; d < S::DT; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) {
-          const f4 x = *(const f4*)(mine + 32 * d + 2 * i);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) w.o[d][i + j] += x[j];
-        }
-    }
-    __syncthreads();
-  }
-  if (wave == 0) store_rows<S>(a, w, it, row0, head, top, sum, slot, 0, parts, stats, tile_rows);
 }
 
 // LDS: strips of keys (or what the waves' results are joined through), the
 // waves' m and l, and their flags.
 template <typename S>
-constexpr int kPrivateBytes = (S::kPrivate > S::kJoin ? S::kPrivate : S::kJoin) + kWaves * kRows * 8;
+constexpr int kPrivateBytes = (S::kPrivate > S::kJoin ? S::kPrivate : S::kJoin) + kWaves * kFew * 8;
 template <typename S, bool MIXED>
 constexpr int kFlagAt = MIXED && S::kShared > kPrivateBytes<S> ? S::kShared : kPrivateBytes<S>;
 
@@ -743,14 +1018,16 @@ __global__ __launch_bounds__(kThreads, S::D <= 128 ? 2 : 1) void attention_kerne
   Item it;
   if (!find_item(a, p, index, (int)split, it)) return;
   const int64_t slot = blockIdx.x;
+  int* flag = (int*)(smem + kFlagAt<S, MIXED>);
   if constexpr (MIXED) {
     if (it.shared) {
-      shared_tile<S>(a, it, (int)head, lds, (int*)(smem + kFlagAt<S, MIXED>), slot, parts, stats);
+      shared_tile<S>(a, it, (int)head, lds, flag, slot, parts, stats);
       return;
     }
   }
-  for (int row0 = 0; row0 < it.rows; row0 += kRows)
-    private_rows<S>(a, it, row0, (int)head, lds, smem, (int*)(smem + kFlagAt<S, MIXED>), slot, parts, stats, MIXED ? kTileRows : kRows);
+  float* ml = (float*)(smem + (S::kPrivate > S::kJoin ? S::kPrivate : S::kJoin));
+  for (int row0 = 0; row0 < it.rows; row0 += kFew)
+    few_rows<S>(a, it, row0, (int)head, lds, smem, ml, flag, slot * (MIXED ? kTileRows : kFew), parts, stats);
 }
 
 // Joins the parts of a tile's keys: one workgroup per tile and key head.
@@ -761,7 +1038,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(KvAttnArgs a, Plan p, co
   const uint32_t head = blockIdx.x % heads, index = blockIdx.x / heads;
   Item it;
   if (!find_item(a, p, index, 0, it) || it.splits < 2) return;
-  const int tile_rows = p.mixed ? kTileRows : kRows;
+  const int tile_rows = p.mixed ? kTileRows : kFew;
   const int G = a.num_heads / a.num_kv_heads;
   const int rows = min(tile_rows, it.rows - it.row0);
   constexpr int per = S::D / 4;
