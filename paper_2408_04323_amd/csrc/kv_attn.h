@@ -4,9 +4,11 @@
 // Mathematics.  A row is one query of one head; the G query heads that share a
 // key head are rows of the same tile, row = token * G + head.  With scores s_t
 // = q . k_t the rows keep m, l and o over the keys seen so far: for every strip
-// of keys, w_t = 2^(c s_t - m), l += sum w_t, o += sum w_t v_t; when a score
-// passes m by more than 2^8, m moves up to it and l and o are multiplied by
-// 2^(old m - m), so w stays below 2^8 and most strips leave o alone.  Parts of
+// of keys, w_t = 2^(c s_t - m), l += sum w_t, o += sum w_t v_t.  m is a score
+// of the row, its largest at some strip; when a strip's weights add up to more
+// than 2^14, m moves up to that strip's largest and l and o are multiplied by
+// 2^(old m - m), so no weight overflows, one at least is 1, and most strips
+// take no maximum and leave o alone.  Parts of
 // the keys that were handled by different waves or workgroups are joined by the
 // same factors.
 //
@@ -51,7 +53,8 @@ constexpr int kFew = 16;                     // rows of a request that one workg
 constexpr int kRows = 32;                    // rows of a wave otherwise,
 constexpr int kTileRows = kRows * kWaves;    // and of its workgroup
 constexpr float kNoScore = -3.0e38f;         // m before any key was seen; finite, so that m - m is 0
-constexpr float kSlack = 8.0f;               // m follows a larger score only past this
+constexpr int kReadsAhead = 4;               // operands of the matrix instructions on their way out of LDS
+constexpr float kMost = 16384.0f;            // m moves once a strip's weights in a lane add up to more
 
 constexpr int gcd256(int x) { return x % 256 == 0 ? 256 : x % 128 == 0 ? 128 : 64; }
 
@@ -125,6 +128,12 @@ __device__ __forceinline__ void wait_vm() {
 // All vector loads, in a form that the compiler takes note of: it then waits for none of them later, in a loop where
 // that would be a wait for the loads to LDS, too.
 __device__ __forceinline__ void settle() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+// A value that the compiler does not take apart: an address of LDS, to which constants are added as the
+// instruction's offset.
+__device__ __forceinline__ uint32_t pinned(uint32_t v) {
+  asm("" : "+v"(v));
+  return v;
+}
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // 64 lanes x 16 bytes from base + off to LDS at `to`, lane after lane; counted
@@ -239,13 +248,15 @@ __device__ __forceinline__ bool find_item(const KvAttnArgs& a, const Plan& p, in
 template <typename S>
 struct Cache {
   const SCOOT_CONST int32_t* table;
+  const int32_t* entries;  // the same, for vector loads
   uint64_t k, v;
   uint64_t block_bytes;  // of all heads
   uint32_t num_blocks;
   int shift, last;       // last entry of the row
 
   __device__ __forceinline__ void setup(const KvAttnArgs& a, int seq, int head) {
-    table = (const SCOOT_CONST int32_t*)(a.block_table + (int64_t)seq * a.table_stride);
+    entries = a.block_table + (int64_t)seq * a.table_stride;
+    table = (const SCOOT_CONST int32_t*)entries;
     const uint64_t head_bytes = (uint64_t)S::RB << a.block_shift;
     block_bytes = head_bytes * a.num_kv_heads;
     k = (uint64_t)a.k_cache + head * head_bytes;
@@ -274,19 +285,56 @@ struct Cache {
   }
 };
 
-// Whether any of the item's keys lies in an entry that names no block; `flag`:
-// a word of LDS for every wave.
+// The table's entries of a wave's next 64 strips, one strip per lane: N groups
+// of eight keys each, `stride` keys from strip to strip.  A scalar load per
+// strip would be waited for together with the reads of LDS.
+template <typename S, int N>
+struct Ahead {
+  uint32_t e[N];
+  int key0, stride, strips, base;
+
+  __device__ __forceinline__ void fill(const Cache<S>& c, int strip) {
+    base = strip;
+    const int lane = threadIdx.x & 63;
+    const int64_t key = key0 + (int64_t)(strip + lane < strips ? strip + lane : strip) * stride;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int64_t i = (key + 8 * j) >> c.shift;
+      e[j] = c.entries[i < c.last ? i : c.last];
+    }
+    settle();
+  }
+  __device__ __forceinline__ void start(const Cache<S>& c, int first, int keys, int n) {
+    key0 = first;
+    stride = keys;
+    strips = n;
+    if (n > 0) fill(c, 0);
+  }
+  // Byte offsets of the groups of a strip, which follows the last one asked for.
+  __device__ __forceinline__ void get(const Cache<S>& c, int strip, uint64_t (&b)[N]) {
+    if (strip - base == 64) fill(c, strip);
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      b[j] = c.at(key0 + strip * stride + 8 * j, (uint32_t)__builtin_amdgcn_readlane((int)e[j], strip - base));
+  }
+};
+
+// Whether `x` holds in any of the workgroup's waves; `flag`: a word of LDS for each.
+__device__ __forceinline__ bool any_wave(bool x, int* flag) {
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) flag[threadIdx.x >> 6] = x;
+  __syncthreads();
+  return uniform(flag[0] | flag[1] | flag[2] | flag[3]) != 0;
+}
+
+// Whether any of the item's keys lies in an entry that names no block.
 __device__ __forceinline__ bool any_holes(const KvAttnArgs& a, const Item& it, int* flag) {
   const int32_t* t = a.block_table + (int64_t)it.seq * a.table_stride;
   bool h = false;
   for (int64_t e = (it.k0 >> a.block_shift) + threadIdx.x; (e << a.block_shift) < it.k1; e += kThreads)
     h = h || (uint32_t)t[e] >= (uint32_t)a.num_blocks;
-  const bool any = __builtin_amdgcn_ballot_w64(h) != 0;
-  if ((threadIdx.x & 63) == 0) flag[threadIdx.x >> 6] = any;
-  __syncthreads();
-  return uniform(flag[0] | flag[1] | flag[2] | flag[3]) != 0;
+  return any_wave(__builtin_amdgcn_ballot_w64(h) != 0, flag);
 }
-
 
 // Eight 8-bit floats as 16-bit ones (exact).
 template <typename R>
@@ -307,7 +355,7 @@ __device__ __forceinline__ typename Vec<R>::v8 widen(int a, int b) {
 }
 
 // Eight weights 2^(scale s - m), rounded, and their sum added to l.  The sum
-// takes them as rounded, like the product.
+// takes them as rounded, like the product does.
 template <typename W, typename F>
 __device__ __forceinline__ typename Vec<W>::v8 eight_weights(F score, float scale, float m, float& l) {
   typename Vec<W>::v8 r;
@@ -326,11 +374,25 @@ __device__ __forceinline__ typename Vec<W>::v8 eight_weights(F score, float scal
   return r;
 }
 
-// Where some rows do not see some keys, 0 * inf must not arise: this takes out
-// of eight keys' values what is not finite, and `bad` tells if any of it lies
-// among the first `seen` keys (add_lost() then puts it back).
+// Where some rows do not see some keys, 0 * inf must not arise.
+//
+// Eight keys' values without those past the first `seen`, which no row sees.
+template <typename V>
+__device__ __forceinline__ V only_seen(V v, int seen) {
+  union {
+    V v;
+    uint32_t w[4];
+  } x;
+  x.v = v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x.w[i] &= (seen > 2 * i ? 0xffffu : 0u) | (seen > 2 * i + 1 ? 0xffff0000u : 0u);
+  return x.v;
+}
+// ... and without what is not finite.  A key that only some rows see and whose
+// value is not finite spoils the others' sums; that shows in the end, and the
+// tile is done again with these values left out and added afterwards.
 template <typename W>
-__device__ __forceinline__ typename Vec<W>::v8 finite(typename Vec<W>::v8 v, int seen, uint32_t& bad) {
+__device__ __forceinline__ typename Vec<W>::v8 only_finite(typename Vec<W>::v8 v) {
   constexpr uint32_t kExp = (std::is_same<W, _Float16>::value ? 0x7c00u : 0x7f80u) * 0x10001u;
   union {
     typename Vec<W>::v8 v;
@@ -339,12 +401,9 @@ __device__ __forceinline__ typename Vec<W>::v8 finite(typename Vec<W>::v8 v, int
   x.v = v;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const uint32_t real = (seen > 2 * i ? 0xffffu : 0u) | (seen > 2 * i + 1 ? 0xffff0000u : 0u);
     // A full exponent carries into the sign's place; from there all over its half.
     const uint32_t e = ((x.w[i] & kExp) + (0x80008000u - kExp)) & 0x80008000u;
-    const uint32_t full = e | (e - (e >> 15));
-    bad |= full & real;
-    x.w[i] &= ~full;
+    x.w[i] &= ~(e | (e - (e >> 15)));
   }
   return x.v;
 }
@@ -461,6 +520,8 @@ struct Tile32 {
       const int d = S::F8 ? (2 * (s / 2) + half) * 16 + 8 * (s & 1) : (2 * s + half) * 8;
       q[s] = *(const T8*)(p + d);
     }
+  }
+  __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -469,32 +530,56 @@ struct Tile32 {
     l = 0.0f;
   }
 
-  // S^T of 32 keys.
-  __device__ __forceinline__ f16v scores(uint32_t lds) const {
-    f16v s;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+  // S^T of a strip.  The reads go ahead of the products that use them: left
+  // alone, the compiler waits for each.
+  __device__ __forceinline__ void scores(uint32_t lds, f16v (&s)[S::SUB]) const {
     constexpr int N = Order::KM / 2;
-    if constexpr (S::F8) {
+    constexpr int R = S::F8 ? KS / 2 : KS;  // reads for 32 keys
+    typedef typename std::conditional<S::F8, i4, T8>::type Piece;
+    uint32_t at[N];
 #pragma unroll
-      for (int u = 0; u < KS / 2; ++u) {
-        const i4 k = *(const SCOOT_LDS i4*)(lds + koff[u % N] + (u / N) * (16 * Order::KM));
+    for (int n = 0; n < N; ++n) at[n] = pinned(lds + koff[n]);
+    auto read = [&](int i) {
+      const int n = i / R, u = i % R;
+      return *(const SCOOT_LDS Piece*)(at[u % N] + n * 32 * S::RB + (u / N) * (16 * Order::KM));
+    };
+    constexpr int kAhead = R < kReadsAhead ? R : kReadsAhead;
+    Piece k[kAhead];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) s = mfma(widen<T>(k[2 * e], k[2 * e + 1]), q[2 * u + e], s);
-      }
-    } else {
+    for (int i = 0; i < kAhead; ++i) k[i] = read(i);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int u = 0; u < KS; ++u) {
-        const T8 k = *(const SCOOT_LDS T8*)(lds + koff[u % N] + (u / N) * (16 * Order::KM));
-        s = mfma(k, q[u], s);
+    for (int n = 0; n < S::SUB; ++n) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[n][i] = 0.0f;
+#pragma unroll
+      for (int u = 0; u < R; ++u) {
+        const int i = n * R + u;
+        const Piece x = k[i % kAhead];
+        if constexpr (S::F8) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) s[n] = mfma(widen<T>(x[2 * e], x[2 * e + 1]), q[2 * u + e], s[n]);
+        } else {
+          s[n] = mfma(x, q[u], s[n]);
+        }
+        if (i + kAhead < S::SUB * R) k[i % kAhead] = read(i + kAhead);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
-    return s;
   }
 
+  struct Lds {
+    uint32_t at[Order::VM];
+  };
+  __device__ __forceinline__ Lds values_at(uint32_t lds) const {
+    Lds r;
+#pragma unroll
+    for (int n = 0; n < Order::VM; ++n) r.at[n] = pinned(lds + voff[n]);
+    return r;
+  }
   // V^T: lane's element d = 32 dt + lane % 32 of the keys 16 ks + 8 half .. + 7.
-  __device__ __forceinline__ W8 values(uint32_t lds, int ks, int dt) const {
-    const uint32_t at = lds + voff[dt % Order::VM] + (dt / Order::VM) * (Order::VM * 16 * Order::U) + ks * 16 * S::RB;
+  __device__ __forceinline__ W8 values(const Lds& v, int ks, int dt) const {
+    const uint32_t at = v.at[dt % Order::VM] + (dt / Order::VM) * (Order::VM * 16 * Order::U) + ks * 16 * S::RB;
     if constexpr (S::F8) {
       const i2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((SCOOT_LDS i2*)at);
       return widen<_Float16>(v[0], v[1]);
@@ -523,44 +608,75 @@ struct Tile32 {
     }
   }
 
-  // Weights of a strip; m, l and o follow.
+  // Weights of a strip; m, l and o follow.  No maximum is taken as long as the
+  // weights stay moderate, which their sum tells.  Whether a row's m moves
+  // depends on that row alone.
   __device__ __forceinline__ void weights(const f16v (&s)[S::SUB], float scale, W8 (&w)[2 * S::SUB]) {
-    float x = s[0][0];
+    float add = 0.0f;
 #pragma unroll
-    for (int n = 0; n < S::SUB; ++n)
+    for (int k = 0; k < 2 * S::SUB; ++k)
+      w[k] = eight_weights<W>([&](int i) { return s[k / 2][8 * (k & 1) + i]; }, scale, m, add);
+    if (__builtin_amdgcn_ballot_w64(!(add <= kMost))) {
+      float x = s[0][0];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) x = fmaxf(x, s[n][i]);
-    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale;
-    if (__builtin_amdgcn_ballot_w64(x > m + kSlack)) {
-      const float up = x > m + kSlack ? x : m, f = __builtin_amdgcn_exp2f(m - up);  // no row's m depends on another row
+      for (int n = 0; n < S::SUB; ++n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x = fmaxf(x, s[n][i]);
+      auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+      x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale;
+      const uint32_t over = !(add <= kMost);
+      sw = __builtin_amdgcn_permlane32_swap(over, over, false, false);
+      const float up = (sw[0] | sw[1]) != 0 && x > m ? x : m, f = __builtin_amdgcn_exp2f(m - up);
       m = up;
       l *= f;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] *= f;
+      add = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 2 * S::SUB; ++k)
+        w[k] = eight_weights<W>([&](int i) { return s[k / 2][8 * (k & 1) + i]; }, scale, m, add);
     }
-#pragma unroll
-    for (int k = 0; k < 2 * S::SUB; ++k)
-      w[k] = eight_weights<W>([&](int i) { return s[k / 2][8 * (k & 1) + i]; }, scale, m, l);
+    l += add;
   }
 
-  __device__ __forceinline__ void product(uint32_t lds, const W8 (&w)[2 * S::SUB]) {
+  // The first reads of V, for before the weights.
+  __device__ __forceinline__ void read_ahead(const Lds& lds, W8 (&v)[kReadsAhead]) const {
 #pragma unroll
-    for (int k = 0; k < 2 * S::SUB; ++k)
-#pragma unroll
-      for (int d = 0; d < DT; ++d) o[d] = mfma(values(lds, k, d), w[k], o[d]);
+    for (int i = 0; i < kReadsAhead; ++i) v[i] = values(lds, i / DT, i % DT);
+    __builtin_amdgcn_sched_barrier(0);
   }
-  __device__ __forceinline__ void product_finite(uint32_t lds, const W8 (&w)[2 * S::SUB], int key0, uint32_t& bad) {
+  __device__ __forceinline__ void product(const Lds& lds, const W8 (&w)[2 * S::SUB], W8 (&v)[kReadsAhead]) {
+#pragma unroll
+    for (int i = 0; i < 2 * S::SUB * DT; ++i) {
+      o[i % DT] = mfma(v[i % kReadsAhead], w[i / DT], o[i % DT]);
+      const int n = i + kReadsAhead;
+      if (n < 2 * S::SUB * DT) v[i % kReadsAhead] = values(lds, n / DT, n % DT);
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+  template <bool FINITE>
+  __device__ __forceinline__ void product_seen(const Lds& lds, const W8 (&w)[2 * S::SUB], int key0) {
 #pragma unroll
     for (int k = 0; k < 2 * S::SUB; ++k)
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
-        o[d] = mfma(finite<W>(values(lds, k, d), see.hi_max + 1 - (key0 + 16 * k + 8 * half), bad), w[k], o[d]);
+      for (int d = 0; d < DT; ++d) {
+        W8 v = only_seen(values(lds, k, d), see.hi_max + 1 - (key0 + 16 * k + 8 * half));
+        if constexpr (FINITE) v = only_finite<W>(v);
+        o[d] = mfma(v, w[k], o[d]);
+      }
+  }
+  __device__ __forceinline__ bool spoilt() const {
+    bool x = false;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x |= !(__builtin_fabsf(o[d][i]) < INFINITY);
+    return __builtin_amdgcn_ballot_w64(x) != 0;
   }
 
-  // Adds the values that product_finite() left out, at the keys k0 .. k1 - 1,
+  // Adds the values that only_finite() left out, at the keys k0 .. k1 - 1,
   // to the rows that see them: a sum with an infinity or a NaN in it.
   __device__ __forceinline__ void add_lost(const Cache<S>& c, int k0, int k1) {
 #pragma unroll 1
@@ -631,27 +747,16 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
 
   // A strip's loads in groups of 16 keys of K or V; every wave takes its share.
   const int share = S::SUB == 2 ? wave : wave & 1;
-  struct Entries {
-    uint32_t e0, e1;
-  };
-  auto entries = [&](int strip) {
-    const int key = it.k0 + strip * S::ST + 16 * share;
-    return Entries{c.entry(key), c.entry(key + 8)};
-  };
-  auto load = [&](int strip, const Entries& e) {
+  Ahead<S, 2> ahead;
+  ahead.start(c, it.k0 + 16 * share, S::ST, strips);
+  auto load = [&](int strip) {
     const uint32_t to = lds + (strip & 1) * (2 * kHalf) + share * 16 * S::RB;
-    const int key = it.k0 + strip * S::ST + 16 * share;
-    const uint64_t b0 = c.at(key, e.e0), b1 = c.at(key + 8, e.e1);
-    if (S::SUB == 2 || wave < 2) load16<S>(w.kdma, to, c.k + b0, c.k + b1);
-    if (S::SUB == 2 || wave >= 2) load16<S>(w.vdma, to + kHalf, c.v + b0, c.v + b1);
+    uint64_t b[2];
+    ahead.get(c, strip, b);
+    if (S::SUB == 2 || wave < 2) load16<S>(w.kdma, to, c.k + b[0], c.k + b[1]);
+    if (S::SUB == 2 || wave >= 2) load16<S>(w.vdma, to + kHalf, c.v + b[0], c.v + b[1]);
   };
-
-  Entries next{};
-  if (strips > 0) {
-    next = entries(0);
-    load(0, next);
-    next = entries(1);
-  }
+  if (strips > 0) load(0);
   const int row0 = it.row0 + wave * kRows;
   w.start(a, it, row0, head);
   const bool holes = any_holes(a, it, flag);
@@ -662,45 +767,47 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
   auto turn = [&](int strip) {
     // This strip has landed, for every wave, and everyone is done with the other buffer.
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (strip + 1 < strips) {
-      load(strip + 1, next);
-      next = entries(strip + 2);
-    }
+    if (strip + 1 < strips) load(strip + 1);
   };
-  uint32_t bad = 0;
-  int strip = 0;
-  while (strip < strips) {
-    if (strip >= u0 && strip < u1) {
-      for (; strip < u1; ++strip) {
+  auto pass = [&](auto finite) {
+    w.clear();
+    int strip = 0;
+    while (strip < strips) {
+      if (strip >= u0 && strip < u1) {
+        for (; strip < u1; ++strip) {
+          turn(strip);
+          const uint32_t at = lds + (strip & 1) * (2 * kHalf);
+          f16v s[S::SUB];
+          w.scores(at, s);
+          typename Tile32<S>::W8 p[2 * S::SUB], v[kReadsAhead];
+          const auto values = w.values_at(at + kHalf);
+          w.read_ahead(values, v);
+          w.weights(s, a.score_scale, p);
+          w.product(values, p, v);
+        }
+      } else {
         turn(strip);
         const uint32_t at = lds + (strip & 1) * (2 * kHalf);
-        f16v s[S::SUB];
+        const int key0 = it.k0 + strip * S::ST;
+        if (key0 <= w.see.hi_max) {
+          f16v s[S::SUB];
+          w.scores(at, s);
 #pragma unroll
-        for (int n = 0; n < S::SUB; ++n) s[n] = w.scores(at + n * 32 * S::RB);
-        typename Tile32<S>::W8 p[2 * S::SUB];
-        w.weights(s, a.score_scale, p);
-        w.product(at + kHalf, p);
-      }
-    } else {
-      turn(strip);
-      const uint32_t at = lds + (strip & 1) * (2 * kHalf);
-      const int key0 = it.k0 + strip * S::ST;
-      if (key0 <= w.see.hi_max) {
-        f16v s[S::SUB];
-#pragma unroll
-        for (int n = 0; n < S::SUB; ++n) {
-          s[n] = w.scores(at + n * 32 * S::RB);
-          w.mask(s[n], key0 + 32 * n, holes ? c.holes(key0 + 32 * n) : 0);
+          for (int n = 0; n < S::SUB; ++n) w.mask(s[n], key0 + 32 * n, holes ? c.holes(key0 + 32 * n) : 0);
+          typename Tile32<S>::W8 p[2 * S::SUB];
+          w.weights(s, a.score_scale, p);
+          w.template product_seen<decltype(finite)::value>(w.values_at(at + kHalf), p, key0);
         }
-        typename Tile32<S>::W8 p[2 * S::SUB];
-        w.weights(s, a.score_scale, p);
-        w.product_finite(at + kHalf, p, key0, bad);
+        ++strip;
       }
-      ++strip;
     }
-  }
-  if (__builtin_amdgcn_ballot_w64(bad != 0)) {  // the strips that went through the mask
-    w.add_lost(c, it.k0, u0 < u1 ? it.k0 + u0 * S::ST : it.k1);
+  };
+  pass(std::false_type{});
+  if (any_wave(w.spoilt(), flag)) {
+    ahead.start(c, it.k0 + 16 * share, S::ST, strips);
+    load(0);
+    pass(std::true_type{});
+    w.add_lost(c, it.k0, u0 < u1 ? it.k0 + u0 * S::ST : it.k1);  // the strips that went through the mask
     if (u0 < u1) w.add_lost(c, it.k0 + u1 * S::ST, it.k1);
   }
   w.store(a, it, row0, head, slot * kTileRows + wave * kRows, parts, stats);
@@ -757,6 +864,8 @@ struct Tile16 {
       const int d = S::F8 ? (4 * (s / 2) + quad) * 16 + 8 * (s & 1) : (4 * s + quad) * 8;
       q[s] = *(const T8*)(p + d);
     }
+  }
+  __device__ __forceinline__ void clear() {
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -767,6 +876,9 @@ struct Tile16 {
 
   // S^T of 32 keys: s[t][i] is key 8 quad + 4 t + i.
   __device__ __forceinline__ void scores(uint32_t lds, f4 (&s)[2]) const {
+    uint32_t from[KN];
+#pragma unroll
+    for (int n = 0; n < KN; ++n) from[n] = pinned(lds + koff[n]);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
@@ -774,7 +886,7 @@ struct Tile16 {
       constexpr int N = S::F8 ? KS / 2 : KS;
 #pragma unroll
       for (int u = 0; u < N; ++u) {
-        const uint32_t at = lds + koff[u % KN] + (u / KN) * (64 * KN) + 4 * t * S::RB;
+        const uint32_t at = from[u % KN] + (u / KN) * (64 * KN) + 4 * t * S::RB;
         if constexpr (S::F8) {
           const i4 k = *(const SCOOT_LDS i4*)at;
 #pragma unroll
@@ -814,33 +926,56 @@ struct Tile16 {
     }
   }
 
+  // As Tile32::weights().
   __device__ __forceinline__ W8 weights(const f4 (&s)[2], float scale) {
-    float x = s[0][0];
+    float add = 0.0f;
+    W8 w = eight_weights<W>([&](int i) { return s[i / 4][i % 4]; }, scale, m, add);
+    if (__builtin_amdgcn_ballot_w64(!(add <= kMost))) {
+      float x = s[0][0];
 #pragma unroll
-    for (int k = 1; k < 8; ++k) x = fmaxf(x, s[k / 4][k % 4]);
-    auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-    sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale;
-    if (__builtin_amdgcn_ballot_w64(x > m + kSlack)) {
-      const float up = x > m + kSlack ? x : m, f = __builtin_amdgcn_exp2f(m - up);
+      for (int k = 1; k < 8; ++k) x = fmaxf(x, s[k / 4][k % 4]);
+      auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+      x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+      sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+      x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale;
+      uint32_t over = !(add <= kMost);
+      sw = __builtin_amdgcn_permlane32_swap(over, over, false, false);
+      over = sw[0] | sw[1];
+      sw = __builtin_amdgcn_permlane16_swap(over, over, false, false);
+      const float up = (sw[0] | sw[1]) != 0 && x > m ? x : m, f = __builtin_amdgcn_exp2f(m - up);
       m = up;
       l *= f;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[d][i] *= f;
+      add = 0.0f;
+      w = eight_weights<W>([&](int i) { return s[i / 4][i % 4]; }, scale, m, add);
     }
-    return eight_weights<W>([&](int i) { return s[i / 4][i % 4]; }, scale, m, l);
+    l += add;
+    return w;
   }
 
   __device__ __forceinline__ void product(uint32_t lds, W8 w) {
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d] = mfma(values(lds, d), w, o[d]);
   }
-  __device__ __forceinline__ void product_finite(uint32_t lds, W8 w, int key0, uint32_t& bad) {
+  template <bool FINITE>
+  __device__ __forceinline__ void product_seen(uint32_t lds, W8 w, int key0) {
 #pragma unroll
-    for (int d = 0; d < DT; ++d) o[d] = mfma(finite<W>(values(lds, d), see.hi_max + 1 - (key0 + 8 * quad), bad), w, o[d]);
+    for (int d = 0; d < DT; ++d) {
+      W8 v = only_seen(values(lds, d), see.hi_max + 1 - (key0 + 8 * quad));
+      if constexpr (FINITE) v = only_finite<W>(v);
+      o[d] = mfma(v, w, o[d]);
+    }
+  }
+  __device__ __forceinline__ bool spoilt() const {
+    bool x = false;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x |= !(__builtin_fabsf(o[d][i]) < INFINITY);
+    return __builtin_amdgcn_ballot_w64(x) != 0;
   }
 
   __device__ __forceinline__ void add_lost(const Cache<S>& c, int k0, int k1) {
@@ -881,24 +1016,11 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
   const uint32_t kat = lds + wave * (2 * kHalf), vat = kat + kHalf;
   const int strips = (it.k1 - it.k0 + 31) / 32;
 
-  struct Entries {
-    uint32_t e[4];
-  };
   struct Base {
     uint64_t b[4];
   };
-  auto entries = [&](int strip) {
-    Entries r;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) r.e[j] = c.entry(it.k0 + strip * 32 + 8 * j);
-    return r;
-  };
-  auto base = [&](int strip, const Entries& e) {
-    Base r;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) r.b[j] = c.at(it.k0 + strip * 32 + 8 * j, e.e[j]);
-    return r;
-  };
+  Ahead<S, 4> ahead;  // its strips: every fourth one
+  ahead.start(c, it.k0 + 32 * wave, 32 * kWaves, (strips - wave + kWaves - 1) / kWaves);
   auto load_k = [&](const Base& b) {
     load16<S>(w.kdma, kat, c.k + b.b[0], c.k + b.b[1]);
     load16<S, Tile16Order<S>::kNext>(w.kdma, kat + 16 * S::RB, c.k + b.b[2], c.k + b.b[3]);
@@ -908,54 +1030,59 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
     load16<S>(w.vdma, vat + 16 * S::RB, c.v + b.b[2], c.v + b.b[3]);
   };
 
-  int strip = wave;
-  Entries next{};
-  if (strip < strips) {
-    next = entries(strip);
-    const Base b = base(strip, next);
+  Base b;
+  auto begin = [&] {
+    if (wave >= strips) return;
+    ahead.get(c, 0, b.b);
     load_k(b);
     load_v(b);
-    next = entries(strip + kWaves);
-  }
+  };
+  begin();
   w.start(a, it, row0, head);
   const bool holes = any_holes(a, it, flag);
   settle();
   int u0, u1;  // strips seen whole by every row
   w.see.whole(it, strips, 32, holes, u0, u1);
 
-  uint32_t bad = 0;
-  auto step = [&](auto masked) {
+  int strip;
+  auto step = [&](auto masked, auto finite) {
     constexpr bool kMasked = decltype(masked)::value;
     const bool more = strip + kWaves < strips;
     const int key0 = it.k0 + strip * 32;
-    Base b{};
     wait_vm<2 * S::NJ>();  // the keys, not the values behind them
     f4 s[2];
     w.scores(kat, s);
     wait_lds();
     if (more) {
-      b = base(strip + kWaves, next);
-      next = entries(strip + 2 * kWaves);
+      ahead.get(c, strip / kWaves + 1, b.b);
       load_k(b);
     }
     if (kMasked) w.mask(s, key0, holes ? c.holes(key0) : 0);
     const typename Tile16<S>::W8 p = w.weights(s, a.score_scale);
     if (more) wait_vm<2 * S::NJ>();
     else wait_vm<0>();
-    if (kMasked) w.product_finite(vat, p, key0, bad);
+    if (kMasked) w.template product_seen<decltype(finite)::value>(vat, p, key0);
     else w.product(vat, p);
     wait_lds();
     if (more) load_v(b);
     strip += kWaves;
   };
-  while (strip < strips) {
-    if (strip >= u0 && strip < u1) {
-      while (strip < u1) step(std::false_type{});
-    } else {
-      step(std::true_type{});
+  auto pass = [&](auto finite) {
+    w.clear();
+    strip = wave;
+    while (strip < strips) {
+      if (strip >= u0 && strip < u1) {
+        while (strip < u1) step(std::false_type{}, finite);
+      } else {
+        step(std::true_type{}, finite);
+      }
     }
-  }
-  if (__builtin_amdgcn_ballot_w64(bad != 0)) {
+  };
+  pass(std::false_type{});
+  if (w.spoilt()) {
+    ahead.start(c, it.k0 + 32 * wave, 32 * kWaves, (strips - wave + kWaves - 1) / kWaves);
+    begin();
+    pass(std::true_type{});
     for (strip = wave; strip < strips; strip += kWaves)
       if (strip < u0 || strip >= u1) w.add_lost(c, it.k0 + strip * 32, min(it.k0 + strip * 32 + 32, it.k1));
   }
@@ -1009,7 +1136,7 @@ template <typename S, bool MIXED>
 constexpr int kFlagAt = MIXED && S::kShared > kPrivateBytes<S> ? S::kShared : kPrivateBytes<S>;
 
 template <typename S, bool MIXED>
-__global__ __launch_bounds__(kThreads, S::D <= 128 ? 2 : 1) void attention_kernel(KvAttnArgs a, Plan p, float* parts, float* stats) {
+__global__ __launch_bounds__(kThreads, S::D <= 64 ? 3 : S::D <= 128 ? 2 : 1) void attention_kernel(KvAttnArgs a, Plan p, float* parts, float* stats) {
   extern __shared__ __attribute__((aligned(256))) char smem[];
   const uint32_t lds = (uint32_t)(uintptr_t)(SCOOT_LDS char*)smem;
   const uint32_t heads = (uint32_t)a.num_kv_heads;
