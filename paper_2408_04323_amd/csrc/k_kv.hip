@@ -21,158 +21,151 @@ namespace {
 // KiB of lengths at 8192 requests, out of L2), keeps them in LDS, and then
 // serves its own share of the tokens, each found by a binary search in LDS.
 // The token that opens a new block writes the table's entry, so no workgroup
-// waits for another.
-constexpr int kAssignThreads = 1024;
-constexpr int kAssignPer = 4;  // requests per thread and tile
-constexpr int kAssignTile = kAssignThreads * kAssignPer;
-constexpr int kAssignTokens = 2048;  // tokens per workgroup, as long as that makes at most kAssignGroups of them
+// waits for another.  The sums are 32-bit ones that stay at their largest
+// value, past every limit they are compared with.
+//
+// Few requests (and so mostly few tokens) go to workgroups of 256 threads, a
+// quarter of the waves to start and to bring together.
+constexpr int kAssignPer = 4;     // requests per thread and tile
+constexpr int kAssignFew = 1024;  // requests that one tile of 256 threads holds
 constexpr int kAssignGroups = 256;
 
-__device__ __forceinline__ int sat32(int64_t v) { return v > 0x7fffffff ? 0x7fffffff : (int)v; }
+__device__ __forceinline__ int sat31(uint32_t v) { return v > 0x7fffffffu ? 0x7fffffff : (int)v; }
+__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
 
-struct Sums {
-  int64_t tokens, blocks;
-};
-
-// Exclusive prefix sums over the workgroup's threads, and the totals.
-__device__ __forceinline__ Sums scan_workgroup(Sums v, Sums* total, Sums* wave_sum) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  Sums x = v;
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t t = __shfl_up((long long)x.tokens, o), b = __shfl_up((long long)x.blocks, o);
-    if (lane >= o) {
-      x.tokens += t;
-      x.blocks += b;
-    }
-  }
-  if (lane == 63) wave_sum[wave] = x;
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t moved(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+}
+// Inclusive sums over a wave's lanes.
+__device__ __forceinline__ uint32_t scan_wave(uint32_t v) {
+  v = add_sat(v, moved<0x111, 0xf>(v));  // from 1, 2, 4, 8 lanes below within a row of 16,
+  v = add_sat(v, moved<0x112, 0xf>(v));
+  v = add_sat(v, moved<0x114, 0xf>(v));
+  v = add_sat(v, moved<0x118, 0xf>(v));
+  v = add_sat(v, moved<0x142, 0xa>(v));  // the last lane of the row below to the rows 1 and 3,
+  return add_sat(v, moved<0x143, 0xc>(v));  // and that of the lower half to the upper one
+}
+// Exclusive sums over a workgroup's threads, and the total.
+template <int THREADS>
+__device__ __forceinline__ uint32_t scan_group(uint32_t v, uint32_t* sums, uint32_t& total) {
+  constexpr int kWaves = THREADS / 64;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t x = scan_wave(v);
+  if (lane == 63) sums[wave] = x;
   __syncthreads();
-  Sums before{0, 0}, all{0, 0};
-  for (int w = 0; w < kAssignThreads / 64; ++w) {
-    if (w < wave) {
-      before.tokens += wave_sum[w].tokens;
-      before.blocks += wave_sum[w].blocks;
-    }
-    all.tokens += wave_sum[w].tokens;
-    all.blocks += wave_sum[w].blocks;
-  }
-  *total = all;
-  return {before.tokens + x.tokens - v.tokens, before.blocks + x.blocks - v.blocks};
+  const uint32_t w = scan_wave(lane < kWaves ? sums[lane] : 0);
+  __syncthreads();
+  total = (uint32_t)__builtin_amdgcn_readlane((int)w, kWaves - 1);
+  const uint32_t before = wave ? (uint32_t)__builtin_amdgcn_readlane((int)w, wave - 1) : 0;
+  const uint32_t below = moved<0x138, 0xf>(x);  // from the lane below, over the whole wave
+  return add_sat(before, lane ? below : 0);
 }
 
-__global__ __launch_bounds__(kAssignThreads) void kv_assign_kernel(KvAssignArgs a, int64_t per_group) {
-  __shared__ Sums wave_sum[kAssignThreads / 64];
-  __shared__ int start[kAssignTile + 1];  // first token of a request, from the tile's first one
-  __shared__ int ctx[kAssignTile];        // cached tokens; -1: not admitted
-  __shared__ int first[kAssignTile];      // first of its new blocks in the free list
-  __shared__ int n_admitted;
-  __shared__ int taken;
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void kv_assign_kernel(KvAssignArgs a, uint32_t per_group) {
+  constexpr int kTile = THREADS * kAssignPer;
+  __shared__ uint32_t sums[THREADS / 64];
+  __shared__ uint32_t start[kTile];      // first token of a request, from the tile's first one
+  __shared__ int ctx[kTile];             // cached tokens; -1: not admitted
+  __shared__ uint32_t first[kTile];      // first of its new blocks in the free list
 
   const int tid = threadIdx.x;
-  const int bs = 1 << a.block_shift;
-  const int64_t t_lo = (int64_t)blockIdx.x * per_group;
-  const int64_t t_hi = t_lo + per_group < a.max_tokens ? t_lo + per_group : a.max_tokens;
-  if (tid == 0) n_admitted = taken = 0;
-  Sums base{0, 0};
-  for (int r0 = 0, tile = 0; r0 < a.num_seqs; r0 += kAssignTile, ++tile) {
+  const uint32_t bs = 1u << a.block_shift;
+  const uint32_t max_tokens = (uint32_t)a.max_tokens, num_free = (uint32_t)a.num_free;
+  const uint32_t t_lo = min(blockIdx.x * per_group, max_tokens);
+  const uint32_t t_hi = max_tokens - t_lo < per_group ? max_tokens : t_lo + per_group;
+  uint32_t tokens = 0, blocks = 0;    // of the tiles before
+  uint32_t admitted = 0, taken = 0;   // of this thread's requests
+  for (int r0 = 0, tile = 0; r0 < a.num_seqs; r0 += kTile, ++tile) {
     const bool writes = tile % (int)gridDim.x == (int)blockIdx.x;  // this workgroup stores the tile's lengths
-    int c[kAssignPer], n[kAssignPer];
-    // First the tokens alone decide which requests ask for blocks.
-    int64_t tok = 0;
+    uint32_t c[kAssignPer], n[kAssignPer], tok = 0;
+#pragma unroll
     for (int j = 0; j < kAssignPer; ++j) {
       const int r = r0 + tid * kAssignPer + j;
-      c[j] = r < a.num_seqs ? max(a.context_len[r], 0) : 0;
-      n[j] = r < a.num_seqs ? max(a.new_len[r], 0) : 0;
-      tok += n[j];
+      c[j] = r < a.num_seqs ? (uint32_t)max(a.context_len[r], 0) : 0;
+      n[j] = r < a.num_seqs ? (uint32_t)max(a.new_len[r], 0) : 0;
+      tok = add_sat(tok, n[j]);
     }
-    Sums total;
-    const Sums st = scan_workgroup({tok, 0}, &total, wave_sum);
-    __syncthreads();
-    int64_t end = base.tokens + st.tokens, blk = 0;
-    int64_t need[kAssignPer];
+    uint32_t tile_tokens, tile_blocks;
+    const uint32_t t0 = scan_group<THREADS>(tok, sums, tile_tokens);  // from the tile's first token
+    // The tokens alone decide which requests ask for blocks.
+    uint32_t end = add_sat(tokens, t0), blk = 0, need[kAssignPer];
     bool fits[kAssignPer];
+#pragma unroll
     for (int j = 0; j < kAssignPer; ++j) {
-      end += n[j];
-      const int64_t used = ((int64_t)c[j] + bs - 1) >> a.block_shift;
-      const int64_t all = ((int64_t)c[j] + n[j] + bs - 1) >> a.block_shift;
-      fits[j] = end <= a.max_tokens && all <= a.max_blocks;
+      end = add_sat(end, n[j]);
+      const uint32_t len = c[j] + n[j];  // below 2^32
+      const uint32_t used = (c[j] + bs - 1) >> a.block_shift, all = (len >> a.block_shift) + ((len & (bs - 1)) != 0);
+      fits[j] = end <= max_tokens && all <= (uint32_t)a.max_blocks;
       need[j] = fits[j] ? all - used : 0;
-      blk += need[j];
+      blk = add_sat(blk, need[j]);
     }
-    Sums total_b;
-    const Sums sb = scan_workgroup({0, blk}, &total_b, wave_sum);
-    int64_t tstart = base.tokens + st.tokens, bstart = base.blocks + sb.blocks;
-    int ok_count = 0, last_taken = 0;
+    uint32_t b0 = add_sat(blocks, scan_group<THREADS>(blk, sums, tile_blocks)), at = t0;
+#pragma unroll
     for (int j = 0; j < kAssignPer; ++j) {
       const int i = tid * kAssignPer + j, r = r0 + i;
-      const bool ok = r < a.num_seqs && fits[j] && (need[j] == 0 || bstart + need[j] <= a.num_free);
-      start[i] = sat32(tstart - base.tokens);
-      ctx[i] = ok ? c[j] : -1;
-      first[i] = sat32(bstart);
-      if (ok) {
-        ++ok_count;
-        if (need[j] > 0) last_taken = sat32(bstart + need[j]);
-      }
+      const uint32_t upto = add_sat(b0, need[j]);
+      const bool ok = r < a.num_seqs && fits[j] && (need[j] == 0 || upto <= num_free);
+      start[i] = at;
+      ctx[i] = ok ? (int)c[j] : -1;
+      first[i] = b0;
+      admitted += ok;
+      if (ok && need[j] > 0) taken = upto;
       if (writes && r < a.num_seqs) {
-        a.query_start[r] = sat32(tstart);
-        a.seq_len[r] = ok ? sat32((int64_t)c[j] + n[j]) : 0;
+        a.query_start[r] = sat31(add_sat(tokens, at));
+        a.seq_len[r] = ok ? (int)(c[j] + n[j]) : 0;
       }
-      tstart += n[j];
-      bstart += need[j];
-    }
-    if (tid == 0) start[kAssignTile] = sat32(total.tokens);
-    if (blockIdx.x == 0 && ok_count) {
-      atomicAdd(&n_admitted, ok_count);
-      atomicMax(&taken, last_taken);
+      at = add_sat(at, n[j]);
+      b0 = upto;
     }
     __syncthreads();
 
     // Tokens of this workgroup that belong to this tile's requests.
-    const int64_t lo = t_lo > base.tokens ? t_lo : base.tokens;
-    const int64_t tile_end = base.tokens + total.tokens;
-    const int64_t hi = t_hi < tile_end ? t_hi : tile_end;
-    for (int64_t t = lo + tid; t < hi; t += kAssignThreads) {
-      const int at = (int)(t - base.tokens);
-      int i = 0, e = kAssignTile;  // start[i] <= at < start[e]
-      while (e - i > 1) {
-        const int m = (i + e) >> 1;
-        if (start[m] <= at) i = m;
-        else e = m;
-      }
+    const uint32_t tile_end = add_sat(tokens, tile_tokens);
+    const uint32_t hi = t_hi < tile_end ? t_hi : tile_end;
+    for (uint32_t t = min(max(t_lo, tokens), hi) + tid; t < hi; t += THREADS) {  // hi is below 2^31
+      const uint32_t my = t - tokens;
+      int i = 0;  // the last request with start <= my; kTile is a power of two
+#pragma unroll
+      for (int step = kTile / 2; step > 0; step /= 2)
+        if (start[i + step] <= my) i += step;
       int pos = -1;
       int64_t slot = -1;
       if (ctx[i] >= 0) {
-        const int r = r0 + i;
-        pos = ctx[i] + at - start[i];
-        const int b = pos >> a.block_shift;
-        const int used = (int)(((int64_t)ctx[i] + bs - 1) >> a.block_shift);
-        int32_t* entry = a.block_table + (int64_t)r * a.table_stride + b;
-        int block;
-        if (b < used) {
-          block = *entry;
-        } else {
-          block = a.free_blocks[first[i] + b - used];
-          if ((pos & (bs - 1)) == 0) *entry = block;
-        }
+        pos = ctx[i] + (int)(my - start[i]);
+        const int b = pos >> a.block_shift, used = (int)((ctx[i] + bs - 1) >> a.block_shift);
+        int32_t* entry = a.block_table + (int64_t)(r0 + i) * a.table_stride + b;
+        const int block = b < used ? *entry : a.free_blocks[first[i] + b - used];
+        if (b >= used && (pos & (bs - 1)) == 0) *entry = block;
         if (block >= 0) slot = ((int64_t)block << a.block_shift) + (pos & (bs - 1));
       }
       a.positions[t] = pos;
       a.slots[t] = slot;
     }
-    base.tokens += total.tokens;
-    base.blocks += total_b.blocks;
+    tokens = tile_end;
+    blocks = add_sat(blocks, tile_blocks);
     __syncthreads();
   }
-  for (int64_t t = (t_lo > base.tokens ? t_lo : base.tokens) + tid; t < t_hi; t += kAssignThreads) {
+  for (uint32_t t = min(max(t_lo, tokens), t_hi) + tid; t < t_hi; t += THREADS) {
     a.positions[t] = -1;
     a.slots[t] = -1;
   }
-  if (blockIdx.x == 0 && tid == 0) {
-    a.query_start[a.num_seqs] = sat32(base.tokens);
-    a.counts[0] = sat32(base.tokens);
-    a.counts[1] = n_admitted;
-    a.counts[2] = taken;
-    a.counts[3] = sat32(base.blocks);
+  if (blockIdx.x == 0) {
+    uint32_t all;
+    scan_group<THREADS>(admitted, sums, all);
+    // The free blocks are taken in order: the last request that got one tells how many.
+    for (int o = 1; o < 64; o <<= 1) taken = max(taken, (uint32_t)__shfl_xor((int)taken, o));
+    if ((tid & 63) == 0) sums[tid >> 6] = taken;
+    __syncthreads();
+    if (tid == 0) {
+      for (int w = 1; w < THREADS / 64; ++w) taken = max(taken, sums[w]);
+      a.query_start[a.num_seqs] = sat31(tokens);
+      a.counts[0] = sat31(tokens);
+      a.counts[1] = (int)all;
+      a.counts[2] = (int)taken;
+      a.counts[3] = sat31(blocks);
+    }
   }
 }
 
@@ -257,10 +250,15 @@ void write_launch(const KvWriteArgs& a, bool aligned, dim3 grid, hipStream_t s) 
 }  // namespace
 
 int launch_kv_assign(const KvAssignArgs& a, void* stream) {
-  const int64_t most = (a.max_tokens + kAssignTokens - 1) / kAssignTokens;
+  const int threads = a.num_seqs <= kAssignFew ? 256 : 1024;
+  const int64_t most = (a.max_tokens + threads - 1) / threads;
   const int groups = (int)std::max<int64_t>(1, std::min<int64_t>(most, kAssignGroups));
-  const int64_t per_group = (a.max_tokens + groups - 1) / groups;
-  hipLaunchKernelGGL(kv_assign_kernel, dim3(groups), dim3(kAssignThreads), 0, (hipStream_t)stream, a, per_group);
+  const uint32_t per_group = (uint32_t)((a.max_tokens + groups - 1) / groups);
+  const hipStream_t s = (hipStream_t)stream;
+  if (threads == 256)
+    hipLaunchKernelGGL((kv_assign_kernel<256>), dim3(groups), dim3(256), 0, s, a, per_group);
+  else
+    hipLaunchKernelGGL((kv_assign_kernel<1024>), dim3(groups), dim3(1024), 0, s, a, per_group);
   return launched("kv assign launch");
 }
 
