@@ -17,14 +17,16 @@ namespace {
 using namespace kvattn;
 
 // Workgroups that the chip holds at once: 256 compute units, two each.
-constexpr int64_t kSlots = 512;
-constexpr int kMinPart = 128;    // keys: a strip of 32 for each wave
+constexpr int64_t kUnits = 256, kSlots = 2 * kUnits;
+constexpr int kMinPart = 128;     // keys: a strip of 32 for each of four waves
+constexpr int kAlone = 2048;      // keys that eight waves of one workgroup do not share with another
+constexpr int kMinPart8 = 1024;
 
 // Requests of at most 16 rows (new tokens x heads per key head) are items of
 // their own; once some have more, tiles of 128 rows are.  Where the items do
-// not fill the chip four times over, their keys are split into parts, so many
-// that they do, of at least kMinPart keys.
-Plan plan(int64_t num_tokens, int num_heads, int num_kv_heads, int num_seqs, int64_t max_new_len, int64_t max_seq_len, int window) {
+// not fill the chip often enough, their keys are split into parts.
+Plan plan(int64_t num_tokens, int num_heads, int num_kv_heads, int row_bytes, int num_seqs, int64_t max_new_len, int64_t max_seq_len,
+          int window) {
   Plan p{};
   const int64_t G = num_heads / num_kv_heads;
   const int64_t longest = std::min<int64_t>(max_new_len, num_tokens);
@@ -34,9 +36,16 @@ Plan plan(int64_t num_tokens, int num_heads, int num_kv_heads, int num_seqs, int
   if (window > 0) keys = std::min<int64_t>(keys, (int64_t)window + (p.mixed ? kTileRows / G : longest) + 32);
   keys = std::max<int64_t>(keys, 1);
   const int64_t groups = std::max<int64_t>(1, p.items * num_kv_heads);
-  const int64_t want = std::max<int64_t>(1, (p.mixed ? 2 : 4) * kSlots / groups);
+  // Few items: eight waves each.
+  p.waves = !p.mixed && groups <= kUnits && row_bytes <= kWideRow ? 8 : kWaves;
+  int64_t want = std::max<int64_t>(1, (p.mixed ? 2 : 4) * kSlots / groups);
+  int64_t least = kMinPart;
+  if (p.waves == 8) {
+    want = keys <= kAlone ? 1 : std::max<int64_t>(1, 4 * kUnits / groups);
+    least = kMinPart8;
+  }
   int64_t part = (keys + want - 1) / want;
-  part = std::max<int64_t>(kMinPart, (part + kMinPart - 1) / kMinPart * kMinPart);
+  part = std::max<int64_t>(least, (part + kMinPart - 1) / kMinPart * kMinPart);
   p.part = (int)std::min<int64_t>(part, (int64_t)1 << 30);
   p.splits = (int)((keys + p.part - 1) / p.part);
   return p;
@@ -49,12 +58,16 @@ int64_t slots(const Plan& p, int num_kv_heads) {
 
 uint64_t kv_attention_workspace_bytes(int64_t num_tokens, int num_heads, int num_kv_heads, int head_dim, int num_seqs,
                                       int64_t max_new_len, int64_t max_seq_len, int window) {
-  const Plan p = plan(num_tokens, num_heads, num_kv_heads, num_seqs, max_new_len, max_seq_len, window);
-  return (uint64_t)slots(p, num_kv_heads) * (head_dim + 2) * 4;
+  int64_t most = 0;  // of a 16-bit and an 8-bit cache
+  for (int bytes = 1; bytes <= 2; ++bytes)
+    most = std::max(most, slots(plan(num_tokens, num_heads, num_kv_heads, head_dim * bytes, num_seqs, max_new_len, max_seq_len, window),
+                                num_kv_heads));
+  return (uint64_t)most * (head_dim + 2) * 4;
 }
 
 int launch_kv_attention(const KvAttnArgs& a, scoot_kv_type type, scoot_kv_type cache_type, void* stream) {
-  const Plan p = plan(a.num_tokens, a.num_heads, a.num_kv_heads, a.num_seqs, a.max_new_len, a.max_seq_len, a.window);
+  const Plan p = plan(a.num_tokens, a.num_heads, a.num_kv_heads, a.head_dim * (cache_type == SCOOT_KV_F8 ? 1 : 2), a.num_seqs,
+                      a.max_new_len, a.max_seq_len, a.window);
   if (p.items * p.splits * a.num_kv_heads > 0x7fffffff)
     return fail_static(SCOOT_ERR_UNSUPPORTED, "kv attention: too many rows for one call");
   float* parts = (float*)a.workspace;

@@ -47,12 +47,13 @@ typedef short s4 __attribute__((ext_vector_type(4)));
 #define SCOOT_LDS __attribute__((address_space(3)))
 #define SCOOT_CONST __attribute__((address_space(4)))
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 4;                    // of a workgroup (one of few rows may have eight)
 constexpr int kThreads = 64 * kWaves;
 constexpr int kFew = 16;                     // rows of a request that one workgroup's waves handle together
 constexpr int kRows = 32;                    // rows of a wave otherwise,
 constexpr int kTileRows = kRows * kWaves;    // and of its workgroup
 constexpr float kNoScore = -3.0e38f;         // m before any key was seen; finite, so that m - m is 0
+constexpr int kWideRow = 256;                // bytes of a cache row up to which eight waves' strips fit the LDS
 constexpr int kReadsAhead = 4;               // operands of the matrix instructions on their way out of LDS
 constexpr float kMost = 16384.0f;            // m moves once a strip's weights in a lane add up to more
 
@@ -72,8 +73,6 @@ struct Shape {
   static constexpr int ST = D <= 128 ? 64 : 32;     // keys per strip of a shared tile
   static constexpr int SUB = ST / 32;
   static constexpr int kShared = 4 * ST * RB;       // two buffers of K and V
-  static constexpr int kPrivate = kWaves * 64 * RB; // per wave one strip of 32 keys of K and V
-  static constexpr int kJoin = kWaves * kFew * (D + 4) * 4;
   // The second product runs in the cache's 16-bit type; 8-bit values are exact in half precision, which rounds the
   // weights eight times finer than bfloat16.
   typedef typename std::conditional<F8, _Float16, T>::type W;
@@ -167,6 +166,7 @@ struct Plan {
   int splits;
   int part;         // keys per part, a multiple of 128
   bool mixed;       // tiles of kTileRows rows; else requests
+  int waves;        // of a workgroup, if not mixed
 };
 
 __device__ __forceinline__ int64_t clamp64(int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; }
@@ -250,17 +250,17 @@ struct Cache {
   const SCOOT_CONST int32_t* table;
   const int32_t* entries;  // the same, for vector loads
   uint64_t k, v;
-  uint64_t block_bytes;  // of all heads
+  uint32_t block_bytes;  // of all heads; at most 1024 heads of 256 keys of 512 bytes
   uint32_t num_blocks;
   int shift, last;       // last entry of the row
 
   __device__ __forceinline__ void setup(const KvAttnArgs& a, int seq, int head) {
     entries = a.block_table + (int64_t)seq * a.table_stride;
     table = (const SCOOT_CONST int32_t*)entries;
-    const uint64_t head_bytes = (uint64_t)S::RB << a.block_shift;
-    block_bytes = head_bytes * a.num_kv_heads;
-    k = (uint64_t)a.k_cache + head * head_bytes;
-    v = (uint64_t)a.v_cache + head * head_bytes;
+    const uint32_t head_bytes = (uint32_t)S::RB << a.block_shift;
+    block_bytes = head_bytes * (uint32_t)a.num_kv_heads;
+    k = (uint64_t)a.k_cache + (uint64_t)head * head_bytes;
+    v = (uint64_t)a.v_cache + (uint64_t)head * head_bytes;
     num_blocks = (uint32_t)a.num_blocks;
     shift = a.block_shift;
     last = a.max_blocks - 1;
@@ -272,7 +272,7 @@ struct Cache {
   }
   // Byte offset of these keys.  An entry that names no block reads block 0, and the mask drops it.
   __device__ __forceinline__ uint64_t at(int key, uint32_t e) const {
-    return (e < num_blocks ? e : 0) * block_bytes + (uint64_t)(key & ((1 << shift) - 1)) * S::RB;
+    return (uint64_t)(e < num_blocks ? e : 0) * block_bytes + (uint32_t)(key & ((1 << shift) - 1)) * S::RB;
   }
   // Which of the four groups of eight keys from `key` on have no block.
   __device__ __forceinline__ int holes(int key) const {
@@ -285,55 +285,71 @@ struct Cache {
   }
 };
 
-// The table's entries of a wave's next 64 strips, one strip per lane: N groups
-// of eight keys each, `stride` keys from strip to strip.  A scalar load per
-// strip would be waited for together with the reads of LDS.
+// Addresses of a wave's next 64 strips, one strip per lane: N groups of eight
+// keys each, `stride` keys from strip to strip.  (By scalars, a strip would
+// cost some forty instructions, and a scalar load is waited for together with
+// the reads of LDS.)
 template <typename S, int N>
 struct Ahead {
-  uint32_t e[N];
+  uint32_t lo[N], hi[N];
+  uint64_t from;  // keys or values
   int key0, stride, strips, base;
 
   __device__ __forceinline__ void fill(const Cache<S>& c, int strip) {
     base = strip;
     const int lane = threadIdx.x & 63;
-    const int64_t key = key0 + (int64_t)(strip + lane < strips ? strip + lane : strip) * stride;
+    const int key = key0 + (strip + lane < strips ? strip + lane : strip) * stride;
+    uint32_t e[N];
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const int64_t i = (key + 8 * j) >> c.shift;
-      e[j] = c.entries[i < c.last ? i : c.last];
+      const int i = (key + 8 * j) >> c.shift;
+      e[j] = (uint32_t)c.entries[i < c.last ? i : c.last];
     }
     settle();
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const uint64_t at = from + c.at(key + 8 * j, e[j]);
+      lo[j] = (uint32_t)at;
+      hi[j] = (uint32_t)(at >> 32);
+    }
   }
-  __device__ __forceinline__ void start(const Cache<S>& c, int first, int keys, int n) {
+  __device__ __forceinline__ void start(const Cache<S>& c, uint64_t cache, int first, int keys, int n) {
+    from = cache;
     key0 = first;
     stride = keys;
     strips = n;
     if (n > 0) fill(c, 0);
   }
-  // Byte offsets of the groups of a strip, which follows the last one asked for.
+  // The groups of a strip, which follows the last one asked for.
   __device__ __forceinline__ void get(const Cache<S>& c, int strip, uint64_t (&b)[N]) {
     if (strip - base == 64) fill(c, strip);
 #pragma unroll
     for (int j = 0; j < N; ++j)
-      b[j] = c.at(key0 + strip * stride + 8 * j, (uint32_t)__builtin_amdgcn_readlane((int)e[j], strip - base));
+      b[j] = (uint32_t)__builtin_amdgcn_readlane((int)lo[j], strip - base) |
+             (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)hi[j], strip - base) << 32;
   }
 };
 
 // Whether `x` holds in any of the workgroup's waves; `flag`: a word of LDS for each.
+template <int W>
 __device__ __forceinline__ bool any_wave(bool x, int* flag) {
   __syncthreads();
   if ((threadIdx.x & 63) == 0) flag[threadIdx.x >> 6] = x;
   __syncthreads();
-  return uniform(flag[0] | flag[1] | flag[2] | flag[3]) != 0;
+  int any = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) any |= flag[w];
+  return uniform(any) != 0;
 }
 
 // Whether any of the item's keys lies in an entry that names no block.
+template <int W>
 __device__ __forceinline__ bool any_holes(const KvAttnArgs& a, const Item& it, int* flag) {
   const int32_t* t = a.block_table + (int64_t)it.seq * a.table_stride;
   bool h = false;
-  for (int64_t e = (it.k0 >> a.block_shift) + threadIdx.x; (e << a.block_shift) < it.k1; e += kThreads)
+  for (int64_t e = (it.k0 >> a.block_shift) + threadIdx.x; (e << a.block_shift) < it.k1; e += 64 * W)
     h = h || (uint32_t)t[e] >= (uint32_t)a.num_blocks;
-  return any_wave(__builtin_amdgcn_ballot_w64(h) != 0, flag);
+  return any_wave<W>(__builtin_amdgcn_ballot_w64(h) != 0, flag);
 }
 
 // Eight 8-bit floats as 16-bit ones (exact).
@@ -690,7 +706,7 @@ struct Tile32 {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const float x = stored<S>(row, 32 * d + 8 * (i / 4) + 4 * half + i % 4);
-          o[d][i] += mine & !(__builtin_fabsf(x) < INFINITY) ? x : 0.0f;
+          o[d][i] += (mine & !(__builtin_fabsf(x) < INFINITY)) ? x : 0.0f;
         }
     }
   }
@@ -748,18 +764,19 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
   // A strip's loads in groups of 16 keys of K or V; every wave takes its share.
   const int share = S::SUB == 2 ? wave : wave & 1;
   Ahead<S, 2> ahead;
-  ahead.start(c, it.k0 + 16 * share, S::ST, strips);
+  ahead.start(c, c.k, it.k0 + 16 * share, S::ST, strips);
+  const uint64_t to_v = c.v - c.k;
   auto load = [&](int strip) {
     const uint32_t to = lds + (strip & 1) * (2 * kHalf) + share * 16 * S::RB;
     uint64_t b[2];
     ahead.get(c, strip, b);
-    if (S::SUB == 2 || wave < 2) load16<S>(w.kdma, to, c.k + b[0], c.k + b[1]);
-    if (S::SUB == 2 || wave >= 2) load16<S>(w.vdma, to + kHalf, c.v + b[0], c.v + b[1]);
+    if (S::SUB == 2 || wave < 2) load16<S>(w.kdma, to, b[0], b[1]);
+    if (S::SUB == 2 || wave >= 2) load16<S>(w.vdma, to + kHalf, to_v + b[0], to_v + b[1]);
   };
   if (strips > 0) load(0);
   const int row0 = it.row0 + wave * kRows;
   w.start(a, it, row0, head);
-  const bool holes = any_holes(a, it, flag);
+  const bool holes = any_holes<kWaves>(a, it, flag);
   settle();
   int u0, u1;
   w.see.whole(it, strips, S::ST, holes, u0, u1);
@@ -803,8 +820,8 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
     }
   };
   pass(std::false_type{});
-  if (any_wave(w.spoilt(), flag)) {
-    ahead.start(c, it.k0 + 16 * share, S::ST, strips);
+  if (any_wave<kWaves>(w.spoilt(), flag)) {
+    ahead.start(c, c.k, it.k0 + 16 * share, S::ST, strips);
     load(0);
     pass(std::true_type{});
     w.add_lost(c, it.k0, u0 < u1 ? it.k0 + u0 * S::ST : it.k1);  // the strips that went through the mask
@@ -990,7 +1007,7 @@ struct Tile16 {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float x = stored<S>(row, 16 * d + 4 * quad + i);
-          o[d][i] += mine & !(__builtin_fabsf(x) < INFINITY) ? x : 0.0f;
+          o[d][i] += (mine & !(__builtin_fabsf(x) < INFINITY)) ? x : 0.0f;
         }
     }
   }
@@ -1003,7 +1020,7 @@ struct Tile16 {
   }
 };
 
-template <typename S>
+template <typename S, int W>
 __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, int row0, int head, uint32_t lds, char* smem,
                                          float* ml, int* flag, int64_t slot_row, float* parts, float* stats) {
   typedef typename S::T T;
@@ -1020,14 +1037,15 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
     uint64_t b[4];
   };
   Ahead<S, 4> ahead;  // its strips: every fourth one
-  ahead.start(c, it.k0 + 32 * wave, 32 * kWaves, (strips - wave + kWaves - 1) / kWaves);
+  ahead.start(c, c.k, it.k0 + 32 * wave, 32 * W, (strips - wave + W - 1) / W);
   auto load_k = [&](const Base& b) {
-    load16<S>(w.kdma, kat, c.k + b.b[0], c.k + b.b[1]);
-    load16<S, Tile16Order<S>::kNext>(w.kdma, kat + 16 * S::RB, c.k + b.b[2], c.k + b.b[3]);
+    load16<S>(w.kdma, kat, b.b[0], b.b[1]);
+    load16<S, Tile16Order<S>::kNext>(w.kdma, kat + 16 * S::RB, b.b[2], b.b[3]);
   };
+  const uint64_t to_v = c.v - c.k;
   auto load_v = [&](const Base& b) {
-    load16<S>(w.vdma, vat, c.v + b.b[0], c.v + b.b[1]);
-    load16<S>(w.vdma, vat + 16 * S::RB, c.v + b.b[2], c.v + b.b[3]);
+    load16<S>(w.vdma, vat, to_v + b.b[0], to_v + b.b[1]);
+    load16<S>(w.vdma, vat + 16 * S::RB, to_v + b.b[2], to_v + b.b[3]);
   };
 
   Base b;
@@ -1039,7 +1057,7 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
   };
   begin();
   w.start(a, it, row0, head);
-  const bool holes = any_holes(a, it, flag);
+  const bool holes = any_holes<W>(a, it, flag);
   settle();
   int u0, u1;  // strips seen whole by every row
   w.see.whole(it, strips, 32, holes, u0, u1);
@@ -1047,14 +1065,14 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
   int strip;
   auto step = [&](auto masked, auto finite) {
     constexpr bool kMasked = decltype(masked)::value;
-    const bool more = strip + kWaves < strips;
+    const bool more = strip + W < strips;
     const int key0 = it.k0 + strip * 32;
     wait_vm<2 * S::NJ>();  // the keys, not the values behind them
     f4 s[2];
     w.scores(kat, s);
     wait_lds();
     if (more) {
-      ahead.get(c, strip / kWaves + 1, b.b);
+      ahead.get(c, strip / W + 1, b.b);
       load_k(b);
     }
     if (kMasked) w.mask(s, key0, holes ? c.holes(key0) : 0);
@@ -1065,7 +1083,7 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
     else w.product(vat, p);
     wait_lds();
     if (more) load_v(b);
-    strip += kWaves;
+    strip += W;
   };
   auto pass = [&](auto finite) {
     w.clear();
@@ -1080,10 +1098,10 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
   };
   pass(std::false_type{});
   if (w.spoilt()) {
-    ahead.start(c, it.k0 + 32 * wave, 32 * kWaves, (strips - wave + kWaves - 1) / kWaves);
+    ahead.start(c, c.k, it.k0 + 32 * wave, 32 * W, (strips - wave + W - 1) / W);
     begin();
     pass(std::true_type{});
-    for (strip = wave; strip < strips; strip += kWaves)
+    for (strip = wave; strip < strips; strip += W)
       if (strip < u0 || strip >= u1) w.add_lost(c, it.k0 + strip * 32, min(it.k0 + strip * 32 + 32, it.k1));
   }
 
@@ -1098,14 +1116,14 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
   __syncthreads();
   const int G = a.num_heads / a.num_kv_heads;
   const int rows = min(kFew, it.rows - row0);
-  for (int i = threadIdx.x; i < rows * (S::D / 4); i += kThreads) {
+  for (int i = threadIdx.x; i < rows * (S::D / 4); i += 64 * W) {
     const int r = i / (S::D / 4), d = i % (S::D / 4) * 4;
     float top = kNoScore, l = 0.0f;
     f4 o = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) top = fmaxf(top, ml[(v * kFew + r) * 2]);
+    for (int v = 0; v < W; ++v) top = fmaxf(top, ml[(v * kFew + r) * 2]);
 #pragma unroll
-    for (int v = 0; v < kWaves; ++v) {
+    for (int v = 0; v < W; ++v) {
       const float f = __builtin_amdgcn_exp2f(ml[(v * kFew + r) * 2] - top);
       l += f * ml[(v * kFew + r) * 2 + 1];
       const f4 x = *(const f4*)((const float*)smem + (v * kFew + r) * kRow + d);
@@ -1128,15 +1146,23 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
   __syncthreads();
 }
 
-// LDS: strips of keys (or what the waves' results are joined through), the
-// waves' m and l, and their flags.
-template <typename S>
-constexpr int kPrivateBytes = (S::kPrivate > S::kJoin ? S::kPrivate : S::kJoin) + kWaves * kFew * 8;
+// LDS of W waves: strips of keys (or what the waves' results are joined
+// through), the waves' m and l, and their flags.
+template <typename S, int W>
+struct FewLds {
+  static constexpr int kStrips = W * 64 * S::RB;  // per wave one strip of 32 keys of K and V
+  static constexpr int kJoin = W * kFew * (S::D + 4) * 4;
+  static constexpr int kStats = kStrips > kJoin ? kStrips : kJoin;
+  static constexpr int kEnd = kStats + W * kFew * 8;
+};
+template <typename S, bool MIXED, int W>
+constexpr int kFlagAt = MIXED && S::kShared > FewLds<S, W>::kEnd ? S::kShared : FewLds<S, W>::kEnd;
+// Waves per SIMD that the registers are to suffice for.
 template <typename S, bool MIXED>
-constexpr int kFlagAt = MIXED && S::kShared > kPrivateBytes<S> ? S::kShared : kPrivateBytes<S>;
+constexpr int kOccupancy = MIXED && S::D <= 64 ? 3 : S::D <= 128 ? 2 : 1;
 
-template <typename S, bool MIXED>
-__global__ __launch_bounds__(kThreads, S::D <= 64 ? 3 : S::D <= 128 ? 2 : 1) void attention_kernel(KvAttnArgs a, Plan p, float* parts, float* stats) {
+template <typename S, bool MIXED, int W>
+__global__ __launch_bounds__(64 * W, (kOccupancy<S, MIXED>)) void attention_kernel(KvAttnArgs a, Plan p, float* parts, float* stats) {
   extern __shared__ __attribute__((aligned(256))) char smem[];
   const uint32_t lds = (uint32_t)(uintptr_t)(SCOOT_LDS char*)smem;
   const uint32_t heads = (uint32_t)a.num_kv_heads;
@@ -1145,16 +1171,16 @@ __global__ __launch_bounds__(kThreads, S::D <= 64 ? 3 : S::D <= 128 ? 2 : 1) voi
   Item it;
   if (!find_item(a, p, index, (int)split, it)) return;
   const int64_t slot = blockIdx.x;
-  int* flag = (int*)(smem + kFlagAt<S, MIXED>);
+  int* flag = (int*)(smem + kFlagAt<S, MIXED, W>);
   if constexpr (MIXED) {
     if (it.shared) {
       shared_tile<S>(a, it, (int)head, lds, flag, slot, parts, stats);
       return;
     }
   }
-  float* ml = (float*)(smem + (S::kPrivate > S::kJoin ? S::kPrivate : S::kJoin));
+  float* ml = (float*)(smem + FewLds<S, W>::kStats);
   for (int row0 = 0; row0 < it.rows; row0 += kFew)
-    few_rows<S>(a, it, row0, (int)head, lds, smem, ml, flag, slot * (MIXED ? kTileRows : kFew), parts, stats);
+    few_rows<S, W>(a, it, row0, (int)head, lds, smem, ml, flag, slot * (MIXED ? kTileRows : kFew), parts, stats);
 }
 
 // Joins the parts of a tile's keys: one workgroup per tile and key head.
@@ -1196,18 +1222,31 @@ __global__ __launch_bounds__(kThreads) void join_kernel(KvAttnArgs a, Plan p, co
   }
 }
 
+template <typename S, bool MIXED, int W>
+int launch_kernel(const KvAttnArgs& a, const Plan& p, float* parts, float* stats, hipStream_t stream) {
+  const int rc = allow_full_lds((const void*)attention_kernel<S, MIXED, W>, "kv attention");
+  if (rc != SCOOT_OK) return rc;
+  hipLaunchKernelGGL((attention_kernel<S, MIXED, W>), dim3((unsigned)(p.items * p.splits * a.num_kv_heads)), dim3(64 * W),
+                     (kFlagAt<S, MIXED, W> + 4 * W), stream, a, p, parts, stats);
+  return SCOOT_OK;
+}
+
 template <typename S>
 int launch(const KvAttnArgs& a, const Plan& p, float* parts, float* stats, hipStream_t stream) {
-  const dim3 grid((unsigned)(p.items * p.splits * a.num_kv_heads)), join((unsigned)(p.items * a.num_kv_heads));
-  const int bytes = (p.mixed ? kFlagAt<S, true> : kFlagAt<S, false>) + 4 * kWaves;
-  const void* f = p.mixed ? (const void*)attention_kernel<S, true> : (const void*)attention_kernel<S, false>;
-  const int rc = allow_full_lds(f, "kv attention");
+  int rc;
+  if (p.mixed) {
+    rc = launch_kernel<S, true, kWaves>(a, p, parts, stats, stream);
+  } else {
+    if constexpr (S::RB <= kWideRow) {
+      if (p.waves == 8) rc = launch_kernel<S, false, 8>(a, p, parts, stats, stream);
+      else rc = launch_kernel<S, false, kWaves>(a, p, parts, stats, stream);
+    } else {
+      rc = launch_kernel<S, false, kWaves>(a, p, parts, stats, stream);
+    }
+  }
   if (rc != SCOOT_OK) return rc;
-  if (p.mixed)
-    hipLaunchKernelGGL((attention_kernel<S, true>), grid, dim3(kThreads), bytes, stream, a, p, parts, stats);
-  else
-    hipLaunchKernelGGL((attention_kernel<S, false>), grid, dim3(kThreads), bytes, stream, a, p, parts, stats);
-  if (p.splits > 1) hipLaunchKernelGGL((join_kernel<S>), join, dim3(kThreads), 0, stream, a, p, parts, stats);
+  if (p.splits > 1)
+    hipLaunchKernelGGL((join_kernel<S>), dim3((unsigned)(p.items * a.num_kv_heads)), dim3(kThreads), 0, stream, a, p, parts, stats);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess) return fail(SCOOT_ERR_DEVICE, std::string("kv attention launch: ") + hipGetErrorString(err));
   return SCOOT_OK;
