@@ -7,6 +7,7 @@ device; torch provides only memory and the stream.  Names follow the C calls
 without the ``scoot_`` prefix.
 """
 import ctypes as C
+import functools
 
 import numpy as np
 
@@ -682,53 +683,77 @@ def known_constraints(Xc, A, b, out=None, stream=None):
 
 
 # ------------------------------------------- the engine's key/value cache
+#
+# These calls take microseconds on the device, so the binding is lean: arguments
+# are tested in one expression, and only a failing one is looked into.
 KV_F16, KV_BF16, KV_F8 = 0, 1, 2
+_kv_types = None
 
 
-def _kv_type(t, name, cache=False):
+def _kv_setup():
+    global _kv_types, _raw_stream, _int32, _int64, _uint8
     import torch
-    if t.dtype == torch.float16:
-        return KV_F16
-    if t.dtype == torch.bfloat16:
-        return KV_BF16
-    if cache and t.dtype == torch.float8_e4m3fn:
-        return KV_F8
-    raise ValueError(f"{name} must be float16 or bfloat16" + (" or float8_e4m3fn" if cache else ""))
+    _int32, _int64, _uint8 = torch.int32, torch.int64, torch.uint8
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    _raw_stream = raw or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+    _kv_types = {torch.float16: KV_F16, torch.bfloat16: KV_BF16, torch.float8_e4m3fn: KV_F8}
+    return _kv_types
 
 
-def _kv_ints(t, name, numel=None):
-    import torch
-    _require_device(t, name, torch.int32, numel)
+def _kv_stream(stream, t):
+    return _raw_stream(t.device.index) if stream is None else int(stream)
 
 
-def _kv_vectors(t, name, heads=None, dim=None):
-    """(tokens, heads, dim) with the last dimension contiguous; other strides are free."""
-    if t.device.type != "cuda":
-        raise ValueError(f"{name} must be a device tensor")
-    if t.dim() != 3 or (heads is not None and t.shape[1] != heads) or (dim is not None and t.shape[2] != dim):
-        raise ValueError(f"{name} must be (tokens, {heads or 'heads'}, {dim or 'head_dim'})")
-    if t.stride(2) != 1 and t.shape[2] != 1:
-        raise ValueError(f"{name} must be contiguous in its last dimension")
+def _kv_refuse(*tests):
+    for ok, what in tests:
+        if not ok:
+            raise ValueError(what)
 
 
-def _kv_table(t, num_seqs=None):
-    import torch
-    if t.device.type != "cuda" or t.dtype != torch.int32 or t.dim() != 2:
-        raise ValueError("block_table must be an int32 (requests, blocks) device tensor")
-    if (t.stride(1) != 1 and t.shape[1] > 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-        raise ValueError("block_table must be contiguous in its last dimension")
-    if num_seqs is not None and t.shape[0] != num_seqs:
-        raise ValueError(f"block_table must have {num_seqs} rows")
+def _is_ints(t):
+    return t.is_cuda and t.dtype is _int32 and t.is_contiguous()
+
+
+def _refuse_ints(t, name, numel=None):
+    _kv_refuse((t.is_cuda, f"{name} must be a device tensor"), (t.dtype is _int32, f"{name} must be int32"),
+               (t.is_contiguous(), f"{name} must be contiguous"),
+               (numel is None or t.numel() == numel, f"{name} must have {numel} elements"))
+
+
+def _is_table(t, rows):
+    return t.is_cuda and t.dtype is _int32 and t.dim() == 2 and t.shape[0] == rows and (
+        t.is_contiguous() or ((t.stride(1) == 1 or t.shape[1] <= 1) and (rows <= 1 or t.stride(0) >= t.shape[1])))
+
+
+def _refuse_table(t, rows):
+    _kv_refuse((t.is_cuda, "block_table must be a device tensor"),
+               (t.dtype is _int32 and t.dim() == 2, "block_table must be int32 (requests, blocks)"),
+               (t.dim() != 2 or t.shape[0] == rows, f"block_table must have {rows} rows"),
+               (_is_table(t, rows), "block_table must be contiguous in its last dimension"))
+
+
+def _refuse_vectors(t, name, heads, dim, types="float16 or bfloat16"):
+    _kv_refuse((t.dtype in _kv_types and _kv_types[t.dtype] != KV_F8, f"{name} must be {types}"),
+               (t.is_cuda, f"{name} must be a device tensor"),
+               (t.dim() == 3 and (heads is None or t.shape[1] == heads) and t.shape[2] == dim,
+                f"{name} must be (tokens, {heads or 'heads'}, {dim})"),
+               (t.dim() != 3 or t.stride(2) == 1, f"{name} must be contiguous in its last dimension"))
+
+
+def _is_vectors(t, heads, dim):
+    return t.is_cuda and t.dim() == 3 and t.shape[2] == dim and t.shape[1] == heads and t.stride(2) == 1
 
 
 def _kv_caches(k_cache, v_cache):
-    kind = _kv_type(k_cache, "k_cache", cache=True)
-    if k_cache.dim() != 4:
-        raise ValueError("k_cache must be (blocks, kv_heads, block_size, head_dim)")
-    _require_device(k_cache, "k_cache")
-    _require_device(v_cache, "v_cache", k_cache.dtype)
-    if v_cache.shape != k_cache.shape:
-        raise ValueError("v_cache must have k_cache's shape")
+    """The caches' type."""
+    kind = _kv_types.get(k_cache.dtype)
+    if not (kind is not None and k_cache.is_cuda and v_cache.is_cuda and k_cache.dim() == 4 and k_cache.is_contiguous()
+            and v_cache.is_contiguous() and v_cache.dtype is k_cache.dtype and v_cache.shape == k_cache.shape):
+        _kv_refuse((kind is not None, "k_cache must be float16, bfloat16 or float8_e4m3fn"),
+                   (k_cache.is_cuda and v_cache.is_cuda, "k_cache and v_cache must be device tensors"),
+                   (k_cache.dim() == 4, "k_cache must be (blocks, kv_heads, block_size, head_dim)"),
+                   (k_cache.is_contiguous() and v_cache.is_contiguous(), "k_cache and v_cache must be contiguous"),
+                   (False, "v_cache must have k_cache's type and shape"))
     return kind
 
 
@@ -742,9 +767,9 @@ class KVBatch:
         import torch
         self.num_seqs, self.max_tokens = int(num_seqs), int(max_tokens)
         self.slots = torch.empty(max_tokens, dtype=torch.int64, device=device)
-        ints = torch.empty(2 * num_seqs + 5 + max_tokens, dtype=torch.int32, device=device)
-        self.query_start, self.seq_len, self.counts, self.positions = ints.split(
-            (num_seqs + 1, num_seqs, 4, max_tokens))
+        self.query_start, self.seq_len, self.counts, self.positions = torch.empty(
+            2 * num_seqs + 5 + max_tokens, dtype=torch.int32, device=device).split_with_sizes(
+                (num_seqs + 1, num_seqs, 4, max_tokens))
 
 
 def kv_assign(context_len, new_len, block_table, free_blocks, block_size, max_tokens, out=None, stream=None):
@@ -753,19 +778,24 @@ def kv_assign(context_len, new_len, block_table, free_blocks, block_size, max_to
     slots and positions, and, from ``free_blocks`` in order, the new entries of
     ``block_table`` (int32 (requests, blocks), updated in place).  Returns a
     KVBatch (``out`` if given); nothing is read back."""
+    _kv_types or _kv_setup()
     n = context_len.numel()
-    _kv_ints(context_len, "context_len")
-    _kv_ints(new_len, "new_len", n)
-    _kv_ints(free_blocks, "free_blocks")
-    _kv_table(block_table, n)
+    if not (_is_ints(context_len) and _is_ints(new_len) and new_len.numel() == n and _is_ints(free_blocks)
+            and _is_table(block_table, n)):
+        _refuse_ints(context_len, "context_len")
+        _refuse_ints(new_len, "new_len", n)
+        _refuse_ints(free_blocks, "free_blocks")
+        _refuse_table(block_table, n)
     b = KVBatch(n, max_tokens, context_len.device) if out is None else out
     if b.num_seqs != n or b.max_tokens != max_tokens:
         raise ValueError("out was made for other sizes")
-    check(lib().scoot_kv_assign(context_len.data_ptr(), new_len.data_ptr(), n, block_size, block_table.data_ptr(),
-                                block_table.shape[1], max(block_table.stride(0), block_table.shape[1]),
-                                free_blocks.data_ptr(), free_blocks.numel(), max_tokens, b.query_start.data_ptr(),
-                                b.seq_len.data_ptr(), b.positions.data_ptr(), b.slots.data_ptr(),
-                                b.counts.data_ptr(), _stream(stream)), "kv_assign")
+    cols = block_table.shape[1]
+    rc = lib().scoot_kv_assign(context_len.data_ptr(), new_len.data_ptr(), n, block_size, block_table.data_ptr(), cols,
+                               max(block_table.stride(0), cols), free_blocks.data_ptr(), free_blocks.numel(), max_tokens,
+                               b.query_start.data_ptr(), b.seq_len.data_ptr(), b.positions.data_ptr(),
+                               b.slots.data_ptr(), b.counts.data_ptr(), _kv_stream(stream, context_len))
+    if rc:
+        check(rc, "kv_assign")
     return b
 
 
@@ -774,18 +804,24 @@ def kv_write(k, v, slots, k_cache, v_cache, k_scale=1.0, v_scale=1.0, stream=Non
     bfloat16, at their slots of the caches (blocks, kv_heads, block_size,
     head_dim) of the same type, or float8_e4m3fn, which holds value / scale
     (scoot_kv_write).  Slots outside the cache are skipped."""
-    import torch
+    _kv_types or _kv_setup()
     cache_type = _kv_caches(k_cache, v_cache)
     blocks, heads, block_size, dim = k_cache.shape
-    kind = _kv_type(k, "k")
-    _kv_vectors(k, "k", heads, dim)
-    _kv_vectors(v, "v", heads, dim)
-    if v.dtype != k.dtype or v.shape[0] != k.shape[0]:
-        raise ValueError("v must have k's type and number of tokens")
-    _require_device(slots, "slots", torch.int64, k.shape[0])
-    check(lib().scoot_kv_write(k.data_ptr(), v.data_ptr(), kind, k.shape[0], heads, dim, k.stride(0), k.stride(1),
-                               v.stride(0), v.stride(1), slots.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-                               cache_type, blocks, block_size, k_scale, v_scale, _stream(stream)), "kv_write")
+    kind = _kv_types.get(k.dtype, KV_F8)
+    if not (kind != KV_F8 and v.dtype is k.dtype and _is_vectors(k, heads, dim) and _is_vectors(v, heads, dim)
+            and v.shape[0] == k.shape[0] == slots.numel() and slots.is_cuda and slots.dtype is _int64
+            and slots.is_contiguous()):
+        _refuse_vectors(k, "k", heads, dim)
+        _refuse_vectors(v, "v", heads, dim)
+        _kv_refuse((v.dtype is k.dtype and v.shape[0] == k.shape[0], "v must have k's type and number of tokens"),
+                   (slots.is_cuda and slots.dtype is _int64 and slots.is_contiguous(),
+                    "slots must be a contiguous int64 device tensor"),
+                   (False, f"slots must have {k.shape[0]} elements"))
+    rc = lib().scoot_kv_write(k.data_ptr(), v.data_ptr(), kind, k.shape[0], heads, dim, k.stride(0), k.stride(1),
+                              v.stride(0), v.stride(1), slots.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+                              cache_type, blocks, block_size, k_scale, v_scale, _kv_stream(stream, k))
+    if rc:
+        check(rc, "kv_write")
 
 
 def kv_attention(q, k_cache, v_cache, block_table, query_start, seq_len, max_new_len, max_seq_len, scale=None,
@@ -798,45 +834,53 @@ def kv_attention(q, k_cache, v_cache, block_table, query_start, seq_len, max_new
     of the step as the caller knows it; ``scale`` defaults to head_dim ** -0.5.
     A ``workspace`` (uint8, at least kv_attention_workspace's bytes) may be
     kept between calls.  Returns ``out``, made if not given."""
-    import torch
+    _kv_types or _kv_setup()
     cache_type = _kv_caches(k_cache, v_cache)
     blocks, kv_heads, block_size, dim = k_cache.shape
-    kind = _kv_type(q, "q")
-    _kv_vectors(q, "q", None, dim)
-    tokens, heads = q.shape[0], q.shape[1]
+    kind = _kv_types.get(q.dtype, KV_F8)
     n = seq_len.numel()
-    _kv_ints(seq_len, "seq_len")
-    _kv_ints(query_start, "query_start", n + 1)
-    _kv_table(block_table, n)
+    if not (kind != KV_F8 and q.is_cuda and q.dim() == 3 and q.shape[2] == dim and q.stride(2) == 1 and _is_ints(seq_len)
+            and _is_ints(query_start) and query_start.numel() == n + 1 and _is_table(block_table, n)):
+        _refuse_vectors(q, "q", None, dim)
+        _refuse_ints(seq_len, "seq_len")
+        _refuse_ints(query_start, "query_start", n + 1)
+        _refuse_table(block_table, n)
+    tokens, heads = q.shape[0], q.shape[1]
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    else:
-        _kv_vectors(out, "out", heads, dim)
-        if out.dtype != q.dtype or out.shape[0] != tokens:
-            raise ValueError("out must have q's type and shape")
+        out = q.new_empty((tokens, heads, dim))
+    elif not (out.dtype is q.dtype and _is_vectors(out, heads, dim) and out.shape[0] == tokens):
+        _refuse_vectors(out, "out", heads, dim)
+        raise ValueError("out must have q's type and shape")
     if workspace is None:
-        need = kv_attention_workspace(tokens, heads, kv_heads, dim, n, max_new_len, max_seq_len, window)
+        need = _kv_workspace(tokens, heads, kv_heads, dim, n, max_new_len, max_seq_len, window)
         if need:
-            workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+            workspace = q.new_empty(need, dtype=_uint8)
     else:
-        _require_device(workspace, "workspace", torch.uint8)
-    check(lib().scoot_kv_attention(q.data_ptr(), kind, tokens, heads, kv_heads, dim, q.stride(0), q.stride(1),
-                                   k_cache.data_ptr(), v_cache.data_ptr(), cache_type, blocks, block_size,
-                                   block_table.data_ptr(), block_table.shape[1],
-                                   max(block_table.stride(0), block_table.shape[1]), query_start.data_ptr(),
-                                   seq_len.data_ptr(), n, max_new_len, max_seq_len,
-                                   dim ** -0.5 if scale is None else scale, window, k_scale, v_scale, out.data_ptr(),
-                                   out.stride(0), out.stride(1), None if workspace is None else workspace.data_ptr(),
-                                   0 if workspace is None else workspace.numel(), _stream(stream)), "kv_attention")
+        need = workspace.numel()
+        _kv_refuse((workspace.is_cuda and workspace.dtype is _uint8 and workspace.is_contiguous(),
+                    "workspace must be a contiguous uint8 device tensor"))
+    cols = block_table.shape[1]
+    rc = lib().scoot_kv_attention(q.data_ptr(), kind, tokens, heads, kv_heads, dim, q.stride(0), q.stride(1),
+                                  k_cache.data_ptr(), v_cache.data_ptr(), cache_type, blocks, block_size,
+                                  block_table.data_ptr(), cols, max(block_table.stride(0), cols), query_start.data_ptr(),
+                                  seq_len.data_ptr(), n, max_new_len, max_seq_len, dim ** -0.5 if scale is None else scale,
+                                  window, k_scale, v_scale, out.data_ptr(), out.stride(0), out.stride(1),
+                                  None if workspace is None else workspace.data_ptr(), need, _kv_stream(stream, q))
+    if rc:
+        check(rc, "kv_attention")
     return out
+
+
+@functools.lru_cache(maxsize=4096)
+def _kv_workspace(*sizes):
+    b = C.c_uint64(0)
+    check(lib().scoot_kv_attention_workspace(*sizes, C.byref(b)), "kv_attention_workspace")
+    return b.value
 
 
 def kv_attention_workspace(tokens, heads, kv_heads, head_dim, num_seqs, max_new_len, max_seq_len, window=0):
     """Bytes that kv_attention needs for these sizes."""
-    b = C.c_uint64(0)
-    check(lib().scoot_kv_attention_workspace(tokens, heads, kv_heads, head_dim, num_seqs, max_new_len, max_seq_len,
-                                             window, C.byref(b)), "kv_attention_workspace")
-    return b.value
+    return _kv_workspace(tokens, heads, kv_heads, head_dim, num_seqs, max_new_len, max_seq_len, window)
 
 
 # ------------------------------------------------------ the suggestion step

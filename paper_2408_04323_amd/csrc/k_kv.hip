@@ -171,8 +171,11 @@ __global__ __launch_bounds__(THREADS) void kv_assign_kernel(KvAssignArgs a, uint
 
 // --------------------------------------------------------------------- writes
 //
-// A thread moves eight elements of one token's key (or value) head; the
-// cache's rows are the vectors' rows, so both sides are whole cache lines.
+// A workgroup takes one head of a few consecutive tokens, a thread eight
+// elements of the key and of the value.  The cache's rows are the vectors'
+// rows, and tokens in order mostly lie next to each other, so a wave reads
+// whole lines and writes 512 bytes (8-bit) or a KiB without a gap.  Bytes
+// bound this: both sides once.
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 template <typename T>
@@ -192,43 +195,43 @@ __device__ __forceinline__ float limit_f8(float x, float scale) {
   return x > 448.0f ? 448.0f : x < -448.0f ? -448.0f : x;
 }
 
-constexpr int kWriteThreads = 256;
+constexpr int kWriteThreads = 256;  // at most: (elements of a head / 8) x tokens
 
 template <typename T, bool F8, bool ALIGNED>
 __global__ __launch_bounds__(kWriteThreads) void kv_write_kernel(KvWriteArgs a) {
-  const uint32_t chunks = (uint32_t)a.head_dim / 8, per_token = chunks * (uint32_t)a.num_heads;
-  const int64_t total = a.num_tokens * per_token;
-  for (int64_t i = (int64_t)blockIdx.x * kWriteThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kWriteThreads) {
-    const int64_t t = i / per_token;
-    const uint32_t r = (uint32_t)(i - t * per_token), h = r / chunks, c = r - h * chunks;
-    const int64_t slot = a.slots[t];
-    if (slot < 0 || slot >= a.num_slots) continue;
-    const int64_t block = slot >> a.block_shift, at = slot & ((1 << a.block_shift) - 1);
-    const int64_t to = ((((block * a.num_heads + h) << a.block_shift) + at) * a.head_dim) + c * 8;
+  const int64_t t = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+  if (t >= a.num_tokens) return;
+  const int64_t slot = a.slots[t];
+  if (slot < 0 || slot >= a.num_slots) return;
+  const uint32_t h = blockIdx.y, c = threadIdx.x;
+  const int64_t block = slot >> a.block_shift, at = slot & ((1 << a.block_shift) - 1);
+  const int64_t to = (((block * a.num_heads + h) << a.block_shift) + at) * a.head_dim + c * 8;
+  typename Vec8<T>::type x[2];
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const T* p = (const T*)a.src[s] + t * a.token_stride[s] + h * a.head_stride[s] + c * 8;
-      typename Vec8<T>::type x;
-      if (ALIGNED) {
-        x = *(const typename Vec8<T>::type*)p;
-      } else {
+  for (int s = 0; s < 2; ++s) {
+    const T* p = (const T*)a.src[s] + t * a.token_stride[s] + h * a.head_stride[s] + c * 8;
+    if (ALIGNED) {
+      x[s] = *(const typename Vec8<T>::type*)p;
+    } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = p[j];
+      for (int j = 0; j < 8; ++j) x[s][j] = p[j];
+    }
+  }
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    if (F8) {
+      int w[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float f[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[k] = limit_f8((float)x[s][4 * j + k], a.scale[s]);
+        w[j] = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
+        w[j] = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], w[j], true);
       }
-      if (F8) {
-        int w[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          float f[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) f[k] = limit_f8((float)x[4 * j + k], a.scale[s]);
-          w[j] = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
-          w[j] = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], w[j], true);
-        }
-        *(int2*)((uint8_t*)a.cache[s] + to) = make_int2(w[0], w[1]);
-      } else {
-        *(typename Vec8<T>::type*)((T*)a.cache[s] + to) = x;
-      }
+      *(int2*)((uint8_t*)a.cache[s] + to) = make_int2(w[0], w[1]);
+    } else {
+      *(typename Vec8<T>::type*)((T*)a.cache[s] + to) = x[s];
     }
   }
 }
@@ -240,11 +243,13 @@ int launched(const char* what) {
 }
 
 template <typename T, bool F8>
-void write_launch(const KvWriteArgs& a, bool aligned, dim3 grid, hipStream_t s) {
+void write_launch(const KvWriteArgs& a, bool aligned, hipStream_t s) {
+  const int chunks = a.head_dim / 8, tokens = kWriteThreads / chunks;  // head_dim <= 1024: two tokens at least
+  const dim3 grid((unsigned)((a.num_tokens + tokens - 1) / tokens), (unsigned)a.num_heads), block(chunks, tokens);
   if (aligned)
-    hipLaunchKernelGGL((kv_write_kernel<T, F8, true>), grid, dim3(kWriteThreads), 0, s, a);
+    hipLaunchKernelGGL((kv_write_kernel<T, F8, true>), grid, block, 0, s, a);
   else
-    hipLaunchKernelGGL((kv_write_kernel<T, F8, false>), grid, dim3(kWriteThreads), 0, s, a);
+    hipLaunchKernelGGL((kv_write_kernel<T, F8, false>), grid, block, 0, s, a);
 }
 
 }  // namespace
@@ -263,19 +268,17 @@ int launch_kv_assign(const KvAssignArgs& a, void* stream) {
 }
 
 int launch_kv_write(const KvWriteArgs& a, scoot_kv_type type, scoot_kv_type cache_type, void* stream) {
-  const int64_t total = a.num_tokens * (a.head_dim / 8) * a.num_heads;
-  const dim3 grid((unsigned)std::min<int64_t>((total + kWriteThreads - 1) / kWriteThreads, 1 << 20));
   const hipStream_t s = (hipStream_t)stream;
   bool aligned = true;  // every row starts on 16 bytes
   for (int i = 0; i < 2; ++i)
     aligned = aligned && ((uintptr_t)a.src[i] & 15) == 0 && ((a.token_stride[i] | a.head_stride[i]) & 7) == 0;
   const bool f8 = cache_type == SCOOT_KV_F8;
   if (type == SCOOT_KV_F16) {
-    if (f8) write_launch<_Float16, true>(a, aligned, grid, s);
-    else write_launch<_Float16, false>(a, aligned, grid, s);
+    if (f8) write_launch<_Float16, true>(a, aligned, s);
+    else write_launch<_Float16, false>(a, aligned, s);
   } else {
-    if (f8) write_launch<__bf16, true>(a, aligned, grid, s);
-    else write_launch<__bf16, false>(a, aligned, grid, s);
+    if (f8) write_launch<__bf16, true>(a, aligned, s);
+    else write_launch<__bf16, false>(a, aligned, s);
   }
   return launched("kv write launch");
 }
