@@ -68,7 +68,7 @@ uint64_t kv_attention_workspace_bytes(int64_t num_tokens, int num_heads, int num
 int launch_kv_attention(const KvAttnArgs& a, scoot_kv_type type, scoot_kv_type cache_type, void* stream) {
   const Plan p = plan(a.num_tokens, a.num_heads, a.num_kv_heads, a.head_dim * (cache_type == SCOOT_KV_F8 ? 1 : 2), a.num_seqs,
                       a.max_new_len, a.max_seq_len, a.window);
-  if (p.items * p.splits * a.num_kv_heads > 0x7fffffff)
+  if (2 * p.items * std::max(p.splits, kTileRows / kFew) * a.num_kv_heads > 0x7fffffff)
     return fail_static(SCOOT_ERR_UNSUPPORTED, "kv attention: too many rows for one call");
   float* parts = (float*)a.workspace;
   float* stats = parts + slots(p, a.num_kv_heads) * a.head_dim;

@@ -1167,10 +1167,15 @@ __global__ __launch_bounds__(64 * W, (kOccupancy<S, MIXED>)) void attention_kern
   const uint32_t lds = (uint32_t)(uintptr_t)(SCOOT_LDS char*)smem;
   const uint32_t heads = (uint32_t)a.num_kv_heads;
   const uint32_t head = blockIdx.x % heads, rest = blockIdx.x / heads;
-  const uint32_t split = rest % (uint32_t)p.splits, index = rest / (uint32_t)p.splits;
+  const uint32_t split = rest % (uint32_t)p.splits;
+  uint32_t index = rest / (uint32_t)p.splits;
+  // Tiles come twice: first those of many rows, which take longest, then those of few.
+  const bool few = MIXED && index >= p.items;
+  if (few) index -= (uint32_t)p.items;
   Item it;
   if (!find_item(a, p, index, (int)split, it)) return;
-  const int64_t slot = blockIdx.x;
+  if (MIXED && it.shared == few) return;
+  const int64_t slot = ((int64_t)index * p.splits + split) * heads + head;
   int* flag = (int*)(smem + kFlagAt<S, MIXED, W>);
   if constexpr (MIXED) {
     if (it.shared) {
@@ -1183,33 +1188,34 @@ __global__ __launch_bounds__(64 * W, (kOccupancy<S, MIXED>)) void attention_kern
     few_rows<S, W>(a, it, row0, (int)head, lds, smem, ml, flag, slot * (MIXED ? kTileRows : kFew), parts, stats);
 }
 
-// Joins the parts of a tile's keys: one workgroup per tile and key head.
+// Joins the parts of a tile's keys: one workgroup per 16 rows of a tile and key head.
 template <typename S>
 __global__ __launch_bounds__(kThreads) void join_kernel(KvAttnArgs a, Plan p, const float* parts, const float* stats) {
   typedef typename S::T T;
   const uint32_t heads = (uint32_t)a.num_kv_heads;
-  const uint32_t head = blockIdx.x % heads, index = blockIdx.x / heads;
+  const int tile_rows = p.mixed ? kTileRows : kFew;
+  const uint32_t chunks = (uint32_t)tile_rows / kFew;
+  const uint32_t head = blockIdx.x % heads, rest = blockIdx.x / heads, first = rest % chunks * kFew, index = rest / chunks;
   Item it;
   if (!find_item(a, p, index, 0, it) || it.splits < 2) return;
-  const int tile_rows = p.mixed ? kTileRows : kFew;
   const int G = a.num_heads / a.num_kv_heads;
-  const int rows = min(tile_rows, it.rows - it.row0);
+  const int rows = min((int)(first + kFew), min(tile_rows, it.rows - it.row0));
   constexpr int per = S::D / 4;
-  for (int i = threadIdx.x; i < rows * per; i += kThreads) {
+  const int64_t step = (int64_t)heads * tile_rows;  // rows of the workspace from part to part
+  for (int i = first * per + threadIdx.x; i < rows * per; i += kThreads) {
     const int r = i / per, d = (i - r * per) * 4;
+    const int64_t at = ((int64_t)index * p.splits * heads + head) * tile_rows + r;
     float top = kNoScore, sum = 0.0f;
     f4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
     for (int s = 0; s < it.splits; ++s) {
-      const int64_t at = (((int64_t)index * p.splits + s) * heads + head) * tile_rows + r;
-      top = fmaxf(top, stats[at * 2]);
-    }
-    for (int s = 0; s < it.splits; ++s) {
-      const int64_t at = (((int64_t)index * p.splits + s) * heads + head) * tile_rows + r;
-      const float f = __builtin_amdgcn_exp2f(stats[at * 2] - top);
-      sum += f * stats[at * 2 + 1];
-      const f4 x = *(const f4*)(parts + at * S::D + d);
+      const float2 ml = *(const float2*)(stats + (at + s * step) * 2);
+      const f4 x = *(const f4*)(parts + (at + s * step) * S::D + d);
+      const float up = fmaxf(top, ml.x), f = __builtin_amdgcn_exp2f(top - up), g = __builtin_amdgcn_exp2f(ml.x - up);
+      top = up;
+      sum = sum * f + ml.y * g;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] += f * x[j];
+      for (int j = 0; j < 4; ++j) o[j] = o[j] * f + x[j] * g;
     }
     const float inv = sum == 0.0f ? 0.0f : a.v_scale / sum;
     const int row = it.row0 + r, tok = row / G, g = row - tok * G;
@@ -1226,7 +1232,7 @@ template <typename S, bool MIXED, int W>
 int launch_kernel(const KvAttnArgs& a, const Plan& p, float* parts, float* stats, hipStream_t stream) {
   const int rc = allow_full_lds((const void*)attention_kernel<S, MIXED, W>, "kv attention");
   if (rc != SCOOT_OK) return rc;
-  hipLaunchKernelGGL((attention_kernel<S, MIXED, W>), dim3((unsigned)(p.items * p.splits * a.num_kv_heads)), dim3(64 * W),
+  hipLaunchKernelGGL((attention_kernel<S, MIXED, W>), dim3((unsigned)((MIXED ? 2 : 1) * p.items * p.splits * a.num_kv_heads)), dim3(64 * W),
                      (kFlagAt<S, MIXED, W> + 4 * W), stream, a, p, parts, stats);
   return SCOOT_OK;
 }
@@ -1246,7 +1252,8 @@ int launch(const KvAttnArgs& a, const Plan& p, float* parts, float* stats, hipSt
   }
   if (rc != SCOOT_OK) return rc;
   if (p.splits > 1)
-    hipLaunchKernelGGL((join_kernel<S>), dim3((unsigned)(p.items * a.num_kv_heads)), dim3(kThreads), 0, stream, a, p, parts, stats);
+    hipLaunchKernelGGL((join_kernel<S>), dim3((unsigned)(p.items * ((p.mixed ? kTileRows : kFew) / kFew) * a.num_kv_heads)), dim3(kThreads),
+                       0, stream, a, p, parts, stats);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess) return fail(SCOOT_ERR_DEVICE, std::string("kv attention launch: ") + hipGetErrorString(err));
   return SCOOT_OK;
