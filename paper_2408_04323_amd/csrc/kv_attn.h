@@ -50,8 +50,11 @@ typedef short s4 __attribute__((ext_vector_type(4)));
 constexpr int kWaves = 4;                    // of a workgroup (one of few rows may have eight)
 constexpr int kThreads = 64 * kWaves;
 constexpr int kFew = 16;                     // rows of a request that one workgroup's waves handle together
-constexpr int kRows = 32;                    // rows of a wave otherwise,
-constexpr int kTileRows = kRows * kWaves;    // and of its workgroup
+constexpr int kRows = 32;                    // rows of a wave otherwise
+// Waves that share their rows otherwise, each with a part of the head dimension of o: of 256 dimensions a whole o does
+// not fit the registers of two waves per SIMD.
+constexpr int shared_by(int head_dim) { return head_dim > 192 ? 2 : 1; }
+constexpr int tile_rows(int head_dim) { return kRows * kWaves / shared_by(head_dim); }
 constexpr float kNoScore = -3.0e38f;         // m before any key was seen; finite, so that m - m is 0
 constexpr int kWideRow = 256;                // bytes of a cache row up to which eight waves' strips fit the LDS
 constexpr int kReadsAhead = 4;               // operands of the matrix instructions on their way out of LDS
@@ -72,7 +75,7 @@ struct Shape {
   static constexpr int NJ = RB / 64;                // loads of 1 KiB for 16 rows
   static constexpr int ST = D <= 128 ? 64 : 32;     // keys per strip of a shared tile
   static constexpr int SUB = ST / 32;
-  static constexpr int kShared = 4 * ST * RB;       // two buffers of K and V
+  static constexpr int kStrip = 2 * ST * RB;        // bytes of a strip of K and V
   // The second product runs in the cache's 16-bit type; 8-bit values are exact in half precision, which rounds the
   // weights eight times finer than bfloat16.
   typedef typename std::conditional<F8, _Float16, T>::type W;
@@ -146,7 +149,7 @@ __device__ __forceinline__ void load_lds(uint32_t to, uint64_t addr) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(addr) : "memory");
 }
 
-// What a workgroup works on: rows row0 .. row0 + 127 (or 15) of a request, one key
+// What a workgroup works on: rows of a request from row0 on (a tile's, or 16), one key
 // head, keys [k0, k1) of the tile's, as split `split` of `splits`.
 struct Item {
   int64_t q0;       // token of the request's row 0
@@ -165,8 +168,9 @@ struct Plan {
   int64_t items;    // tiles or requests
   int splits;
   int part;         // keys per part, a multiple of 128
-  bool mixed;       // tiles of kTileRows rows; else requests
-  int waves;        // of a workgroup, if not mixed
+  int tile_rows;    // rows of a tile; 0: the items are requests, of few rows each
+  int waves;        // of a workgroup then
+  bool deep;        // tiles: at most one workgroup per compute unit, which may have more LDS
 };
 
 __device__ __forceinline__ int64_t clamp64(int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; }
@@ -176,14 +180,14 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 // Finds the item: false if there is none.  All values are the same in every lane.
 //
 // Tiles need no list: request i, whose tokens start at s_i, owns the numbers
-// from floor(s_i G / 128) + i on, which are enough for its ceil(n_i G / 128)
-// tiles whatever n_i is; the request of a number is searched for 64-fold.
+// from floor(s_i G / R) + i on (R rows per tile), which are enough for its
+// ceil(n_i G / R) tiles whatever n_i is; the request of a number is searched for 64-fold.
 __device__ __forceinline__ bool find_item(const KvAttnArgs& a, const Plan& p, int64_t index, int split, Item& it) {
   const int G = a.num_heads / a.num_kv_heads;
   const SCOOT_CONST int32_t* qs = (const SCOOT_CONST int32_t*)a.query_start;
   int seq;
   int64_t first = 0;
-  if (p.mixed) {
+  if (p.tile_rows) {
     const int lane = threadIdx.x & 63;
     int lo = 0, hi = a.num_seqs;
     bool any = true;
@@ -191,7 +195,7 @@ __device__ __forceinline__ bool find_item(const KvAttnArgs& a, const Plan& p, in
       const int step = (hi - lo + 63) / 64;
       const int64_t i = lo + (int64_t)lane * step;
       bool below = false;
-      if (i < hi) below = clamp64(a.query_start[i], 0, a.num_tokens) * G / kTileRows + i <= index;
+      if (i < hi) below = clamp64(a.query_start[i], 0, a.num_tokens) * G / p.tile_rows + i <= index;
       const int n = __popcll(__builtin_amdgcn_ballot_w64(below));
       if (n == 0) {
         any = false;
@@ -202,7 +206,7 @@ __device__ __forceinline__ bool find_item(const KvAttnArgs& a, const Plan& p, in
     } while (hi - lo > 1);
     if (!any) return false;
     seq = uniform(lo);
-    first = clamp64(qs[seq], 0, a.num_tokens) * G / kTileRows + seq;
+    first = clamp64(qs[seq], 0, a.num_tokens) * G / p.tile_rows + seq;
   } else {
     seq = uniform((int)index);
   }
@@ -216,17 +220,17 @@ __device__ __forceinline__ bool find_item(const KvAttnArgs& a, const Plan& p, in
   it.rows = rows > 0x7fffffff ? 0x7fffffff : (int)rows;
   it.seq = seq;
   it.len = (int)clamp64(len, 0, (int64_t)a.max_blocks << a.block_shift);
-  it.shared = p.mixed && rows > kFew;
+  it.shared = p.tile_rows && rows > kFew;
   int last_row = it.rows - 1;
   int splits = p.splits;
   if (it.shared) {
-    const int tiles = (it.rows + kTileRows - 1) / kTileRows;
+    const int tiles = (int)(((int64_t)it.rows + p.tile_rows - 1) / p.tile_rows);
     const int64_t t = index - first;
     if (t >= tiles) return false;
-    it.row0 = (tiles - 1 - (int)t) * kTileRows;  // the tiles that see most come first
-    if (it.row0 + kTileRows - 1 < last_row) last_row = it.row0 + kTileRows - 1;
+    it.row0 = (tiles - 1 - (int)t) * p.tile_rows;  // the tiles that see most come first
+    if (last_row - it.row0 >= p.tile_rows) last_row = it.row0 + p.tile_rows - 1;
   } else {
-    if (p.mixed && index != first) return false;
+    if (p.tile_rows && index != first) return false;
     it.row0 = 0;
     if (it.rows > kFew) splits = 1;  // more rows than the caller announced: one workgroup, tile after tile
   }
@@ -293,7 +297,8 @@ template <typename S, int N>
 struct Ahead {
   uint32_t lo[N], hi[N];
   uint64_t from;  // keys or values
-  int key0, stride, strips, base;
+  int key0, stride, strips, base, end;
+  bool holes;     // some group below key `end` of the 64 strips has no block
 
   __device__ __forceinline__ void fill(const Cache<S>& c, int strip) {
     base = strip;
@@ -306,18 +311,23 @@ struct Ahead {
       e[j] = (uint32_t)c.entries[i < c.last ? i : c.last];
     }
     settle();
+    bool hole = false;
 #pragma unroll
     for (int j = 0; j < N; ++j) {
+      hole |= (key + 8 * j < end) & (e[j] >= c.num_blocks);
       const uint64_t at = from + c.at(key + 8 * j, e[j]);
       lo[j] = (uint32_t)at;
       hi[j] = (uint32_t)(at >> 32);
     }
+    holes = __builtin_amdgcn_ballot_w64(hole) != 0;
   }
-  __device__ __forceinline__ void start(const Cache<S>& c, uint64_t cache, int first, int keys, int n) {
+  __device__ __forceinline__ void start(const Cache<S>& c, uint64_t cache, int first, int keys, int n, int last) {
     from = cache;
     key0 = first;
     stride = keys;
     strips = n;
+    end = last;
+    holes = false;
     if (n > 0) fill(c, 0);
   }
   // The groups of a strip, which follows the last one asked for.
@@ -493,7 +503,7 @@ __device__ __forceinline__ float stored(uint64_t row, int d) {
 // ------------------------------------------------------------- shared tiles
 //
 // More than 16 rows: the four waves take 32 rows each and share strips of keys
-// through two LDS buffers.
+// through LDS buffers, R of them, the loads R - 1 strips ahead.
 template <typename S>
 struct Tile32 {
   typedef typename S::T T;
@@ -502,20 +512,23 @@ struct Tile32 {
   typedef typename Vec<W>::v8 W8;
   typedef Tile32Order<S> Order;
   static constexpr int KS = S::D / 16;  // steps of the first product
-  static constexpr int DT = S::D / 32;  // tiles of O^T
+  static constexpr int SH = shared_by(S::D);
+  static constexpr int DT = S::D / 32 / SH;  // tiles of this wave's part of O^T
+  static constexpr int VN = Order::VM < DT ? Order::VM : DT;
 
-  int lane, half;
+  int lane, half, d0;  // d0: first dimension of the part
   Sight see;
   T8 q[KS];
   f16v o[DT];
   float m, l;
   int koff[Order::KM / 2];  // LDS offsets of this lane's reads
-  int voff[Order::VM];
+  int voff[VN];
   uint32_t kdma[S::NJ], vdma[S::NJ];
 
-  __device__ __forceinline__ void setup() {
+  __device__ __forceinline__ void setup(int wave) {
     lane = threadIdx.x & 63;
     half = lane >> 5;
+    d0 = wave % SH * (32 * DT);
     const int key = key_of_row(lane & 31);
 #pragma unroll
     for (int n = 0; n < Order::KM / 2; ++n) koff[n] = key * S::RB + ((2 * n + half) ^ Order::k(key)) * 16;
@@ -523,7 +536,7 @@ struct Tile32 {
     const int row = 8 * half + (S::F8 ? n16 >> 1 : n16 >> 2);
     const int in = S::F8 ? dhalf * 16 + (n16 & 1) * 8 : dhalf * 32 + (n16 & 3) * 8;
 #pragma unroll
-    for (int n = 0; n < Order::VM; ++n) voff[n] = row * S::RB + (n ^ Order::v(row)) * (16 * Order::U) + in;
+    for (int n = 0; n < VN; ++n) voff[n] = row * S::RB + ((d0 / 32 + n) ^ Order::v(row)) * (16 * Order::U) + in;
     load_offsets<S, Order>(kdma, vdma);
   }
 
@@ -585,17 +598,17 @@ struct Tile32 {
   }
 
   struct Lds {
-    uint32_t at[Order::VM];
+    uint32_t at[VN];
   };
   __device__ __forceinline__ Lds values_at(uint32_t lds) const {
     Lds r;
 #pragma unroll
-    for (int n = 0; n < Order::VM; ++n) r.at[n] = pinned(lds + voff[n]);
+    for (int n = 0; n < VN; ++n) r.at[n] = pinned(lds + voff[n]);
     return r;
   }
-  // V^T: lane's element d = 32 dt + lane % 32 of the keys 16 ks + 8 half .. + 7.
+  // V^T: lane's element d = d0 + 32 dt + lane % 32 of the keys 16 ks + 8 half .. + 7.
   __device__ __forceinline__ W8 values(const Lds& v, int ks, int dt) const {
-    const uint32_t at = v.at[dt % Order::VM] + (dt / Order::VM) * (Order::VM * 16 * Order::U) + ks * 16 * S::RB;
+    const uint32_t at = v.at[dt % VN] + (dt / VN) * (VN * 16 * Order::U) + ks * 16 * S::RB;
     if constexpr (S::F8) {
       const i2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((SCOOT_LDS i2*)at);
       return widen<_Float16>(v[0], v[1]);
@@ -705,7 +718,7 @@ struct Tile32 {
       for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float x = stored<S>(row, 32 * d + 8 * (i / 4) + 4 * half + i % 4);
+          const float x = stored<S>(row, d0 + 32 * d + 8 * (i / 4) + 4 * half + i % 4);
           o[d][i] += (mine & !(__builtin_fabsf(x) < INFINITY)) ? x : 0.0f;
         }
     }
@@ -723,8 +736,8 @@ struct Tile32 {
     if (row0 + (lane & 31) >= it.rows) return;
     if (it.splits > 1) {
       at += lane & 31;
-      if (half == 0) *(float2*)(stats + at * 2) = make_float2(m, sum);
-      float* p = parts + at * S::D + 4 * half;
+      if (half == 0 && d0 == 0) *(float2*)(stats + at * 2) = make_float2(m, sum);
+      float* p = parts + at * S::D + d0 + 4 * half;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -736,7 +749,7 @@ struct Tile32 {
     }
     const float inv = sum == 0.0f ? 0.0f : a.v_scale / sum;  // a row that saw nothing has o = 0, too
     const int G = a.num_heads / a.num_kv_heads;
-    T* p = (T*)a.out + (it.q0 + see.tok) * a.out_token_stride + (int64_t)(head * G + see.g) * a.out_head_stride + 4 * half;
+    T* p = (T*)a.out + (it.q0 + see.tok) * a.out_token_stride + (int64_t)(head * G + see.g) * a.out_head_stride + d0 + 4 * half;
     typedef T T4 __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -750,13 +763,13 @@ struct Tile32 {
   }
 };
 
-template <typename S>
+template <typename S, int R>
 __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it, int head, uint32_t lds, int* flag,
                                             int64_t slot, float* parts, float* stats) {
   const int wave = uniform(threadIdx.x >> 6);
   Tile32<S> w;
   Cache<S> c;
-  w.setup();
+  w.setup(wave);
   c.setup(a, it.seq, head);
   constexpr int kHalf = S::ST * S::RB;  // bytes of a strip's keys
   const int strips = (it.k1 - it.k0 + S::ST - 1) / S::ST;
@@ -764,27 +777,33 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
   // A strip's loads in groups of 16 keys of K or V; every wave takes its share.
   const int share = S::SUB == 2 ? wave : wave & 1;
   Ahead<S, 2> ahead;
-  ahead.start(c, c.k, it.k0 + 16 * share, S::ST, strips);
+  ahead.start(c, c.k, it.k0 + 16 * share, S::ST, strips, it.k1);
   const uint64_t to_v = c.v - c.k;
   auto load = [&](int strip) {
-    const uint32_t to = lds + (strip & 1) * (2 * kHalf) + share * 16 * S::RB;
+    const uint32_t to = lds + (strip & (R - 1)) * S::kStrip + share * 16 * S::RB;
     uint64_t b[2];
     ahead.get(c, strip, b);
     if (S::SUB == 2 || wave < 2) load16<S>(w.kdma, to, b[0], b[1]);
     if (S::SUB == 2 || wave >= 2) load16<S>(w.vdma, to + kHalf, to_v + b[0], to_v + b[1]);
   };
-  if (strips > 0) load(0);
-  const int row0 = it.row0 + wave * kRows;
+  auto begin = [&] {
+    for (int i = 0; i < R - 1 && i < strips; ++i) load(i);
+  };
+  begin();
+  const int row0 = it.row0 + wave / shared_by(S::D) * kRows;
   w.start(a, it, row0, head);
-  const bool holes = any_holes<kWaves>(a, it, flag);
+  // The waves' first addresses tell of their entries.
+  const bool holes = strips <= 64 ? any_wave<kWaves>(ahead.holes, flag) : any_holes<kWaves>(a, it, flag);
   settle();
   int u0, u1;
   w.see.whole(it, strips, S::ST, holes, u0, u1);
 
   auto turn = [&](int strip) {
-    // This strip has landed, for every wave, and everyone is done with the other buffer.
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (strip + 1 < strips) load(strip + 1);
+    // This strip has landed, for every wave, and everyone is done with the one before, whose place the next load takes.
+    if (R > 2 && strip + R - 2 < strips) wait_vm<(R - 2) * S::SUB * S::NJ>();
+    else wait_vm<0>();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (strip + R - 1 < strips) load(strip + R - 1);
   };
   auto pass = [&](auto finite) {
     w.clear();
@@ -793,7 +812,7 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
       if (strip >= u0 && strip < u1) {
         for (; strip < u1; ++strip) {
           turn(strip);
-          const uint32_t at = lds + (strip & 1) * (2 * kHalf);
+          const uint32_t at = lds + (strip & (R - 1)) * S::kStrip;
           f16v s[S::SUB];
           w.scores(at, s);
           typename Tile32<S>::W8 p[2 * S::SUB], v[kReadsAhead];
@@ -804,7 +823,7 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
         }
       } else {
         turn(strip);
-        const uint32_t at = lds + (strip & 1) * (2 * kHalf);
+        const uint32_t at = lds + (strip & (R - 1)) * S::kStrip;
         const int key0 = it.k0 + strip * S::ST;
         if (key0 <= w.see.hi_max) {
           f16v s[S::SUB];
@@ -821,13 +840,13 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
   };
   pass(std::false_type{});
   if (any_wave<kWaves>(w.spoilt(), flag)) {
-    ahead.start(c, c.k, it.k0 + 16 * share, S::ST, strips);
-    load(0);
+    ahead.start(c, c.k, it.k0 + 16 * share, S::ST, strips, it.k1);
+    begin();
     pass(std::true_type{});
     w.add_lost(c, it.k0, u0 < u1 ? it.k0 + u0 * S::ST : it.k1);  // the strips that went through the mask
     if (u0 < u1) w.add_lost(c, it.k0 + u1 * S::ST, it.k1);
   }
-  w.store(a, it, row0, head, slot * kTileRows + wave * kRows, parts, stats);
+  w.store(a, it, row0, head, slot * tile_rows(S::D) + (row0 - it.row0), parts, stats);
 }
 
 // --------------------------------------------------------------- few rows
@@ -1037,7 +1056,7 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
     uint64_t b[4];
   };
   Ahead<S, 4> ahead;  // its strips: every fourth one
-  ahead.start(c, c.k, it.k0 + 32 * wave, 32 * W, (strips - wave + W - 1) / W);
+  ahead.start(c, c.k, it.k0 + 32 * wave, 32 * W, (strips - wave + W - 1) / W, it.k1);
   auto load_k = [&](const Base& b) {
     load16<S>(w.kdma, kat, b.b[0], b.b[1]);
     load16<S, Tile16Order<S>::kNext>(w.kdma, kat + 16 * S::RB, b.b[2], b.b[3]);
@@ -1057,7 +1076,9 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
   };
   begin();
   w.start(a, it, row0, head);
-  const bool holes = any_holes<W>(a, it, flag);
+  // The first addresses tell of their entries.
+  bool holes = ahead.holes;
+  if (strips > 64 * W) holes = any_holes<W>(a, it, flag);
   settle();
   int u0, u1;  // strips seen whole by every row
   w.see.whole(it, strips, 32, holes, u0, u1);
@@ -1098,7 +1119,7 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
   };
   pass(std::false_type{});
   if (w.spoilt()) {
-    ahead.start(c, c.k, it.k0 + 32 * wave, 32 * W, (strips - wave + W - 1) / W);
+    ahead.start(c, c.k, it.k0 + 32 * wave, 32 * W, (strips - wave + W - 1) / W, it.k1);
     begin();
     pass(std::true_type{});
     for (strip = wave; strip < strips; strip += W)
@@ -1155,105 +1176,120 @@ struct FewLds {
   static constexpr int kStats = kStrips > kJoin ? kStrips : kJoin;
   static constexpr int kEnd = kStats + W * kFew * 8;
 };
-template <typename S, bool MIXED, int W>
-constexpr int kFlagAt = MIXED && S::kShared > FewLds<S, W>::kEnd ? S::kShared : FewLds<S, W>::kEnd;
+// R > 0: tiles through R buffers, requests of few rows among them; R = 0: these alone.
+template <typename S, int R, int W>
+constexpr int kFlagAt = R * S::kStrip > FewLds<S, W>::kEnd ? R * S::kStrip : FewLds<S, W>::kEnd;
 // Waves per SIMD that the registers are to suffice for.
-template <typename S, bool MIXED>
-constexpr int kOccupancy = MIXED && S::D <= 64 ? 3 : S::D <= 128 ? 2 : 1;
+template <typename S, int R>
+constexpr int kOccupancy = R == 2 && S::D == 64 ? 3 : R > 0 && S::D == 192 ? 1 : 2;
 
-template <typename S, bool MIXED, int W>
-__global__ __launch_bounds__(64 * W, (kOccupancy<S, MIXED>)) void attention_kernel(KvAttnArgs a, Plan p, float* parts, float* stats) {
+template <typename S, int R, int W>
+__global__ __launch_bounds__(64 * W, (kOccupancy<S, R>)) void attention_kernel(KvAttnArgs a, Plan p, float* parts, float* stats) {
   extern __shared__ __attribute__((aligned(256))) char smem[];
   const uint32_t lds = (uint32_t)(uintptr_t)(SCOOT_LDS char*)smem;
   const uint32_t heads = (uint32_t)a.num_kv_heads;
   const uint32_t head = blockIdx.x % heads, rest = blockIdx.x / heads;
-  const uint32_t split = rest % (uint32_t)p.splits;
-  uint32_t index = rest / (uint32_t)p.splits;
-  // Tiles come twice: first those of many rows, which take longest, then those of few.
-  const bool few = MIXED && index >= p.items;
-  if (few) index -= (uint32_t)p.items;
+  const uint32_t split = rest % (uint32_t)p.splits, index = rest / (uint32_t)p.splits;
   Item it;
   if (!find_item(a, p, index, (int)split, it)) return;
-  if (MIXED && it.shared == few) return;
-  const int64_t slot = ((int64_t)index * p.splits + split) * heads + head;
-  int* flag = (int*)(smem + kFlagAt<S, MIXED, W>);
-  if constexpr (MIXED) {
+  const int64_t slot = blockIdx.x;
+  int* flag = (int*)(smem + kFlagAt<S, R, W>);
+  if constexpr (R > 0) {
     if (it.shared) {
-      shared_tile<S>(a, it, (int)head, lds, flag, slot, parts, stats);
+      shared_tile<S, R>(a, it, (int)head, lds, flag, slot, parts, stats);
       return;
     }
   }
   float* ml = (float*)(smem + FewLds<S, W>::kStats);
   for (int row0 = 0; row0 < it.rows; row0 += kFew)
-    few_rows<S, W>(a, it, row0, (int)head, lds, smem, ml, flag, slot * (MIXED ? kTileRows : kFew), parts, stats);
+    few_rows<S, W>(a, it, row0, (int)head, lds, smem, ml, flag, slot * (R > 0 ? tile_rows(S::D) : kFew), parts, stats);
 }
 
-// Joins the parts of a tile's keys: one workgroup per 16 rows of a tile and key head.
+// Joins the parts of a tile's keys: one workgroup per key head and as many rows
+// as it has threads for, four dimensions each.  Latency bounds this, so the
+// parts are read eight at a time.
 template <typename S>
-__global__ __launch_bounds__(kThreads) void join_kernel(KvAttnArgs a, Plan p, const float* parts, const float* stats) {
+constexpr int kJoinRows = kThreads / (S::D / 4);
+
+template <typename S>
+__global__ __launch_bounds__(kThreads) void join_kernel(KvAttnArgs a, Plan p, const float* parts, const float* stats, int chunks) {
   typedef typename S::T T;
   const uint32_t heads = (uint32_t)a.num_kv_heads;
-  const int tile_rows = p.mixed ? kTileRows : kFew;
-  const uint32_t chunks = (uint32_t)tile_rows / kFew;
-  const uint32_t head = blockIdx.x % heads, rest = blockIdx.x / heads, first = rest % chunks * kFew, index = rest / chunks;
+  const int tile = p.tile_rows ? p.tile_rows : kFew;
+  const uint32_t head = blockIdx.x % heads, rest = blockIdx.x / heads, index = rest / (uint32_t)chunks;
+  constexpr int per = S::D / 4;
+  const int r = (int)(rest % (uint32_t)chunks) * kJoinRows<S> + (int)threadIdx.x / per, d = (int)threadIdx.x % per * 4;
   Item it;
   if (!find_item(a, p, index, 0, it) || it.splits < 2) return;
+  if ((int)threadIdx.x >= kJoinRows<S> * per || r >= min(tile, it.rows - it.row0)) return;
   const int G = a.num_heads / a.num_kv_heads;
-  const int rows = min((int)(first + kFew), min(tile_rows, it.rows - it.row0));
-  constexpr int per = S::D / 4;
-  const int64_t step = (int64_t)heads * tile_rows;  // rows of the workspace from part to part
-  for (int i = first * per + threadIdx.x; i < rows * per; i += kThreads) {
-    const int r = i / per, d = (i - r * per) * 4;
-    const int64_t at = ((int64_t)index * p.splits * heads + head) * tile_rows + r;
-    float top = kNoScore, sum = 0.0f;
-    f4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-    for (int s = 0; s < it.splits; ++s) {
-      const float2 ml = *(const float2*)(stats + (at + s * step) * 2);
-      const f4 x = *(const f4*)(parts + (at + s * step) * S::D + d);
-      const float up = fmaxf(top, ml.x), f = __builtin_amdgcn_exp2f(top - up), g = __builtin_amdgcn_exp2f(ml.x - up);
-      top = up;
-      sum = sum * f + ml.y * g;
+  const int64_t step = (int64_t)heads * tile;  // rows of the workspace from part to part
+  const int64_t at = ((int64_t)index * p.splits * heads + head) * tile + r;
+  float top = kNoScore, sum = 0.0f;
+  f4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int s0 = 0; s0 < it.splits; s0 += 8) {
+    float2 ml[8];
+    f4 x[8];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] = o[j] * f + x[j] * g;
+    for (int j = 0; j < 8; ++j) {
+      const int64_t from = at + min(s0 + j, it.splits - 1) * step;
+      ml[j] = *(const float2*)(stats + from * 2);
+      x[j] = *(const f4*)(parts + from * S::D + d);
     }
-    const float inv = sum == 0.0f ? 0.0f : a.v_scale / sum;
-    const int row = it.row0 + r, tok = row / G, g = row - tok * G;
-    T* out = (T*)a.out + (it.q0 + tok) * a.out_token_stride + (int64_t)(head * G + g) * a.out_head_stride + d;
-    typedef T T4 __attribute__((ext_vector_type(4)));
-    T4 x;
+    float up = top;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = (T)(o[j] * inv);
-    *(T4*)out = x;
+    for (int j = 0; j < 8; ++j) up = fmaxf(up, ml[j].x);  // the last part's again is no harm
+    const float f = __builtin_amdgcn_exp2f(top - up);
+    top = up;
+    sum *= f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] *= f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float g = s0 + j < it.splits ? __builtin_amdgcn_exp2f(ml[j].x - up) : 0.0f;
+      sum += s0 + j < it.splits ? ml[j].y * g : 0.0f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] += s0 + j < it.splits ? x[j][i] * g : 0.0f;
+    }
   }
+  const float inv = sum == 0.0f ? 0.0f : a.v_scale / sum;
+  const int row = it.row0 + r, tok = row / G, g = row - tok * G;
+  T* out = (T*)a.out + (it.q0 + tok) * a.out_token_stride + (int64_t)(head * G + g) * a.out_head_stride + d;
+  typedef T T4 __attribute__((ext_vector_type(4)));
+  T4 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = (T)(o[i] * inv);
+  *(T4*)out = y;
 }
 
-template <typename S, bool MIXED, int W>
+template <typename S, int R, int W>
 int launch_kernel(const KvAttnArgs& a, const Plan& p, float* parts, float* stats, hipStream_t stream) {
-  const int rc = allow_full_lds((const void*)attention_kernel<S, MIXED, W>, "kv attention");
+  const int rc = allow_full_lds((const void*)attention_kernel<S, R, W>, "kv attention");
   if (rc != SCOOT_OK) return rc;
-  hipLaunchKernelGGL((attention_kernel<S, MIXED, W>), dim3((unsigned)((MIXED ? 2 : 1) * p.items * p.splits * a.num_kv_heads)), dim3(64 * W),
-                     (kFlagAt<S, MIXED, W> + 4 * W), stream, a, p, parts, stats);
+  hipLaunchKernelGGL((attention_kernel<S, R, W>), dim3((unsigned)(p.items * p.splits * a.num_kv_heads)), dim3(64 * W),
+                     (kFlagAt<S, R, W> + 4 * W), stream, a, p, parts, stats);
   return SCOOT_OK;
 }
 
 template <typename S>
 int launch(const KvAttnArgs& a, const Plan& p, float* parts, float* stats, hipStream_t stream) {
   int rc;
-  if (p.mixed) {
-    rc = launch_kernel<S, true, kWaves>(a, p, parts, stats, stream);
+  if (p.tile_rows) {
+    rc = p.deep ? launch_kernel<S, 4, kWaves>(a, p, parts, stats, stream) : launch_kernel<S, 2, kWaves>(a, p, parts, stats, stream);
   } else {
     if constexpr (S::RB <= kWideRow) {
-      if (p.waves == 8) rc = launch_kernel<S, false, 8>(a, p, parts, stats, stream);
-      else rc = launch_kernel<S, false, kWaves>(a, p, parts, stats, stream);
+      if (p.waves == 8) rc = launch_kernel<S, 0, 8>(a, p, parts, stats, stream);
+      else rc = launch_kernel<S, 0, kWaves>(a, p, parts, stats, stream);
     } else {
-      rc = launch_kernel<S, false, kWaves>(a, p, parts, stats, stream);
+      rc = launch_kernel<S, 0, kWaves>(a, p, parts, stats, stream);
     }
   }
   if (rc != SCOOT_OK) return rc;
-  if (p.splits > 1)
-    hipLaunchKernelGGL((join_kernel<S>), dim3((unsigned)(p.items * ((p.mixed ? kTileRows : kFew) / kFew) * a.num_kv_heads)), dim3(kThreads),
-                       0, stream, a, p, parts, stats);
+  if (p.splits > 1) {
+    const int chunks = ((p.tile_rows ? p.tile_rows : kFew) + kJoinRows<S> - 1) / kJoinRows<S>;
+    hipLaunchKernelGGL((join_kernel<S>), dim3((unsigned)(p.items * chunks * a.num_kv_heads)), dim3(kThreads), 0, stream, a, p, parts,
+                       stats, chunks);
+  }
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess) return fail(SCOOT_ERR_DEVICE, std::string("kv attention launch: ") + hipGetErrorString(err));
   return SCOOT_OK;
