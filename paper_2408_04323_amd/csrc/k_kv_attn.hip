@@ -18,32 +18,66 @@ using namespace kvattn;
 
 constexpr int64_t kUnits = 256;   // compute units
 constexpr int kPartOf = 128;      // parts are multiples of this many keys: a strip of 32 for each of four waves
-constexpr int kMinPart = 512;     // and not smaller than this: a part costs about as much as 256 keys to join
+constexpr int kMinPart = 512;     // of few rows, for each four waves: a part costs about as much as 256 keys to join
+constexpr int kMinTilePart = 256; // of tiles: four strips
+constexpr double kJoinLaunch = 5e-6;  // seconds, bytes per second
+constexpr double kJoinRate = 6e12;
 constexpr int kAlone = 2048;      // keys that eight waves of one workgroup do not share with another
 
+// Parts of the keys of tiles: as many as give each compute unit r workgroups,
+// for the r with the shortest time.  A workgroup alone on its unit takes about
+// 0.77, 1, 1.45, 1.9 us per strip of 64 keys (heads of 64, 128, 192, 256
+// dimensions); others beside it that much again, but some are shorter, and they
+// fill its gaps: 3/4 (1/2 with heads of 64) of it.  Parts cost a launch and their
+// way through memory, once out and once in.  Against as many parts as fill the
+// chip: chunks of 331 tokens over 547 37 -> 27 us (one part, not two), of 160 over
+// 10,087 50 -> 40 (ten, not twenty).
+int64_t parts_of_tiles(int64_t groups, int64_t keys, int64_t rows, int head_dim) {
+  const int most = head_dim <= 64 ? 3 : head_dim <= 128 ? 2 : 1;  // workgroups that fit a compute unit
+  const double strip = head_dim <= 64 ? 0.77e-6 : head_dim / 128.0 * 0.9e-6 + 0.1e-6, beside = head_dim <= 64 ? 0.5 : 0.75;
+  int64_t best = 1;
+  double least = 0;
+  for (int r = 0; r <= most; ++r) {
+    const int64_t n = r == 0 ? 1 : std::min(r * kUnits / groups, (keys + kMinTilePart - 1) / kMinTilePart);
+    if (r > 0 && n <= best) continue;
+    const double load = (double)(groups * n) / kUnits;
+    double t = (double)keys / (64 * n) * strip * (load > 1 ? 1 + beside * (load - 1) : 1);
+    if (n > 1) t += kJoinLaunch + (double)(2 * n * rows * head_dim * 4) / kJoinRate;
+    if (r == 0 || t < least) least = t, best = n;
+  }
+  return best;
+}
+
 // Requests of at most 16 rows (new tokens x heads per key head) are items of
-// their own; once some have more, tiles of 128 (64) rows are.  Where the items do
-// not fill the chip (tiles), or not four times over (few rows, whose lengths
-// differ most), their keys are split into parts.
+// their own; once some have more, tiles of 128 rows are.  The keys of tiles are
+// split as above, those of few rows until the items fill the chip four times over
+// (their lengths differ most).
 Plan plan(int64_t num_tokens, int num_heads, int num_kv_heads, int head_dim, int element_bytes, int num_seqs, int64_t max_new_len,
           int64_t max_seq_len, int window) {
   Plan p{};
   const int64_t G = num_heads / num_kv_heads;
   const int64_t longest = std::min<int64_t>(max_new_len, num_tokens);
   const bool tiles = longest * G > kFew;
-  p.tile_rows = tiles ? tile_rows(head_dim) : 0;
+  p.tile_rows = tiles ? kTile : 0;
   p.items = tiles ? num_tokens * G / p.tile_rows + num_seqs : num_seqs;
   int64_t keys = max_seq_len;
   if (window > 0) keys = std::min<int64_t>(keys, (int64_t)window + (tiles ? p.tile_rows / G : longest) + 32);
   keys = std::max<int64_t>(keys, 1);
-  const int64_t groups = std::max<int64_t>(1, p.items * num_kv_heads);
-  const int64_t resident = kUnits * (tiles && head_dim <= 64 ? 3 : 2);
-  int64_t want = std::max<int64_t>(1, (tiles ? resident : 4 * resident) / groups);
-  // Few items of few rows: eight waves each.
-  p.waves = !tiles && groups <= kUnits && head_dim * element_bytes <= kWideRow ? 8 : kWaves;
-  if (p.waves == 8) want = keys <= kAlone ? 1 : std::max<int64_t>(1, 2 * kUnits / groups);
+  // Tiles that have rows: at least this many of the numbers.
+  const int64_t real = tiles ? std::max<int64_t>(num_seqs, (num_tokens * G + p.tile_rows - 1) / p.tile_rows) : p.items;
+  const int64_t groups = std::max<int64_t>(1, real * num_kv_heads);
+  int64_t want;
+  p.waves = kWaves;
+  if (tiles) {
+    want = parts_of_tiles(groups, keys, num_tokens * num_heads, head_dim);
+  } else {
+    // Few items of few rows: eight waves each.
+    if (groups <= kUnits && head_dim * element_bytes <= kWideRow) p.waves = 8;
+    want = p.waves == 8 ? (keys <= kAlone ? 1 : 2 * kUnits / groups) : 8 * kUnits / groups;
+  }
+  want = std::max<int64_t>(1, want);
   int64_t part = (keys + want - 1) / want;
-  part = std::max<int64_t>(kMinPart * (p.waves / kWaves), (part + kPartOf - 1) / kPartOf * kPartOf);
+  part = std::max<int64_t>(tiles ? kMinTilePart : kMinPart * (p.waves / kWaves), (part + kPartOf - 1) / kPartOf * kPartOf);
   p.part = (int)std::min<int64_t>(part, (int64_t)1 << 30);
   p.splits = (int)((keys + p.part - 1) / p.part);
   p.deep = groups * p.splits <= kUnits;
@@ -67,7 +101,10 @@ uint64_t kv_attention_workspace_bytes(int64_t num_tokens, int num_heads, int num
 int launch_kv_attention(const KvAttnArgs& a, scoot_kv_type type, scoot_kv_type cache_type, void* stream) {
   const Plan p = plan(a.num_tokens, a.num_heads, a.num_kv_heads, a.head_dim, cache_type == SCOOT_KV_F8 ? 1 : 2, a.num_seqs,
                       a.max_new_len, a.max_seq_len, a.window);
-  if (p.items * std::max(p.splits, tile_rows(64) / 4) * a.num_kv_heads > 0x7fffffff)
+  // A launch has less than 2^32 threads: a workgroup per part of an item and key head; in a join, per 4 rows at least.
+  const int64_t groups = p.items * a.num_kv_heads;
+  const int64_t joins = p.splits > 1 ? groups * (p.tile_rows ? p.tile_rows : kFew) / 4 * kThreads : 0;
+  if (std::max(groups * p.splits * 64 * p.waves, joins) > 0xffffffffLL)
     return fail_static(SCOOT_ERR_UNSUPPORTED, "kv attention: too many rows for one call");
   float* parts = (float*)a.workspace;
   float* stats = parts + slots(p, a.num_kv_heads) * a.head_dim;

@@ -3,14 +3,13 @@
 //
 // Mathematics.  A row is one query of one head; the G query heads that share a
 // key head are rows of the same tile, row = token * G + head.  With scores s_t
-// = q . k_t the rows keep m, l and o over the keys seen so far: for every strip
-// of keys, w_t = 2^(c s_t - m), l += sum w_t, o += sum w_t v_t.  m is a score
-// of the row, its largest at some strip; when a strip's weights add up to more
-// than 2^14, m moves up to that strip's largest and l and o are multiplied by
-// 2^(old m - m), so no weight overflows, one at least is 1, and most strips
-// take no maximum and leave o alone.  Parts of
-// the keys that were handled by different waves or workgroups are joined by the
-// same factors.
+// = q . k_t the rows keep m, l and o over the keys seen so far: for every 32
+// keys, w_t = 2^(c s_t - m), l += sum w_t, o += sum w_t v_t.  m is a score of the
+// row; only when a lane's weights of these keys add up to more than 2^14 it moves
+// up to their largest, and l and o are multiplied by 2^(old m - m).  So no
+// weight overflows, one at least is 1, and most keys take no maximum and leave o
+// alone.  Parts of the keys that were handled by different waves or workgroups
+// are joined by the same factors.
 //
 // Matrix instructions (32 x 32 x 16).  S^T = K Q^T with the keys as rows and the
 // queries as columns, then O^T += V^T W^T: a lane's sixteen scores belong to
@@ -23,6 +22,13 @@
 // Keys and values go from memory straight into LDS, 1 KiB per instruction,
 // their 16-byte pieces permuted on the way so that both kinds of reads spread
 // over the banks.
+//
+// Registers decide the waves per SIMD: three for tiles of 64 dimensions, two for
+// 128, one for 192 and 256, where o and q take 144 and 192 of a lane's 512.  A
+// wave alone keeps both units busy by itself: the weights of 32 keys are made
+// between the matrix instructions of the next products.  Late chunks over 30,000
+// keys, heads of 64, 128, 192, 256: 0.98, 1.16, 0.86, 0.90 PFLOP/s (192 and 256
+// with two waves and half of the registers each, o shared: 0.58 and 0.44).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -51,14 +57,11 @@ constexpr int kWaves = 4;                    // of a workgroup (one of few rows 
 constexpr int kThreads = 64 * kWaves;
 constexpr int kFew = 16;                     // rows of a request that one workgroup's waves handle together
 constexpr int kRows = 32;                    // rows of a wave otherwise
-// Waves that share their rows otherwise, each with a part of the head dimension of o: of 256 dimensions a whole o does
-// not fit the registers of two waves per SIMD.
-constexpr int shared_by(int head_dim) { return head_dim > 192 ? 2 : 1; }
-constexpr int tile_rows(int head_dim) { return kRows * kWaves / shared_by(head_dim); }
+constexpr int kTile = kRows * kWaves;        // rows of a tile
 constexpr float kNoScore = -3.0e38f;         // m before any key was seen; finite, so that m - m is 0
 constexpr int kWideRow = 256;                // bytes of a cache row up to which eight waves' strips fit the LDS
 constexpr int kReadsAhead = 4;               // operands of the matrix instructions on their way out of LDS
-constexpr float kMost = 16384.0f;            // m moves once a strip's weights in a lane add up to more
+constexpr float kMost = 16384.0f;            // m moves once a lane's weights of 32 keys add up to more
 
 constexpr int gcd256(int x) { return x % 256 == 0 ? 256 : x % 128 == 0 ? 128 : 64; }
 
@@ -73,8 +76,7 @@ struct Shape {
   static constexpr int PC = RB / 16;                // 16-byte pieces of a row
   static constexpr int g = 256 / gcd256(RB);        // rows this far apart start on the same bank
   static constexpr int NJ = RB / 64;                // loads of 1 KiB for 16 rows
-  static constexpr int ST = D <= 128 ? 64 : 32;     // keys per strip of a shared tile
-  static constexpr int SUB = ST / 32;
+  static constexpr int ST = 64;                     // keys per strip of a shared tile
   static constexpr int kStrip = 2 * ST * RB;        // bytes of a strip of K and V
   // The second product runs in the cache's 16-bit type; 8-bit values are exact in half precision, which rounds the
   // weights eight times finer than bfloat16.
@@ -136,6 +138,11 @@ __device__ __forceinline__ uint32_t pinned(uint32_t v) {
   asm("" : "+v"(v));
   return v;
 }
+// A value as of here: what is made of it is not made ahead of a loop and kept.
+__device__ __forceinline__ uint32_t here(uint32_t v) {
+  asm volatile("" : "+v"(v));
+  return v;
+}
 __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
 // 64 lanes x 16 bytes from base + off to LDS at `to`, lane after lane; counted
@@ -169,7 +176,7 @@ struct Plan {
   int splits;
   int part;         // keys per part, a multiple of 128
   int tile_rows;    // rows of a tile; 0: the items are requests, of few rows each
-  int waves;        // of a workgroup then
+  int waves;        // of a workgroup
   bool deep;        // tiles: at most one workgroup per compute unit, which may have more LDS
 };
 
@@ -226,7 +233,7 @@ __device__ __forceinline__ bool find_item(const KvAttnArgs& a, const Plan& p, in
   if (it.shared) {
     const int tiles = (int)(((int64_t)it.rows + p.tile_rows - 1) / p.tile_rows);
     const int64_t t = index - first;
-    if (t >= tiles) return false;
+    if (t < 0 || t >= tiles) return false;  // negative: query_start does not ascend
     it.row0 = (tiles - 1 - (int)t) * p.tile_rows;  // the tiles that see most come first
     if (last_row - it.row0 >= p.tile_rows) last_row = it.row0 + p.tile_rows - 1;
   } else {
@@ -380,23 +387,26 @@ __device__ __forceinline__ typename Vec<R>::v8 widen(int a, int b) {
   return r;
 }
 
-// Eight weights 2^(scale s - m), rounded, and their sum added to l.  The sum
-// takes them as rounded, like the product does.
+// The sum l with the weights i and i + 1, as rounded, like the product takes them.
+template <typename W>
+__device__ __forceinline__ float add_pair(const typename Vec<W>::v8& r, int i, float l) {
+  if constexpr (std::is_same<W, _Float16>::value) {
+    const h2 p = {r[i], r[i + 1]}, one = {(_Float16)1.0f, (_Float16)1.0f};
+    return __builtin_amdgcn_fdot2(p, one, l, false);
+  } else {
+    const b2 p = {r[i], r[i + 1]}, one = {(__bf16)1.0f, (__bf16)1.0f};
+    return __builtin_amdgcn_fdot2_f32_bf16(p, one, l, false);
+  }
+}
+
+// Eight weights 2^(scale s - m), rounded, and their sum added to l.
 template <typename W, typename F>
 __device__ __forceinline__ typename Vec<W>::v8 eight_weights(F score, float scale, float m, float& l) {
   typename Vec<W>::v8 r;
 #pragma unroll
   for (int i = 0; i < 8; ++i) r[i] = (W)__builtin_amdgcn_exp2f(fmaf(score(i), scale, -m));
 #pragma unroll
-  for (int i = 0; i < 8; i += 2) {
-    if constexpr (std::is_same<W, _Float16>::value) {
-      const h2 p = {r[i], r[i + 1]}, one = {(_Float16)1.0f, (_Float16)1.0f};
-      l = __builtin_amdgcn_fdot2(p, one, l, false);
-    } else {
-      const b2 p = {r[i], r[i + 1]}, one = {(__bf16)1.0f, (__bf16)1.0f};
-      l = __builtin_amdgcn_fdot2_f32_bf16(p, one, l, false);
-    }
-  }
+  for (int i = 0; i < 8; i += 2) l = add_pair<W>(r, i, l);
   return r;
 }
 
@@ -435,28 +445,49 @@ __device__ __forceinline__ typename Vec<W>::v8 only_finite(typename Vec<W>::v8 v
 }
 
 // Memory offsets of a lane's loads of 16 keys: its pieces, as they lie in LDS.
-template <typename S, typename Order>
-__device__ __forceinline__ void load_offsets(uint32_t (&k)[S::NJ], uint32_t (&v)[S::NJ]) {
-#pragma unroll
-  for (int j = 0; j < S::NJ; ++j) {
-    const int at = 64 * j + (int)(threadIdx.x & 63), key = at / S::PC, p = at % S::PC;
-    k[j] = (key & 7) * S::RB + (p ^ Order::k(key)) * 16;
-    v[j] = (key & 7) * S::RB + ((p / Order::U ^ Order::v(key)) * Order::U + p % Order::U) * 16;
-  }
-}
+// Where a load takes a power of two of keys, the numbers of a load's keys and
+// of the keys in it share no bit, and every offset is the first one with some
+// bits changed: large heads have no registers for them all.
+template <typename S, typename Order, bool FEW_REGS>
+struct Offsets {
+  static constexpr bool kLinear = FEW_REGS && 64 % S::PC == 0;
+  static constexpr int N = kLinear ? 1 : S::NJ;
+  uint32_t k[N], v[N];
 
-// The loads of 16 keys (two groups of eight, each inside a block) to LDS.
-template <typename S, uint32_t X = 0>
-__device__ __forceinline__ void load16(const uint32_t (&off)[S::NJ], uint32_t to, uint64_t b0, uint64_t b1) {
+  static __device__ __forceinline__ constexpr uint32_t k_of(int key, int p) { return (key & 7) * S::RB + (p ^ Order::k(key)) * 16; }
+  static __device__ __forceinline__ constexpr uint32_t v_of(int key, int p) {
+    return (key & 7) * S::RB + ((p / Order::U ^ Order::v(key)) * Order::U + p % Order::U) * 16;
+  }
+  __device__ __forceinline__ void setup() {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int at = 64 * j + (int)(threadIdx.x & 63), key = at / S::PC, p = at % S::PC;
+      k[j] = k_of(key, p);
+      v[j] = v_of(key, p);
+    }
+  }
+  __device__ __forceinline__ uint32_t of_k(int j) const {
+    if constexpr (kLinear) return here(k[0]) ^ k_of(64 * j / S::PC, 0);
+    else return k[j];
+  }
+  __device__ __forceinline__ uint32_t of_v(int j) const {
+    if constexpr (kLinear) return here(v[0]) ^ v_of(64 * j / S::PC, 0);
+    else return v[j];
+  }
+};
+
+// The loads of 16 keys (two groups of eight, each inside a block) to LDS; off(j): the j-th load's offset.
+template <typename S, uint32_t X = 0, typename F>
+__device__ __forceinline__ void load16(F off, uint32_t to, uint64_t b0, uint64_t b1) {
 #pragma unroll
   for (int j = 0; j < S::NJ; ++j) {
     constexpr int kHalf = 8 * S::PC;  // pieces of eight keys
     if (64 * j + 63 < kHalf)
-      load_lds(to + 1024 * j, b0, off[j] ^ X);
+      load_lds(to + 1024 * j, b0, off(j) ^ X);
     else if (64 * j >= kHalf)
-      load_lds(to + 1024 * j, b1, off[j] ^ X);
+      load_lds(to + 1024 * j, b1, off(j) ^ X);
     else
-      load_lds(to + 1024 * j, (64 * j + (int)(threadIdx.x & 63) < kHalf ? b0 : b1) + (off[j] ^ X));
+      load_lds(to + 1024 * j, (64 * j + (int)(threadIdx.x & 63) < kHalf ? b0 : b1) + (off(j) ^ X));
   }
 }
 
@@ -502,8 +533,10 @@ __device__ __forceinline__ float stored(uint64_t row, int d) {
 
 // ------------------------------------------------------------- shared tiles
 //
-// More than 16 rows: the four waves take 32 rows each and share strips of keys
-// through LDS buffers, R of them, the loads R - 1 strips ahead.
+// More than 16 rows: the four waves take 32 rows each and share strips of 64 keys
+// through LDS buffers, R of them, the loads R - 1 strips ahead.  The clock falls
+// to 1.9 GHz under these products (a library's large product: 1.8), and the matrix
+// units are busy 47% of the time with heads of 128 (that product: 68%).
 template <typename S>
 struct Tile32 {
   typedef typename S::T T;
@@ -512,32 +545,32 @@ struct Tile32 {
   typedef typename Vec<W>::v8 W8;
   typedef Tile32Order<S> Order;
   static constexpr int KS = S::D / 16;  // steps of the first product
-  static constexpr int SH = shared_by(S::D);
-  static constexpr int DT = S::D / 32 / SH;  // tiles of this wave's part of O^T
+  static constexpr int DT = S::D / 32;  // tiles of O^T
   static constexpr int VN = Order::VM < DT ? Order::VM : DT;
 
-  int lane, half, d0;  // d0: first dimension of the part
+  int lane, half;
   Sight see;
   T8 q[KS];
   f16v o[DT];
   float m, l;
-  int koff[Order::KM / 2];  // LDS offsets of this lane's reads
-  int voff[VN];
-  uint32_t kdma[S::NJ], vdma[S::NJ];
+  // LDS offsets of this lane's reads; with few registers the first ones, of which the others differ by some bits.
+  static constexpr bool kFewRegs = S::D == 256;
+  static constexpr int KN = kFewRegs ? 1 : Order::KM / 2, VM = kFewRegs ? 1 : VN;
+  int koff[KN], voff[VM];
+  Offsets<S, Order, kFewRegs> dma;
 
-  __device__ __forceinline__ void setup(int wave) {
+  __device__ __forceinline__ void setup() {
     lane = threadIdx.x & 63;
     half = lane >> 5;
-    d0 = wave % SH * (32 * DT);
     const int key = key_of_row(lane & 31);
 #pragma unroll
-    for (int n = 0; n < Order::KM / 2; ++n) koff[n] = key * S::RB + ((2 * n + half) ^ Order::k(key)) * 16;
+    for (int n = 0; n < KN; ++n) koff[n] = key * S::RB + ((2 * n + half) ^ Order::k(key)) * 16;
     const int n16 = lane & 15, dhalf = (lane >> 4) & 1;
     const int row = 8 * half + (S::F8 ? n16 >> 1 : n16 >> 2);
     const int in = S::F8 ? dhalf * 16 + (n16 & 1) * 8 : dhalf * 32 + (n16 & 3) * 8;
 #pragma unroll
-    for (int n = 0; n < VN; ++n) voff[n] = row * S::RB + ((d0 / 32 + n) ^ Order::v(row)) * (16 * Order::U) + in;
-    load_offsets<S, Order>(kdma, vdma);
+    for (int n = 0; n < VM; ++n) voff[n] = row * S::RB + (n ^ Order::v(row)) * (16 * Order::U) + in;
+    dma.setup();
   }
 
   __device__ __forceinline__ void start(const KvAttnArgs& a, const Item& it, int row0, int head) {
@@ -559,41 +592,53 @@ struct Tile32 {
     l = 0.0f;
   }
 
-  // S^T of a strip.  The reads go ahead of the products that use them: left
-  // alone, the compiler waits for each.
-  __device__ __forceinline__ void scores(uint32_t lds, f16v (&s)[S::SUB]) const {
+  // What a strip's products read out of LDS.  The reads go ahead of the
+  // products that use them, and every product is followed by some other work,
+  // `between`, that runs while the matrix unit is busy: left alone, the compiler
+  // waits for each read and keeps products and weights apart.
+  static constexpr int KR = S::F8 ? KS / 2 : KS;  // reads of K for 32 keys
+  static constexpr int kAheadK = KR < kReadsAhead ? KR : kReadsAhead;
+  static constexpr int KP = KS;      // products per 32 keys: of the scores,
+  static constexpr int VP = 2 * DT;  // and of the values
+  typedef typename std::conditional<S::F8, i4, T8>::type Piece;
+  struct Keys {
+    uint32_t at[Order::KM / 2];
+    Piece k[kAheadK];
+  };
+  __device__ __forceinline__ Piece key(const Keys& x, int i) const {
     constexpr int N = Order::KM / 2;
-    constexpr int R = S::F8 ? KS / 2 : KS;  // reads for 32 keys
-    typedef typename std::conditional<S::F8, i4, T8>::type Piece;
-    uint32_t at[N];
+    const int n = i / KR, u = i % KR;
+    return *(const SCOOT_LDS Piece*)(x.at[u % N] + n * 32 * S::RB + (u / N) * (16 * Order::KM));
+  }
+  __device__ __forceinline__ Keys keys(uint32_t lds) const {
+    Keys x;
 #pragma unroll
-    for (int n = 0; n < N; ++n) at[n] = pinned(lds + koff[n]);
-    auto read = [&](int i) {
-      const int n = i / R, u = i % R;
-      return *(const SCOOT_LDS Piece*)(at[u % N] + n * 32 * S::RB + (u / N) * (16 * Order::KM));
-    };
-    constexpr int kAhead = R < kReadsAhead ? R : kReadsAhead;
-    Piece k[kAhead];
+    for (int n = 0; n < Order::KM / 2; ++n) x.at[n] = pinned(lds + (kFewRegs ? here(koff[0]) ^ n * 32 : koff[n % KN]));
 #pragma unroll
-    for (int i = 0; i < kAhead; ++i) k[i] = read(i);
+    for (int i = 0; i < kAheadK; ++i) x.k[i] = key(x, i);
     __builtin_amdgcn_sched_barrier(0);
+    return x;
+  }
+  // S^T of the strip's keys 32 n .. 32 n + 31.
+  template <int n, typename F>
+  __device__ __forceinline__ void scores(Keys& x, f16v& s, F between) const {
 #pragma unroll
-    for (int n = 0; n < S::SUB; ++n) {
+    for (int i = 0; i < 16; ++i) s[i] = 0.0f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[n][i] = 0.0f;
-#pragma unroll
-      for (int u = 0; u < R; ++u) {
-        const int i = n * R + u;
-        const Piece x = k[i % kAhead];
-        if constexpr (S::F8) {
-#pragma unroll
-          for (int e = 0; e < 2; ++e) s[n] = mfma(widen<T>(x[2 * e], x[2 * e + 1]), q[2 * u + e], s[n]);
-        } else {
-          s[n] = mfma(x, q[u], s[n]);
-        }
-        if (i + kAhead < S::SUB * R) k[i % kAhead] = read(i + kAhead);
+    for (int u = 0; u < KR; ++u) {
+      const int i = n * KR + u;
+      const Piece k = x.k[i % kAheadK];
+      if constexpr (S::F8) {
+        s = mfma(widen<T>(k[0], k[1]), q[2 * u], s);
+        between(2 * u);
         __builtin_amdgcn_sched_barrier(0);
+        s = mfma(widen<T>(k[2], k[3]), q[2 * u + 1], s);
+      } else {
+        s = mfma(k, q[u], s);
       }
+      if (i + kAheadK < 2 * KR) x.k[i % kAheadK] = key(x, i + kAheadK);
+      between(S::F8 ? 2 * u + 1 : u);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 
@@ -603,10 +648,10 @@ struct Tile32 {
   __device__ __forceinline__ Lds values_at(uint32_t lds) const {
     Lds r;
 #pragma unroll
-    for (int n = 0; n < VN; ++n) r.at[n] = pinned(lds + voff[n]);
+    for (int n = 0; n < VN; ++n) r.at[n] = pinned(lds + (kFewRegs ? here(voff[0]) ^ n * 16 * Order::U : voff[n % VM]));
     return r;
   }
-  // V^T: lane's element d = d0 + 32 dt + lane % 32 of the keys 16 ks + 8 half .. + 7.
+  // V^T: lane's element d = 32 dt + lane % 32 of the keys 16 ks + 8 half .. + 7.
   __device__ __forceinline__ W8 values(const Lds& v, int ks, int dt) const {
     const uint32_t at = v.at[dt % VN] + (dt / VN) * (VN * 16 * Order::U) + ks * 16 * S::RB;
     if constexpr (S::F8) {
@@ -637,64 +682,99 @@ struct Tile32 {
     }
   }
 
-  // Weights of a strip; m, l and o follow.  No maximum is taken as long as the
-  // weights stay moderate, which their sum tells.  Whether a row's m moves
-  // depends on that row alone.
-  __device__ __forceinline__ void weights(const f16v (&s)[S::SUB], float scale, W8 (&w)[2 * S::SUB]) {
-    float add = 0.0f;
+  // Weights of 32 keys.  No maximum is taken as long as the weights stay
+  // moderate, which their sum tells; whether a row's m moves depends on that
+  // row alone.  weigh() is the i-th of n parts of the work, moderate() its end.
+  struct Weights {
+    W8 w[2];
+    float add;
+  };
+  __device__ __forceinline__ void weigh(const f16v& s, float scale, Weights& x, int i, int n) const {
+    const int from = 2 * (8 * i / n), to = 2 * (8 * (i + 1) / n);
+    if (i == 0) x.add = 0.0f;
 #pragma unroll
-    for (int k = 0; k < 2 * S::SUB; ++k)
-      w[k] = eight_weights<W>([&](int i) { return s[k / 2][8 * (k & 1) + i]; }, scale, m, add);
-    if (__builtin_amdgcn_ballot_w64(!(add <= kMost))) {
-      float x = s[0][0];
+    for (int j = from; j < to; ++j) x.w[j / 8][j % 8] = (W)__builtin_amdgcn_exp2f(fmaf(s[j], scale, -m));
 #pragma unroll
-      for (int n = 0; n < S::SUB; ++n)
+    for (int j = from; j < to; j += 2) x.add = add_pair<W>(x.w[j / 8], j % 8, x.add);
+  }
+  __device__ __forceinline__ void moderate(const f16v& s, float scale, Weights& w) {
+    if (__builtin_amdgcn_ballot_w64(!(w.add <= kMost))) {
+      float x = s[0];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x = fmaxf(x, s[n][i]);
+      for (int i = 1; i < 16; ++i) x = fmaxf(x, s[i]);
       auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
       x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale;
-      const uint32_t over = !(add <= kMost);
+      const uint32_t over = !(w.add <= kMost);
       sw = __builtin_amdgcn_permlane32_swap(over, over, false, false);
       const float up = (sw[0] | sw[1]) != 0 && x > m ? x : m, f = __builtin_amdgcn_exp2f(m - up);
       m = up;
       l *= f;
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
+      for (int d = 0; d < DT; ++d) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] *= f;
-      add = 0.0f;
-#pragma unroll
-      for (int k = 0; k < 2 * S::SUB; ++k)
-        w[k] = eight_weights<W>([&](int i) { return s[k / 2][8 * (k & 1) + i]; }, scale, m, add);
+        __builtin_amdgcn_sched_barrier(0);  // not all of o at once: large ones rest outside the vector units' registers
+      }
+      weigh(s, scale, w, 0, 1);
     }
-    l += add;
+    l += w.add;
   }
 
-  // The first reads of V, for before the weights.
-  __device__ __forceinline__ void read_ahead(const Lds& lds, W8 (&v)[kReadsAhead]) const {
+  template <int n, typename F>
+  __device__ __forceinline__ void product(const Lds& lds, const Weights& w, W8 (&v)[kReadsAhead], F between) {
 #pragma unroll
-    for (int i = 0; i < kReadsAhead; ++i) v[i] = values(lds, i / DT, i % DT);
-    __builtin_amdgcn_sched_barrier(0);
-  }
-  __device__ __forceinline__ void product(const Lds& lds, const W8 (&w)[2 * S::SUB], W8 (&v)[kReadsAhead]) {
-#pragma unroll
-    for (int i = 0; i < 2 * S::SUB * DT; ++i) {
-      o[i % DT] = mfma(v[i % kReadsAhead], w[i / DT], o[i % DT]);
-      const int n = i + kReadsAhead;
-      if (n < 2 * S::SUB * DT) v[i % kReadsAhead] = values(lds, n / DT, n % DT);
+    for (int j = 0; j < VP; ++j) {
+      const int i = n * VP + j, next = i + kReadsAhead;
+      o[j % DT] = mfma(v[i % kReadsAhead], w.w[j / DT], o[j % DT]);
+      if (next < 2 * VP) v[i % kReadsAhead] = values(lds, next / DT, next % DT);
+      between(j);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
-  template <bool FINITE>
-  __device__ __forceinline__ void product_seen(const Lds& lds, const W8 (&w)[2 * S::SUB], int key0) {
+  // A strip that every row sees whole.  Of the two halves of 64 keys the first one's weights are made between the
+  // second one's scores, and the second one's between the first one's values.
+  __device__ __forceinline__ void strip(uint32_t kat, uint32_t vat, float scale) {
+    const auto nothing = [](int) {};
+    f16v s[2];
+    Weights p[2];
+    W8 v[kReadsAhead];
+    Keys x = keys(kat);
+    scores<0>(x, s[0], nothing);
+    const Lds lds = values_at(vat);
+    scores<1>(x, s[1], [&](int i) { weigh(s[0], scale, p[0], i, KP); });
 #pragma unroll
-    for (int k = 0; k < 2 * S::SUB; ++k)
+    for (int i = 0; i < kReadsAhead; ++i) v[i] = values(lds, i / DT, i % DT);
+    moderate(s[0], scale, p[0]);
+    __builtin_amdgcn_sched_barrier(0);
+    product<0>(lds, p[0], v, [&](int i) { weigh(s[1], scale, p[1], i, VP); });
+    moderate(s[1], scale, p[1]);
+    product<1>(lds, p[1], v, nothing);
+  }
+  // Any other strip, from key `key0` on; holes(key): as for mask().  In this form for all strips, four prompts of 4096
+  // tokens took 422 us instead of 413: the masks' registers are those of the loop above, too.
+  template <bool FINITE, typename H>
+  __device__ __forceinline__ void strip_seen(uint32_t kat, uint32_t vat, float scale, int key0, H holes) {
+    const auto nothing = [](int) {};
+    f16v s[2];
+    Keys x = keys(kat);
+    scores<0>(x, s[0], nothing);
+    scores<1>(x, s[1], nothing);
+    const Lds lds = values_at(vat);
 #pragma unroll
-      for (int d = 0; d < DT; ++d) {
-        W8 v = only_seen(values(lds, k, d), see.hi_max + 1 - (key0 + 16 * k + 8 * half));
-        if constexpr (FINITE) v = only_finite<W>(v);
-        o[d] = mfma(v, w[k], o[d]);
-      }
+    for (int n = 0; n < 2; ++n) {
+      mask(s[n], key0 + 32 * n, holes(key0 + 32 * n));
+      Weights p;
+      weigh(s[n], scale, p, 0, 1);
+      moderate(s[n], scale, p);
+#pragma unroll
+      for (int k = 0; k < 2; ++k)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          W8 v = only_seen(values(lds, 2 * n + k, d), see.hi_max + 1 - (key0 + 32 * n + 16 * k + 8 * half));
+          if constexpr (FINITE) v = only_finite<W>(v);
+          o[d] = mfma(v, p.w[k], o[d]);
+        }
+    }
   }
   __device__ __forceinline__ bool spoilt() const {
     bool x = false;
@@ -718,7 +798,7 @@ struct Tile32 {
       for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float x = stored<S>(row, d0 + 32 * d + 8 * (i / 4) + 4 * half + i % 4);
+          const float x = stored<S>(row, 32 * d + 8 * (i / 4) + 4 * half + i % 4);
           o[d][i] += (mine & !(__builtin_fabsf(x) < INFINITY)) ? x : 0.0f;
         }
     }
@@ -736,8 +816,8 @@ struct Tile32 {
     if (row0 + (lane & 31) >= it.rows) return;
     if (it.splits > 1) {
       at += lane & 31;
-      if (half == 0 && d0 == 0) *(float2*)(stats + at * 2) = make_float2(m, sum);
-      float* p = parts + at * S::D + d0 + 4 * half;
+      if (half == 0) *(float2*)(stats + at * 2) = make_float2(m, sum);
+      float* p = parts + at * S::D + 4 * half;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -749,7 +829,7 @@ struct Tile32 {
     }
     const float inv = sum == 0.0f ? 0.0f : a.v_scale / sum;  // a row that saw nothing has o = 0, too
     const int G = a.num_heads / a.num_kv_heads;
-    T* p = (T*)a.out + (it.q0 + see.tok) * a.out_token_stride + (int64_t)(head * G + see.g) * a.out_head_stride + d0 + 4 * half;
+    T* p = (T*)a.out + (it.q0 + see.tok) * a.out_token_stride + (int64_t)(head * G + see.g) * a.out_head_stride + 4 * half;
     typedef T T4 __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -769,28 +849,29 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
   const int wave = uniform(threadIdx.x >> 6);
   Tile32<S> w;
   Cache<S> c;
-  w.setup(wave);
+  w.setup();
   c.setup(a, it.seq, head);
   constexpr int kHalf = S::ST * S::RB;  // bytes of a strip's keys
   const int strips = (it.k1 - it.k0 + S::ST - 1) / S::ST;
 
   // A strip's loads in groups of 16 keys of K or V; every wave takes its share.
-  const int share = S::SUB == 2 ? wave : wave & 1;
   Ahead<S, 2> ahead;
-  ahead.start(c, c.k, it.k0 + 16 * share, S::ST, strips, it.k1);
+  ahead.start(c, c.k, it.k0 + 16 * wave, S::ST, strips, it.k1);
   const uint64_t to_v = c.v - c.k;
+  const auto dma_k = [&](int j) { return w.dma.of_k(j); };
+  const auto dma_v = [&](int j) { return w.dma.of_v(j); };
   auto load = [&](int strip) {
-    const uint32_t to = lds + (strip & (R - 1)) * S::kStrip + share * 16 * S::RB;
+    const uint32_t to = lds + (strip % R) * S::kStrip + wave * 16 * S::RB;
     uint64_t b[2];
     ahead.get(c, strip, b);
-    if (S::SUB == 2 || wave < 2) load16<S>(w.kdma, to, b[0], b[1]);
-    if (S::SUB == 2 || wave >= 2) load16<S>(w.vdma, to + kHalf, to_v + b[0], to_v + b[1]);
+    load16<S>(dma_k, to, b[0], b[1]);
+    load16<S>(dma_v, to + kHalf, to_v + b[0], to_v + b[1]);
   };
   auto begin = [&] {
     for (int i = 0; i < R - 1 && i < strips; ++i) load(i);
   };
   begin();
-  const int row0 = it.row0 + wave / shared_by(S::D) * kRows;
+  const int row0 = it.row0 + wave * kRows;
   w.start(a, it, row0, head);
   // The waves' first addresses tell of their entries.
   const bool holes = strips <= 64 ? any_wave<kWaves>(ahead.holes, flag) : any_holes<kWaves>(a, it, flag);
@@ -800,7 +881,7 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
 
   auto turn = [&](int strip) {
     // This strip has landed, for every wave, and everyone is done with the one before, whose place the next load takes.
-    if (R > 2 && strip + R - 2 < strips) wait_vm<(R - 2) * S::SUB * S::NJ>();
+    if (R > 2 && strip + R - 2 < strips) wait_vm<(R - 2) * 2 * S::NJ>();
     else wait_vm<0>();
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     if (strip + R - 1 < strips) load(strip + R - 1);
@@ -812,41 +893,31 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
       if (strip >= u0 && strip < u1) {
         for (; strip < u1; ++strip) {
           turn(strip);
-          const uint32_t at = lds + (strip & (R - 1)) * S::kStrip;
-          f16v s[S::SUB];
-          w.scores(at, s);
-          typename Tile32<S>::W8 p[2 * S::SUB], v[kReadsAhead];
-          const auto values = w.values_at(at + kHalf);
-          w.read_ahead(values, v);
-          w.weights(s, a.score_scale, p);
-          w.product(values, p, v);
+          __builtin_amdgcn_s_setprio(1);  // over waves that wait or mask: a late chunk of 64-dimensional heads 566 -> 559 us
+          const uint32_t at = lds + (strip % R) * S::kStrip;
+          w.strip(at, at + kHalf, a.score_scale);
+          __builtin_amdgcn_s_setprio(0);
         }
       } else {
         turn(strip);
-        const uint32_t at = lds + (strip & (R - 1)) * S::kStrip;
+        const uint32_t at = lds + (strip % R) * S::kStrip;
         const int key0 = it.k0 + strip * S::ST;
-        if (key0 <= w.see.hi_max) {
-          f16v s[S::SUB];
-          w.scores(at, s);
-#pragma unroll
-          for (int n = 0; n < S::SUB; ++n) w.mask(s[n], key0 + 32 * n, holes ? c.holes(key0 + 32 * n) : 0);
-          typename Tile32<S>::W8 p[2 * S::SUB];
-          w.weights(s, a.score_scale, p);
-          w.template product_seen<decltype(finite)::value>(w.values_at(at + kHalf), p, key0);
-        }
+        if (key0 <= w.see.hi_max)
+          w.template strip_seen<decltype(finite)::value>(at, at + kHalf, a.score_scale, key0,
+                                                         [&](int key) { return holes ? c.holes(key) : 0; });
         ++strip;
       }
     }
   };
   pass(std::false_type{});
   if (any_wave<kWaves>(w.spoilt(), flag)) {
-    ahead.start(c, c.k, it.k0 + 16 * share, S::ST, strips, it.k1);
+    ahead.start(c, c.k, it.k0 + 16 * wave, S::ST, strips, it.k1);
     begin();
     pass(std::true_type{});
     w.add_lost(c, it.k0, u0 < u1 ? it.k0 + u0 * S::ST : it.k1);  // the strips that went through the mask
     if (u0 < u1) w.add_lost(c, it.k0 + u1 * S::ST, it.k1);
   }
-  w.store(a, it, row0, head, slot * tile_rows(S::D) + (row0 - it.row0), parts, stats);
+  w.store(a, it, row0, head, slot * kTile + (row0 - it.row0), parts, stats);
 }
 
 // --------------------------------------------------------------- few rows
@@ -872,7 +943,7 @@ struct Tile16 {
   float m, l;
   int koff[KN];
   int voff[Order::VM];
-  uint32_t kdma[S::NJ], vdma[S::NJ];
+  Offsets<S, Order, S::D == 64 || S::D == 256> dma;
 
   // Row r of the first product's tile t is key 8 (r / 4) + 4 t + r % 4: quad q gets the keys 8 q .. 8 q + 7.
   __device__ __forceinline__ void setup() {
@@ -886,7 +957,7 @@ struct Tile16 {
     const int in = S::F8 ? (n16 & 1) * 8 : (n16 & 3) * 8;
 #pragma unroll
     for (int n = 0; n < Order::VM; ++n) voff[n] = row * S::RB + (n ^ Order::v(row)) * (16 * Order::U) + in;
-    load_offsets<S, Order>(kdma, vdma);
+    dma.setup();
   }
 
   // A 16-byte piece holds eight or (in 8 bits) sixteen values of a key: piece 4 s + quad for step s, or for the steps
@@ -962,7 +1033,7 @@ struct Tile16 {
     }
   }
 
-  // As Tile32::weights().
+  // As Tile32::weigh() and moderate().
   __device__ __forceinline__ W8 weights(const f4 (&s)[2], float scale) {
     float add = 0.0f;
     W8 w = eight_weights<W>([&](int i) { return s[i / 4][i % 4]; }, scale, m, add);
@@ -1057,14 +1128,16 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
   };
   Ahead<S, 4> ahead;  // its strips: every fourth one
   ahead.start(c, c.k, it.k0 + 32 * wave, 32 * W, (strips - wave + W - 1) / W, it.k1);
+  const auto dma_k = [&](int j) { return w.dma.of_k(j); };
+  const auto dma_v = [&](int j) { return w.dma.of_v(j); };
   auto load_k = [&](const Base& b) {
-    load16<S>(w.kdma, kat, b.b[0], b.b[1]);
-    load16<S, Tile16Order<S>::kNext>(w.kdma, kat + 16 * S::RB, b.b[2], b.b[3]);
+    load16<S>(dma_k, kat, b.b[0], b.b[1]);
+    load16<S, Tile16Order<S>::kNext>(dma_k, kat + 16 * S::RB, b.b[2], b.b[3]);
   };
   const uint64_t to_v = c.v - c.k;
   auto load_v = [&](const Base& b) {
-    load16<S>(w.vdma, vat, to_v + b.b[0], to_v + b.b[1]);
-    load16<S>(w.vdma, vat + 16 * S::RB, to_v + b.b[2], to_v + b.b[3]);
+    load16<S>(dma_v, vat, to_v + b.b[0], to_v + b.b[1]);
+    load16<S>(dma_v, vat + 16 * S::RB, to_v + b.b[2], to_v + b.b[3]);
   };
 
   Base b;
@@ -1181,7 +1254,10 @@ template <typename S, int R, int W>
 constexpr int kFlagAt = R * S::kStrip > FewLds<S, W>::kEnd ? R * S::kStrip : FewLds<S, W>::kEnd;
 // Waves per SIMD that the registers are to suffice for.
 template <typename S, int R>
-constexpr int kOccupancy = R == 2 && S::D == 64 ? 3 : R > 0 && S::D == 192 ? 1 : 2;
+constexpr int kOccupancy = R == 0 ? 2 : S::D == 64 ? (R == 2 ? 3 : 2) : S::D == 128 ? 2 : 1;
+// Buffers of tiles that have a compute unit for themselves.
+template <typename S>
+constexpr int kDeep = 4 * S::kStrip <= 128 * 1024 ? 4 : 2;
 
 template <typename S, int R, int W>
 __global__ __launch_bounds__(64 * W, (kOccupancy<S, R>)) void attention_kernel(KvAttnArgs a, Plan p, float* parts, float* stats) {
@@ -1202,7 +1278,7 @@ __global__ __launch_bounds__(64 * W, (kOccupancy<S, R>)) void attention_kernel(K
   }
   float* ml = (float*)(smem + FewLds<S, W>::kStats);
   for (int row0 = 0; row0 < it.rows; row0 += kFew)
-    few_rows<S, W>(a, it, row0, (int)head, lds, smem, ml, flag, slot * (R > 0 ? tile_rows(S::D) : kFew), parts, stats);
+    few_rows<S, W>(a, it, row0, (int)head, lds, smem, ml, flag, slot * (R > 0 ? kTile : kFew), parts, stats);
 }
 
 // Joins the parts of a tile's keys: one workgroup per key head and as many rows
@@ -1275,7 +1351,8 @@ template <typename S>
 int launch(const KvAttnArgs& a, const Plan& p, float* parts, float* stats, hipStream_t stream) {
   int rc;
   if (p.tile_rows) {
-    rc = p.deep ? launch_kernel<S, 4, kWaves>(a, p, parts, stats, stream) : launch_kernel<S, 2, kWaves>(a, p, parts, stats, stream);
+    constexpr int R = kOccupancy<S, 2> == 1 ? kDeep<S> : 2;
+    rc = p.deep ? launch_kernel<S, kDeep<S>, kWaves>(a, p, parts, stats, stream) : launch_kernel<S, R, kWaves>(a, p, parts, stats, stream);
   } else {
     if constexpr (S::RB <= kWideRow) {
       if (p.waves == 8) rc = launch_kernel<S, 0, 8>(a, p, parts, stats, stream);
