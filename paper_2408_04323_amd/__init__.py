@@ -684,34 +684,34 @@ def known_constraints(Xc, A, b, out=None, stream=None):
 
 # ------------------------------------------- the engine's key/value cache
 #
-# These calls take microseconds on the device, so the binding is lean: arguments
-# are tested in one expression, and only a failing one is looked into.
+# These calls take microseconds on the device, so a module in C++ looks at the
+# tensors and makes them (binding/kv_torch.cpp); it answers None where something
+# does not fit, and the functions here say what.
 KV_F16, KV_BF16, KV_F8 = 0, 1, 2
-_kv_types = None
+_kv = None
 
 
 def _kv_setup():
-    global _kv_types, _raw_stream, _int32, _int64, _uint8
+    global _kv, _kv_types, _int32, _int64, _uint8
     import torch
+
+    from ._native import kv_module
     _int32, _int64, _uint8 = torch.int32, torch.int64, torch.uint8
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    _raw_stream = raw or (lambda device: torch.cuda.current_stream(device).cuda_stream)
     _kv_types = {torch.float16: KV_F16, torch.bfloat16: KV_BF16, torch.float8_e4m3fn: KV_F8}
-    return _kv_types
+    _kv = kv_module(getattr(torch._C, "_cuda_getCurrentRawStream", None)
+                    or (lambda device: torch.cuda.current_stream(device).cuda_stream))
 
 
-def _kv_stream(stream, t):
-    return _raw_stream(t.device.index) if stream is None else int(stream)
+def _kv_on(stream, t):
+    """What a call makes on a stream that is not the current one belongs to it, workspaces among that."""
+    import torch
+    return torch.cuda.stream(torch.cuda.ExternalStream(int(stream), t.device))
 
 
 def _kv_refuse(*tests):
     for ok, what in tests:
         if not ok:
             raise ValueError(what)
-
-
-def _is_ints(t):
-    return t.is_cuda and t.dtype is _int32 and t.is_contiguous()
 
 
 def _refuse_ints(t, name, numel=None):
@@ -740,21 +740,12 @@ def _refuse_vectors(t, name, heads, dim, types="float16 or bfloat16"):
                (t.dim() != 3 or t.stride(2) == 1, f"{name} must be contiguous in its last dimension"))
 
 
-def _is_vectors(t, heads, dim):
-    return t.is_cuda and t.dim() == 3 and t.shape[2] == dim and t.shape[1] == heads and t.stride(2) == 1
-
-
-def _kv_caches(k_cache, v_cache):
-    """The caches' type."""
-    kind = _kv_types.get(k_cache.dtype)
-    if not (kind is not None and k_cache.is_cuda and v_cache.is_cuda and k_cache.dim() == 4 and k_cache.is_contiguous()
-            and v_cache.is_contiguous() and v_cache.dtype is k_cache.dtype and v_cache.shape == k_cache.shape):
-        _kv_refuse((kind is not None, "k_cache must be float16, bfloat16 or float8_e4m3fn"),
-                   (k_cache.is_cuda and v_cache.is_cuda, "k_cache and v_cache must be device tensors"),
-                   (k_cache.dim() == 4, "k_cache must be (blocks, kv_heads, block_size, head_dim)"),
-                   (k_cache.is_contiguous() and v_cache.is_contiguous(), "k_cache and v_cache must be contiguous"),
-                   (False, "v_cache must have k_cache's type and shape"))
-    return kind
+def _refuse_caches(k_cache, v_cache):
+    _kv_refuse((k_cache.dtype in _kv_types, "k_cache must be float16, bfloat16 or float8_e4m3fn"),
+               (k_cache.is_cuda and v_cache.is_cuda, "k_cache and v_cache must be device tensors"),
+               (k_cache.dim() == 4, "k_cache must be (blocks, kv_heads, block_size, head_dim)"),
+               (k_cache.is_contiguous() and v_cache.is_contiguous(), "k_cache and v_cache must be contiguous"),
+               (v_cache.dtype is k_cache.dtype and v_cache.shape == k_cache.shape, "v_cache must have k_cache's type and shape"))
 
 
 class KVBatch:
@@ -778,25 +769,34 @@ def kv_assign(context_len, new_len, block_table, free_blocks, block_size, max_to
     slots and positions, and, from ``free_blocks`` in order, the new entries of
     ``block_table`` (int32 (requests, blocks), updated in place).  Returns a
     KVBatch (``out`` if given); nothing is read back."""
-    _kv_types or _kv_setup()
-    n = context_len.numel()
-    if not (_is_ints(context_len) and _is_ints(new_len) and new_len.numel() == n and _is_ints(free_blocks)
-            and _is_table(block_table, n)):
+    _kv or _kv_setup()
+    args = context_len, new_len, block_table, free_blocks, block_size, max_tokens
+    if out is not None:
+        if out.num_seqs != context_len.numel() or out.max_tokens != max_tokens:
+            raise ValueError("out was made for other sizes")
+        rc = _kv.assign(*args, stream, out.query_start, out.seq_len, out.positions, out.slots, out.counts)
+    else:
+        if stream is None:
+            got = _kv.assign(*args, None)
+        else:
+            with _kv_on(stream, context_len):
+                got = _kv.assign(*args, None)
+        if got is not None:
+            out = KVBatch.__new__(KVBatch)
+            rc, out.query_start, out.seq_len, out.positions, out.slots, out.counts = got
+            out.num_seqs, out.max_tokens = context_len.numel(), max_tokens
+        else:
+            rc = None
+    if rc is None:
+        n = context_len.numel()
         _refuse_ints(context_len, "context_len")
         _refuse_ints(new_len, "new_len", n)
         _refuse_ints(free_blocks, "free_blocks")
         _refuse_table(block_table, n)
-    b = KVBatch(n, max_tokens, context_len.device) if out is None else out
-    if b.num_seqs != n or b.max_tokens != max_tokens:
-        raise ValueError("out was made for other sizes")
-    cols = block_table.shape[1]
-    rc = lib().scoot_kv_assign(context_len.data_ptr(), new_len.data_ptr(), n, block_size, block_table.data_ptr(), cols,
-                               max(block_table.stride(0), cols), free_blocks.data_ptr(), free_blocks.numel(), max_tokens,
-                               b.query_start.data_ptr(), b.seq_len.data_ptr(), b.positions.data_ptr(),
-                               b.slots.data_ptr(), b.counts.data_ptr(), _kv_stream(stream, context_len))
+        raise ValueError("max_tokens must not be negative")
     if rc:
         check(rc, "kv_assign")
-    return b
+    return out
 
 
 def kv_write(k, v, slots, k_cache, v_cache, k_scale=1.0, v_scale=1.0, stream=None):
@@ -804,22 +804,17 @@ def kv_write(k, v, slots, k_cache, v_cache, k_scale=1.0, v_scale=1.0, stream=Non
     bfloat16, at their slots of the caches (blocks, kv_heads, block_size,
     head_dim) of the same type, or float8_e4m3fn, which holds value / scale
     (scoot_kv_write).  Slots outside the cache are skipped."""
-    _kv_types or _kv_setup()
-    cache_type = _kv_caches(k_cache, v_cache)
-    blocks, heads, block_size, dim = k_cache.shape
-    kind = _kv_types.get(k.dtype, KV_F8)
-    if not (kind != KV_F8 and v.dtype is k.dtype and _is_vectors(k, heads, dim) and _is_vectors(v, heads, dim)
-            and v.shape[0] == k.shape[0] == slots.numel() and slots.is_cuda and slots.dtype is _int64
-            and slots.is_contiguous()):
+    _kv or _kv_setup()
+    rc = _kv.write(k, v, slots, k_cache, v_cache, k_scale, v_scale, stream)
+    if rc is None:
+        _refuse_caches(k_cache, v_cache)
+        _, heads, _, dim = k_cache.shape
         _refuse_vectors(k, "k", heads, dim)
         _refuse_vectors(v, "v", heads, dim)
         _kv_refuse((v.dtype is k.dtype and v.shape[0] == k.shape[0], "v must have k's type and number of tokens"),
                    (slots.is_cuda and slots.dtype is _int64 and slots.is_contiguous(),
                     "slots must be a contiguous int64 device tensor"),
                    (False, f"slots must have {k.shape[0]} elements"))
-    rc = lib().scoot_kv_write(k.data_ptr(), v.data_ptr(), kind, k.shape[0], heads, dim, k.stride(0), k.stride(1),
-                              v.stride(0), v.stride(1), slots.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-                              cache_type, blocks, block_size, k_scale, v_scale, _kv_stream(stream, k))
     if rc:
         check(rc, "kv_write")
 
@@ -834,40 +829,29 @@ def kv_attention(q, k_cache, v_cache, block_table, query_start, seq_len, max_new
     of the step as the caller knows it; ``scale`` defaults to head_dim ** -0.5.
     A ``workspace`` (uint8, at least kv_attention_workspace's bytes) may be
     kept between calls.  Returns ``out``, made if not given."""
-    _kv_types or _kv_setup()
-    cache_type = _kv_caches(k_cache, v_cache)
-    blocks, kv_heads, block_size, dim = k_cache.shape
-    kind = _kv_types.get(q.dtype, KV_F8)
-    n = seq_len.numel()
-    if not (kind != KV_F8 and q.is_cuda and q.dim() == 3 and q.shape[2] == dim and q.stride(2) == 1 and _is_ints(seq_len)
-            and _is_ints(query_start) and query_start.numel() == n + 1 and _is_table(block_table, n)):
+    _kv or _kv_setup()
+    args = (q, k_cache, v_cache, block_table, query_start, seq_len, max_new_len, max_seq_len, scale, window, k_scale, v_scale,
+            out, workspace)
+    if stream is None or (out is not None and workspace is not None):
+        got = _kv.attention(*args, stream)
+    else:
+        with _kv_on(stream, q):
+            got = _kv.attention(*args, None)
+    if got is None:
+        _refuse_caches(k_cache, v_cache)
+        n, dim = seq_len.numel(), k_cache.shape[3]
         _refuse_vectors(q, "q", None, dim)
         _refuse_ints(seq_len, "seq_len")
         _refuse_ints(query_start, "query_start", n + 1)
         _refuse_table(block_table, n)
-    tokens, heads = q.shape[0], q.shape[1]
-    if out is None:
-        out = q.new_empty((tokens, heads, dim))
-    elif not (out.dtype is q.dtype and _is_vectors(out, heads, dim) and out.shape[0] == tokens):
-        _refuse_vectors(out, "out", heads, dim)
-        raise ValueError("out must have q's type and shape")
-    if workspace is None:
-        need = _kv_workspace(tokens, heads, kv_heads, dim, n, max_new_len, max_seq_len, window)
-        if need:
-            workspace = q.new_empty(need, dtype=_uint8)
-    else:
-        need = workspace.numel()
-        _kv_refuse((workspace.is_cuda and workspace.dtype is _uint8 and workspace.is_contiguous(),
-                    "workspace must be a contiguous uint8 device tensor"))
-    cols = block_table.shape[1]
-    rc = lib().scoot_kv_attention(q.data_ptr(), kind, tokens, heads, kv_heads, dim, q.stride(0), q.stride(1),
-                                  k_cache.data_ptr(), v_cache.data_ptr(), cache_type, blocks, block_size,
-                                  block_table.data_ptr(), cols, max(block_table.stride(0), cols), query_start.data_ptr(),
-                                  seq_len.data_ptr(), n, max_new_len, max_seq_len, dim ** -0.5 if scale is None else scale,
-                                  window, k_scale, v_scale, out.data_ptr(), out.stride(0), out.stride(1),
-                                  None if workspace is None else workspace.data_ptr(), need, _kv_stream(stream, q))
-    if rc:
-        check(rc, "kv_attention")
+        if out is not None:
+            _refuse_vectors(out, "out", q.shape[1], dim)
+            _kv_refuse((out.dtype is q.dtype and out.shape == q.shape, "out must have q's type and shape"))
+        raise ValueError("workspace must be a contiguous uint8 device tensor")
+    if out is None and not isinstance(got, int):
+        return got
+    if got:
+        check(got, "kv_attention")
     return out
 
 

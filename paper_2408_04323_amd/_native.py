@@ -119,3 +119,16 @@ def check(status, what):
         L = lib()
         raise ScootError(status, f"{what}: {L.scoot_status_string(status).decode()}: "
                                  f"{L.scoot_last_error().decode()}")
+
+
+def kv_module(raw_stream):
+    """The module that makes the key/value cache calls from torch tensors, bound to the loaded library; ``raw_stream``
+    gives a device's current stream."""
+    path = os.path.join(HERE, "_kv_torch.so")
+    if not os.path.exists(path):
+        raise RuntimeError(f"{path} is missing: build it with paper_2408_04323_amd.build.build()")
+    from . import _kv_torch
+    at = [C.cast(getattr(lib(), name), c_vp).value
+          for name in ("scoot_kv_assign", "scoot_kv_write", "scoot_kv_attention_workspace", "scoot_kv_attention")]
+    _kv_torch.bind(*at, raw_stream)
+    return _kv_torch

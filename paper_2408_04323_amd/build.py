@@ -2,7 +2,8 @@
 
 Every ``csrc/*.hip`` file is compiled by hipcc for --offload-arch=gfx950 with
 packed-fp32 instructions disabled; host-only ``csrc/*.cpp`` files by g++.  The
-shared library lands next to this file, where the binding loads it from.
+shared library lands next to this file, where the binding loads it from, and
+beside it the module of binding/kv_torch.cpp, which calls it with torch tensors.
 """
 import concurrent.futures as cf
 import os
@@ -15,6 +16,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT_DIR = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libscoot.so")
+MODULE = os.path.join(HERE, "_kv_torch.so")
 ARCH = "gfx950"
 
 HIP_FLAGS = ["-O3", "-fPIC", "-std=c++17", f"--offload-arch={ARCH}",
@@ -42,13 +44,31 @@ def _compile(src, hipcc):
     return obj
 
 
+def _build_module():
+    """The Python module over torch's tensors (host code only)."""
+    import sysconfig
+
+    import torch
+    base = os.path.dirname(torch.__file__)
+    tmp = MODULE + ".tmp"
+    cmd = ["g++", "-O2", "-fPIC", "-std=c++17", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-I", os.path.join(base, "include"), "-I", os.path.join(base, "include", "torch", "csrc", "api", "include"),
+           "-I", sysconfig.get_paths()["include"], os.path.join(HERE, "binding", "kv_torch.cpp"), "-o", tmp,
+           "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, MODULE)
+
+
 def build(jobs=None, verbose=False):
-    """Compile every source and link libscoot.so.  Always rebuilds."""
+    """Compile every source, link libscoot.so and the module over it.  Always rebuilds."""
     os.makedirs(OUT_DIR, exist_ok=True)
     hipcc = _hipcc()
     srcs = sorted(os.path.join(CSRC, f) for f in os.listdir(CSRC) if f.endswith((".hip", ".cpp")))
     jobs = jobs or min(len(srcs), max(1, min(16, os.cpu_count() or 1)))
     with cf.ThreadPoolExecutor(jobs) as ex:
+        module = ex.submit(_build_module)
         objs = list(ex.map(lambda s: _compile(s, hipcc), srcs))
     tmp = LIB + ".tmp"
     cmd = [hipcc, "-shared", "-fPIC", f"--offload-arch={ARCH}", *objs, "-o", tmp]
@@ -56,8 +76,9 @@ def build(jobs=None, verbose=False):
     if r.returncode != 0:
         raise RuntimeError(f"link failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB)
+    module.result()
     if verbose:
-        print(f"built {LIB}")
+        print(f"built {LIB} and {MODULE}")
     return LIB
 
 

@@ -186,6 +186,11 @@ ATTEND = {
     "stale_inf": _case([(70, 3), (9, 1)], stale=float("inf"), hq=4, hkv=2, d=128, kind="f16"),
     "scale_zero": _case([(30, 20)], scale=0.0),
     "scale_sharp": _case([(200, 150)], scale=3.0, hq=4, hkv=2, d=128, stale=0.0),
+    "wide_parts": _case([(3000, 30), (700, 1)], hq=8, hkv=1, d=256, bs=32),
+    "wide_parts_192": _case([(1500, 70), (10, 1)], hq=6, hkv=2, d=192, bs=8, kind="f16"),
+    "wide_parts_f8": _case([(2100, 25)], cache="f8", hq=8, hkv=1, d=256),
+    "narrow_parts": _case([(2500, 60), (1, 1), (90, 2)], hq=15, hkv=5, d=64, bs=16),
+    "window_wide": _case([(400, 90)], window=70, hq=4, hkv=1, d=256, kind="f16"),
     "hints_small": _case([(1500, 90), (20, 1), (0, 300)], hints=(1, 1), hq=8, hkv=2, d=64),
     "hints_large": _case([(40, 2), (20, 1)], hints=(5000, 100000), hq=8, hkv=2, d=64),
 }
@@ -319,6 +324,61 @@ def test_later_tokens_do_not_reach_earlier_rows(bad, cache):
             assert np.array_equal(g[np.isinf(g)], ref[np.isinf(ref)])
         elif bad != bad:
             assert torch.isnan(got[50:100]).all()
+
+
+@pytest.mark.parametrize("d,kind,cache", [(64, "bf16", "bf16"), (192, "f16", "f16"), (256, "bf16", "bf16"), (256, "f16", "f8")])
+def test_later_values_that_are_not_finite(d, kind, cache):
+    """Heads of all widths, in tiles and in few rows: NaN in a value reaches exactly the rows that see it."""
+    c = _case([(40, 100), (10, 3)], hq=8, hkv=2, d=d, kind=kind, cache=cache, stale=0.0)
+    s = _attend_inputs(c)
+    clean = _call(c, s)
+    x = s["v"].float()
+    x[int(s["table"][0, 90 // 16]), 1, 90 % 16, d - 3] = float("nan")
+    x[int(s["table"][1, 11 // 16]), 0, 11 % 16, 2] = float("nan")
+    t = dict(s, v=x.to(s["v"].dtype))
+    got = _call(c, t)
+    nan = torch.zeros(103, 8, d, dtype=torch.bool, device=DEV)
+    nan[50:100, 4:, d - 3] = True
+    nan[101:, :4, 2] = True
+    assert torch.equal(torch.isnan(got), nan)
+    ref = _reference(c, s)
+    _check(np.where(nan.cpu().numpy(), ref[0], f64(got)), ref[0], _bound(c, s, ref))
+    assert torch.equal(got[:50], clean[:50])
+
+
+def test_calls_on_a_stream_that_is_not_current():
+    """Results and workspaces belong to the stream that the call names, whatever the current one does with freed memory."""
+    c = ATTEND["decode_long"]
+    s = _attend_inputs(c)
+    want = _call(c, s)
+    table, start, seq = dev(s["table"], torch.int32), dev(s["start"], torch.int32), dev(s["seq"], torch.int32)
+    ctx, new = dev([5, 0], torch.int32), dev([3, 9], torch.int32)
+    tab, free = torch.tensor([[1, -1], [-1, -1]], dtype=torch.int32, device=DEV), dev([4, 2, 7], torch.int32)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for i in range(20):
+        got = S.kv_attention(s["q"], s["k"], s["v"], table, start, seq, 1, 9001, stream=side.cuda_stream)
+        junk = torch.full((1 << 22,), float("nan"), device=DEV)  # takes freed memory of the current stream
+        side.synchronize()
+        assert torch.equal(got, want), i
+        del junk
+    b = S.kv_assign(ctx, new, tab, free, 8, 12, stream=side.cuda_stream)
+    side.synchronize()
+    assert b.counts.tolist() == [12, 2, 2, 2] and b.slots.tolist() == [13, 14, 15] + list(range(32, 40)) + [16]
+    assert b.num_seqs == 2 and b.max_tokens == 12
+    zero = S.kv_attention(s["q"], s["k"], s["v"], table, start, seq, 1, 9001, stream=0)
+    torch.cuda.synchronize()
+    assert torch.equal(zero, want)
+
+
+def test_attention_of_offsets_that_do_not_ascend():
+    """Rows of such requests are anyone's; no other row is written."""
+    c = _case([(20, 60), (30, 40), (0, 90)], hq=4, hkv=2, d=64)
+    s = _attend_inputs(c)
+    out = torch.full_like(s["q"], 7.0)
+    start = dev([150, 20, 60, 40], torch.int32)
+    S.kv_attention(s["q"], s["k"], s["v"], dev(s["table"], torch.int32), start, dev(s["seq"], torch.int32), 90, 90, out=out)
+    assert (out[:20] == 7).all() and (out[60:] == 7).all()
 
 
 def test_attention_strides_and_kept_buffers():
