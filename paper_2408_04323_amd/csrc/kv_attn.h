@@ -26,9 +26,11 @@
 // Registers decide the waves per SIMD: three for tiles of 64 dimensions, two for
 // 128, one for 192 and 256, where o and q take 144 and 192 of a lane's 512.  A
 // wave alone keeps both units busy by itself: the weights of 32 keys are made
-// between the matrix instructions of the next products.  Late chunks over 30,000
-// keys, heads of 64, 128, 192, 256: 0.98, 1.16, 0.86, 0.90 PFLOP/s (192 and 256
-// with two waves and half of the registers each, o shared: 0.58 and 0.44).
+// between the matrix instructions of the next products, and a strip's loads go
+// between those of the first scores (in a row they hold the wave up: 192 427 ->
+// 396 us).  Late chunks over 30,000 keys, heads of 64, 128, 192, 256: 0.94, 1.16,
+// 0.97, 0.99 PFLOP/s (192 and 256 with two waves and half of the registers each,
+// o shared: 0.58 and 0.44).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -476,19 +478,21 @@ struct Offsets {
   }
 };
 
-// The loads of 16 keys (two groups of eight, each inside a block) to LDS; off(j): the j-th load's offset.
+// The j-th load of 16 keys (two groups of eight, each inside a block) to LDS; off(j): its offset.
+template <typename S, uint32_t X = 0, typename F>
+__device__ __forceinline__ void load16(F off, uint32_t to, uint64_t b0, uint64_t b1, int j) {
+  constexpr int kHalf = 8 * S::PC;  // pieces of eight keys
+  if (64 * j + 63 < kHalf)
+    load_lds(to + 1024 * j, b0, off(j) ^ X);
+  else if (64 * j >= kHalf)
+    load_lds(to + 1024 * j, b1, off(j) ^ X);
+  else
+    load_lds(to + 1024 * j, (64 * j + (int)(threadIdx.x & 63) < kHalf ? b0 : b1) + (off(j) ^ X));
+}
 template <typename S, uint32_t X = 0, typename F>
 __device__ __forceinline__ void load16(F off, uint32_t to, uint64_t b0, uint64_t b1) {
 #pragma unroll
-  for (int j = 0; j < S::NJ; ++j) {
-    constexpr int kHalf = 8 * S::PC;  // pieces of eight keys
-    if (64 * j + 63 < kHalf)
-      load_lds(to + 1024 * j, b0, off(j) ^ X);
-    else if (64 * j >= kHalf)
-      load_lds(to + 1024 * j, b1, off(j) ^ X);
-    else
-      load_lds(to + 1024 * j, (64 * j + (int)(threadIdx.x & 63) < kHalf ? b0 : b1) + (off(j) ^ X));
-  }
+  for (int j = 0; j < S::NJ; ++j) load16<S, X>(off, to, b0, b1, j);
 }
 
 // What `count` rows from row0 on see: a lane's row (row0 + r) keys lo < k <=
@@ -732,14 +736,16 @@ struct Tile32 {
     }
   }
   // A strip that every row sees whole.  Of the two halves of 64 keys the first one's weights are made between the
-  // second one's scores, and the second one's between the first one's values.
-  __device__ __forceinline__ void strip(uint32_t kat, uint32_t vat, float scale) {
+  // second one's scores, and the second one's between the first one's values; load(i), i < KP, the i-th part of a
+  // strip's loads, goes between the first one's scores.
+  template <typename L>
+  __device__ __forceinline__ void strip(uint32_t kat, uint32_t vat, float scale, L load) {
     const auto nothing = [](int) {};
     f16v s[2];
     Weights p[2];
     W8 v[kReadsAhead];
     Keys x = keys(kat);
-    scores<0>(x, s[0], nothing);
+    scores<0>(x, s[0], load);
     const Lds lds = values_at(vat);
     scores<1>(x, s[1], [&](int i) { weigh(s[0], scale, p[0], i, KP); });
 #pragma unroll
@@ -757,11 +763,13 @@ struct Tile32 {
     const auto nothing = [](int) {};
     f16v s[2];
     Keys x = keys(kat);
+    const bool two = key0 + 32 <= see.hi_max;  // some row sees the second half's keys
     scores<0>(x, s[0], nothing);
-    scores<1>(x, s[1], nothing);
+    if (two) scores<1>(x, s[1], nothing);
     const Lds lds = values_at(vat);
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
+      if (n && !two) break;
       mask(s[n], key0 + 32 * n, holes(key0 + 32 * n));
       Weights p;
       weigh(s[n], scale, p, 0, 1);
@@ -860,12 +868,24 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
   const uint64_t to_v = c.v - c.k;
   const auto dma_k = [&](int j) { return w.dma.of_k(j); };
   const auto dma_v = [&](int j) { return w.dma.of_v(j); };
-  auto load = [&](int strip) {
-    const uint32_t to = lds + (strip % R) * S::kStrip + wave * 16 * S::RB;
+  struct Next {
     uint64_t b[2];
-    ahead.get(c, strip, b);
-    load16<S>(dma_k, to, b[0], b[1]);
-    load16<S>(dma_v, to + kHalf, to_v + b[0], to_v + b[1]);
+    uint32_t to;
+  };
+  auto next = [&](int strip) {
+    Next n;
+    n.to = lds + (strip % R) * S::kStrip + wave * 16 * S::RB;
+    ahead.get(c, strip, n.b);
+    return n;
+  };
+  auto part = [&](const Next& n, int i) {
+    if (i < S::NJ) load16<S>(dma_k, n.to, n.b[0], n.b[1], i);
+    else if (i < 2 * S::NJ) load16<S>(dma_v, n.to + kHalf, to_v + n.b[0], to_v + n.b[1], i - S::NJ);
+  };
+  auto load = [&](int strip) {
+    const Next n = next(strip);
+#pragma unroll
+    for (int i = 0; i < 2 * S::NJ; ++i) part(n, i);
   };
   auto begin = [&] {
     for (int i = 0; i < R - 1 && i < strips; ++i) load(i);
@@ -884,22 +904,28 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
     if (R > 2 && strip + R - 2 < strips) wait_vm<(R - 2) * 2 * S::NJ>();
     else wait_vm<0>();
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (strip + R - 1 < strips) load(strip + R - 1);
   };
   auto pass = [&](auto finite) {
     w.clear();
     int strip = 0;
     while (strip < strips) {
       if (strip >= u0 && strip < u1) {
+        __builtin_amdgcn_s_setprio(1);  // over waves that wait or mask: a late chunk of 64-dimensional heads 566 -> 559 us
+        for (; strip < min(u1, strips - (R - 1)); ++strip) {
+          turn(strip);
+          const Next n = next(strip + R - 1);
+          const uint32_t at = lds + (strip % R) * S::kStrip;
+          w.strip(at, at + kHalf, a.score_scale, [&](int i) { part(n, i); });
+        }
         for (; strip < u1; ++strip) {
           turn(strip);
-          __builtin_amdgcn_s_setprio(1);  // over waves that wait or mask: a late chunk of 64-dimensional heads 566 -> 559 us
           const uint32_t at = lds + (strip % R) * S::kStrip;
-          w.strip(at, at + kHalf, a.score_scale);
-          __builtin_amdgcn_s_setprio(0);
+          w.strip(at, at + kHalf, a.score_scale, [](int) {});
         }
+        __builtin_amdgcn_s_setprio(0);
       } else {
         turn(strip);
+        if (strip + R - 1 < strips) load(strip + R - 1);
         const uint32_t at = lds + (strip % R) * S::kStrip;
         const int key0 = it.k0 + strip * S::ST;
         if (key0 <= w.see.hi_max)
