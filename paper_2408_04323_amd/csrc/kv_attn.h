@@ -4,12 +4,16 @@
 // Mathematics.  A row is one query of one head; the G query heads that share a
 // key head are rows of the same tile, row = token * G + head.  With scores s_t
 // = q . k_t the rows keep m, l and o over the keys seen so far: for every 32
-// keys, w_t = 2^(c s_t - m), l += sum w_t, o += sum w_t v_t.  m is a score of the
-// row; only when a lane's weights of these keys add up to more than 2^14 it moves
-// up to their largest, and l and o are multiplied by 2^(old m - m).  So no
-// weight overflows, one at least is 1, and most keys take no maximum and leave o
-// alone.  Parts of the keys that were handled by different waves or workgroups
-// are joined by the same factors.
+// keys, w_t = 2^(c s_t - m), l += sum w_t, o += sum w_t v_t.  m stays near the
+// row's largest score: only when a lane's weights of these keys add up to more
+// than 2^14 it moves up, to 6 below their largest, and l and o are multiplied by
+// 2^(old m - m).  So no weight overflows, one at least is 64 or more, and most
+// keys take no maximum and leave o alone.  Parts of the keys that were handled
+// by different waves or workgroups are joined by the same factors.
+//
+// Rounding: scores, m, l and o are in float; a weight is rounded once, to the 16
+// bits that the matrix instructions take, and l adds the rounded weights, so that
+// a row of equal values gives that value.
 //
 // Matrix instructions (32 x 32 x 16).  S^T = K Q^T with the keys as rows and the
 // queries as columns, then O^T += V^T W^T: a lane's sixteen scores belong to
@@ -63,7 +67,9 @@ constexpr int kTile = kRows * kWaves;        // rows of a tile
 constexpr float kNoScore = -3.0e38f;         // m before any key was seen; finite, so that m - m is 0
 constexpr int kWideRow = 256;                // bytes of a cache row up to which eight waves' strips fit the LDS
 constexpr int kReadsAhead = 4;               // operands of the matrix instructions on their way out of LDS
-constexpr float kMost = 16384.0f;            // m moves once a lane's weights of 32 keys add up to more
+constexpr float kMost = 16384.0f;            // m moves once a lane's weights of 32 keys add up to more,
+constexpr float kBelow = 6.0f;               // to this much below their largest: half precision holds 64 as well as 1, and
+                                             // weights down to 2^-30 of the largest, which counts where many keys are small
 
 constexpr int gcd256(int x) { return x % 256 == 0 ? 256 : x % 128 == 0 ? 128 : 64; }
 
@@ -707,7 +713,7 @@ struct Tile32 {
 #pragma unroll
       for (int i = 1; i < 16; ++i) x = fmaxf(x, s[i]);
       auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-      x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale;
+      x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale - kBelow;
       const uint32_t over = !(w.add <= kMost);
       sw = __builtin_amdgcn_permlane32_swap(over, over, false, false);
       const float up = (sw[0] | sw[1]) != 0 && x > m ? x : m, f = __builtin_amdgcn_exp2f(m - up);
@@ -1070,7 +1076,7 @@ struct Tile16 {
       auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
       x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
       sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-      x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale;
+      x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale - kBelow;
       uint32_t over = !(add <= kMost);
       sw = __builtin_amdgcn_permlane32_swap(over, over, false, false);
       over = sw[0] | sw[1];

@@ -285,6 +285,24 @@ def test_attention_rows_without_keys_are_zero():
     _check(got, ref[0], _bound(c, s, ref))
 
 
+@pytest.mark.parametrize("tokens", [4, 24])
+def test_many_small_weights_beside_a_large_one(tokens):
+    """One key far above all others in half precision: what many weights below 2^-24 of the largest add up to is kept.
+    Weights are exact to 2^-31 of the largest (2^6 finer than where the largest is 1), so that part of the bound is less."""
+    c = _case([(20000 - tokens, tokens)], hq=4, hkv=1, d=128, kind="f16", stale=0.0)
+    s = _attend_inputs(c)
+    rng = np.random.default_rng(2)
+    q = np.ones((tokens, 4, 128))
+    k = 0.1 * rng.standard_normal(tuple(s["k"].shape))
+    v = 1.0 + 0.1 * rng.standard_normal(tuple(s["v"].shape))
+    first = int(s["table"][0, 0])
+    k[first, :, 0], v[first, :, 0] = 17.0 / 128 ** 0.5, 0.0
+    s.update(q=dev(q, torch.float16), k=dev(k, torch.float16), v=dev(v, torch.float16))
+    got, ref = f64(_call(c, s)), _reference(c, s)
+    assert ref[0].max() < 2e-3
+    _check(got, ref[0], _bound(c, s, ref, vmax=np.abs(f64(s["v"])).max() / 64))
+
+
 def test_attention_skips_missing_blocks():
     c = _case([(200, 30), (130, 1)], hq=8, hkv=2, d=64, bs=8)
     s = _attend_inputs(c)
