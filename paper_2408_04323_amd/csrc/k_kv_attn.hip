@@ -21,29 +21,34 @@ constexpr int kPartOf = 128;      // parts are multiples of this many keys: a st
 constexpr int kMinPart = 512;     // of few rows, for each four waves: a part costs about as much as 256 keys to join
 constexpr int kMinTilePart = 256; // of tiles: four strips
 constexpr double kJoinLaunch = 5e-6;  // seconds, bytes per second
-constexpr double kJoinRate = 6e12;
+constexpr double kJoinRate = 4e12;
 constexpr int kAlone = 2048;      // keys that eight waves of one workgroup do not share with another
 
-// Parts of the keys of tiles: as many as give each compute unit r workgroups,
-// for the r with the shortest time.  A workgroup alone on its unit takes about
-// 0.77, 1, 1.45, 1.9 us per strip of 64 keys (heads of 64, 128, 192, 256
-// dimensions); others beside it that much again, but some are shorter, and they
-// fill its gaps: 3/4 (1/2 with heads of 64) of it.  Parts cost a launch and their
-// way through memory, once out and once in.  Against as many parts as fill the
-// chip: chunks of 331 tokens over 547 37 -> 27 us (one part, not two), of 160 over
-// 10,087 50 -> 40 (ten, not twenty).
+// Parts of the keys of tiles: the number with the shortest time.  A strip of 64
+// keys takes a workgroup as long as strip_time() says with one, two or three of
+// them on its compute unit (heads of 128: 1.15 and 1.81 us); what does not fit at
+// once follows.  Parts cost a launch and their way through memory, once out and
+// once in.  Against as many parts as fill the chip: chunks of 331 tokens over 547
+// 37 -> 27 us (one part, not two), of 160 over 10,087 50 -> 40 (ten, not twenty), of
+// 270 over 24,258 347 -> 257 (more than fit at once, not two).
+double strip_time(int head_dim, int beside) {
+  if (head_dim <= 64) return (beside == 0 ? 0.77e-6 : beside == 1 ? 1.1e-6 : 1.63e-6);
+  if (head_dim <= 128) return beside == 0 ? 1.15e-6 : 1.81e-6;
+  return head_dim * 7.4e-9;  // 192: 1.4 us, 256: 1.9 us
+}
+
 int64_t parts_of_tiles(int64_t groups, int64_t keys, int64_t rows, int head_dim) {
-  const int most = head_dim <= 64 ? 3 : head_dim <= 128 ? 2 : 1;  // workgroups that fit a compute unit
-  const double strip = head_dim <= 64 ? 0.77e-6 : head_dim / 128.0 * 0.9e-6 + 0.1e-6, beside = head_dim <= 64 ? 0.5 : 0.75;
+  const int fit = head_dim <= 64 ? 3 : head_dim <= 128 ? 2 : 1;  // workgroups that a compute unit holds
+  const int64_t most = (keys + kMinTilePart - 1) / kMinTilePart;
   int64_t best = 1;
   double least = 0;
-  for (int r = 0; r <= most; ++r) {
-    const int64_t n = r == 0 ? 1 : std::min(r * kUnits / groups, (keys + kMinTilePart - 1) / kMinTilePart);
-    if (r > 0 && n <= best) continue;
-    const double load = (double)(groups * n) / kUnits;
-    double t = (double)keys / (64 * n) * strip * (load > 1 ? 1 + beside * (load - 1) : 1);
+  for (int i = 1; i <= 8 + fit; ++i) {  // few parts, and as many as give every unit one, two, three workgroups
+    const int64_t n = i <= 8 ? i : (i - 8) * kUnits / groups;
+    if (n > most || (i > 8 && n <= 8)) continue;
+    const int64_t beside = std::min<int64_t>((groups * n - 1) / kUnits, fit - 1);
+    double t = (double)keys / (64 * n) * strip_time(head_dim, (int)beside) * std::max(1.0, (double)(groups * n) / (fit * kUnits));
     if (n > 1) t += kJoinLaunch + (double)(2 * n * rows * head_dim * 4) / kJoinRate;
-    if (r == 0 || t < least) least = t, best = n;
+    if (i == 1 || t < least) least = t, best = n;
   }
   return best;
 }
@@ -63,8 +68,10 @@ Plan plan(int64_t num_tokens, int num_heads, int num_kv_heads, int head_dim, int
   int64_t keys = max_seq_len;
   if (window > 0) keys = std::min<int64_t>(keys, (int64_t)window + (tiles ? p.tile_rows / G : longest) + 32);
   keys = std::max<int64_t>(keys, 1);
-  // Tiles that have rows: at least this many of the numbers.
-  const int64_t real = tiles ? std::max<int64_t>(num_seqs, (num_tokens * G + p.tile_rows - 1) / p.tile_rows) : p.items;
+  // Tiles that have rows: as many as the numbers if all requests but one are single tokens, else fewer, at least one for
+  // every request and for every 128 rows.
+  const int64_t least = std::max<int64_t>(num_seqs, (num_tokens * G + kTile - 1) / kTile);
+  const int64_t real = tiles ? (p.items + least) / 2 : p.items;
   const int64_t groups = std::max<int64_t>(1, real * num_kv_heads);
   int64_t want;
   p.waves = kWaves;
