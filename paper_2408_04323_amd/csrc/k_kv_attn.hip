@@ -69,9 +69,10 @@ Plan plan(int64_t num_tokens, int num_heads, int num_kv_heads, int head_dim, int
   if (window > 0) keys = std::min<int64_t>(keys, (int64_t)window + (tiles ? p.tile_rows / G : longest) + 32);
   keys = std::max<int64_t>(keys, 1);
   // Tiles that have rows: as many as the numbers if all requests but one are single tokens, else fewer, at least one for
-  // every request and for every 128 rows.
+  // every request and for every 128 rows; so many if there is one request.
   const int64_t least = std::max<int64_t>(num_seqs, (num_tokens * G + kTile - 1) / kTile);
-  const int64_t real = tiles ? (p.items + least) / 2 : p.items;
+  const int64_t most = tiles && num_seqs == 1 ? least : p.items;
+  const int64_t real = tiles ? (most + least) / 2 : p.items;
   const int64_t groups = std::max<int64_t>(1, real * num_kv_heads);
   int64_t want;
   p.waves = kWaves;
@@ -87,7 +88,7 @@ Plan plan(int64_t num_tokens, int num_heads, int num_kv_heads, int head_dim, int
   part = std::max<int64_t>(tiles ? kMinTilePart : kMinPart * (p.waves / kWaves), (part + kPartOf - 1) / kPartOf * kPartOf);
   p.part = (int)std::min<int64_t>(part, (int64_t)1 << 30);
   p.splits = (int)((keys + p.part - 1) / p.part);
-  p.deep = groups * p.splits <= kUnits;
+  p.deep = most * num_kv_heads * p.splits <= kUnits;  // one more would follow all others
   return p;
 }
 
