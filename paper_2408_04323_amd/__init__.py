@@ -6,6 +6,7 @@ library's HIP kernels.  Device arrays are torch tensors on the current HIP
 device; torch provides only memory and the stream.  Names follow the C calls
 without the ``scoot_`` prefix.
 """
+import contextlib
 import ctypes as C
 import functools
 
@@ -705,7 +706,11 @@ def _kv_setup():
 def _kv_on(stream, t):
     """What a call makes on a stream that is not the current one belongs to it, workspaces among that."""
     import torch
-    return torch.cuda.stream(torch.cuda.ExternalStream(int(stream), t.device))
+    if not t.is_cuda:
+        return contextlib.nullcontext()  # refused by the call
+    # ExternalStream would take 0 for no handle at all and give a stream of torch's pool.
+    return torch.cuda.stream(torch.cuda.ExternalStream(int(stream), t.device) if int(stream)
+                             else torch.cuda.default_stream(t.device))
 
 
 def _kv_refuse(*tests):
