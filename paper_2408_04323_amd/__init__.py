@@ -719,8 +719,9 @@ def _kv_refuse(*tests):
             raise ValueError(what)
 
 
-def _refuse_ints(t, name, numel=None):
-    _kv_refuse((t.is_cuda, f"{name} must be a device tensor"), (t.dtype is _int32, f"{name} must be int32"),
+def _refuse_ints(t, name, numel=None, dtype=None):
+    dtype = dtype or _int32  # known once the module is loaded
+    _kv_refuse((t.is_cuda, f"{name} must be a device tensor"), (t.dtype is dtype, f"{name} must be {str(dtype)[6:]}"),
                (t.is_contiguous(), f"{name} must be contiguous"),
                (numel is None or t.numel() == numel, f"{name} must have {numel} elements"))
 
@@ -798,7 +799,11 @@ def kv_assign(context_len, new_len, block_table, free_blocks, block_size, max_to
         _refuse_ints(new_len, "new_len", n)
         _refuse_ints(free_blocks, "free_blocks")
         _refuse_table(block_table, n)
-        raise ValueError("max_tokens must not be negative")
+        _kv_refuse((max_tokens >= 0, "max_tokens must not be negative"))
+        for name, size, dtype in (("query_start", n + 1, _int32), ("seq_len", n, _int32), ("positions", max_tokens, _int32),
+                                  ("slots", max_tokens, _int64), ("counts", 4, _int32)):
+            _refuse_ints(getattr(out, name), f"out.{name}", size, dtype)
+        raise ValueError("kv_assign takes tensors")
     if rc:
         check(rc, "kv_assign")
     return out

@@ -138,12 +138,16 @@ PyObject* assign(PyObject*, PyObject* const* args, Py_ssize_t n) {
     Py_RETURN_NONE;
   int64_t block_size, max_tokens;
   void* stream;
-  if (!get(args[4], block_size) || !get(args[5], max_tokens) || !get_stream(args[6], ctx, stream)) return nullptr;
+  if (!get(args[4], block_size) || !get(args[5], max_tokens)) return nullptr;
+  if (max_tokens < 0) Py_RETURN_NONE;
   at::Tensor r[5];
   if (n == 12) {
-    for (int i = 0; i < 5; ++i) r[i] = THPVariable_Unpack(args[7 + i]);
+    const int64_t size[5] = {seqs + 1, seqs, max_tokens, max_tokens, 4};
+    for (int i = 0; i < 5; ++i) {
+      r[i] = THPVariable_Unpack(args[7 + i]);
+      if (!is_list(r[i], i == 3 ? at::kLong : at::kInt) || r[i].numel() != size[i]) Py_RETURN_NONE;
+    }
   } else {
-    if (max_tokens < 0) Py_RETURN_NONE;
     const at::Tensor all = make({8 * max_tokens + 4 * (2 * seqs + 5 + max_tokens)}, at::kByte, ctx);
     r[3] = part(all, at::kLong, 0, max_tokens);
     int64_t from = 2 * max_tokens;
@@ -153,6 +157,7 @@ PyObject* assign(PyObject*, PyObject* const* args, Py_ssize_t n) {
       from += size;
     }
   }
+  if (!get_stream(args[6], ctx, stream)) return nullptr;
   const int rc = assign_fn(ctx.data_ptr(), add.data_ptr(), narrow(seqs), narrow(block_size), table.data_ptr(), narrow(table.size(1)),
                            stride_of(table), free.data_ptr(), narrow(free.numel()), max_tokens, r[0].data_ptr(), r[1].data_ptr(),
                            r[2].data_ptr(), r[3].data_ptr(), r[4].data_ptr(), stream);
