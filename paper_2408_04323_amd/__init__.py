@@ -719,6 +719,11 @@ def _kv_refuse(*tests):
             raise ValueError(what)
 
 
+def _refuse_mixed(like, **others):
+    for name, t in others.items():
+        _kv_refuse((t is None or t.device == like.device, f"{name} must be on the device of the others, {like.device}"))
+
+
 def _refuse_ints(t, name, numel=None, dtype=None):
     dtype = dtype or _int32  # known once the module is loaded
     _kv_refuse((t.is_cuda, f"{name} must be a device tensor"), (t.dtype is dtype, f"{name} must be {str(dtype)[6:]}"),
@@ -799,10 +804,12 @@ def kv_assign(context_len, new_len, block_table, free_blocks, block_size, max_to
         _refuse_ints(new_len, "new_len", n)
         _refuse_ints(free_blocks, "free_blocks")
         _refuse_table(block_table, n)
+        _refuse_mixed(context_len, new_len=new_len, free_blocks=free_blocks, block_table=block_table)
         _kv_refuse((max_tokens >= 0, "max_tokens must not be negative"))
         for name, size, dtype in (("query_start", n + 1, _int32), ("seq_len", n, _int32), ("positions", max_tokens, _int32),
                                   ("slots", max_tokens, _int64), ("counts", 4, _int32)):
             _refuse_ints(getattr(out, name), f"out.{name}", size, dtype)
+            _refuse_mixed(context_len, **{f"out.{name}": getattr(out, name)})
         raise ValueError("kv_assign takes tensors")
     if rc:
         check(rc, "kv_assign")
@@ -823,8 +830,9 @@ def kv_write(k, v, slots, k_cache, v_cache, k_scale=1.0, v_scale=1.0, stream=Non
         _refuse_vectors(v, "v", heads, dim)
         _kv_refuse((v.dtype is k.dtype and v.shape[0] == k.shape[0], "v must have k's type and number of tokens"),
                    (slots.is_cuda and slots.dtype is _int64 and slots.is_contiguous(),
-                    "slots must be a contiguous int64 device tensor"),
-                   (False, f"slots must have {k.shape[0]} elements"))
+                    "slots must be a contiguous int64 device tensor"))
+        _refuse_mixed(k, v=v, slots=slots, k_cache=k_cache, v_cache=v_cache)
+        _kv_refuse((False, f"slots must have {k.shape[0]} elements"))
     if rc:
         check(rc, "kv_write")
 
@@ -854,6 +862,8 @@ def kv_attention(q, k_cache, v_cache, block_table, query_start, seq_len, max_new
         _refuse_ints(seq_len, "seq_len")
         _refuse_ints(query_start, "query_start", n + 1)
         _refuse_table(block_table, n)
+        _refuse_mixed(q, k_cache=k_cache, v_cache=v_cache, seq_len=seq_len, query_start=query_start, block_table=block_table,
+                      out=out, workspace=workspace)
         if out is not None:
             _refuse_vectors(out, "out", q.shape[1], dim)
             _kv_refuse((out.dtype is q.dtype and out.shape == q.shape, "out must have q's type and shape"))

@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -59,6 +60,30 @@ bool are_caches(const at::Tensor& k, const at::Tensor& v) {
   return type_of(k) != kNoType && k.is_cuda() && v.is_cuda() && k.dim() == 4 && k.is_contiguous() && v.is_contiguous() &&
          v.scalar_type() == k.scalar_type() && v.sizes() == k.sizes();
 }
+
+bool with(const at::Tensor& t, std::initializer_list<const at::Tensor*> others) {
+  for (const at::Tensor* o : others)
+    if (o->get_device() != t.get_device()) return false;
+  return true;
+}
+
+// The library launches on the current device: while one of these lives, that is the tensor's.
+class OnDeviceOf {
+ public:
+  explicit OnDeviceOf(const at::Tensor& t) : impl_(t.device().type()), before_(impl_.getDevice()), other_(before_ != t.device()) {
+    if (other_) impl_.setDevice(t.device());
+  }
+  ~OnDeviceOf() {
+    if (other_) impl_.uncheckedSetDevice(before_);
+  }
+  OnDeviceOf(const OnDeviceOf&) = delete;
+  OnDeviceOf& operator=(const OnDeviceOf&) = delete;
+
+ private:
+  const c10::impl::VirtualGuardImpl impl_;
+  const c10::Device before_;
+  const bool other_;
+};
 
 // What does not fit becomes what the library refuses.
 int narrow(int64_t v) { return v > INT_MAX ? INT_MAX : v < INT_MIN ? INT_MIN : (int)v; }
@@ -134,7 +159,8 @@ PyObject* assign(PyObject*, PyObject* const* args, Py_ssize_t n) {
   const at::Tensor &ctx = THPVariable_Unpack(args[0]), &add = THPVariable_Unpack(args[1]), &table = THPVariable_Unpack(args[2]),
                    &free = THPVariable_Unpack(args[3]);
   const int64_t seqs = ctx.numel();
-  if (!(is_list(ctx, at::kInt) && is_list(add, at::kInt) && add.numel() == seqs && is_list(free, at::kInt) && is_table(table, seqs)))
+  if (!(is_list(ctx, at::kInt) && is_list(add, at::kInt) && add.numel() == seqs && is_list(free, at::kInt) && is_table(table, seqs) &&
+        with(ctx, {&add, &table, &free})))
     Py_RETURN_NONE;
   int64_t block_size, max_tokens;
   void* stream;
@@ -145,7 +171,7 @@ PyObject* assign(PyObject*, PyObject* const* args, Py_ssize_t n) {
     const int64_t size[5] = {seqs + 1, seqs, max_tokens, max_tokens, 4};
     for (int i = 0; i < 5; ++i) {
       r[i] = THPVariable_Unpack(args[7 + i]);
-      if (!is_list(r[i], i == 3 ? at::kLong : at::kInt) || r[i].numel() != size[i]) Py_RETURN_NONE;
+      if (!is_list(r[i], i == 3 ? at::kLong : at::kInt) || r[i].numel() != size[i] || !with(ctx, {&r[i]})) Py_RETURN_NONE;
     }
   } else {
     const at::Tensor all = make({8 * max_tokens + 4 * (2 * seqs + 5 + max_tokens)}, at::kByte, ctx);
@@ -158,6 +184,7 @@ PyObject* assign(PyObject*, PyObject* const* args, Py_ssize_t n) {
     }
   }
   if (!get_stream(args[6], ctx, stream)) return nullptr;
+  const OnDeviceOf on(ctx);
   const int rc = assign_fn(ctx.data_ptr(), add.data_ptr(), narrow(seqs), narrow(block_size), table.data_ptr(), narrow(table.size(1)),
                            stride_of(table), free.data_ptr(), narrow(free.numel()), max_tokens, r[0].data_ptr(), r[1].data_ptr(),
                            r[2].data_ptr(), r[3].data_ptr(), r[4].data_ptr(), stream);
@@ -180,11 +207,12 @@ PyObject* write(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (!are_caches(kc, vc)) Py_RETURN_NONE;
   const int64_t heads = kc.size(1), dim = kc.size(3), tokens = slots.numel();
   if (!(type_of(k) < kF8 && v.scalar_type() == k.scalar_type() && is_vectors(k, heads, dim) && is_vectors(v, heads, dim) &&
-        k.size(0) == tokens && v.size(0) == tokens && is_list(slots, at::kLong)))
+        k.size(0) == tokens && v.size(0) == tokens && is_list(slots, at::kLong) && with(k, {&v, &slots, &kc, &vc})))
     Py_RETURN_NONE;
   float ks, vs;
   void* stream;
   if (!get(args[5], ks) || !get(args[6], vs) || !get_stream(args[7], k, stream)) return nullptr;
+  const OnDeviceOf on(k);
   return PyLong_FromLong(write_fn(k.data_ptr(), v.data_ptr(), type_of(k), tokens, narrow(heads), narrow(dim), k.stride(0), k.stride(1),
                                   v.stride(0), v.stride(1), slots.data_ptr(), kc.data_ptr(), vc.data_ptr(), type_of(kc), kc.size(0),
                                   narrow(kc.size(2)), ks, vs, stream));
@@ -202,7 +230,8 @@ PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (!are_caches(kc, vc)) Py_RETURN_NONE;
   const int64_t kv_heads = kc.size(1), dim = kc.size(3), seqs = len.numel();
   if (!(type_of(q) < kF8 && q.is_cuda() && q.dim() == 3 && q.size(2) == dim && q.stride(2) == 1 && is_list(len, at::kInt) &&
-        is_list(start, at::kInt) && start.numel() == seqs + 1 && is_table(table, seqs)))
+        is_list(start, at::kInt) && start.numel() == seqs + 1 && is_table(table, seqs) &&
+        with(q, {&kc, &vc, &table, &start, &len})))
     Py_RETURN_NONE;
   const int64_t tokens = q.size(0), heads = q.size(1);
   at::Tensor out, space;
@@ -210,7 +239,8 @@ PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
   if (!made) {
     if (!THPVariable_Check(args[12])) Py_RETURN_NONE;
     out = THPVariable_Unpack(args[12]);
-    if (!(out.scalar_type() == q.scalar_type() && is_vectors(out, heads, dim) && out.size(0) == tokens)) Py_RETURN_NONE;
+    if (!(out.scalar_type() == q.scalar_type() && is_vectors(out, heads, dim) && out.size(0) == tokens && with(q, {&out})))
+      Py_RETURN_NONE;
   }
   int64_t max_new, max_seq, window;
   float scale = (float)(1.0 / std::sqrt((double)std::max<int64_t>(dim, 1))), ks, vs;
@@ -226,10 +256,11 @@ PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
   } else {
     if (!THPVariable_Check(args[13])) Py_RETURN_NONE;
     space = THPVariable_Unpack(args[13]);
-    if (!is_list(space, at::kByte)) Py_RETURN_NONE;
+    if (!is_list(space, at::kByte) || !with(q, {&space})) Py_RETURN_NONE;
     need = (uint64_t)space.numel();
   }
   if (made) out = make({tokens, heads, dim}, q.scalar_type(), q);
+  const OnDeviceOf on(q);
   const int rc = attention_fn(q.data_ptr(), type_of(q), tokens, narrow(heads), narrow(kv_heads), narrow(dim), q.stride(0), q.stride(1),
                               kc.data_ptr(), vc.data_ptr(), type_of(kc), kc.size(0), narrow(kc.size(2)), table.data_ptr(),
                               narrow(table.size(1)), stride_of(table), start.data_ptr(), len.data_ptr(), narrow(seqs), max_new, max_seq,

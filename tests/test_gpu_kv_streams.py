@@ -54,3 +54,21 @@ def test_a_step_on_handle_0_is_in_order():
             torch.cuda.synchronize()
             want = got
     assert want[2].tolist() == [60, 10] and torch.isfinite(want[0]).all() and (want[0] != 0).any()
+
+
+@pytest.mark.skipif(not torch.cuda.is_available() or torch.cuda.device_count() < 2, reason="needs a second GPU")
+def test_a_step_on_a_device_that_is_not_current():
+    """Streams and kernels are those of the tensors' device."""
+    g = torch.Generator().manual_seed(3)
+    qkv, got = torch.randn(70, 12, 64, generator=g).to(torch.bfloat16), []
+    torch.cuda.set_device(0)
+    for at in ("cuda:0", "cuda:1"):
+        lens = torch.tensor([[0, 0], [60, 10]], dtype=torch.int32, device=at)
+        table, free = torch.full((2, 8), -1, dtype=torch.int32, device=at), torch.arange(16, dtype=torch.int32, device=at)
+        kc, vc = torch.zeros(2, 16, 2, 16, 64, dtype=torch.bfloat16, device=at)
+        x = qkv.to(at)
+        b = S.kv_assign(lens[0], lens[1], table, free, 16, 70)
+        S.kv_write(x[:, 8:10], x[:, 10:], b.slots, kc, vc)
+        got.append(S.kv_attention(x[:, :8], kc, vc, table, b.query_start, b.seq_len, 60, 60).cpu())
+        assert torch.cuda.current_device() == 0
+    assert torch.equal(*got)
