@@ -688,8 +688,9 @@ int scoot_kv_write(const void* k, const void* v, scoot_kv_type type, int64_t num
  *   out = sum_t softmax_t(scale * k_scale * q . k_t) * v_scale * v_t
  * for query head h over key head h / (num_heads / num_kv_heads).  A query
  * that sees nothing gets zeros; what it does not see (stale or unwritten
- * memory, infinities and NaN included) does not reach its result.  Rows of
- * out that belong to no request are not written.  Sums and the softmax are in
+ * memory, infinities and NaN included) does not reach its result; one whose
+ * scores are all -inf, or one of them +inf, gets NaN, as the formula has it.
+ * Rows of out that belong to no request are not written.  Sums and the softmax are in
  * float; its weights are rounded to 16 bits for the product with v.
  *   q, out        [num_tokens][num_heads][head_dim] of `type` (F16 or BF16),
  *                 strides in elements, 16-byte aligned, the last dimension

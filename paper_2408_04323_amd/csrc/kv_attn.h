@@ -64,7 +64,7 @@ constexpr int kThreads = 64 * kWaves;
 constexpr int kFew = 16;                     // rows of a request that one workgroup's waves handle together
 constexpr int kRows = 32;                    // rows of a wave otherwise
 constexpr int kTile = kRows * kWaves;        // rows of a tile
-constexpr float kNoScore = -3.0e38f;         // m before any key was seen; finite, so that m - m is 0
+constexpr float kNoScore = -3.40282347e38f;  // m before any key was seen; finite, so that m - m is 0, and below no finite score
 constexpr int kWideRow = 256;                // bytes of a cache row up to which eight waves' strips fit the LDS
 constexpr int kReadsAhead = 4;               // operands of the matrix instructions on their way out of LDS
 constexpr float kMost = 16384.0f;            // m moves once a lane's weights of 32 keys add up to more,
@@ -534,6 +534,34 @@ struct Sight {
   }
 };
 
+// Whether the lane's row sees any of the item's keys, in a block that there is.  All lanes take part: 64 entries of the
+// table at a time.
+__device__ __forceinline__ bool sees_any(const KvAttnArgs& a, const Item& it, const Sight& see) {
+  const int32_t* t = a.block_table + (int64_t)it.seq * a.table_stride;
+  const int first = max(see.lo + 1, it.k0), last = min(see.hi, it.k1 - 1);
+  const int to = min(see.hi_max, it.k1 - 1) >> a.block_shift;
+  bool any = false;
+#pragma unroll 1
+  for (int e0 = it.k0 >> a.block_shift; e0 <= to; e0 += 64) {
+    const int e = e0 + (int)(threadIdx.x & 63);
+    const uint64_t real = __builtin_amdgcn_ballot_w64(e <= to && (uint32_t)t[e < to ? e : to] < (uint32_t)a.num_blocks);
+    const int i = max((first >> a.block_shift) - e0, 0), j = min((last >> a.block_shift) - e0, 63);
+    if (first <= last && i <= j) any |= real >> i << (63 - j + i) != 0;
+  }
+  return any;
+}
+// Rows whose weights add up to 0 either see nothing, which gives 0, or have scores of -inf alone, whose softmax is no
+// number.  Their part of the keys tells by m: kNoScore, or -inf for the latter, which counts if all parts' weights are 0.
+__device__ __forceinline__ float told(const KvAttnArgs& a, const Item& it, const Sight& see, float m, float sum) {
+  const bool none = sum == 0.0f && min(see.hi, it.k1 - 1) >= max(see.lo + 1, it.k0);
+  if (__builtin_expect(__builtin_amdgcn_ballot_w64(none) == 0, 1)) return m;
+  return sees_any(a, it, see) && none ? -INFINITY : m;
+}
+// What the sums of values times weights are multiplied by.
+__device__ __forceinline__ float inverse(float v_scale, float sum, bool lost) {
+  return sum == 0.0f ? (lost ? __builtin_nanf("") : 0.0f) : v_scale / sum;
+}
+
 // Value d of the key's row as it is stored.
 template <typename S>
 __device__ __forceinline__ float stored(uint64_t row, int d) {
@@ -826,11 +854,11 @@ struct Tile32 {
   // Result rows: into `out`, or unscaled into the workspace (row `at` on).
   __device__ __forceinline__ void store(const KvAttnArgs& a, const Item& it, int row0, int head, int64_t at, float* parts,
                                         float* stats) const {
-    const float sum = row_sum();
+    const float sum = row_sum(), top = told(a, it, see, m, sum);
     if (row0 + (lane & 31) >= it.rows) return;
     if (it.splits > 1) {
       at += lane & 31;
-      if (half == 0) *(float2*)(stats + at * 2) = make_float2(m, sum);
+      if (half == 0) *(float2*)(stats + at * 2) = make_float2(top, sum);
       float* p = parts + at * S::D + 4 * half;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
@@ -841,7 +869,7 @@ struct Tile32 {
         }
       return;
     }
-    const float inv = sum == 0.0f ? 0.0f : a.v_scale / sum;  // a row that saw nothing has o = 0, too
+    const float inv = inverse(a.v_scale, sum, top == -INFINITY);  // a row that saw nothing has o = 0, too
     const int G = a.num_heads / a.num_kv_heads;
     T* p = (T*)a.out + (it.q0 + see.tok) * a.out_token_stride + (int64_t)(head * G + see.g) * a.out_head_stride + 4 * half;
     typedef T T4 __attribute__((ext_vector_type(4)));
@@ -1232,9 +1260,9 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
   }
 
   // Join the waves, in their order.
-  const float sum = w.row_sum();
+  const float sum = w.row_sum(), m = wave < strips ? told(a, it, w.see, w.m, sum) : kNoScore;
   __syncthreads();
-  if (w.quad == 0) *(float2*)(ml + (wave * kFew + w.lane) * 2) = make_float2(w.m, sum);
+  if (w.quad == 0) *(float2*)(ml + (wave * kFew + w.lane) * 2) = make_float2(m, sum);
   constexpr int kRow = S::D + 4;  // floats of a row, off by 16 bytes so that rows start on different banks
   float* mine = (float*)smem + (wave * kFew + (w.lane & 15)) * kRow + 4 * w.quad;
 #pragma unroll
@@ -1256,11 +1284,14 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
 #pragma unroll
       for (int j = 0; j < 4; ++j) o[j] += f * x[j];
     }
+    bool lost = false;
+    if (l == 0.0f)
+      for (int v = 0; v < W; ++v) lost |= ml[(v * kFew + r) * 2] == -INFINITY;
     if (it.splits > 1) {
-      if (d == 0) *(float2*)(stats + (slot_row + r) * 2) = make_float2(top, l);
+      if (d == 0) *(float2*)(stats + (slot_row + r) * 2) = make_float2(lost ? -INFINITY : top, l);
       *(f4*)(parts + (slot_row + r) * S::D + d) = o;
     } else {
-      const float inv = l == 0.0f ? 0.0f : a.v_scale / l;
+      const float inv = inverse(a.v_scale, l, lost);
       const int row = row0 + r, tok = row / G, g = row - tok * G;
       typedef T T4 __attribute__((ext_vector_type(4)));
       T4 y;
@@ -1360,7 +1391,10 @@ __global__ __launch_bounds__(kThreads) void join_kernel(KvAttnArgs a, Plan p, co
       for (int i = 0; i < 4; ++i) o[i] += s0 + j < it.splits ? x[j][i] * g : 0.0f;
     }
   }
-  const float inv = sum == 0.0f ? 0.0f : a.v_scale / sum;
+  bool lost = false;
+  if (sum == 0.0f)
+    for (int s = 0; s < it.splits; ++s) lost |= stats[(at + s * step) * 2] == -INFINITY;
+  const float inv = inverse(a.v_scale, sum, lost);
   const int row = it.row0 + r, tok = row / G, g = row - tok * G;
   T* out = (T*)a.out + (it.q0 + tok) * a.out_token_stride + (int64_t)(head * G + g) * a.out_head_stride + d;
   typedef T T4 __attribute__((ext_vector_type(4)));
