@@ -1002,7 +1002,11 @@ struct Tile16 {
   f4 o[DT];
   float m, l;
   int koff[KN];
-  int voff[Order::VM];
+  // LDS offsets of V's reads; for 8-bit heads of 256, which would have sixteen, the first one, of which the others differ
+  // by some bits.
+  static constexpr bool kFewRegs = S::F8 && S::D == 256;
+  static constexpr int VN = kFewRegs ? 1 : Order::VM;
+  int voff[VN];
   Offsets<S, Order, S::D == 64 || S::D == 256> dma;
 
   // Row r of the first product's tile t is key 8 (r / 4) + 4 t + r % 4: quad q gets the keys 8 q .. 8 q + 7.
@@ -1016,7 +1020,7 @@ struct Tile16 {
     const int row = 8 * quad + (S::F8 ? n16 >> 1 : n16 >> 2);
     const int in = S::F8 ? (n16 & 1) * 8 : (n16 & 3) * 8;
 #pragma unroll
-    for (int n = 0; n < Order::VM; ++n) voff[n] = row * S::RB + (n ^ Order::v(row)) * (16 * Order::U) + in;
+    for (int n = 0; n < VN; ++n) voff[n] = row * S::RB + (n ^ Order::v(row)) * (16 * Order::U) + in;
     dma.setup();
   }
 
@@ -1067,7 +1071,8 @@ struct Tile16 {
 
   // V^T: lane's element d = 16 dt + lane % 16 of the keys 8 quad .. + 7.
   __device__ __forceinline__ W8 values(uint32_t lds, int dt) const {
-    const uint32_t at = lds + voff[dt % Order::VM] + (dt / Order::VM) * (Order::VM * 16 * Order::U);
+    const int n = dt % Order::VM;
+    const uint32_t at = lds + (kFewRegs ? here(voff[0]) ^ n * 16 * Order::U : voff[n % VN]) + (dt / Order::VM) * (Order::VM * 16 * Order::U);
     if constexpr (S::F8) {
       const i2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((SCOOT_LDS i2*)at);
       return widen<_Float16>(v[0], v[1]);
@@ -1364,7 +1369,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(KvAttnArgs a, Plan p, co
   const int G = a.num_heads / a.num_kv_heads;
   const int64_t step = (int64_t)heads * tile;  // rows of the workspace from part to part
   const int64_t at = ((int64_t)index * p.splits * heads + head) * tile + r;
-  float top = kNoScore, sum = 0.0f;
+  float top = kNoScore, least = INFINITY, sum = 0.0f;
   f4 o = {0.0f, 0.0f, 0.0f, 0.0f};
   for (int s0 = 0; s0 < it.splits; s0 += 8) {
     float2 ml[8];
@@ -1377,7 +1382,10 @@ __global__ __launch_bounds__(kThreads) void join_kernel(KvAttnArgs a, Plan p, co
     }
     float up = top;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) up = fmaxf(up, ml[j].x);  // the last part's again is no harm
+    for (int j = 0; j < 8; ++j) {  // the last part's again is no harm
+      up = fmaxf(up, ml[j].x);
+      least = fminf(least, ml[j].x);
+    }
     const float f = __builtin_amdgcn_exp2f(top - up);
     top = up;
     sum *= f;
@@ -1391,10 +1399,7 @@ __global__ __launch_bounds__(kThreads) void join_kernel(KvAttnArgs a, Plan p, co
       for (int i = 0; i < 4; ++i) o[i] += s0 + j < it.splits ? x[j][i] * g : 0.0f;
     }
   }
-  bool lost = false;
-  if (sum == 0.0f)
-    for (int s = 0; s < it.splits; ++s) lost |= stats[(at + s * step) * 2] == -INFINITY;
-  const float inv = inverse(a.v_scale, sum, lost);
+  const float inv = inverse(a.v_scale, sum, least == -INFINITY);
   const int row = it.row0 + r, tok = row / G, g = row - tok * G;
   T* out = (T*)a.out + (it.q0 + tok) * a.out_token_stride + (int64_t)(head * G + g) * a.out_head_stride + d;
   typedef T T4 __attribute__((ext_vector_type(4)));
