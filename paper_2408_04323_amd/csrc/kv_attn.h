@@ -71,6 +71,8 @@ constexpr float kMost = 16384.0f;            // m moves once a lane's weights of
 constexpr float kBelow = 6.0f;               // to this much below their largest: half precision holds 64 as well as 1, and
                                              // weights down to 2^-30 of the largest, which counts where many keys are small
 
+constexpr float kLimit = 14.0f;              // of a weight's exponent where it moved: no other weight is above kMost
+
 constexpr int gcd256(int x) { return x % 256 == 0 ? 256 : x % 128 == 0 ? 128 : 64; }
 
 // Sizes of a cache row in LDS.
@@ -407,12 +409,25 @@ __device__ __forceinline__ float add_pair(const typename Vec<W>::v8& r, int i, f
   }
 }
 
+// m for a largest score of s.  The exponents scale s - m are exact, but m is as far off as a float is: from 2^27 on by 16
+// and more, so that the weight of the largest score would overflow or vanish.  There m goes below by so much that this
+// weight is always above kMost and then limited; scores that are limited with it are within the error of a float sum.
+__device__ __forceinline__ float below(float s, float scale) {
+  const float x = s * scale, e = __builtin_fabsf(x);
+  return x - (e >= 0x1p27f && e < INFINITY ? e * 0x1p-22f : 0.0f) - kBelow;
+}
+// Not above the limit; NaN stays.
+__device__ __forceinline__ float limited(float x, float limit) { return __builtin_elementwise_minimum(x, limit); }
+
 // Eight weights 2^(scale s - m), rounded, and their sum added to l.
-template <typename W, typename F>
-__device__ __forceinline__ typename Vec<W>::v8 eight_weights(F score, float scale, float m, float& l) {
+template <typename W, bool LIMITED, typename F>
+__device__ __forceinline__ typename Vec<W>::v8 eight_weights(F score, float scale, float m, float limit, float& l) {
   typename Vec<W>::v8 r;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) r[i] = (W)__builtin_amdgcn_exp2f(fmaf(score(i), scale, -m));
+  for (int i = 0; i < 8; ++i) {
+    const float x = fmaf(score(i), scale, -m);
+    r[i] = (W)__builtin_amdgcn_exp2f(LIMITED ? limited(x, limit) : x);
+  }
 #pragma unroll
   for (int i = 0; i < 8; i += 2) l = add_pair<W>(r, i, l);
   return r;
@@ -727,11 +742,15 @@ struct Tile32 {
     W8 w[2];
     float add;
   };
-  __device__ __forceinline__ void weigh(const f16v& s, float scale, Weights& x, int i, int n) const {
+  template <bool LIMITED = false>
+  __device__ __forceinline__ void weigh(const f16v& s, float scale, Weights& x, int i, int n, float limit = 0.0f) const {
     const int from = 2 * (8 * i / n), to = 2 * (8 * (i + 1) / n);
     if (i == 0) x.add = 0.0f;
 #pragma unroll
-    for (int j = from; j < to; ++j) x.w[j / 8][j % 8] = (W)__builtin_amdgcn_exp2f(fmaf(s[j], scale, -m));
+    for (int j = from; j < to; ++j) {
+      const float e = fmaf(s[j], scale, -m);
+      x.w[j / 8][j % 8] = (W)__builtin_amdgcn_exp2f(LIMITED ? limited(e, limit) : e);
+    }
 #pragma unroll
     for (int j = from; j < to; j += 2) x.add = add_pair<W>(x.w[j / 8], j % 8, x.add);
   }
@@ -741,10 +760,11 @@ struct Tile32 {
 #pragma unroll
       for (int i = 1; i < 16; ++i) x = fmaxf(x, s[i]);
       auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-      x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale - kBelow;
+      x = below(fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])), scale);
       const uint32_t over = !(w.add <= kMost);
       sw = __builtin_amdgcn_permlane32_swap(over, over, false, false);
-      const float up = (sw[0] | sw[1]) != 0 && x > m ? x : m, f = __builtin_amdgcn_exp2f(m - up);
+      const bool moves = (sw[0] | sw[1]) != 0;
+      const float up = moves && x > m ? x : m, f = __builtin_amdgcn_exp2f(m - up);
       m = up;
       l *= f;
 #pragma unroll
@@ -753,7 +773,7 @@ struct Tile32 {
         for (int i = 0; i < 16; ++i) o[d][i] *= f;
         __builtin_amdgcn_sched_barrier(0);  // not all of o at once: large ones rest outside the vector units' registers
       }
-      weigh(s, scale, w, 0, 1);
+      weigh<true>(s, scale, w, 0, 1, moves ? kLimit : INFINITY);
     }
     l += w.add;
   }
@@ -1101,7 +1121,7 @@ struct Tile16 {
   // As Tile32::weigh() and moderate().
   __device__ __forceinline__ W8 weights(const f4 (&s)[2], float scale) {
     float add = 0.0f;
-    W8 w = eight_weights<W>([&](int i) { return s[i / 4][i % 4]; }, scale, m, add);
+    W8 w = eight_weights<W, false>([&](int i) { return s[i / 4][i % 4]; }, scale, m, 0.0f, add);
     if (__builtin_amdgcn_ballot_w64(!(add <= kMost))) {
       float x = s[0][0];
 #pragma unroll
@@ -1109,12 +1129,13 @@ struct Tile16 {
       auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
       x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
       sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-      x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale - kBelow;
+      x = below(fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])), scale);
       uint32_t over = !(add <= kMost);
       sw = __builtin_amdgcn_permlane32_swap(over, over, false, false);
       over = sw[0] | sw[1];
       sw = __builtin_amdgcn_permlane16_swap(over, over, false, false);
-      const float up = (sw[0] | sw[1]) != 0 && x > m ? x : m, f = __builtin_amdgcn_exp2f(m - up);
+      const bool moves = (sw[0] | sw[1]) != 0;
+      const float up = moves && x > m ? x : m, f = __builtin_amdgcn_exp2f(m - up);
       m = up;
       l *= f;
 #pragma unroll
@@ -1122,7 +1143,7 @@ struct Tile16 {
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[d][i] *= f;
       add = 0.0f;
-      w = eight_weights<W>([&](int i) { return s[i / 4][i % 4]; }, scale, m, add);
+      w = eight_weights<W, true>([&](int i) { return s[i / 4][i % 4]; }, scale, m, moves ? kLimit : INFINITY, add);
     }
     l += add;
     return w;

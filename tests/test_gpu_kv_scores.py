@@ -1,6 +1,6 @@
-"""Scores that are not finite: a row that sees keys, all of them with scores of -inf, has no softmax, and a row that sees
-nothing is zero.  The two differ in nothing but what they see, so both stand side by side here, in every way that the keys
-are gone through: few rows and tiles, in one part and in several, with windows and with blocks that are missing."""
+"""Scores that are not finite or very large.  A row that sees keys, all of them with scores of -inf, has no softmax, and a row
+that sees nothing is zero.  The two differ in nothing but what they see, so both stand side by side here, in every way that
+the keys are gone through: few rows and tiles, in one part and in several, with windows and with blocks that are missing."""
 import sys
 
 import numpy as np
@@ -112,3 +112,36 @@ def test_rows_that_see_nothing_beside_them(name):
         s["seq"][1] = max(0, lens[1][1] - 1)  # its first token stands before the cache's start
     sees = _check(s)
     assert not sees.all()
+
+
+@pytest.mark.parametrize("d,length", [(64, 16), (64, 700), (128, 5000), (256, 300)])
+@pytest.mark.parametrize("tokens", [1, 4, 40])
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+def test_large_scores_have_a_softmax(kind, tokens, d, length):
+    """Scores up to the largest float, where a float's steps are far larger than what a softmax tells apart.  Every third key
+    has the score x, the others 1.5 x (x negative) or 0.5 x (positive), 70,000 and more apart: the result is the mean of the
+    every-third values that a row sees, up to the rounding of these values' mean (|v| < 5) and of a sum in float."""
+    print("[case] large scores", kind, tokens, d, length, flush=True)
+    t, blocks = TYPES[kind], -(-length // 16)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    v = torch.randn(blocks, 1, 16, d, generator=g, device=DEV).clamp_(-5, 5).to(t)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    third = torch.arange(blocks * 16, device=DEV) % 3 == 0
+    flat = v.view(-1, d).double() * third[:, None]
+    mean = (flat.cumsum(0) / third.cumsum(0)[:, None])[:length]
+    table = torch.arange(blocks, dtype=torch.int32, device=DEV)[None]
+    bits = 9 if kind == "bf16" else 12
+    for size, at in ((1e5, 1.0), (3e7, 1.0), (1.1e8, 1.0), (1.9e8, 1.0), (7e8, 3e4), (3e9, 3e4), (1e15, 3e4), (1e30, 1e10), (1e37, 1e10), (2.2e38, 1e10)):
+        if kind == "f16" and size > 1e9:
+            continue
+        for sign in (-1.0, 1.0):
+            k = torch.zeros(blocks * 16, d, device=DEV)
+            k[:, 1] = at * torch.where(third, 1.0, 1.5 if sign < 0 else 0.5)
+            q = torch.zeros(tokens, 2, d, dtype=t, device=DEV)
+            q[..., 1] = sign * min(size / at, 6e4 if kind == "f16" else 3e38)
+            kc = k.to(t).view(blocks, 1, 16, d)
+            n = min(tokens, length)
+            scale = size / (float(q[0, 0, 1].abs()) * float(kc[0, 0, 0, 1]))
+            got = S.kv_attention(q, kc, v, table, i32(0, tokens), i32(length), tokens, length, scale=scale)
+            off = (got[tokens - n:].double() - mean[length - n:, None]).abs().max()
+            assert off <= 5 * (2.0 ** -bits + length * 2.0 ** -23), (size, sign, float(off))
