@@ -14,6 +14,8 @@ int shift_of(int bs) { return __builtin_ctz((unsigned)bs); }
 bool scale_ok(float s) { return s > 0.0f && std::isfinite(s); }
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 constexpr int64_t kMaxTokens = ((int64_t)1 << 31) - 1;
+// Of a request, where attention counts keys in 32 bits, up to the end of a strip that the last one lies in.
+constexpr int64_t kMaxKeys = ((int64_t)1 << 31) - 256;
 constexpr int kMaxSeqs = 1 << 20;
 constexpr int kMaxHeads = 1024;
 constexpr int64_t kMaxBlocks = ((int64_t)1 << 31) - 1;  // tables hold 32-bit block numbers
@@ -152,7 +154,7 @@ int scoot_kv_attention(const void* q, scoot_kv_type type, int64_t num_tokens, in
   if (rc != SCOOT_OK) return rc;
   if (!std::isfinite(scale) || scale < 0.0f)
     return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: scale must be finite and not negative");
-  if (max_blocks < 0 || max_blocks > (int)(kMaxTokens / block_size) || table_stride < max_blocks || !stride_ok(table_stride))
+  if (max_blocks < 0 || max_blocks > (int)(kMaxKeys / block_size) || table_stride < max_blocks || !stride_ok(table_stride))
     return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: max_blocks or table_stride out of range");
   if (!stride_ok(q_token_stride) || !stride_ok(q_head_stride) || !stride_ok(out_token_stride) || !stride_ok(out_head_stride))
     return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: stride out of range");

@@ -111,3 +111,13 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
     with pytest.raises(ValueError, match="float16"):
         S.kv_attention(k.float(), cache.float(), cache.float(), torch.zeros(1, 2, dtype=torch.int32), z[:2], z[:1], 1, 1)
     assert np.array_equal(z.numpy(), np.zeros(4))
+
+
+@pytest.mark.parametrize("block_size", [8, 16, 32, 64, 128, 256])
+def test_attention_refuses_tables_past_its_key_numbers(block_size):
+    """Keys are counted in 32 bits, and strips of 64 of them may start 32 before the last one: such a table's end would
+    wrap around."""
+    most = (2 ** 31 - 256) // block_size
+    fits = dict(ATTEND, block_size=block_size, max_blocks=most, table_stride=most, num_tokens=0)  # no tokens: nothing is launched
+    assert lib().scoot_kv_attention(*fits.values()) == 0
+    _refused(lib().scoot_kv_attention, ATTEND, INVALID, block_size=block_size, max_blocks=most + 1, table_stride=most + 1, num_tokens=0)
