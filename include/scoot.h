@@ -695,6 +695,7 @@ int scoot_kv_write(const void* k, const void* v, scoot_kv_type type, int64_t num
  *   q, out        [num_tokens][num_heads][head_dim] of `type` (F16 or BF16),
  *                 strides in elements, 16-byte aligned, the last dimension
  *                 contiguous; head_dim 64, 128, 192 or 256.
+ *   scale         >= 0; scale * k_scale * log2(e) finite in float.
  *   max_blocks    entries of a table's row: at most 2^31 - 256 tokens.
  *   max_new_len, max_seq_len  what the caller knows of the longest request (of
  *                 its new tokens, and of its tokens after the step); they choose

@@ -154,6 +154,9 @@ int scoot_kv_attention(const void* q, scoot_kv_type type, int64_t num_tokens, in
   if (rc != SCOOT_OK) return rc;
   if (!std::isfinite(scale) || scale < 0.0f)
     return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: scale must be finite and not negative");
+  const float score_scale = scale * k_scale * 1.44269504088896340736f;  // log2(e): weights are powers of two
+  if (!std::isfinite(score_scale))
+    return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: scale * k_scale is too large");
   if (max_blocks < 0 || max_blocks > (int)(kMaxKeys / block_size) || table_stride < max_blocks || !stride_ok(table_stride))
     return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: max_blocks or table_stride out of range");
   if (!stride_ok(q_token_stride) || !stride_ok(q_head_stride) || !stride_ok(out_token_stride) || !stride_ok(out_head_stride))
@@ -193,7 +196,7 @@ int scoot_kv_attention(const void* q, scoot_kv_type type, int64_t num_tokens, in
   a.block_shift = shift_of(block_size);
   a.window = window;
   // The smallest positive float in the place of 0: it leaves nothing of a score, and -inf stays -inf.
-  a.score_scale = std::max(scale * k_scale * 1.44269504088896340736f, 1.4e-45f);
+  a.score_scale = std::max(score_scale, 1.4e-45f);
   a.v_scale = v_scale;
   a.workspace = workspace;
   return launch_kv_attention(a, type, cache_type, stream);

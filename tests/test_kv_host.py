@@ -121,3 +121,11 @@ def test_attention_refuses_tables_past_its_key_numbers(block_size):
     fits = dict(ATTEND, block_size=block_size, max_blocks=most, table_stride=most, num_tokens=0)  # no tokens: nothing is launched
     assert lib().scoot_kv_attention(*fits.values()) == 0
     _refused(lib().scoot_kv_attention, ATTEND, INVALID, block_size=block_size, max_blocks=most + 1, table_stride=most + 1, num_tokens=0)
+
+
+@pytest.mark.parametrize("change", [dict(scale=3e38), dict(scale=1e20, k_scale=1e20, cache_type=2), dict(scale=2.4e38)], ids=str)
+def test_attention_refuses_scales_whose_product_overflows(change):
+    """A score of 0 would become 0 * inf."""
+    _refused(lib().scoot_kv_attention, ATTEND, INVALID, **change)
+    fits = dict(ATTEND, num_tokens=0, scale=2.3e38)  # nothing is launched
+    assert lib().scoot_kv_attention(*fits.values()) == 0
