@@ -671,7 +671,9 @@ int scoot_kv_assign(const int32_t* context_len, const int32_t* new_len, int num_
 /* Stores the keys and values [num_tokens][num_kv_heads][head_dim] of a step
  * (elements of `type`, F16 or BF16; token and head strides in elements, the
  * last dimension contiguous) at their slots.  Slots outside the cache (-1
- * among them) are skipped; of tokens with the same slot one is stored.
+ * among them) are skipped.  The others must be distinct: heads, keys, values
+ * and pieces of 8 elements are stored independently, so a slot that two tokens
+ * name is left with a mixture of both (other slots are not affected).
  * k_scale, v_scale > 0: the scales of an 8-bit cache, 1 otherwise.
  * Errors: INVALID_ARG, UNSUPPORTED (head_dim not a multiple of 8), DEVICE. */
 int scoot_kv_write(const void* k, const void* v, scoot_kv_type type, int64_t num_tokens, int num_kv_heads,

@@ -820,7 +820,8 @@ def kv_write(k, v, slots, k_cache, v_cache, k_scale=1.0, v_scale=1.0, stream=Non
     """Stores keys and values (tokens, kv_heads, head_dim), float16 or
     bfloat16, at their slots of the caches (blocks, kv_heads, block_size,
     head_dim) of the same type, or float8_e4m3fn, which holds value / scale
-    (scoot_kv_write).  Slots outside the cache are skipped."""
+    (scoot_kv_write).  Slots outside the cache are skipped; the others must be
+    distinct (one that two tokens name is left with a mixture of them)."""
     _kv or _kv_setup()
     rc = _kv.write(k, v, slots, k_cache, v_cache, k_scale, v_scale, stream)
     if rc is None:
