@@ -44,8 +44,29 @@ def _compile(src, hipcc):
     return obj
 
 
+def _module_needs():
+    """What the module is compiled against and this machine lacks: torch's or Python's headers."""
+    import sysconfig
+    try:
+        import torch
+    except ImportError:
+        return "torch"
+    for path in (os.path.join(os.path.dirname(torch.__file__), "include", "ATen", "ATen.h"),
+                 os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        if not os.path.exists(path):
+            return path
+    return None
+
+
 def _build_module():
-    """The Python module over torch's tensors (host code only)."""
+    """The Python module over torch's tensors (host code only).  libscoot.so does without it: where its headers are
+    missing it is left out, and only the calls that need it raise.  Returns whether it was built."""
+    lacks = _module_needs()
+    if lacks:
+        if os.path.exists(MODULE):
+            os.remove(MODULE)  # of another build of the library
+        print(f"{os.path.basename(MODULE)} (calls of the cache operators from torch) not built: {lacks} is missing", file=sys.stderr)
+        return False
     import sysconfig
 
     import torch
@@ -59,6 +80,7 @@ def _build_module():
     if r.returncode != 0:
         raise RuntimeError(f"compile failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, MODULE)
+    return True
 
 
 def build(jobs=None, verbose=False):
@@ -76,9 +98,9 @@ def build(jobs=None, verbose=False):
     if r.returncode != 0:
         raise RuntimeError(f"link failed: {' '.join(cmd)}\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, LIB)
-    module.result()
+    both = module.result()
     if verbose:
-        print(f"built {LIB} and {MODULE}")
+        print(f"built {LIB} and {MODULE}" if both else f"built {LIB}")
     return LIB
 
 
