@@ -158,13 +158,18 @@ __device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)"
 // 64 lanes x 16 bytes from base + off to LDS at `to`, lane after lane; counted
 // by vmcnt.  The compiler does not know of the write: whoever reads it waits
 // first.  Written out because the compiler, for the builtin, waits for all
-// loads in flight before any read of LDS.
+// loads in flight before any read of LDS.  m0 is named as changed, so that the
+// compiler's own uses of it stay in order with these; it warns that it does
+// not keep the register's value, and nothing here needs that.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void load_lds(uint32_t to, uint64_t base, uint32_t off) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(base) : "memory", "m0");
 }
 __device__ __forceinline__ void load_lds(uint32_t to, uint64_t addr) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(addr) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(addr) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 
 // What a workgroup works on: rows of a request from row0 on (a tile's, or 16), one key
 // head, keys [k0, k1) of the tile's, as split `split` of `splits`.
