@@ -16,82 +16,6 @@ int launch_dim<256>(const KvAttnArgs&, const Plan&, scoot_kv_type, bool, float*,
 namespace {
 using namespace kvattn;
 
-constexpr int64_t kUnits = 256;   // compute units
-constexpr int kPartOf = 128;      // parts are multiples of this many keys: a strip of 32 for each of four waves
-constexpr int kMinPart = 512;     // of few rows, for each four waves: a part costs about as much as 256 keys to join
-constexpr int kMinTilePart = 256; // of tiles: four strips
-constexpr double kJoinLaunch = 5e-6;  // seconds, bytes per second
-constexpr double kJoinRate = 4e12;
-constexpr int kAlone = 2048;      // keys that eight waves of one workgroup do not share with another
-
-// Parts of the keys of tiles: the number with the shortest time.  A strip of 64
-// keys takes a workgroup as long as strip_time() says with one, two or three of
-// them on its compute unit (heads of 128: 1.15 and 1.81 us); what does not fit at
-// once follows.  Parts cost a launch and their way through memory, once out and
-// once in.  Against as many parts as fill the chip: chunks of 331 tokens over 547
-// 37 -> 27 us (one part, not two), of 160 over 10,087 50 -> 40 (ten, not twenty), of
-// 270 over 24,258 347 -> 257 (more than fit at once, not two).
-double strip_time(int head_dim, int beside) {
-  if (head_dim <= 64) return (beside == 0 ? 0.77e-6 : beside == 1 ? 1.1e-6 : 1.63e-6);
-  if (head_dim <= 128) return beside == 0 ? 1.15e-6 : 1.81e-6;
-  return head_dim * 7.4e-9;  // 192: 1.4 us, 256: 1.9 us
-}
-
-int64_t parts_of_tiles(int64_t groups, int64_t keys, int64_t rows, int head_dim) {
-  const int fit = head_dim <= 64 ? 3 : head_dim <= 128 ? 2 : 1;  // workgroups that a compute unit holds
-  const int64_t most = (keys + kMinTilePart - 1) / kMinTilePart;
-  int64_t best = 1;
-  double least = 0;
-  for (int i = 1; i <= 8 + fit; ++i) {  // few parts, and as many as give every unit one, two, three workgroups
-    const int64_t n = i <= 8 ? i : (i - 8) * kUnits / groups;
-    if (n > most || (i > 8 && n <= 8)) continue;
-    const int64_t beside = std::min<int64_t>((groups * n - 1) / kUnits, fit - 1);
-    double t = (double)keys / (64 * n) * strip_time(head_dim, (int)beside) * std::max(1.0, (double)(groups * n) / (fit * kUnits));
-    if (n > 1) t += kJoinLaunch + (double)(2 * n * rows * head_dim * 4) / kJoinRate;
-    if (i == 1 || t < least) least = t, best = n;
-  }
-  return best;
-}
-
-// Requests of at most 16 rows (new tokens x heads per key head) are items of
-// their own; once some have more, tiles of 128 rows are.  The keys of tiles are
-// split as above, those of few rows until the items fill the chip four times over
-// (their lengths differ most).
-Plan plan(int64_t num_tokens, int num_heads, int num_kv_heads, int head_dim, int element_bytes, int num_seqs, int64_t max_new_len,
-          int64_t max_seq_len, int window) {
-  Plan p{};
-  const int64_t G = num_heads / num_kv_heads;
-  const int64_t longest = std::min<int64_t>(max_new_len, num_tokens);
-  const bool tiles = longest * G > kFew;
-  p.tile_rows = tiles ? kTile : 0;
-  p.items = tiles ? num_tokens * G / p.tile_rows + num_seqs : num_seqs;
-  int64_t keys = max_seq_len;
-  if (window > 0) keys = std::min<int64_t>(keys, (int64_t)window + (tiles ? p.tile_rows / G : longest) + 32);
-  keys = std::max<int64_t>(keys, 1);
-  // Tiles that have rows: as many as the numbers if all requests but one are single tokens, else fewer, at least one for
-  // every request and for every 128 rows; so many if there is one request.
-  const int64_t least = std::max<int64_t>(num_seqs, (num_tokens * G + kTile - 1) / kTile);
-  const int64_t most = tiles && num_seqs == 1 ? least : p.items;
-  const int64_t real = tiles ? (most + least) / 2 : p.items;
-  const int64_t groups = std::max<int64_t>(1, real * num_kv_heads);
-  int64_t want;
-  p.waves = kWaves;
-  if (tiles) {
-    want = parts_of_tiles(groups, keys, num_tokens * num_heads, head_dim);
-  } else {
-    // Few items of few rows: eight waves each.
-    if (groups <= kUnits && head_dim * element_bytes <= kWideRow) p.waves = 8;
-    want = p.waves == 8 ? (keys <= kAlone ? 1 : 2 * kUnits / groups) : 8 * kUnits / groups;
-  }
-  want = std::max<int64_t>(1, want);
-  int64_t part = (keys + want - 1) / want;
-  part = std::max<int64_t>(tiles ? kMinTilePart : kMinPart * (p.waves / kWaves), (part + kPartOf - 1) / kPartOf * kPartOf);
-  p.part = (int)std::min<int64_t>(part, (int64_t)1 << 30);
-  p.splits = (int)((keys + p.part - 1) / p.part);
-  p.deep = most * num_kv_heads * p.splits <= kUnits;  // one more would follow all others
-  return p;
-}
-
 int64_t slots(const Plan& p, int num_kv_heads) {
   return p.splits > 1 ? p.items * p.splits * num_kv_heads * (p.tile_rows ? p.tile_rows : kFew) : 0;
 }

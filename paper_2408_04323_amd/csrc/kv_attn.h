@@ -42,6 +42,7 @@
 #include <type_traits>
 
 #include "kv.h"
+#include "kv_plan.h"
 
 namespace scoot {
 namespace kvattn {
@@ -59,13 +60,8 @@ typedef short s4 __attribute__((ext_vector_type(4)));
 #define SCOOT_LDS __attribute__((address_space(3)))
 #define SCOOT_CONST __attribute__((address_space(4)))
 
-constexpr int kWaves = 4;                    // of a workgroup (one of few rows may have eight)
 constexpr int kThreads = 64 * kWaves;
-constexpr int kFew = 16;                     // rows of a request that one workgroup's waves handle together
-constexpr int kRows = 32;                    // rows of a wave otherwise
-constexpr int kTile = kRows * kWaves;        // rows of a tile
 constexpr float kNoScore = -3.40282347e38f;  // m before any key was seen; finite, so that m - m is 0, and below no finite score
-constexpr int kWideRow = 256;                // bytes of a cache row up to which eight waves' strips fit the LDS
 constexpr int kReadsAhead = 4;               // operands of the matrix instructions on their way out of LDS
 constexpr float kMost = 16384.0f;            // m moves once a lane's weights of 32 keys add up to more,
 constexpr float kBelow = 6.0f;               // to this much below their largest: half precision holds 64 as well as 1, and
@@ -86,8 +82,8 @@ struct Shape {
   static constexpr int PC = RB / 16;                // 16-byte pieces of a row
   static constexpr int g = 256 / gcd256(RB);        // rows this far apart start on the same bank
   static constexpr int NJ = RB / 64;                // loads of 1 KiB for 16 rows
-  static constexpr int ST = 64;                     // keys per strip of a shared tile
-  static constexpr int kStrip = 2 * ST * RB;        // bytes of a strip of K and V
+  static constexpr int ST = kStripKeys;             // keys per strip of a shared tile
+  static constexpr int kStrip = strip_bytes(RB);    // of K and V
   // The second product runs in the cache's 16-bit type; 8-bit values are exact in half precision, which rounds the
   // weights eight times finer than bfloat16.
   typedef typename std::conditional<F8, _Float16, T>::type W;
@@ -184,15 +180,6 @@ struct Item {
   int split;
   int seq;
   bool shared;      // the waves share the keys (more than kFew rows), else each wave takes strips of its own
-};
-
-struct Plan {
-  int64_t items;    // tiles or requests
-  int splits;
-  int part;         // keys per part, a multiple of 128
-  int tile_rows;    // rows of a tile; 0: the items are requests, of few rows each
-  int waves;        // of a workgroup
-  bool deep;        // tiles: at most one workgroup per compute unit, which may have more LDS
 };
 
 __device__ __forceinline__ int64_t clamp64(int64_t v, int64_t lo, int64_t hi) { return v < lo ? lo : v > hi ? hi : v; }
@@ -1346,15 +1333,8 @@ struct FewLds {
 // R > 0: tiles through R buffers, requests of few rows among them; R = 0: these alone.
 template <typename S, int R, int W>
 constexpr int kFlagAt = R * S::kStrip > FewLds<S, W>::kEnd ? R * S::kStrip : FewLds<S, W>::kEnd;
-// Waves per SIMD that the registers are to suffice for.
-template <typename S, int R>
-constexpr int kOccupancy = R == 0 ? 2 : S::D == 64 ? (R == 2 ? 3 : 2) : S::D == 128 ? 2 : 1;
-// Buffers of tiles that have a compute unit for themselves.
-template <typename S>
-constexpr int kDeep = 4 * S::kStrip <= 128 * 1024 ? 4 : 2;
-
 template <typename S, int R, int W>
-__global__ __launch_bounds__(64 * W, (kOccupancy<S, R>)) void attention_kernel(KvAttnArgs a, Plan p, float* parts, float* stats) {
+__global__ __launch_bounds__(64 * W, (waves_per_simd(S::D, R))) void attention_kernel(KvAttnArgs a, Plan p, float* parts, float* stats) {
   extern __shared__ __attribute__((aligned(256))) char smem[];
   const uint32_t lds = (uint32_t)(uintptr_t)(SCOOT_LDS char*)smem;
   const uint32_t heads = (uint32_t)a.num_kv_heads;
@@ -1448,8 +1428,8 @@ template <typename S>
 int launch(const KvAttnArgs& a, const Plan& p, float* parts, float* stats, hipStream_t stream) {
   int rc;
   if (p.tile_rows) {
-    constexpr int R = kOccupancy<S, 2> == 1 ? kDeep<S> : 2;
-    rc = p.deep ? launch_kernel<S, kDeep<S>, kWaves>(a, p, parts, stats, stream) : launch_kernel<S, R, kWaves>(a, p, parts, stats, stream);
+    rc = p.deep ? launch_kernel<S, buffers(S::D, S::RB, true), kWaves>(a, p, parts, stats, stream)
+                : launch_kernel<S, buffers(S::D, S::RB, false), kWaves>(a, p, parts, stats, stream);
   } else {
     if constexpr (S::RB <= kWideRow) {
       if (p.waves == 8) rc = launch_kernel<S, 0, 8>(a, p, parts, stats, stream);

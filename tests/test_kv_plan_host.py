@@ -1,0 +1,47 @@
+"""Which form of the attention kernel the cases of tests/kv_cases.py take, by the library's own plan (tests/kv_plan_check.cpp,
+built here against its internal header): every form has cases whose values are compared on the GPU, also when the plan's
+thresholds change."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+import kv_cases
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    cxx = shutil.which("g++")
+    if cxx is None:
+        pytest.skip("no host C++ compiler")
+    exe = str(tmp_path_factory.mktemp("plan") / "kv_plan_check")
+    subprocess.run([cxx, "-O1", "-std=c++17", "-I", os.path.join(ROOT, "paper_2408_04323_amd", "csrc"),
+                    os.path.join(ROOT, "tests", "kv_plan_check.cpp"), "-o", exe], check=True)
+
+    def ask(lines):
+        out = subprocess.run([exe], input="\n".join(lines) + "\n", capture_output=True, text=True, check=True).stdout.splitlines()
+        assert len(out) == len(lines)
+        return [(a, int(w), int(b), int(s)) for a, w, b, s in (x.split() for x in out)]
+    return ask
+
+
+def test_the_cases_take_the_forms_that_they_are_for(plan):
+    names = list(kv_cases.CASES)
+    for name, (kind, waves, buffers, parts) in zip(names, plan([kv_cases.plan_line(kv_cases.CASES[n]) for n in names])):
+        assert (kind, waves, buffers, parts > 1) == kv_cases.CASES[name]["form"], (name, parts)
+
+
+def test_every_form_has_a_case():
+    have = {(c["d"], c["kind"], c["cache"] == "f8") + c["form"] for c in kv_cases.CASES.values()}
+    for d in kv_cases.DIMS:
+        for kind in kv_cases.TYPES:
+            for f8 in (False, True):
+                wide = d * (1 if f8 else 2) > 256
+                tiles = {2} if wide else {4} if d >= 192 else {2, 4}
+                want = {("few", w, 0) for w in ({4} if wide else {4, 8})} | {("tiles", 4, b) for b in tiles}
+                for form in want:
+                    for parts in (False, True):
+                        assert (d, kind, f8) + form + (parts,) in have, (d, kind, f8, form, parts)
