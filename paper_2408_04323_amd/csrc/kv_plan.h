@@ -37,11 +37,12 @@ constexpr int buffers(int head_dim, int row_bytes, bool deep) {
 
 constexpr int64_t kUnits = 256;   // compute units
 constexpr int kPartOf = 128;      // parts are multiples of this many keys: a strip of 32 for each of four waves
-constexpr int kMinPart = 512;     // of few rows, for each four waves: a part costs about as much as 256 keys to join
+constexpr int kMinPart = 256;     // of few rows
 constexpr int kMinTilePart = 256; // of tiles: four strips
 constexpr double kJoinLaunch = 5e-6;  // seconds, bytes per second
 constexpr double kJoinRate = 4e12;
-constexpr int kAlone = 2048;      // keys that eight waves of one workgroup do not share with another
+constexpr int kAlone8 = 1024;     // keys that eight waves of one workgroup do not share with another,
+constexpr int kAlone4 = 768;      // and four waves
 
 // Parts of the keys of tiles: the number with the shortest time.  A strip of 64
 // keys takes a workgroup as long as strip_time() says with one, two or three of
@@ -72,10 +73,32 @@ inline int64_t parts_of_tiles(int64_t groups, int64_t keys, int64_t rows, int he
   return best;
 }
 
+// Parts of the keys of few rows.  A part costs its share of a second launch and of
+// memory; what it gives is more workgroups, as long as they do not already draw
+// what the memory gives.  Measured with caches in memory (not in L2), in us:
+// * One request, heads of 128 (eight waves): 800 keys 9.8 in one part, 11.1 in
+//   four; 1000 11.1, 11.3; 1500 13.7, 11.6; 2000 17.4, 12.8; 4000 39.8 in one, 15.1 in
+//   eight, 14.1 in sixteen.  Heads of 192 (four waves): 600 12.3 in one part, 13.1
+//   in two; 800 13.7, 13.3 in three; 1000 15.4, 13.5.  So kAlone8 and kAlone4, and then
+//   parts of 256 keys and more: 9000 keys, heads of 256: 25 in 8 parts, 21 in 16, 19 in 32.
+// * Parts until every unit has one workgroup, not several: 100 requests of up to
+//   16,000, heads of 256 278 with 256 workgroups, 283 with 512, 294 with 1024; 8 of up to
+//   16,000, heads of 128 68, 77, 77; 4 of 16,000, 8 bits 32, 38, 48.
+// * ... of ten keys for every workgroup at least: 16 of 4000, heads of 64 (256 workgroups)
+//   49 in one part, 56 in two; 16 of 1000, heads of 256 26 in one, 19 in three.
+// * More workgroups than units get parts for the units that have one more, and for unequal
+//   lengths, of seven keys for every workgroup at least.  288 workgroups, all of 4095 keys,
+//   131 in one part, 120 in two; 400 of up to 16,000, heads of 192 595 in one part, 587 in
+//   four, 521 in five; 512 of up to 4095, heads of 256 258 in one, 275 in two.
+// All of 182 such calls: 2.4% over the best of seven rules each, at most 16%.
+inline int64_t parts_of_few(int64_t groups, int64_t keys, int waves) {
+  if (keys <= (waves == 8 ? kAlone8 : kAlone4)) return 1;
+  const bool more = groups > kUnits;
+  return std::min((more ? 8 : 1) * kUnits / groups, keys / std::max<int64_t>(kMinPart, (more ? 7 : 10) * groups));
+}
+
 // Requests of at most 16 rows (new tokens x heads per key head) are items of
-// their own; once some have more, tiles of 128 rows are.  The keys of tiles are
-// split as above, those of few rows until the items fill the chip four times over
-// (their lengths differ most).
+// their own; once some have more, tiles of 128 rows are.
 inline Plan plan(int64_t num_tokens, int num_heads, int num_kv_heads, int head_dim, int element_bytes, int num_seqs, int64_t max_new_len,
           int64_t max_seq_len, int window) {
   Plan p{};
@@ -98,15 +121,16 @@ inline Plan plan(int64_t num_tokens, int num_heads, int num_kv_heads, int head_d
   if (tiles) {
     want = parts_of_tiles(groups, keys, num_tokens * num_heads, head_dim);
   } else {
-    // Few items of few rows: eight waves each.
+    // Few items of few rows: eight waves each (one request of 1000 keys, heads of 128, in one part 11.6 -> 10.5 us; of 130
+    // keys 7.5 -> 7.8).
     if (groups <= kUnits && head_dim * element_bytes <= kWideRow) p.waves = 8;
-    want = p.waves == 8 ? (keys <= kAlone ? 1 : 2 * kUnits / groups) : 8 * kUnits / groups;
+    want = parts_of_few(groups, keys, p.waves);
   }
   want = std::max<int64_t>(1, want);
   int64_t part = (keys + want - 1) / want;
-  part = std::max<int64_t>(tiles ? kMinTilePart : kMinPart * (p.waves / kWaves), (part + kPartOf - 1) / kPartOf * kPartOf);
+  part = std::max<int64_t>(tiles ? kMinTilePart : kPartOf, (part + kPartOf - 1) / kPartOf * kPartOf);
   p.part = (int)std::min<int64_t>(part, (int64_t)1 << 30);
-  p.splits = (int)((keys + p.part - 1) / p.part);
+  p.splits = (int)std::max<int64_t>(1, (keys + p.part - kPartOf) / p.part);  // less than kPartOf keys go to the part before
   p.deep = most * num_kv_heads * p.splits <= kUnits;  // one more would follow all others
   return p;
 }

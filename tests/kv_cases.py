@@ -10,7 +10,7 @@ MANY = [(i * 13 % 60, 1) for i in range(7)]
 def _lens():
     """(lens, kv_heads): more than 256 items and key heads, and fewer."""
     return {
-        "few": MANY + [(300, 3), (0, 2)], "few_parts": MANY + [(2500, 2), (0, 1)],
+        "few": MANY + [(300, 3), (0, 2)], "few_parts": MANY + [(6200, 2), (0, 1)],
         "tiles": MANY + [(70, 20), (0, 40)], "tiles_parts": MANY + [(2300, 24), (0, 17)],
     }
 

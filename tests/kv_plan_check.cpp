@@ -1,5 +1,6 @@
 // Which form of the attention kernel calls take: reads "tokens heads kv_heads head_dim element_bytes requests max_new_len
-// max_seq_len window" line by line and prints "few" or "tiles", waves, LDS buffers (0: few rows) and parts.
+// max_seq_len window" line by line and prints "few" or "tiles", waves, LDS buffers (0: few rows), parts
+// and keys per part.
 #include <cstdio>
 
 #include "kv_plan.h"
@@ -11,8 +12,8 @@ int main() {
   while (std::scanf("%lld %lld %lld %lld %lld %lld %lld %lld %lld", &tokens, &heads, &kv_heads, &dim, &bytes, &seqs, &max_new, &max_seq,
                     &window) == 9) {
     const Plan p = plan(tokens, (int)heads, (int)kv_heads, (int)dim, (int)bytes, (int)seqs, max_new, max_seq, (int)window);
-    std::printf("%s %d %d %d\n", p.tile_rows ? "tiles" : "few", p.waves,
-                p.tile_rows ? buffers((int)dim, (int)(dim * bytes), p.deep) : 0, p.splits);
+    std::printf("%s %d %d %d %d\n", p.tile_rows ? "tiles" : "few", p.waves,
+                p.tile_rows ? buffers((int)dim, (int)(dim * bytes), p.deep) : 0, p.splits, p.part);
   }
   return 0;
 }

@@ -24,13 +24,13 @@ def plan(tmp_path_factory):
     def ask(lines):
         out = subprocess.run([exe], input="\n".join(lines) + "\n", capture_output=True, text=True, check=True).stdout.splitlines()
         assert len(out) == len(lines)
-        return [(a, int(w), int(b), int(s)) for a, w, b, s in (x.split() for x in out)]
+        return [tuple(x if i == 0 else int(x) for i, x in enumerate(line.split())) for line in out]
     return ask
 
 
 def test_the_cases_take_the_forms_that_they_are_for(plan):
     names = list(kv_cases.CASES)
-    for name, (kind, waves, buffers, parts) in zip(names, plan([kv_cases.plan_line(kv_cases.CASES[n]) for n in names])):
+    for name, (kind, waves, buffers, parts, _) in zip(names, plan([kv_cases.plan_line(kv_cases.CASES[n]) for n in names])):
         assert (kind, waves, buffers, parts > 1) == kv_cases.CASES[name]["form"], (name, parts)
 
 
@@ -45,3 +45,20 @@ def test_every_form_has_a_case():
                 for form in want:
                     for parts in (False, True):
                         assert (d, kind, f8) + form + (parts,) in have, (d, kind, f8, form, parts)
+
+
+def test_parts_of_few_rows(plan):
+    """No launch that joins parts for few keys: one part up to 768 keys (four waves) and 1024 (eight), then none of less than
+    128, few workgroups more than compute units unless they are more anyway, and never more parts than can be asked for."""
+    asked = [(seqs, heads, dim, size, keys) for seqs in (1, 3, 16, 40, 300) for heads in (1, 8) for dim in (64, 128, 192, 256)
+             for size in (1, 2) for keys in (1, 129, 513, 768, 769, 1024, 1025, 1500, 2047, 4000, 4097, 9000, 65536, 2 ** 30)]
+    got = plan([f"{s} {h} {h} {d} {b} {s} 1 {k} 0" for s, h, d, b, k in asked])
+    for (seqs, heads, dim, size, keys), (kind, waves, _, parts, part) in zip(asked, got):
+        at = (seqs, heads, dim, size, keys, waves, parts, part)
+        assert kind == "few" and parts >= 1 and part % 128 == 0, at
+        assert (parts - 1) * part < keys and parts * part + 128 > keys, at
+        if keys <= (1024 if waves == 8 else 768):
+            assert parts == 1, at
+        if parts > 1:
+            assert keys - (parts - 1) * part >= 128 and part >= 256, at
+            assert seqs * heads * parts <= (256 if seqs * heads <= 256 else 2048), at
