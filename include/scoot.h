@@ -662,7 +662,7 @@ typedef enum scoot_kv_type { SCOOT_KV_F16 = 0, SCOOT_KV_BF16 = 1, SCOOT_KV_F8 = 
  *   counts        [4] out: tokens, admitted requests, blocks taken, blocks
  *                 that admitting every request that passes the first two
  *                 tests would have taken.
- * num_seqs <= 2^20.  Errors: INVALID_ARG, DEVICE. */
+ * num_seqs <= 2^20.  Errors: INVALID_ARG, DEVICE, NO_MEMORY. */
 int scoot_kv_assign(const int32_t* context_len, const int32_t* new_len, int num_seqs, int block_size,
                     int32_t* block_table, int max_blocks, int64_t table_stride, const int32_t* free_blocks,
                     int num_free, int64_t max_tokens, int32_t* query_start, int32_t* seq_len, int32_t* positions,
@@ -675,7 +675,8 @@ int scoot_kv_assign(const int32_t* context_len, const int32_t* new_len, int num_
  * and pieces of 8 elements are stored independently, so a slot that two tokens
  * name is left with a mixture of both (other slots are not affected).
  * k_scale, v_scale > 0: the scales of an 8-bit cache, 1 otherwise.
- * Errors: INVALID_ARG, UNSUPPORTED (head_dim not a multiple of 8), DEVICE. */
+ * Errors: INVALID_ARG, UNSUPPORTED (head_dim not a multiple of 8), DEVICE,
+ * NO_MEMORY. */
 int scoot_kv_write(const void* k, const void* v, scoot_kv_type type, int64_t num_tokens, int num_kv_heads,
                    int head_dim, int64_t k_token_stride, int64_t k_head_stride, int64_t v_token_stride,
                    int64_t v_head_stride, const int64_t* slots, void* k_cache, void* v_cache,
@@ -706,7 +707,8 @@ int scoot_kv_write(const void* k, const void* v, scoot_kv_type type, int64_t num
  *   workspace     of at least scoot_kv_attention_workspace's bytes, 16-byte
  *                 aligned (may be NULL if that is 0); no call that may run at
  *                 the same time shares it.
- * Errors: INVALID_ARG (also a workspace too small), UNSUPPORTED, DEVICE. */
+ * Errors: INVALID_ARG (also a workspace too small), UNSUPPORTED, DEVICE,
+ * NO_MEMORY. */
 int scoot_kv_attention_workspace(int64_t num_tokens, int num_heads, int num_kv_heads, int head_dim, int num_seqs,
                                  int64_t max_new_len, int64_t max_seq_len, int window, uint64_t* bytes);
 int scoot_kv_attention(const void* q, scoot_kv_type type, int64_t num_tokens, int num_heads, int num_kv_heads,

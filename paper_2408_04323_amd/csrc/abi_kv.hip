@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <new>
 
 #include "kv.h"
 
@@ -37,6 +38,16 @@ int check_cache(scoot_kv_type type, scoot_kv_type cache_type, int num_kv_heads, 
   if (cache_type != SCOOT_KV_F8 && (k_scale != 1.0f || v_scale != 1.0f))
     return fail_static(SCOOT_ERR_INVALID_ARG, "kv cache: scales other than 1 need an 8-bit cache");
   return SCOOT_OK;
+}
+
+// No exception leaves a C entry.
+template <typename F>
+int guarded(F launch) {
+  try {
+    return launch();
+  } catch (const std::bad_alloc&) {
+    return fail_static(SCOOT_ERR_NO_MEMORY, "kv cache: host allocation failed");
+  }
 }
 
 int check_attention_sizes(int64_t num_tokens, int num_heads, int num_kv_heads, int head_dim, int num_seqs,
@@ -89,7 +100,7 @@ int scoot_kv_assign(const int32_t* context_len, const int32_t* new_len, int num_
   a.max_blocks = max_blocks;
   a.num_free = num_free;
   a.block_shift = shift_of(block_size);
-  return launch_kv_assign(a, stream);
+  return guarded([&] { return launch_kv_assign(a, stream); });
 }
 
 int scoot_kv_write(const void* k, const void* v, scoot_kv_type type, int64_t num_tokens, int num_kv_heads,
@@ -127,7 +138,7 @@ int scoot_kv_write(const void* k, const void* v, scoot_kv_type type, int64_t num
   a.num_heads = num_kv_heads;
   a.head_dim = head_dim;
   a.block_shift = shift_of(block_size);
-  return launch_kv_write(a, type, cache_type, stream);
+  return guarded([&] { return launch_kv_write(a, type, cache_type, stream); });
 }
 
 int scoot_kv_attention_workspace(int64_t num_tokens, int num_heads, int num_kv_heads, int head_dim, int num_seqs,
@@ -199,7 +210,7 @@ int scoot_kv_attention(const void* q, scoot_kv_type type, int64_t num_tokens, in
   a.score_scale = std::max(score_scale, 1.4e-45f);
   a.v_scale = v_scale;
   a.workspace = workspace;
-  return launch_kv_attention(a, type, cache_type, stream);
+  return guarded([&] { return launch_kv_attention(a, type, cache_type, stream); });
 }
 
 }  // extern "C"
