@@ -1429,8 +1429,7 @@ template <typename S>
 int launch(const KvAttnArgs& a, const Plan& p, float* parts, float* stats, hipStream_t stream) {
   int rc;
   if (p.tile_rows) {
-    rc = p.deep ? launch_kernel<S, buffers(S::D, S::RB, true), kWaves>(a, p, parts, stats, stream)
-                : launch_kernel<S, buffers(S::D, S::RB, false), kWaves>(a, p, parts, stats, stream);
+    rc = launch_kernel<S, buffers(S::D, S::RB), kWaves>(a, p, parts, stats, stream);
   } else {
     if constexpr (S::RB <= kWideRow) {
       if (p.waves == 8) rc = launch_kernel<S, 0, 8>(a, p, parts, stats, stream);

@@ -21,18 +21,20 @@ struct Plan {
   int part;         // keys per part, a multiple of 128
   int tile_rows;    // rows of a tile; 0: the items are requests, of few rows each
   int waves;        // of a workgroup
-  bool deep;        // tiles: at most one workgroup per compute unit, which may have more LDS
 };
 
 // Bytes of a strip of K and V.
 constexpr int strip_bytes(int row_bytes) { return 2 * kStripKeys * row_bytes; }
 // Waves per SIMD that the registers are to suffice for; no buffers: few rows.
 constexpr int waves_per_simd(int head_dim, int buffers) {
-  return buffers == 0 ? 2 : head_dim == 64 ? (buffers == 2 ? 3 : 2) : head_dim == 128 ? 2 : 1;
+  return buffers == 0 ? 2 : head_dim == 64 ? 3 : head_dim == 128 ? 2 : 1;
 }
-// Buffers of tiles, more where a workgroup has a compute unit for itself.
-constexpr int buffers(int head_dim, int row_bytes, bool deep) {
-  return (deep || waves_per_simd(head_dim, 2) == 1) && 4 * strip_bytes(row_bytes) <= 128 * 1024 ? 4 : 2;
+// Buffers of tiles.  Four gain something where the registers leave a compute unit one workgroup and the buffers take
+// less than 128 KiB: 8-bit heads of 192, 500 tokens over 30,000 323 -> 317 us.  8-bit heads of 256 193 -> 194; heads of 64
+// and 128 with a compute unit for every workgroup: one prompt of 300 tokens 9.7 -> 10.0 and 12.8 -> 13.1, 500 tokens over
+// 30,000 152 and 251 with either.
+constexpr int buffers(int head_dim, int row_bytes) {
+  return waves_per_simd(head_dim, 2) == 1 && 4 * strip_bytes(row_bytes) < 128 * 1024 ? 4 : 2;
 }
 
 constexpr int64_t kUnits = 256;   // compute units
@@ -131,7 +133,6 @@ inline Plan plan(int64_t num_tokens, int num_heads, int num_kv_heads, int head_d
   part = std::max<int64_t>(tiles ? kMinTilePart : kPartOf, (part + kPartOf - 1) / kPartOf * kPartOf);
   p.part = (int)std::min<int64_t>(part, (int64_t)1 << 30);
   p.splits = (int)std::max<int64_t>(1, (keys + p.part - kPartOf) / p.part);  // less than kPartOf keys go to the part before
-  p.deep = most * num_kv_heads * p.splits <= kUnits;  // one more would follow all others
   return p;
 }
 

@@ -13,7 +13,7 @@ int main() {
                     &window) == 9) {
     const Plan p = plan(tokens, (int)heads, (int)kv_heads, (int)dim, (int)bytes, (int)seqs, max_new, max_seq, (int)window);
     std::printf("%s %d %d %d %d\n", p.tile_rows ? "tiles" : "few", p.waves,
-                p.tile_rows ? buffers((int)dim, (int)(dim * bytes), p.deep) : 0, p.splits, p.part);
+                p.tile_rows ? buffers((int)dim, (int)(dim * bytes)) : 0, p.splits, p.part);
   }
   return 0;
 }

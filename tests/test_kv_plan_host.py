@@ -40,8 +40,7 @@ def test_every_form_has_a_case():
         for kind in kv_cases.TYPES:
             for f8 in (False, True):
                 wide = d * (1 if f8 else 2) > 256
-                tiles = {2} if wide else {4} if d >= 192 else {2, 4}
-                want = {("few", w, 0) for w in ({4} if wide else {4, 8})} | {("tiles", 4, b) for b in tiles}
+                want = {("few", w, 0) for w in ({4} if wide else {4, 8})} | {("tiles", 4, 4 if d == 192 and f8 else 2)}
                 for form in want:
                     for parts in (False, True):
                         assert (d, kind, f8) + form + (parts,) in have, (d, kind, f8, form, parts)
