@@ -40,7 +40,8 @@ constexpr int buffers(int head_dim, int row_bytes) {
 constexpr int64_t kUnits = 256;   // compute units
 constexpr int kPartOf = 128;      // parts are multiples of this many keys: a strip of 32 for each of four waves
 constexpr int kMinPart = 256;     // of few rows
-constexpr int kMinTilePart = 256; // of tiles: four strips
+constexpr int kMinTilePart = 256; // of tiles: four strips (940 keys, heads of 128: 16.0 us, 19.6 with 512; with 128 540 keys
+                                  // 17.1 -> 16.5, but 2040 keys, heads of 64, 14.0 -> 15.2)
 constexpr double kJoinLaunch = 5e-6;  // seconds, bytes per second
 constexpr double kJoinRate = 4e12;
 constexpr int kAlone8 = 1024;     // keys that eight waves of one workgroup do not share with another,
@@ -132,7 +133,9 @@ inline Plan plan(int64_t num_tokens, int num_heads, int num_kv_heads, int head_d
   int64_t part = (keys + want - 1) / want;
   part = std::max<int64_t>(tiles ? kMinTilePart : kPartOf, (part + kPartOf - 1) / kPartOf * kPartOf);
   p.part = (int)std::min<int64_t>(part, (int64_t)1 << 30);
-  p.splits = (int)std::max<int64_t>(1, (keys + p.part - kPartOf) / p.part);  // less than kPartOf keys go to the part before
+  // Of few rows, less than kPartOf keys go to the part before; a tile's parts are done by their time, and the longest
+  // decides (40 tokens over 540 keys in parts of 256, 256 and 28: heads of 256 26.9 us, 29.8 with 256 and 284).
+  p.splits = (int)std::max<int64_t>(1, (keys + p.part - (tiles ? 1 : kPartOf)) / p.part);
   return p;
 }
 
