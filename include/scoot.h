@@ -694,7 +694,9 @@ int scoot_kv_write(const void* k, const void* v, scoot_kv_type type, int64_t num
  * memory, infinities and NaN included) does not reach its result; one whose
  * scores are all -inf, or one of them +inf, gets NaN, as the formula has it.
  * Rows of out that belong to no request are not written.  Sums and the softmax are in
- * float; its weights are rounded to 16 bits for the product with v.
+ * float; its weights are rounded to 16 bits for the product with v (to the
+ * cache's type, half precision for an 8-bit cache), which shows beside the
+ * result's own rounding where the values have no mean: 1.4 times its error.
  *   q, out        [num_tokens][num_heads][head_dim] of `type` (F16 or BF16),
  *                 strides in elements, 16-byte aligned, the last dimension
  *                 contiguous; head_dim 64, 128, 192 or 256.

@@ -25,10 +25,13 @@ namespace {
 // value, past every limit they are compared with.
 //
 // Few requests (and so mostly few tokens) go to workgroups of 256 threads, a
-// quarter of the waves to start and to bring together.  Lengths come four at a
-// time, those of the next tile during the sums of this one: 8192 requests 11.8 ->
-// 8.6 us, 20,000 22.8 -> 15.3.  Tiles of eight requests per thread were slower
-// (18.5 and 37: LDS banks).  64 requests take 4.1 us.
+// quarter of the waves to start and to bring together (calls in a row, 256 and
+// 1024 threads: 64 requests 4.7 and 5.1 us, 1000 4.6 and 5.6, 2000 5.3 and 5.6, 8192 12.0
+// and 8.5; the limit is what one tile holds).  Lengths come four at a time, those
+// of the next tile during the sums of this one: 8192 requests 11.8 -> 8.4 us, 20,000
+// 22.8 -> 15.3.  Tiles of eight requests per thread were slower (18.5 and 37: LDS
+// banks).  64 requests take 3.7 us without the host's side.  Workgroups: 100
+// requests of up to 2000 new tokens 6.0 us with 128, 4.9 with 256, 4.7 with 512.
 constexpr int kAssignPer = 4;     // requests per thread and tile
 constexpr int kAssignFew = 1024;  // requests that one tile of 256 threads holds
 constexpr int kAssignGroups = 256;

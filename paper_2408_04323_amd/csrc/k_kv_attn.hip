@@ -1,4 +1,4 @@
-// How an attention call over the block cache is split, and its launches.
+// Attention over the block cache: a call's plan, workspace and limits, and the way to the launches of its head dimension.
 #include "kv_attn.h"
 
 namespace scoot {
