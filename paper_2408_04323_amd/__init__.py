@@ -779,7 +779,9 @@ def kv_assign(context_len, new_len, block_table, free_blocks, block_size, max_to
     the requests' cached and new lengths (int32 (requests,)) the new tokens'
     slots and positions, and, from ``free_blocks`` in order, the new entries of
     ``block_table`` (int32 (requests, blocks), updated in place).  Returns a
-    KVBatch (``out`` if given); nothing is read back."""
+    KVBatch (``out`` if given); nothing is read back.  ``stream`` (this call's
+    and the next two's): a stream's handle, 0 for the default one; what a call
+    makes belongs to the stream that it runs on."""
     _kv or _kv_setup()
     args = context_len, new_len, block_table, free_blocks, block_size, max_tokens
     if out is not None:
@@ -847,7 +849,8 @@ def kv_attention(q, k_cache, v_cache, block_table, query_start, seq_len, max_new
     these, if given).  ``max_new_len`` and ``max_seq_len``: the longest request
     of the step as the caller knows it; ``scale`` defaults to head_dim ** -0.5.
     A ``workspace`` (uint8, at least kv_attention_workspace's bytes) may be
-    kept between calls.  Returns ``out``, made if not given."""
+    kept between calls.  Returns ``out``, made if not given; no gradient is
+    defined over a cache that is written in place, and it has none."""
     _kv or _kv_setup()
     args = (q, k_cache, v_cache, block_table, query_start, seq_len, max_new_len, max_seq_len, scale, window, k_scale, v_scale,
             out, workspace)
