@@ -39,8 +39,8 @@
 // wave alone keeps both units busy by itself: the weights of 32 keys are made
 // between the matrix instructions of the next products, and a strip's loads go
 // between those of the first scores (in a row they hold the wave up: 192 427 ->
-// 396 us).  Late chunks over 30,000 keys, heads of 64, 128, 192, 256: 0.94, 1.16,
-// 0.97, 0.99 PFLOP/s (192 and 256 with two waves and half of the registers each,
+// 396 us).  Late chunks over 30,000 keys, heads of 64, 128, 192, 256: 0.95, 1.14,
+// 0.90, 0.88 PFLOP/s (192 and 256 with two waves and half of the registers each,
 // o shared: 0.58 and 0.44).
 #pragma once
 
