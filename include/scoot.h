@@ -721,6 +721,96 @@ int scoot_kv_attention(const void* q, scoot_kv_type type, int64_t num_tokens, in
                        int window, float k_scale, float v_scale, void* out, int64_t out_token_stride,
                        int64_t out_head_stride, void* workspace, uint64_t workspace_bytes, void* stream);
 
+/* Rotations by position.  Pair i of a vector at position p is turned by the
+ * angle p * freqs[i] (radians):
+ *   a' = a c - b s,  b' = b c + a s,  (c, s) = magnitude * (cos, sin),
+ * for the first 2 * pairs = rotary_dim elements of every head, as the pairs
+ * (i, i + rotary_dim / 2), or, interleaved, (2 i, 2 i + 1); the other elements
+ * stay.  Angles, cosines and sines are in double, c and s rounded to float, the
+ * products in float, the result rounded once.  freqs is a device array of
+ * rotary_dim / 2 doubles, from scoot_rotary_frequencies or any other source.
+ *
+ * scoot_rotary_frequencies (host): freqs[dim / 2] and the magnitude for
+ * f_i = base^(-2 i / dim), scaled for contexts `factor` >= 1 times as long as
+ * those that a model knows:
+ *   NONE    f_i (factor, length, low and high are not used).
+ *   LINEAR  f_i / factor: positions come closer together.
+ *   BASE    base becomes base * factor^(dim / (dim - 2)): the slowest pair
+ *           gets `factor` times slower, the fastest stays.
+ *   RAMP    pairs that turn more than `high` times over `length` positions
+ *           stay, those that turn less than `low` times go `factor` times
+ *           slower, with a line over the pairs' numbers in between (its ends
+ *           rounded outwards to whole pairs); magnitude 0.1 ln(factor) + 1.
+ *   BANDS   the same with a line over the number of turns; magnitude 1.
+ * Errors: INVALID_ARG. */
+typedef enum scoot_rotary_scaling {
+  SCOOT_ROTARY_NONE = 0,
+  SCOOT_ROTARY_LINEAR = 1,
+  SCOOT_ROTARY_BASE = 2,
+  SCOOT_ROTARY_RAMP = 3,
+  SCOOT_ROTARY_BANDS = 4
+} scoot_rotary_scaling;
+int scoot_rotary_frequencies(int dim, double base, int scaling, double factor, double length, double low, double high,
+                             double* freqs, double* magnitude);
+
+/* Turns the vectors x [num_tokens][num_heads][head_dim] (elements of `type`,
+ * F16 or BF16; strides in elements, the last dimension contiguous) by their
+ * tokens' positions into out, which may be x itself (with the same strides),
+ * and else does not overlap it.  Rows of tokens with a negative position are
+ * not written.  reverse: the other way (the same magnitude), which is what the
+ * gradient of x is of the gradient of out.
+ * head_dim: a multiple of 8, at most 1024; rotary_dim even, 0 .. head_dim.
+ * Rows that start on 16 bytes, and rotary_dim a multiple of 16 (interleaved:
+ * of 8), are faster.  Errors: INVALID_ARG, UNSUPPORTED, DEVICE, NO_MEMORY. */
+int scoot_rotate(const void* x, scoot_kv_type type, int64_t num_tokens, int num_heads, int head_dim, int64_t x_token_stride,
+                 int64_t x_head_stride, const int32_t* positions, const double* freqs, int rotary_dim, int interleaved,
+                 double magnitude, int reverse, void* out, int64_t out_token_stride, int64_t out_head_stride, void* stream);
+
+/* scoot_kv_write with the rotation on the way: keys are turned by their
+ * tokens' positions before they are stored (rounded once), values stored as
+ * they are, and queries q [num_tokens][num_heads][head_dim], if given
+ * (num_heads > 0), turned into q_out, which may be q itself.  rotary_dim 0:
+ * nothing is turned, positions and freqs are not used, and there are no
+ * queries.  A token with a negative position is skipped whole, one whose slot
+ * is outside the cache has its queries turned and nothing stored.
+ *
+ * k_scales, v_scales (both or neither; an 8-bit cache): [num_blocks]
+ * [num_kv_heads] scales of every block and head, in and out, in the place of
+ * k_scale and v_scale, which are 1 then.  A block of head h holds
+ * value / scale.  Each block that gets values gets, for every head, the
+ * smallest power of two E (2^-64 .. 2^64) with |value| <= 448 E for its new
+ * finite values as its scale, or keeps the scale that it has if it holds
+ * earlier values (its first new slot is not its first one) and that is no
+ * smaller.  Where the scale grows, the earlier values (those before the first
+ * new slot) are stored anew, times old / new scale; the scale of a block with
+ * earlier values that is not positive and finite is replaced and they stay as
+ * they are.  Infinities are limited to 448 E, NaN is kept.  With scales, the
+ * tokens of one block have to be rows in a row, with slots that ascend, as
+ * scoot_kv_assign gives them; otherwise that block's values and scales are
+ * undefined (other blocks are not affected).
+ * Errors: INVALID_ARG, UNSUPPORTED, DEVICE, NO_MEMORY. */
+int scoot_kv_append(const void* q, int num_heads, int64_t q_token_stride, int64_t q_head_stride, void* q_out,
+                    int64_t q_out_token_stride, int64_t q_out_head_stride, const void* k, const void* v, scoot_kv_type type,
+                    int64_t num_tokens, int num_kv_heads, int head_dim, int64_t k_token_stride, int64_t k_head_stride,
+                    int64_t v_token_stride, int64_t v_head_stride, const int32_t* positions, const int64_t* slots,
+                    const double* freqs, int rotary_dim, int interleaved, double magnitude, void* k_cache, void* v_cache,
+                    scoot_kv_type cache_type, int64_t num_blocks, int block_size, float k_scale, float v_scale,
+                    float* k_scales, float* v_scales, void* stream);
+
+/* scoot_kv_attention over an 8-bit cache with a scale for every block and
+ * head, k_scales and v_scales [num_blocks][num_kv_heads], positive and from
+ * 2^-64 to 2^64 (a scale that is not makes results of the rows that see its
+ * block undefined, and no others):
+ *   out = sum_t softmax_t(scale * k_scales[b_t] * q . k_t) * v_scales[b_t] * v_t
+ * The workspace is scoot_kv_attention_workspace's. */
+int scoot_kv_attention_scaled(const void* q, scoot_kv_type type, int64_t num_tokens, int num_heads, int num_kv_heads,
+                              int head_dim, int64_t q_token_stride, int64_t q_head_stride, const void* k_cache,
+                              const void* v_cache, int64_t num_blocks, int block_size, const int32_t* block_table,
+                              int max_blocks, int64_t table_stride, const int32_t* query_start, const int32_t* seq_len,
+                              int num_seqs, int64_t max_new_len, int64_t max_seq_len, float scale, int window,
+                              const float* k_scales, const float* v_scales, void* out, int64_t out_token_stride,
+                              int64_t out_head_stride, void* workspace, uint64_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -759,6 +759,31 @@ def _refuse_caches(k_cache, v_cache):
                (v_cache.dtype is k_cache.dtype and v_cache.shape == k_cache.shape, "v_cache must have k_cache's type and shape"))
 
 
+def _refuse_scales(k_scale, v_scale, k_cache):
+    """Scales of every block and head, or numbers."""
+    import torch
+    both = [isinstance(t, torch.Tensor) and t.dim() > 0 for t in (k_scale, v_scale)]
+    _kv_refuse((both[0] == both[1], "k_scale and v_scale must both be numbers or both be tensors"))
+    if not all(both):
+        return
+    _kv_refuse((_kv_types[k_cache.dtype] == KV_F8, "scales of blocks need a float8_e4m3fn cache"))
+    for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
+        _kv_refuse((t.is_cuda, f"{name} must be a device tensor"), (t.dtype is torch.float32, f"{name} must be float32"),
+                   (t.shape == k_cache.shape[:2], f"{name} must be (blocks, kv_heads), {tuple(k_cache.shape[:2])}"),
+                   (t.is_contiguous(), f"{name} must be contiguous"))
+
+
+def _refuse_rotary(rotary, positions, tokens, dim):
+    import torch
+    _kv_refuse((isinstance(rotary, Rotary), "rotary must be a Rotary"))
+    f = rotary.freqs
+    _kv_refuse((isinstance(f, torch.Tensor) and f.is_cuda and f.dtype is torch.float64 and f.dim() == 1 and f.is_contiguous(),
+                "the rotary's freqs must be a contiguous float64 device tensor (pairs,)"),
+               (isinstance(positions, torch.Tensor), "positions must be a device tensor"))
+    _kv_refuse((2 * f.numel() <= dim, f"the rotary has more pairs than a head of {dim} elements"))
+    _refuse_ints(positions, "positions", tokens)
+
+
 class KVBatch:
     """Caller-owned outputs of kv_assign for ``num_seqs`` requests and at most
     ``max_tokens`` new tokens: query_start (num_seqs + 1), seq_len (num_seqs),
@@ -840,6 +865,127 @@ def kv_write(k, v, slots, k_cache, v_cache, k_scale=1.0, v_scale=1.0, stream=Non
         check(rc, "kv_write")
 
 
+class Rotary:
+    """Rotations by position: ``freqs`` (float64 (pairs,), on the device), the
+    angle of every pair per position in radians, and the ``magnitude`` that
+    every pair is multiplied by.  The pairs are the first 2 * pairs elements of
+    a head, as (i, i + pairs) or, ``interleaved``, (2 i, 2 i + 1).
+    rotary_create makes the usual ones."""
+    __slots__ = ("freqs", "magnitude", "interleaved")
+
+    def __init__(self, freqs, magnitude=1.0, interleaved=False):
+        self.freqs, self.magnitude, self.interleaved = freqs, magnitude, interleaved
+
+
+ROTARY_SCALINGS = {None: 0, "none": 0, "linear": 1, "base": 2, "ramp": 3, "bands": 4}
+
+
+def rotary_frequencies(dim, base=10000.0, scaling=None, factor=1.0, length=0, low=1.0, high=32.0):
+    """Frequencies (float64 (dim / 2,), host) and magnitude of the rotations of
+    ``dim`` elements (scoot_rotary_frequencies): base ** (-2 i / dim), and
+    ``scaling`` for contexts ``factor`` times as long as before: "linear",
+    "base", and "ramp" or "bands", which leave pairs that turn more than
+    ``high`` times over ``length`` positions as they are and slow those down
+    that turn less than ``low`` times."""
+    if scaling not in ROTARY_SCALINGS:
+        raise ValueError(f"scaling must be one of {list(ROTARY_SCALINGS)}")
+    freqs, magnitude = np.zeros(max(int(dim) // 2, 1), dtype=np.float64), C.c_double(0.0)
+    check(lib().scoot_rotary_frequencies(int(dim), float(base), ROTARY_SCALINGS[scaling], float(factor), float(length), float(low),
+                                         float(high), freqs.ctypes.data_as(C.POINTER(C.c_double)), C.byref(magnitude)),
+          "rotary_frequencies")
+    return freqs, magnitude.value
+
+
+def rotary_create(dim, base=10000.0, scaling=None, factor=1.0, length=0, low=1.0, high=32.0, interleaved=False, device="cuda"):
+    """A Rotary of rotary_frequencies on ``device``."""
+    import torch
+    freqs, magnitude = rotary_frequencies(dim, base, scaling, factor, length, low, high)
+    return Rotary(torch.from_numpy(freqs).to(device), magnitude, interleaved)
+
+
+def rotate(x, positions, rotary, reverse=False, out=None, stream=None):
+    """Vectors x (tokens, heads, head_dim), float16 or bfloat16, turned by their
+    tokens' ``positions`` (int32 (tokens,)) (scoot_rotate).  ``reverse`` turns
+    the other way: the gradient of x is rotate(the gradient of the result,
+    ..., reverse=True); nothing is recorded for autograd.  Returns ``out``,
+    made if not given, which may be x; rows of tokens with a negative position
+    are not written."""
+    _kv or _kv_setup()
+    got = None
+    if isinstance(rotary, Rotary):
+        args = x, positions, rotary.freqs, rotary.magnitude, rotary.interleaved, reverse, out
+        if stream is None or out is not None:
+            got = _kv.rotate(*args, stream)
+        else:
+            with _kv_on(stream, x):
+                got = _kv.rotate(*args, None)
+    if got is None:
+        _refuse_vectors(x, "x", None, x.shape[-1])
+        _refuse_rotary(rotary, positions, x.shape[0], x.shape[2])
+        _refuse_mixed(x, positions=positions, out=out, **{"the rotary's freqs": rotary.freqs})
+        _refuse_vectors(out, "out", x.shape[1], x.shape[2])
+        _kv_refuse((False, "out must have x's type and shape"))
+    if out is None and not isinstance(got, int):
+        return got
+    if got:
+        check(got, "rotate")
+    return out
+
+
+def kv_append(k, v, positions, slots, k_cache, v_cache, rotary=None, k_scale=1.0, v_scale=1.0, q=None, out=None, stream=None):
+    """kv_write with the rotation on the way (scoot_kv_append): keys are turned
+    by their tokens' ``positions`` (kv_assign's) before they are stored, and
+    queries ``q`` (tokens, heads, head_dim), if given, into ``out``, which may
+    be q and is made if not given.  Without a ``rotary`` nothing is turned,
+    and ``positions`` may be None.
+
+    ``k_scale`` and ``v_scale``: numbers, as for kv_write, or, of a
+    float8_e4m3fn cache, float32 tensors (blocks, kv_heads), updated in place:
+    every block's scale is the smallest power of two that its values of a head
+    need, and grows with them.  The tokens of one block have to be rows in a
+    row then, with slots that ascend, as kv_assign gives them.  Returns
+    ``out`` (None without queries); nothing is recorded for autograd."""
+    _kv or _kv_setup()
+    got = None
+    if rotary is None or isinstance(rotary, Rotary):
+        turn = (None, 1.0, False) if rotary is None else (rotary.freqs, rotary.magnitude, rotary.interleaved)
+        args = (k, v, positions, slots, k_cache, v_cache, *turn, k_scale, v_scale, q, out)
+        if stream is None or q is None or out is not None:
+            got = _kv.append(*args, stream)
+        else:
+            with _kv_on(stream, k):
+                got = _kv.append(*args, None)
+    if got is None:
+        _refuse_caches(k_cache, v_cache)
+        _, heads, _, dim = k_cache.shape
+        _refuse_vectors(k, "k", heads, dim)
+        _refuse_vectors(v, "v", heads, dim)
+        _kv_refuse((v.dtype is k.dtype and v.shape[0] == k.shape[0], "v must have k's type and number of tokens"),
+                   (slots.is_cuda and slots.dtype is _int64 and slots.is_contiguous(),
+                    "slots must be a contiguous int64 device tensor"),
+                   (slots.numel() == k.shape[0], f"slots must have {k.shape[0]} elements"))
+        _refuse_mixed(k, v=v, slots=slots, k_cache=k_cache, v_cache=v_cache)
+        if rotary is not None:
+            _refuse_rotary(rotary, positions, k.shape[0], dim)
+            _refuse_mixed(k, positions=positions, **{"the rotary's freqs": rotary.freqs})
+        _refuse_scales(k_scale, v_scale, k_cache)
+        _kv_refuse((q is None or rotary is not None, "queries need a rotary"), (q is not None or out is None, "out needs queries"))
+        if q is not None:
+            _refuse_vectors(q, "q", None, dim)
+            _kv_refuse((q.dtype is k.dtype and q.shape[0] == k.shape[0], "q must have k's type and number of tokens"))
+            _refuse_mixed(k, q=q, out=out)
+            if out is not None:
+                _refuse_vectors(out, "out", q.shape[1], dim)
+                _kv_refuse((out.dtype is q.dtype and out.shape == q.shape, "out must have q's type and shape"))
+        _refuse_mixed(k, **{n: t for n, t in (("k_scale", k_scale), ("v_scale", v_scale)) if hasattr(t, "device")})
+        raise ValueError("kv_append takes tensors")
+    if q is None or out is not None or isinstance(got, int):
+        if got:
+            check(got, "kv_append")
+        return out
+    return got
+
+
 def kv_attention(q, k_cache, v_cache, block_table, query_start, seq_len, max_new_len, max_seq_len, scale=None,
                  window=0, k_scale=1.0, v_scale=1.0, out=None, workspace=None, stream=None):
     """Attention of a step's queries (tokens, heads, head_dim) over the block
@@ -848,7 +994,9 @@ def kv_attention(q, k_cache, v_cache, block_table, query_start, seq_len, max_new
     query sees what stands up to its own position (the last ``window`` of
     these, if given).  ``max_new_len`` and ``max_seq_len``: the longest request
     of the step as the caller knows it; ``scale`` defaults to head_dim ** -0.5.
-    A ``workspace`` (uint8, at least kv_attention_workspace's bytes) may be
+    ``k_scale`` and ``v_scale``: numbers, or, over a float8_e4m3fn cache,
+    float32 tensors (blocks, kv_heads), a scale for every block and head as
+    kv_append keeps them (scoot_kv_attention_scaled).  A ``workspace`` (uint8, at least kv_attention_workspace's bytes) may be
     kept between calls.  Returns ``out``, made if not given; no gradient is
     defined over a cache that is written in place, and it has none."""
     _kv or _kv_setup()
@@ -868,6 +1016,8 @@ def kv_attention(q, k_cache, v_cache, block_table, query_start, seq_len, max_new
         _refuse_table(block_table, n)
         _refuse_mixed(q, k_cache=k_cache, v_cache=v_cache, seq_len=seq_len, query_start=query_start, block_table=block_table,
                       out=out, workspace=workspace)
+        _refuse_scales(k_scale, v_scale, k_cache)
+        _refuse_mixed(q, **{n: t for n, t in (("k_scale", k_scale), ("v_scale", v_scale)) if hasattr(t, "device") and t.dim()})
         if out is not None:
             _refuse_vectors(out, "out", q.shape[1], dim)
             _kv_refuse((out.dtype is q.dtype and out.shape == q.shape, "out must have q's type and shape"))

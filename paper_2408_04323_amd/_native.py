@@ -80,6 +80,15 @@ SIGNATURES = {
     "scoot_kv_attention": [c_vp, c_int, c_i64, c_int, c_int, c_int, c_i64, c_i64, c_vp, c_vp, c_int, c_i64, c_int, c_vp,
                            c_int, c_i64, c_vp, c_vp, c_int, c_i64, c_i64, C.c_float, c_int, C.c_float, C.c_float,
                            c_vp, c_i64, c_i64, c_vp, C.c_uint64, c_vp],
+    "scoot_rotary_frequencies": [c_int, c_dbl, c_int, c_dbl, c_dbl, c_dbl, c_dbl, P_dbl, P_dbl],
+    "scoot_rotate": [c_vp, c_int, c_i64, c_int, c_int, c_i64, c_i64, c_vp, c_vp, c_int, c_int, c_dbl, c_int, c_vp, c_i64,
+                     c_i64, c_vp],
+    "scoot_kv_append": [c_vp, c_int, c_i64, c_i64, c_vp, c_i64, c_i64, c_vp, c_vp, c_int, c_i64, c_int, c_int, c_i64, c_i64,
+                        c_i64, c_i64, c_vp, c_vp, c_vp, c_int, c_int, c_dbl, c_vp, c_vp, c_int, c_i64, c_int, C.c_float,
+                        C.c_float, c_vp, c_vp, c_vp],
+    "scoot_kv_attention_scaled": [c_vp, c_int, c_i64, c_int, c_int, c_int, c_i64, c_i64, c_vp, c_vp, c_i64, c_int, c_vp, c_int,
+                                  c_i64, c_vp, c_vp, c_int, c_i64, c_i64, C.c_float, c_int, c_vp, c_vp, c_vp, c_i64, c_i64,
+                                  c_vp, C.c_uint64, c_vp],
 }
 RESTYPES = {"scoot_status_string": C.c_char_p, "scoot_last_error": C.c_char_p}
 
@@ -129,6 +138,7 @@ def kv_module(raw_stream):
         raise RuntimeError(f"{path} is missing: build it with paper_2408_04323_amd.build.build()")
     from . import _kv_torch
     at = [C.cast(getattr(lib(), name), c_vp).value
-          for name in ("scoot_kv_assign", "scoot_kv_write", "scoot_kv_attention_workspace", "scoot_kv_attention")]
+          for name in ("scoot_kv_assign", "scoot_kv_write", "scoot_kv_attention_workspace", "scoot_kv_attention", "scoot_rotate",
+                       "scoot_kv_append", "scoot_kv_attention_scaled")]
     _kv_torch.bind(*at, raw_stream)
     return _kv_torch

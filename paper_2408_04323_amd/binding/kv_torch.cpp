@@ -28,10 +28,21 @@ typedef int (*WorkspaceFn)(int64_t, int, int, int, int, int64_t, int64_t, int, u
 typedef int (*AttentionFn)(const void*, int, int64_t, int, int, int, int64_t, int64_t, const void*, const void*, int, int64_t, int,
                            const void*, int, int64_t, const void*, const void*, int, int64_t, int64_t, float, int, float, float, void*,
                            int64_t, int64_t, void*, uint64_t, void*);
+typedef int (*RotateFn)(const void*, int, int64_t, int, int, int64_t, int64_t, const void*, const void*, int, int, double, int, void*,
+                        int64_t, int64_t, void*);
+typedef int (*AppendFn)(const void*, int, int64_t, int64_t, void*, int64_t, int64_t, const void*, const void*, int, int64_t, int, int,
+                        int64_t, int64_t, int64_t, int64_t, const void*, const void*, const void*, int, int, double, void*, void*, int,
+                        int64_t, int, float, float, void*, void*, void*);
+typedef int (*ScaledFn)(const void*, int, int64_t, int, int, int, int64_t, int64_t, const void*, const void*, int64_t, int, const void*,
+                        int, int64_t, const void*, const void*, int, int64_t, int64_t, float, int, const void*, const void*, void*,
+                        int64_t, int64_t, void*, uint64_t, void*);
 AssignFn assign_fn;
 WriteFn write_fn;
 WorkspaceFn workspace_fn;
 AttentionFn attention_fn;
+RotateFn rotate_fn;
+AppendFn append_fn;
+ScaledFn scaled_fn;
 PyObject* raw_stream;  // torch's: device index -> stream
 
 enum { kF16, kBF16, kF8, kNoType };
@@ -60,6 +71,19 @@ bool are_caches(const at::Tensor& k, const at::Tensor& v) {
   return type_of(k) != kNoType && k.is_cuda() && v.is_cuda() && k.dim() == 4 && k.is_contiguous() && v.is_contiguous() &&
          v.scalar_type() == k.scalar_type() && v.sizes() == k.sizes();
 }
+
+// Scales of every block and key head of a cache.
+bool are_scales(PyObject* k, PyObject* v, const at::Tensor& cache) {
+  for (PyObject* o : {k, v}) {
+    if (!THPVariable_Check(o)) return false;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!(is_list(t, at::kFloat) && t.dim() == 2 && t.size(0) == cache.size(0) && t.size(1) == cache.size(1) &&
+          t.get_device() == cache.get_device()))
+      return false;
+  }
+  return type_of(cache) == kF8;
+}
+bool is_scales(PyObject* o) { return THPVariable_Check(o) && THPVariable_Unpack(o).dim() > 0; }
 
 bool with(const at::Tensor& t, std::initializer_list<const at::Tensor*> others) {
   for (const at::Tensor* o : others)
@@ -100,9 +124,15 @@ bool get(PyObject* o, int64_t& v) {
   v = PyLong_AsLongLong(o);
   return !(v == -1 && PyErr_Occurred());
 }
+bool get(PyObject* o, double& v) {
+  v = PyFloat_AsDouble(o);
+  return !(v == -1.0 && PyErr_Occurred());
+}
 bool get(PyObject* o, float& v) {
-  v = (float)PyFloat_AsDouble(o);
-  return !(v == -1.0f && PyErr_Occurred());
+  double d;
+  const bool ok = get(o, d);
+  v = (float)d;
+  return ok;
 }
 bool get_stream(PyObject* o, const at::Tensor& t, void*& stream) {
   int64_t v;
@@ -134,19 +164,22 @@ at::Tensor part(const at::Tensor& bytes, at::ScalarType type, int64_t from, int6
   return t;
 }
 
-// bind(assign, write, workspace, attention, raw_stream): addresses of the library's functions.
+// bind(assign, write, workspace, attention, rotate, append, scaled, raw_stream): addresses of the library's functions.
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  int64_t at[4];
-  if (n != 5) return PyErr_Format(PyExc_TypeError, "bind takes 5 arguments");
-  for (int i = 0; i < 4; ++i)
+  int64_t at[7];
+  if (n != 8) return PyErr_Format(PyExc_TypeError, "bind takes 8 arguments");
+  for (int i = 0; i < 7; ++i)
     if (!get(args[i], at[i])) return nullptr;
   assign_fn = (AssignFn)at[0];
   write_fn = (WriteFn)at[1];
   workspace_fn = (WorkspaceFn)at[2];
   attention_fn = (AttentionFn)at[3];
-  Py_INCREF(args[4]);
+  rotate_fn = (RotateFn)at[4];
+  append_fn = (AppendFn)at[5];
+  scaled_fn = (ScaledFn)at[6];
+  Py_INCREF(args[7]);
   Py_XDECREF(raw_stream);
-  raw_stream = args[4];
+  raw_stream = args[7];
   Py_RETURN_NONE;
 }
 
@@ -219,8 +252,99 @@ PyObject* write(PyObject*, PyObject* const* args, Py_ssize_t n) {
   END_HANDLE_TH_ERRORS
 }
 
+bool is_freqs(const at::Tensor& t, int64_t dim) { return is_list(t, at::kDouble) && t.dim() == 1 && 2 * t.size(0) <= dim; }
+
+// rotate(x, positions, freqs, magnitude, interleaved, reverse, out or None, stream) -> status, or out if it was made here
+PyObject* rotate(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 8) return PyErr_Format(PyExc_TypeError, "rotate takes 8 arguments");
+  if (!tensors(args, {0, 1, 2})) Py_RETURN_NONE;
+  const at::Tensor &x = THPVariable_Unpack(args[0]), &pos = THPVariable_Unpack(args[1]), &freqs = THPVariable_Unpack(args[2]);
+  if (!(type_of(x) < kF8 && x.is_cuda() && x.dim() == 3 && x.stride(2) == 1 && is_list(pos, at::kInt) && pos.numel() == x.size(0) &&
+        is_freqs(freqs, x.size(2)) && with(x, {&pos, &freqs})))
+    Py_RETURN_NONE;
+  at::Tensor out;
+  const bool made = args[6] == Py_None;
+  if (!made) {
+    if (!THPVariable_Check(args[6])) Py_RETURN_NONE;
+    out = THPVariable_Unpack(args[6]);
+    if (!(out.scalar_type() == x.scalar_type() && is_vectors(out, x.size(1), x.size(2)) && out.size(0) == x.size(0) && with(x, {&out})))
+      Py_RETURN_NONE;
+  }
+  double magnitude;
+  int64_t interleaved, reverse;
+  void* stream;
+  if (!get(args[3], magnitude) || !get(args[4], interleaved) || !get(args[5], reverse) || !get_stream(args[7], x, stream)) return nullptr;
+  if (made) out = make(x.sizes(), x.scalar_type(), x);
+  const OnDeviceOf on(x);
+  const int rc = rotate_fn(x.data_ptr(), type_of(x), x.size(0), narrow(x.size(1)), narrow(x.size(2)), x.stride(0), x.stride(1),
+                           pos.data_ptr(), freqs.data_ptr(), 2 * narrow(freqs.size(0)), narrow(interleaved), magnitude, narrow(reverse),
+                           out.data_ptr(), out.stride(0), out.stride(1), stream);
+  if (rc != 0 || !made) return PyLong_FromLong(rc);
+  return THPVariable_Wrap(std::move(out));
+  END_HANDLE_TH_ERRORS
+}
+
+// append(k, v, positions or None, slots, k_cache, v_cache, freqs or None, magnitude, interleaved, k_scale, v_scale (numbers or
+// tensors), q or None, out or None, stream) -> status, or out if it was made here
+PyObject* append(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  HANDLE_TH_ERRORS
+  if (n != 14) return PyErr_Format(PyExc_TypeError, "append takes 14 arguments");
+  if (!tensors(args, {0, 1, 3, 4, 5})) Py_RETURN_NONE;
+  const at::Tensor &k = THPVariable_Unpack(args[0]), &v = THPVariable_Unpack(args[1]), &slots = THPVariable_Unpack(args[3]),
+                   &kc = THPVariable_Unpack(args[4]), &vc = THPVariable_Unpack(args[5]);
+  if (!are_caches(kc, vc)) Py_RETURN_NONE;
+  const int64_t heads = kc.size(1), dim = kc.size(3), tokens = slots.numel();
+  if (!(type_of(k) < kF8 && v.scalar_type() == k.scalar_type() && is_vectors(k, heads, dim) && is_vectors(v, heads, dim) &&
+        k.size(0) == tokens && v.size(0) == tokens && is_list(slots, at::kLong) && with(k, {&v, &slots, &kc, &vc})))
+    Py_RETURN_NONE;
+  const bool turns = args[6] != Py_None;
+  at::Tensor pos, freqs, q, out;
+  if (turns) {
+    if (!tensors(args, {2, 6})) Py_RETURN_NONE;
+    pos = THPVariable_Unpack(args[2]);
+    freqs = THPVariable_Unpack(args[6]);
+    if (!(is_list(pos, at::kInt) && pos.numel() == tokens && is_freqs(freqs, dim) && with(k, {&pos, &freqs}))) Py_RETURN_NONE;
+  }
+  const bool queries = args[11] != Py_None, made = queries && args[12] == Py_None;
+  if (queries != (queries && turns) || (!queries && args[12] != Py_None)) Py_RETURN_NONE;
+  if (queries) {
+    if (!THPVariable_Check(args[11])) Py_RETURN_NONE;
+    q = THPVariable_Unpack(args[11]);
+    if (!(q.scalar_type() == k.scalar_type() && q.dim() == 3 && is_vectors(q, q.size(1), dim) && q.size(0) == tokens && with(k, {&q})))
+      Py_RETURN_NONE;
+    if (!made) {
+      if (!THPVariable_Check(args[12])) Py_RETURN_NONE;
+      out = THPVariable_Unpack(args[12]);
+      if (!(out.scalar_type() == q.scalar_type() && is_vectors(out, q.size(1), dim) && out.size(0) == tokens && with(k, {&out})))
+        Py_RETURN_NONE;
+    }
+  }
+  const bool scaled = is_scales(args[9]) || is_scales(args[10]);
+  if (scaled && !are_scales(args[9], args[10], kc)) Py_RETURN_NONE;
+  double magnitude;
+  int64_t interleaved;
+  float ks = 1.0f, vs = 1.0f;
+  void* stream;
+  if (!get(args[7], magnitude) || !get(args[8], interleaved) || (!scaled && (!get(args[9], ks) || !get(args[10], vs))) ||
+      !get_stream(args[13], k, stream))
+    return nullptr;
+  if (made) out = make(q.sizes(), q.scalar_type(), q);
+  const OnDeviceOf on(k);
+  const int rc = append_fn(
+      queries ? q.data_ptr() : nullptr, queries ? narrow(q.size(1)) : 0, queries ? q.stride(0) : 0, queries ? q.stride(1) : 0,
+      queries ? out.data_ptr() : nullptr, queries ? out.stride(0) : 0, queries ? out.stride(1) : 0, k.data_ptr(), v.data_ptr(), type_of(k),
+      tokens, narrow(heads), narrow(dim), k.stride(0), k.stride(1), v.stride(0), v.stride(1), turns ? pos.data_ptr() : nullptr,
+      slots.data_ptr(), turns ? freqs.data_ptr() : nullptr, turns ? 2 * narrow(freqs.size(0)) : 0, narrow(interleaved), magnitude,
+      kc.data_ptr(), vc.data_ptr(), type_of(kc), kc.size(0), narrow(kc.size(2)), ks, vs,
+      scaled ? THPVariable_Unpack(args[9]).data_ptr() : nullptr, scaled ? THPVariable_Unpack(args[10]).data_ptr() : nullptr, stream);
+  if (rc != 0 || !made) return PyLong_FromLong(rc);
+  return THPVariable_Wrap(std::move(out));
+  END_HANDLE_TH_ERRORS
+}
+
 // attention(q, k_cache, v_cache, block_table, query_start, seq_len, max_new_len, max_seq_len, scale or None, window, k_scale,
-// v_scale, out or None, workspace or None, stream) -> status, or out if it was made here
+// v_scale (numbers or tensors), out or None, workspace or None, stream) -> status, or out if it was made here
 PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
   HANDLE_TH_ERRORS
   if (n != 15) return PyErr_Format(PyExc_TypeError, "attention takes 15 arguments");
@@ -243,10 +367,12 @@ PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
       Py_RETURN_NONE;
   }
   int64_t max_new, max_seq, window;
-  float scale = (float)(1.0 / std::sqrt((double)std::max<int64_t>(dim, 1))), ks, vs;
+  float scale = (float)(1.0 / std::sqrt((double)std::max<int64_t>(dim, 1))), ks = 1.0f, vs = 1.0f;
   void* stream;
+  const bool scaled = is_scales(args[10]) || is_scales(args[11]);
+  if (scaled && !are_scales(args[10], args[11], kc)) Py_RETURN_NONE;
   if (!get(args[6], max_new) || !get(args[7], max_seq) || (args[8] != Py_None && !get(args[8], scale)) || !get(args[9], window) ||
-      !get(args[10], ks) || !get(args[11], vs) || !get_stream(args[14], q, stream))
+      (!scaled && (!get(args[10], ks) || !get(args[11], vs))) || !get_stream(args[14], q, stream))
     return nullptr;
   uint64_t need = 0;
   if (args[13] == Py_None) {
@@ -261,11 +387,19 @@ PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
   }
   if (made) out = make({tokens, heads, dim}, q.scalar_type(), q);
   const OnDeviceOf on(q);
-  const int rc = attention_fn(q.data_ptr(), type_of(q), tokens, narrow(heads), narrow(kv_heads), narrow(dim), q.stride(0), q.stride(1),
-                              kc.data_ptr(), vc.data_ptr(), type_of(kc), kc.size(0), narrow(kc.size(2)), table.data_ptr(),
-                              narrow(table.size(1)), stride_of(table), start.data_ptr(), len.data_ptr(), narrow(seqs), max_new, max_seq,
-                              scale, narrow(window), ks, vs, out.data_ptr(), out.stride(0), out.stride(1),
-                              need ? space.data_ptr() : nullptr, need, stream);
+  int rc;
+  if (scaled)
+    rc = scaled_fn(q.data_ptr(), type_of(q), tokens, narrow(heads), narrow(kv_heads), narrow(dim), q.stride(0), q.stride(1), kc.data_ptr(),
+                   vc.data_ptr(), kc.size(0), narrow(kc.size(2)), table.data_ptr(), narrow(table.size(1)), stride_of(table),
+                   start.data_ptr(), len.data_ptr(), narrow(seqs), max_new, max_seq, scale, narrow(window),
+                   THPVariable_Unpack(args[10]).data_ptr(), THPVariable_Unpack(args[11]).data_ptr(), out.data_ptr(), out.stride(0),
+                   out.stride(1), need ? space.data_ptr() : nullptr, need, stream);
+  else
+    rc = attention_fn(q.data_ptr(), type_of(q), tokens, narrow(heads), narrow(kv_heads), narrow(dim), q.stride(0), q.stride(1),
+                      kc.data_ptr(), vc.data_ptr(), type_of(kc), kc.size(0), narrow(kc.size(2)), table.data_ptr(),
+                      narrow(table.size(1)), stride_of(table), start.data_ptr(), len.data_ptr(), narrow(seqs), max_new, max_seq,
+                      scale, narrow(window), ks, vs, out.data_ptr(), out.stride(0), out.stride(1),
+                      need ? space.data_ptr() : nullptr, need, stream);
   if (rc != 0 || !made) return PyLong_FromLong(rc);
   return THPVariable_Wrap(std::move(out));
   END_HANDLE_TH_ERRORS
@@ -274,6 +408,8 @@ PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
 PyMethodDef kMethods[] = {{"bind", (PyCFunction)(void (*)())bind, METH_FASTCALL, nullptr},
                           {"assign", (PyCFunction)(void (*)())assign, METH_FASTCALL, nullptr},
                           {"write", (PyCFunction)(void (*)())write, METH_FASTCALL, nullptr},
+                          {"rotate", (PyCFunction)(void (*)())rotate, METH_FASTCALL, nullptr},
+                          {"append", (PyCFunction)(void (*)())append, METH_FASTCALL, nullptr},
                           {"attention", (PyCFunction)(void (*)())attention, METH_FASTCALL, nullptr},
                           {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_kv_torch", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};

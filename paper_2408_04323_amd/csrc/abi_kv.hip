@@ -64,6 +64,80 @@ int check_attention_sizes(int64_t num_tokens, int num_heads, int num_kv_heads, i
   if (window < 0) return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: window must be >= 0");
   return SCOOT_OK;
 }
+
+int check_rotation(int head_dim, int rotary_dim, int interleaved, double magnitude) {
+  if (head_dim < 8 || head_dim > 1024 || head_dim % 8 != 0)
+    return fail_static(SCOOT_ERR_UNSUPPORTED, "kv rotation: head_dim must be a multiple of 8, at most 1024");
+  if (rotary_dim < 0 || rotary_dim > head_dim || rotary_dim % 2 != 0)
+    return fail_static(SCOOT_ERR_INVALID_ARG, "kv rotation: rotary_dim must be even, in 0..head_dim");
+  if (interleaved != 0 && interleaved != 1) return fail_static(SCOOT_ERR_INVALID_ARG, "kv rotation: interleaved must be 0 or 1");
+  if (!std::isfinite(magnitude)) return fail_static(SCOOT_ERR_INVALID_ARG, "kv rotation: magnitude must be finite");
+  return SCOOT_OK;
+}
+
+// scoot_kv_attention, and scoot_kv_attention_scaled with k_scales and v_scales.
+int attend(const void* q, scoot_kv_type type, int64_t num_tokens, int num_heads, int num_kv_heads, int head_dim,
+           int64_t q_token_stride, int64_t q_head_stride, const void* k_cache, const void* v_cache, scoot_kv_type cache_type,
+           int64_t num_blocks, int block_size, const int32_t* block_table, int max_blocks, int64_t table_stride,
+           const int32_t* query_start, const int32_t* seq_len, int num_seqs, int64_t max_new_len, int64_t max_seq_len, float scale,
+           int window, float k_scale, float v_scale, const float* k_scales, const float* v_scales, void* out,
+           int64_t out_token_stride, int64_t out_head_stride, void* workspace, uint64_t workspace_bytes, void* stream) {
+  clear_error();
+  int rc = check_cache(type, cache_type, num_kv_heads, num_blocks, block_size, k_scale, v_scale);
+  if (rc == SCOOT_OK)
+    rc = check_attention_sizes(num_tokens, num_heads, num_kv_heads, head_dim, num_seqs, max_new_len, max_seq_len, window);
+  if (rc != SCOOT_OK) return rc;
+  if (!std::isfinite(scale) || scale < 0.0f)
+    return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: scale must be finite and not negative");
+  const float score_scale = scale * k_scale * 1.44269504088896340736f;  // log2(e): weights are powers of two
+  if (!std::isfinite(score_scale))
+    return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: scale * k_scale is too large");
+  if (max_blocks < 0 || max_blocks > (int)(kMaxKeys / block_size) || table_stride < max_blocks || !stride_ok(table_stride))
+    return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: max_blocks or table_stride out of range");
+  if (!stride_ok(q_token_stride) || !stride_ok(q_head_stride) || !stride_ok(out_token_stride) || !stride_ok(out_head_stride))
+    return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: stride out of range");
+  if (num_tokens == 0 || num_seqs == 0) return SCOOT_OK;
+  if (!q || !out || !query_start || !seq_len || (max_blocks > 0 && !block_table) || (num_blocks > 0 && (!k_cache || !v_cache)))
+    return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: null pointer");
+  if (!aligned16(q) || !aligned16(out) || !aligned16(k_cache) || !aligned16(v_cache) ||
+      ((q_token_stride | q_head_stride | out_token_stride | out_head_stride) & 7))
+    return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: q, out and the cache must be 16-byte aligned, rows included");
+  const uint64_t need =
+      kv_attention_workspace_bytes(num_tokens, num_heads, num_kv_heads, head_dim, num_seqs, max_new_len, max_seq_len, window);
+  if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
+    return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: workspace missing, too small or not 16-byte aligned");
+  KvAttnArgs a{};
+  a.q = q;
+  a.out = out;
+  a.k_cache = k_cache;
+  a.v_cache = v_cache;
+  a.block_table = block_table;
+  a.query_start = query_start;
+  a.seq_len = seq_len;
+  a.q_token_stride = q_token_stride;
+  a.q_head_stride = q_head_stride;
+  a.out_token_stride = out_token_stride;
+  a.out_head_stride = out_head_stride;
+  a.table_stride = table_stride;
+  a.num_tokens = num_tokens;
+  a.num_blocks = num_blocks;
+  a.max_new_len = max_new_len;
+  a.max_seq_len = max_seq_len;
+  a.num_heads = num_heads;
+  a.num_kv_heads = num_kv_heads;
+  a.head_dim = head_dim;
+  a.num_seqs = num_seqs;
+  a.max_blocks = num_blocks > 0 ? max_blocks : 0;  // a cache without blocks holds no tokens
+  a.block_shift = shift_of(block_size);
+  a.window = window;
+  // The smallest positive float in the place of 0: it leaves nothing of a score, and -inf stays -inf.
+  a.score_scale = std::max(score_scale, 1.4e-45f);
+  a.v_scale = v_scale;
+  a.k_scales = k_scales;
+  a.v_scales = v_scales;
+  a.workspace = workspace;
+  return guarded([&] { return launch_kv_attention(a, type, cache_type, stream); });
+}
 }  // namespace
 
 extern "C" {
@@ -151,6 +225,107 @@ int scoot_kv_attention_workspace(int64_t num_tokens, int num_heads, int num_kv_h
   return SCOOT_OK;
 }
 
+int scoot_rotate(const void* x, scoot_kv_type type, int64_t num_tokens, int num_heads, int head_dim, int64_t x_token_stride,
+                 int64_t x_head_stride, const int32_t* positions, const double* freqs, int rotary_dim, int interleaved,
+                 double magnitude, int reverse, void* out, int64_t out_token_stride, int64_t out_head_stride, void* stream) {
+  clear_error();
+  if (!vector_type(type)) return fail_static(SCOOT_ERR_INVALID_ARG, "rotate: type must be F16 or BF16");
+  if (num_heads < 1 || num_heads > kMaxHeads) return fail_static(SCOOT_ERR_INVALID_ARG, "rotate: num_heads must be in 1..1024");
+  int rc = check_rotation(head_dim, rotary_dim, interleaved, magnitude);
+  if (rc != SCOOT_OK) return rc;
+  if (num_tokens < 0 || num_tokens > kMaxTokens) return fail_static(SCOOT_ERR_INVALID_ARG, "rotate: num_tokens out of range");
+  if (!stride_ok(x_token_stride) || !stride_ok(x_head_stride) || !stride_ok(out_token_stride) || !stride_ok(out_head_stride))
+    return fail_static(SCOOT_ERR_INVALID_ARG, "rotate: stride out of range");
+  if (num_tokens == 0) return SCOOT_OK;
+  if (!x || !out || (rotary_dim > 0 && (!positions || !freqs))) return fail_static(SCOOT_ERR_INVALID_ARG, "rotate: null pointer");
+  if ((((uintptr_t)x | (uintptr_t)out) & 1) || ((uintptr_t)freqs & 7) || ((uintptr_t)positions & 3))
+    return fail_static(SCOOT_ERR_INVALID_ARG, "rotate: arrays not aligned to their elements");
+  KvAppendArgs a{};
+  a.q = x;
+  a.out = out;
+  a.positions = positions;
+  a.freqs = freqs;
+  a.magnitude = magnitude;
+  a.q_token_stride = x_token_stride;
+  a.q_head_stride = x_head_stride;
+  a.out_token_stride = out_token_stride;
+  a.out_head_stride = out_head_stride;
+  a.num_tokens = num_tokens;
+  a.num_heads = num_heads;
+  a.head_dim = head_dim;
+  a.turned = rotary_dim;
+  a.interleaved = interleaved != 0;
+  a.reverse = reverse != 0;
+  return guarded([&] { return launch_kv_append(a, type, type, stream); });
+}
+
+int scoot_kv_append(const void* q, int num_heads, int64_t q_token_stride, int64_t q_head_stride, void* q_out,
+                    int64_t q_out_token_stride, int64_t q_out_head_stride, const void* k, const void* v, scoot_kv_type type,
+                    int64_t num_tokens, int num_kv_heads, int head_dim, int64_t k_token_stride, int64_t k_head_stride,
+                    int64_t v_token_stride, int64_t v_head_stride, const int32_t* positions, const int64_t* slots,
+                    const double* freqs, int rotary_dim, int interleaved, double magnitude, void* k_cache, void* v_cache,
+                    scoot_kv_type cache_type, int64_t num_blocks, int block_size, float k_scale, float v_scale,
+                    float* k_scales, float* v_scales, void* stream) {
+  clear_error();
+  int rc = check_cache(type, cache_type, num_kv_heads, num_blocks, block_size, k_scale, v_scale);
+  if (rc == SCOOT_OK) rc = check_rotation(head_dim, rotary_dim, interleaved, magnitude);
+  if (rc != SCOOT_OK) return rc;
+  if (num_heads < 0 || num_heads > kMaxHeads) return fail_static(SCOOT_ERR_INVALID_ARG, "kv append: num_heads must be in 0..1024");
+  if (num_heads > 0 && rotary_dim == 0) return fail_static(SCOOT_ERR_INVALID_ARG, "kv append: queries need a rotation");
+  if (num_tokens < 0 || num_tokens > kMaxTokens) return fail_static(SCOOT_ERR_INVALID_ARG, "kv append: num_tokens out of range");
+  if (!stride_ok(q_token_stride) || !stride_ok(q_head_stride) || !stride_ok(q_out_token_stride) || !stride_ok(q_out_head_stride) ||
+      !stride_ok(k_token_stride) || !stride_ok(k_head_stride) || !stride_ok(v_token_stride) || !stride_ok(v_head_stride))
+    return fail_static(SCOOT_ERR_INVALID_ARG, "kv append: stride out of range");
+  if ((k_scales == nullptr) != (v_scales == nullptr))
+    return fail_static(SCOOT_ERR_INVALID_ARG, "kv append: k_scales and v_scales go together");
+  if (k_scales && (cache_type != SCOOT_KV_F8 || k_scale != 1.0f || v_scale != 1.0f))
+    return fail_static(SCOOT_ERR_INVALID_ARG, "kv append: scales of blocks need an 8-bit cache and no other scale");
+  if (k_scales && k_scales == v_scales) return fail_static(SCOOT_ERR_INVALID_ARG, "kv append: k_scales and v_scales must differ");
+  if (num_tokens == 0) return SCOOT_OK;
+  const bool stores = num_blocks > 0;  // a cache without blocks holds no tokens
+  if (!stores && num_heads == 0) return SCOOT_OK;
+  if (!k || !v || !slots || (stores && (!k_cache || !v_cache)) || (num_heads > 0 && (!q || !q_out)) ||
+      (rotary_dim > 0 && (!positions || !freqs)))
+    return fail_static(SCOOT_ERR_INVALID_ARG, "kv append: null pointer");
+  if ((((uintptr_t)k | (uintptr_t)v | (uintptr_t)q | (uintptr_t)q_out) & 1) || ((uintptr_t)freqs & 7) ||
+      (((uintptr_t)positions | (uintptr_t)k_scales | (uintptr_t)v_scales) & 3) || ((uintptr_t)slots & 7))
+    return fail_static(SCOOT_ERR_INVALID_ARG, "kv append: arrays not aligned to their elements");
+  if (!aligned16(k_cache) || !aligned16(v_cache))
+    return fail_static(SCOOT_ERR_INVALID_ARG, "kv append: the cache must be 16-byte aligned");
+  KvAppendArgs a{};
+  a.q = q;
+  a.out = q_out;
+  a.q_token_stride = q_token_stride;
+  a.q_head_stride = q_head_stride;
+  a.out_token_stride = q_out_token_stride;
+  a.out_head_stride = q_out_head_stride;
+  a.src[0] = k;
+  a.src[1] = v;
+  a.cache[0] = k_cache;
+  a.cache[1] = v_cache;
+  a.scales[0] = k_scales;
+  a.scales[1] = v_scales;
+  a.slots = slots;
+  a.positions = positions;
+  a.freqs = freqs;
+  a.magnitude = magnitude;
+  a.token_stride[0] = k_token_stride;
+  a.token_stride[1] = v_token_stride;
+  a.head_stride[0] = k_head_stride;
+  a.head_stride[1] = v_head_stride;
+  a.num_tokens = num_tokens;
+  a.num_slots = num_blocks * block_size;
+  a.scale[0] = k_scale;
+  a.scale[1] = v_scale;
+  a.num_heads = num_heads;
+  a.num_kv_heads = num_kv_heads;
+  a.head_dim = head_dim;
+  a.turned = rotary_dim;
+  a.block_shift = shift_of(block_size);
+  a.interleaved = interleaved != 0;
+  return guarded([&] { return launch_kv_append(a, type, cache_type, stream); });
+}
+
 int scoot_kv_attention(const void* q, scoot_kv_type type, int64_t num_tokens, int num_heads, int num_kv_heads,
                        int head_dim, int64_t q_token_stride, int64_t q_head_stride, const void* k_cache,
                        const void* v_cache, scoot_kv_type cache_type, int64_t num_blocks, int block_size,
@@ -158,59 +333,31 @@ int scoot_kv_attention(const void* q, scoot_kv_type type, int64_t num_tokens, in
                        const int32_t* seq_len, int num_seqs, int64_t max_new_len, int64_t max_seq_len, float scale,
                        int window, float k_scale, float v_scale, void* out, int64_t out_token_stride,
                        int64_t out_head_stride, void* workspace, uint64_t workspace_bytes, void* stream) {
-  clear_error();
-  int rc = check_cache(type, cache_type, num_kv_heads, num_blocks, block_size, k_scale, v_scale);
-  if (rc == SCOOT_OK)
-    rc = check_attention_sizes(num_tokens, num_heads, num_kv_heads, head_dim, num_seqs, max_new_len, max_seq_len, window);
-  if (rc != SCOOT_OK) return rc;
-  if (!std::isfinite(scale) || scale < 0.0f)
-    return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: scale must be finite and not negative");
-  const float score_scale = scale * k_scale * 1.44269504088896340736f;  // log2(e): weights are powers of two
-  if (!std::isfinite(score_scale))
-    return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: scale * k_scale is too large");
-  if (max_blocks < 0 || max_blocks > (int)(kMaxKeys / block_size) || table_stride < max_blocks || !stride_ok(table_stride))
-    return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: max_blocks or table_stride out of range");
-  if (!stride_ok(q_token_stride) || !stride_ok(q_head_stride) || !stride_ok(out_token_stride) || !stride_ok(out_head_stride))
-    return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: stride out of range");
-  if (num_tokens == 0 || num_seqs == 0) return SCOOT_OK;
-  if (!q || !out || !query_start || !seq_len || (max_blocks > 0 && !block_table) || (num_blocks > 0 && (!k_cache || !v_cache)))
-    return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: null pointer");
-  if (!aligned16(q) || !aligned16(out) || !aligned16(k_cache) || !aligned16(v_cache) ||
-      ((q_token_stride | q_head_stride | out_token_stride | out_head_stride) & 7))
-    return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: q, out and the cache must be 16-byte aligned, rows included");
-  const uint64_t need =
-      kv_attention_workspace_bytes(num_tokens, num_heads, num_kv_heads, head_dim, num_seqs, max_new_len, max_seq_len, window);
-  if (need > 0 && (!workspace || workspace_bytes < need || !aligned16(workspace)))
-    return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: workspace missing, too small or not 16-byte aligned");
-  KvAttnArgs a{};
-  a.q = q;
-  a.out = out;
-  a.k_cache = k_cache;
-  a.v_cache = v_cache;
-  a.block_table = block_table;
-  a.query_start = query_start;
-  a.seq_len = seq_len;
-  a.q_token_stride = q_token_stride;
-  a.q_head_stride = q_head_stride;
-  a.out_token_stride = out_token_stride;
-  a.out_head_stride = out_head_stride;
-  a.table_stride = table_stride;
-  a.num_tokens = num_tokens;
-  a.num_blocks = num_blocks;
-  a.max_new_len = max_new_len;
-  a.max_seq_len = max_seq_len;
-  a.num_heads = num_heads;
-  a.num_kv_heads = num_kv_heads;
-  a.head_dim = head_dim;
-  a.num_seqs = num_seqs;
-  a.max_blocks = num_blocks > 0 ? max_blocks : 0;  // a cache without blocks holds no tokens
-  a.block_shift = shift_of(block_size);
-  a.window = window;
-  // The smallest positive float in the place of 0: it leaves nothing of a score, and -inf stays -inf.
-  a.score_scale = std::max(score_scale, 1.4e-45f);
-  a.v_scale = v_scale;
-  a.workspace = workspace;
-  return guarded([&] { return launch_kv_attention(a, type, cache_type, stream); });
+  return attend(q, type, num_tokens, num_heads, num_kv_heads, head_dim, q_token_stride, q_head_stride, k_cache, v_cache,
+                cache_type, num_blocks, block_size, block_table, max_blocks, table_stride, query_start, seq_len, num_seqs,
+                max_new_len, max_seq_len, scale, window, k_scale, v_scale, nullptr, nullptr, out, out_token_stride,
+                out_head_stride, workspace, workspace_bytes, stream);
+}
+
+int scoot_kv_attention_scaled(const void* q, scoot_kv_type type, int64_t num_tokens, int num_heads, int num_kv_heads,
+                              int head_dim, int64_t q_token_stride, int64_t q_head_stride, const void* k_cache,
+                              const void* v_cache, int64_t num_blocks, int block_size, const int32_t* block_table,
+                              int max_blocks, int64_t table_stride, const int32_t* query_start, const int32_t* seq_len,
+                              int num_seqs, int64_t max_new_len, int64_t max_seq_len, float scale, int window,
+                              const float* k_scales, const float* v_scales, void* out, int64_t out_token_stride,
+                              int64_t out_head_stride, void* workspace, uint64_t workspace_bytes, void* stream) {
+  if (num_blocks > 0 && num_tokens > 0 && num_seqs > 0 && (!k_scales || !v_scales)) {
+    clear_error();
+    return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: null scales");
+  }
+  if (((uintptr_t)k_scales | (uintptr_t)v_scales) & 3) {
+    clear_error();
+    return fail_static(SCOOT_ERR_INVALID_ARG, "kv attention: scales not aligned to their elements");
+  }
+  return attend(q, type, num_tokens, num_heads, num_kv_heads, head_dim, q_token_stride, q_head_stride, k_cache, v_cache,
+                SCOOT_KV_F8, num_blocks, block_size, block_table, max_blocks, table_stride, query_start, seq_len, num_seqs,
+                max_new_len, max_seq_len, scale, window, 1.0f, 1.0f, k_scales, v_scales, out, out_token_stride,
+                out_head_stride, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"

@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include "kv.h"
+#include "kv_vec.h"
 
 namespace scoot {
 namespace {
@@ -201,25 +202,6 @@ __global__ __launch_bounds__(THREADS) void kv_assign_kernel(KvAssignArgs a, uint
 // whole lines and writes 512 bytes (8-bit) or a KiB without a gap.  Bytes
 // bound this: both sides once; 45,993 tokens into 8 bits take 18.6 us (4.8 TB/s,
 // a large copy's rate).
-typedef _Float16 h8 __attribute__((ext_vector_type(8)));
-typedef __bf16 b8 __attribute__((ext_vector_type(8)));
-template <typename T>
-struct Vec8;
-template <>
-struct Vec8<_Float16> {
-  typedef h8 type;
-};
-template <>
-struct Vec8<__bf16> {
-  typedef b8 type;
-};
-
-// Nearest 8-bit float (e4m3) of x / scale, limited to the largest finite one; NaN stays NaN.
-__device__ __forceinline__ float limit_f8(float x, float scale) {
-  x /= scale;
-  return x > 448.0f ? 448.0f : x < -448.0f ? -448.0f : x;
-}
-
 constexpr int kWriteThreads = 256;  // at most: (elements of a head / 8) x tokens
 
 template <typename T, bool F8, bool ALIGNED>
@@ -245,26 +227,14 @@ __global__ __launch_bounds__(kWriteThreads) void kv_write_kernel(KvWriteArgs a) 
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     if (F8) {
-      int w[2];
+      float f[8];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        float f[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) f[k] = limit_f8((float)x[s][4 * j + k], a.scale[s]);
-        w[j] = __builtin_amdgcn_cvt_pk_fp8_f32(f[0], f[1], 0, false);
-        w[j] = __builtin_amdgcn_cvt_pk_fp8_f32(f[2], f[3], w[j], true);
-      }
-      *(int2*)((uint8_t*)a.cache[s] + to) = make_int2(w[0], w[1]);
+      for (int j = 0; j < 8; ++j) f[j] = limit_f8((float)x[s][j], a.scale[s]);
+      *(int2*)((uint8_t*)a.cache[s] + to) = to_f8(f);
     } else {
       *(typename Vec8<T>::type*)((T*)a.cache[s] + to) = x[s];
     }
   }
-}
-
-int launched(const char* what) {
-  const hipError_t err = hipGetLastError();
-  if (err != hipSuccess) return fail(SCOOT_ERR_DEVICE, std::string(what) + ": " + hipGetErrorString(err));
-  return SCOOT_OK;
 }
 
 template <typename T, bool F8>

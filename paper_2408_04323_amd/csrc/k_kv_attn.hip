@@ -3,7 +3,7 @@
 
 namespace scoot {
 namespace kvattn {
-// Instantiated in k_kv_attn_<dim>.hip.
+// Instantiated in k_kv_attn_<dim>.hip and k_kv_attn_scaled_<dim>.hip.
 template <>
 int launch_dim<64>(const KvAttnArgs&, const Plan&, scoot_kv_type, bool, float*, float*, hipStream_t);
 template <>
@@ -12,6 +12,14 @@ template <>
 int launch_dim<192>(const KvAttnArgs&, const Plan&, scoot_kv_type, bool, float*, float*, hipStream_t);
 template <>
 int launch_dim<256>(const KvAttnArgs&, const Plan&, scoot_kv_type, bool, float*, float*, hipStream_t);
+template <>
+int launch_scaled<64>(const KvAttnArgs&, const Plan&, scoot_kv_type, float*, float*, hipStream_t);
+template <>
+int launch_scaled<128>(const KvAttnArgs&, const Plan&, scoot_kv_type, float*, float*, hipStream_t);
+template <>
+int launch_scaled<192>(const KvAttnArgs&, const Plan&, scoot_kv_type, float*, float*, hipStream_t);
+template <>
+int launch_scaled<256>(const KvAttnArgs&, const Plan&, scoot_kv_type, float*, float*, hipStream_t);
 }  // namespace kvattn
 namespace {
 using namespace kvattn;
@@ -42,6 +50,14 @@ int launch_kv_attention(const KvAttnArgs& a, scoot_kv_type type, scoot_kv_type c
   float* stats = parts + slots(p, a.num_kv_heads) * a.head_dim;
   const hipStream_t s = (hipStream_t)stream;
   const bool f8 = cache_type == SCOOT_KV_F8;
+  if (a.k_scales) {
+    switch (a.head_dim) {
+      case 64: return launch_scaled<64>(a, p, type, parts, stats, s);
+      case 128: return launch_scaled<128>(a, p, type, parts, stats, s);
+      case 192: return launch_scaled<192>(a, p, type, parts, stats, s);
+      default: return launch_scaled<256>(a, p, type, parts, stats, s);
+    }
+  }
   switch (a.head_dim) {
     case 64: return launch_dim<64>(a, p, type, f8, parts, stats, s);
     case 128: return launch_dim<128>(a, p, type, f8, parts, stats, s);

@@ -1,0 +1,4 @@
+// Attention over the block cache with scales of blocks and heads, for heads of 64 dimensions.
+#include "kv_attn.h"
+
+SCOOT_KV_ATTN_SCALED_DIM(64)

@@ -1,5 +1,6 @@
 // Attention over the block cache: the kernels and their launches, for one head
-// dimension per translation unit (k_kv_attn_<dim>.hip).  kv_plan.h says how a
+// dimension per translation unit (k_kv_attn_<dim>.hip and, with scales of
+// blocks, k_kv_attn_scaled_<dim>.hip).  kv_plan.h says how a
 // call is split, k_kv_attn.hip takes it to its head dimension.
 //
 // Mathematics.  A row is one query of one head; the G query heads that share a
@@ -34,6 +35,17 @@
 // their 16-byte pieces permuted on the way so that both kinds of reads spread
 // over the banks.
 //
+// Scales of blocks and heads (8-bit caches).  Eight keys of a lane lie in one
+// block, so its scale a of the keys takes the place of the one scale in their
+// exponents.  The scale b of the values is 2^e f, 1 <= f < 2: the values are
+// widened to half precision times 2^(e - r), which the conversion does by the
+// way, with r the largest e so far; f goes to the weights before they are
+// rounded, and l adds the rounded weights over f.  So m, the weights and l are
+// those of one scale, whatever the scores; values lose nothing down to scales of
+// 2^-15 of the largest, and 2^-34 of the largest value below that.  A weight
+// costs one product more.  The scales of 64 strips at a time are fetched with
+// their addresses and wait in LDS.
+//
 // Registers decide the waves per SIMD: three for tiles of 64 dimensions, two for
 // 128, one for 192 and 256, where o and q take 144 and 192 of a lane's 512.  A
 // wave alone keeps both units busy by itself: the weights of 32 keys are made
@@ -59,6 +71,7 @@ typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 typedef float f16v __attribute__((ext_vector_type(16)));
+typedef float f2 __attribute__((ext_vector_type(2)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef int i4 __attribute__((ext_vector_type(4)));
 typedef int i2 __attribute__((ext_vector_type(2)));
@@ -74,15 +87,19 @@ constexpr float kMost = 16384.0f;            // m moves once a lane's weights of
 constexpr float kBelow = 6.0f;               // to this much below their largest: half precision holds 64 as well as 1, and
                                              // weights down to 2^-30 of the largest, which counts where many keys are small
 
+constexpr int kStripScales = 64;          // bytes of the scales of a tile's strip,
+constexpr int kWaveScales = 64 * 4 * 8;   // and of a wave's 64 strips
+
 constexpr float kLimit = 14.0f;              // of a weight's exponent where it moved: no other weight is above kMost
 
 constexpr int gcd256(int x) { return x % 256 == 0 ? 256 : x % 128 == 0 ? 128 : 64; }
 
 // Sizes of a cache row in LDS.
-template <typename T_, bool F8_, int D_>
+template <typename T_, bool F8_, int D_, bool SCALED_ = false>
 struct Shape {
   typedef T_ T;
   static constexpr bool F8 = F8_;
+  static constexpr bool SCALED = SCALED_;           // blocks have scales
   static constexpr int D = D_;
   static constexpr int EB = F8 ? 1 : 2;
   static constexpr int RB = D * EB;                 // bytes of a row
@@ -183,6 +200,7 @@ struct Item {
   int row0;         // first row of the tile
   int len;          // cached tokens that have table entries
   int k0, k1;       // keys of this workgroup; k0 is a multiple of 32
+  int seen;         // first key that any row of the tile sees
   int splits;       // parts that the tile's keys are in
   int split;
   int seq;
@@ -253,8 +271,8 @@ __device__ __forceinline__ bool find_item(const KvAttnArgs& a, const Plan& p, in
   // The tile's keys, and this split's part of them.
   const int64_t top = it.pos0 + last_row / G;
   const int end = (int)clamp64(top + 1, 0, it.len);
-  int begin = 0;
-  if (a.window > 0) begin = (int)clamp64(it.pos0 + it.row0 / G - a.window + 1, 0, end) & ~31;
+  it.seen = a.window > 0 ? (int)clamp64(it.pos0 + it.row0 / G - a.window + 1, 0, end) : 0;
+  const int begin = it.seen & ~31;
   const int parts = end > begin ? (int)(((int64_t)end - begin + p.part - 1) / p.part) : 1;
   it.splits = parts < splits ? parts : splits;
   it.split = split;
@@ -263,6 +281,17 @@ __device__ __forceinline__ bool find_item(const KvAttnArgs& a, const Plan& p, in
   it.k1 = split == it.splits - 1 ? end : it.k0 + p.part;
   return true;
 }
+
+// A scale b = 2^e f of values at the reference r, 2^(e - r) f (r with the bias of a float), and its two parts.
+__device__ __forceinline__ float referred(float b, int r) {
+  const uint32_t x = __float_as_uint(b);
+  return __uint_as_float((uint32_t)max((int)(x >> 23) - r + 127, 1) << 23 | (x & 0x7fffffu));
+}
+__device__ __forceinline__ float fraction(float b) { return __uint_as_float((__float_as_uint(b) & 0x7fffffu) | 0x3f800000u); }
+__device__ __forceinline__ float power(float b) { return __uint_as_float(__float_as_uint(b) & 0x7f800000u); }
+// What a sum at the reference r is multiplied by for one at 2^0, and for one at a larger reference.
+__device__ __forceinline__ float power_of(int r) { return __uint_as_float((uint32_t)r << 23); }
+__device__ __forceinline__ float to_reference(int r, int larger) { return __uint_as_float((uint32_t)max(127 + r - larger, 0) << 23); }
 
 // Blocks of the cache, as scalars.
 template <typename S>
@@ -273,6 +302,10 @@ struct Cache {
   uint32_t block_bytes;  // of all heads; at most 1024 heads of 256 keys of 512 bytes
   uint32_t num_blocks;
   int shift, last;       // last entry of the row
+  const float* k_scales;  // of the head, num_kv_heads apart
+  const float* v_scales;
+  uint32_t heads;
+  float score_scale;
 
   __device__ __forceinline__ void setup(const KvAttnArgs& a, int seq, int head) {
     entries = a.block_table + (int64_t)seq * a.table_stride;
@@ -284,6 +317,19 @@ struct Cache {
     num_blocks = (uint32_t)a.num_blocks;
     shift = a.block_shift;
     last = a.max_blocks - 1;
+    if constexpr (S::SCALED) {
+      k_scales = a.k_scales + head;
+      v_scales = a.v_scales + head;
+      heads = (uint32_t)a.num_kv_heads;
+      score_scale = a.score_scale;
+    }
+  }
+  // What the scores of a block are multiplied by, and its values.  Of a block that no row sees, which may hold anything:
+  // numbers that keep 0 * inf out of what is masked, and do not count for the largest.  No memory's content gives others.
+  __device__ __forceinline__ f2 scales(float k, float v, bool seen) const {
+    const f2 r = {seen ? __builtin_fminf(__builtin_fmaxf(score_scale * k, 1.4e-45f), 3.4e38f) : 1.0f,
+                  seen && v > 0.0f && v < INFINITY ? v : 0x1p-126f};
+    return r;
   }
   // The entry of eight keys from `key` on (inside one block), for at().
   __device__ __forceinline__ uint32_t entry(int key) const {
@@ -315,6 +361,9 @@ struct Ahead {
   uint64_t from;  // keys or values
   int key0, stride, strips, base, end;
   bool holes;     // some group below key `end` of the 64 strips has no block
+  float ks[S::SCALED ? N : 1], vs[S::SCALED ? N : 1];
+  int seen;       // first key that counts
+  int there;      // which groups of the lane's strip have a block
 
   __device__ __forceinline__ void fill(const Cache<S>& c, int strip) {
     base = strip;
@@ -334,11 +383,39 @@ struct Ahead {
       const uint64_t at = from + c.at(key + 8 * j, e[j]);
       lo[j] = (uint32_t)at;
       hi[j] = (uint32_t)(at >> 32);
+      if constexpr (S::SCALED) {
+        const bool real = e[j] < c.num_blocks;
+        const int64_t of = (int64_t)(real ? e[j] : 0) * c.heads;
+        there = (j ? there : 0) | (int)real << j;
+        ks[j] = c.k_scales[of];
+        vs[j] = c.v_scales[of];
+      }
     }
     holes = __builtin_amdgcn_ballot_w64(hole) != 0;
   }
-  __device__ __forceinline__ void start(const Cache<S>& c, uint64_t cache, int first, int keys, int n, int last) {
+  // The scales that fill() fetched: put(strip of 64, group, scales); refer(the largest exponent of the values' scales) goes
+  // before, for the reference that they are put at.
+  template <typename F, typename G>
+  __device__ __forceinline__ void scales(const Cache<S>& c, F refer, G put) const {
+    const int lane = threadIdx.x & 63, strip = base + lane;
+    f2 x[N];
+    int top = 0;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const int key = key0 + strip * stride + 8 * j;
+      x[j] = c.scales(ks[j], vs[j], strip < strips && key < end && key + 8 > seen && there >> j & 1);
+      top = max(top, (int)(__float_as_uint(x[j][1]) >> 23));
+    }
+    const int r = refer(top);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      x[j][1] = referred(x[j][1], r);
+      put(lane, j, x[j]);
+    }
+  }
+  __device__ __forceinline__ void start(const Cache<S>& c, uint64_t cache, int first, int keys, int n, int last, int from_key) {
     from = cache;
+    seen = from_key;
     key0 = first;
     stride = keys;
     strips = n;
@@ -347,8 +424,15 @@ struct Ahead {
     if (n > 0) fill(c, 0);
   }
   // The groups of a strip, which follows the last one asked for.
-  __device__ __forceinline__ void get(const Cache<S>& c, int strip, uint64_t (&b)[N]) {
-    if (strip - base == 64) fill(c, strip);
+  template <typename F>
+  __device__ __forceinline__ void get(const Cache<S>& c, int strip, uint64_t (&b)[N], F refilled) {
+    if (strip - base == 64) {
+      fill(c, strip);
+      if constexpr (S::SCALED) {
+        settle();
+        refilled();
+      }
+    }
 #pragma unroll
     for (int j = 0; j < N; ++j)
       b[j] = (uint32_t)__builtin_amdgcn_readlane((int)lo[j], strip - base) |
@@ -378,18 +462,36 @@ __device__ __forceinline__ bool any_holes(const KvAttnArgs& a, const Item& it, i
   return any_wave<W>(__builtin_amdgcn_ballot_w64(h) != 0, flag);
 }
 
-// Eight 8-bit floats as 16-bit ones (exact).
+// The largest exponent of the values' scales of a tile's keys.
+__device__ __forceinline__ int largest_exponent(const KvAttnArgs& a, const Item& it, int head, int* flag) {
+  const int32_t* t = a.block_table + (int64_t)it.seq * a.table_stride;
+  int top = 1;
+  const int from = it.k0 > it.seen ? it.k0 : it.seen;
+  for (int64_t e = (from >> a.block_shift) + threadIdx.x; (e << a.block_shift) < it.k1; e += kThreads) {
+    const uint32_t block = (uint32_t)t[e];
+    const float v = block < (uint32_t)a.num_blocks ? a.v_scales[(int64_t)block * a.num_kv_heads + head] : 0.0f;
+    top = max(top, v > 0.0f && v < INFINITY ? (int)(__float_as_uint(v) >> 23) : 1);
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) top = max(top, __shfl_xor(top, o));
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) flag[threadIdx.x >> 6] = top;
+  __syncthreads();
+  return uniform(max(max(flag[0], flag[1]), max(flag[2], flag[3])));
+}
+
+// Eight 8-bit floats as 16-bit ones, exact, times a power of two.
 template <typename R>
-__device__ __forceinline__ typename Vec<R>::v8 widen(int a, int b) {
+__device__ __forceinline__ typename Vec<R>::v8 widen(int a, int b, float by = 1.0f) {
   typename Vec<R>::v8 r;
   if constexpr (std::is_same<R, _Float16>::value) {
-    const h2 x[4] = {__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, 1.0f, true),
-                     __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, 1.0f, true)};
+    const h2 x[4] = {__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, by, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(a, by, true),
+                     __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, by, false), __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(b, by, true)};
 #pragma unroll
     for (int i = 0; i < 8; ++i) r[i] = x[i / 2][i % 2];
   } else {
-    const b2 x[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true),
-                     __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true)};
+    const b2 x[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, by, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, by, true),
+                     __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, by, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, by, true)};
 #pragma unroll
     for (int i = 0; i < 8; ++i) r[i] = x[i / 2][i % 2];
   }
@@ -418,14 +520,14 @@ __device__ __forceinline__ float below(float s, float scale) {
 // Not above the limit; NaN stays.
 __device__ __forceinline__ float limited(float x, float limit) { return __builtin_elementwise_minimum(x, limit); }
 
-// Eight weights 2^(scale s - m), rounded, and their sum added to l.
-template <typename W, bool LIMITED, typename F>
-__device__ __forceinline__ typename Vec<W>::v8 eight_weights(F score, float scale, float m, float limit, float& l) {
+// Eight weights 2^(scale s - m) (SCALED: times f), rounded, and their sum added to l.
+template <typename W, bool LIMITED, bool SCALED, typename F>
+__device__ __forceinline__ typename Vec<W>::v8 eight_weights(F score, float scale, float m, float limit, float f, float& l) {
   typename Vec<W>::v8 r;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float x = fmaf(score(i), scale, -m);
-    r[i] = (W)__builtin_amdgcn_exp2f(LIMITED ? limited(x, limit) : x);
+    const float x = fmaf(score(i), scale, -m), w = __builtin_amdgcn_exp2f(LIMITED ? limited(x, limit) : x);
+    r[i] = (W)(SCALED ? w * f : w);
   }
 #pragma unroll
   for (int i = 0; i < 8; i += 2) l = add_pair<W>(r, i, l);
@@ -606,6 +708,7 @@ struct Tile32 {
   T8 q[KS];
   f16v o[DT];
   float m, l;
+  int ref;  // o is at 2^-ref (with a float's bias); the same in all lanes
   // LDS offsets of this lane's reads; with few registers the first ones, of which the others differ by some bits.
   static constexpr bool kFewRegs = S::D == 256;
   static constexpr int KN = kFewRegs ? 1 : Order::KM / 2, VM = kFewRegs ? 1 : VN;
@@ -704,12 +807,13 @@ struct Tile32 {
     for (int n = 0; n < VN; ++n) r.at[n] = pinned(lds + (kFewRegs ? here(voff[0]) ^ n * 16 * Order::U : voff[n % VM]));
     return r;
   }
-  // V^T: lane's element d = 32 dt + lane % 32 of the keys 16 ks + 8 half .. + 7.
-  __device__ __forceinline__ W8 values(const Lds& v, int ks, int dt) const {
+  // V^T: lane's element d = 32 dt + lane % 32 of the keys 16 ks + 8 half .. + 7, times powers of two if there are any.
+  template <typename... By>
+  __device__ __forceinline__ W8 values(const Lds& v, int ks, int dt, By... by) const {
     const uint32_t at = v.at[dt % VN] + (dt / VN) * (VN * 16 * Order::U) + ks * 16 * S::RB;
     if constexpr (S::F8) {
       const i2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((SCOOT_LDS i2*)at);
-      return widen<_Float16>(v[0], v[1]);
+      return widen<_Float16>(v[0], v[1], by...);
     } else {
       union {
         s4 h[2];
@@ -740,28 +844,51 @@ struct Tile32 {
   // row alone.  weigh() is the i-th of n parts of the work, moderate() its end.
   struct Weights {
     W8 w[2];
-    float add;
+    float add[S::SCALED ? 2 : 1];  // of each block's keys, or of all
+    __device__ __forceinline__ float all() const { return S::SCALED ? add[0] + add[S::SCALED] : add[0]; }
   };
+  // What the scores of 32 keys are multiplied by: one number, or that and the values' scale of a lane's two blocks.
+  typedef typename std::conditional<S::SCALED, f4, float>::type Scale;
   template <bool LIMITED = false>
-  __device__ __forceinline__ void weigh(const f16v& s, float scale, Weights& x, int i, int n, float limit = 0.0f) const {
+  __device__ __forceinline__ void weigh(const f16v& s, Scale scale, Weights& x, int i, int n, float limit = 0.0f) const {
     const int from = 2 * (8 * i / n), to = 2 * (8 * (i + 1) / n);
-    if (i == 0) x.add = 0.0f;
+    if constexpr (S::SCALED) {
+      if (i == 0) x.add[0] = x.add[1] = 0.0f;
 #pragma unroll
-    for (int j = from; j < to; ++j) {
-      const float e = fmaf(s[j], scale, -m);
-      x.w[j / 8][j % 8] = (W)__builtin_amdgcn_exp2f(LIMITED ? limited(e, limit) : e);
+      for (int j = from; j < to; ++j) {
+        const float e = fmaf(s[j], scale[j / 8 * 2], -m), w = __builtin_amdgcn_exp2f(LIMITED ? limited(e, limit) : e);
+        x.w[j / 8][j % 8] = (W)(w * fraction(scale[j / 8 * 2 + 1]));
+      }
+#pragma unroll
+      for (int j = from; j < to; j += 2) x.add[j / 8] = add_pair<W>(x.w[j / 8], j % 8, x.add[j / 8]);
+    } else {
+      if (i == 0) x.add[0] = 0.0f;
+#pragma unroll
+      for (int j = from; j < to; ++j) {
+        const float e = fmaf(s[j], scale, -m);
+        x.w[j / 8][j % 8] = (W)__builtin_amdgcn_exp2f(LIMITED ? limited(e, limit) : e);
+      }
+#pragma unroll
+      for (int j = from; j < to; j += 2) x.add[0] = add_pair<W>(x.w[j / 8], j % 8, x.add[0]);
     }
-#pragma unroll
-    for (int j = from; j < to; j += 2) x.add = add_pair<W>(x.w[j / 8], j % 8, x.add);
   }
-  __device__ __forceinline__ void moderate(const f16v& s, float scale, Weights& w) {
-    if (__builtin_amdgcn_ballot_w64(!(w.add <= kMost))) {
+  __device__ __forceinline__ void moderate(const f16v& s, Scale scale, Weights& w) {
+    if (__builtin_amdgcn_ballot_w64(!(w.all() <= kMost))) {
       float x = s[0];
+      if constexpr (S::SCALED) {
+        float y = s[8];
 #pragma unroll
-      for (int i = 1; i < 16; ++i) x = fmaxf(x, s[i]);
+        for (int i = 1; i < 8; ++i) x = fmaxf(x, s[i]), y = fmaxf(y, s[8 + i]);
+        x = fmaxf(x * scale[0], y * scale[2]);
+      } else {
+#pragma unroll
+        for (int i = 1; i < 16; ++i) x = fmaxf(x, s[i]);
+      }
       auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-      x = below(fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])), scale);
-      const uint32_t over = !(w.add <= kMost);
+      x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+      if constexpr (S::SCALED) x = below(x, 1.0f);
+      else x = below(x, scale);
+      const uint32_t over = !(w.all() <= kMost);
       sw = __builtin_amdgcn_permlane32_swap(over, over, false, false);
       const bool moves = (sw[0] | sw[1]) != 0;
       const float up = moves && x > m ? x : m, f = __builtin_amdgcn_exp2f(m - up);
@@ -775,45 +902,65 @@ struct Tile32 {
       }
       weigh<true>(s, scale, w, 0, 1, moves ? kLimit : INFINITY);
     }
-    l += w.add;
+    if constexpr (S::SCALED)
+      l += w.add[0] * __builtin_amdgcn_rcpf(fraction(scale[1])) + w.add[1] * __builtin_amdgcn_rcpf(fraction(scale[3]));
+    else
+      l += w.add[0];
   }
 
-  template <int n, typename F>
-  __device__ __forceinline__ void product(const Lds& lds, const Weights& w, W8 (&v)[kReadsAhead], F between) {
+  template <int n, typename F, typename... Scales>
+  __device__ __forceinline__ void product(const Lds& lds, const Weights& w, W8 (&v)[kReadsAhead], F between, const Scales&... scale) {
 #pragma unroll
     for (int j = 0; j < VP; ++j) {
       const int i = n * VP + j, next = i + kReadsAhead;
       o[j % DT] = mfma(v[i % kReadsAhead], w.w[j / DT], o[j % DT]);
-      if (next < 2 * VP) v[i % kReadsAhead] = values(lds, next / DT, next % DT);
+      if (next < 2 * VP) v[i % kReadsAhead] = values(lds, next / DT, next % DT, power_at(scale[next / VP], next / DT % 2)...);
       between(j);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
+  // What the values of the lane's block k (of two) of 32 keys are multiplied by.
+  static __device__ __forceinline__ float power_at(Scale scale, int k) {
+    return power(k ? scale[3] : scale[1]);
+  }
   // A strip that every row sees whole.  Of the two halves of 64 keys the first one's weights are made between the
   // second one's scores, and the second one's between the first one's values; load(i), i < KP, the i-th part of a
   // strip's loads, goes between the first one's scores.
-  template <typename L>
-  __device__ __forceinline__ void strip(uint32_t kat, uint32_t vat, float scale, L load) {
+  // scales: of the strip's two halves, by their numbers.
+  template <typename F, typename L>
+  __device__ __forceinline__ void strip(uint32_t kat, uint32_t vat, F scales, L load) {
     const auto nothing = [](int) {};
     f16v s[2];
     Weights p[2];
     W8 v[kReadsAhead];
     Keys x = keys(kat);
     scores<0>(x, s[0], load);
+    const Scale scale = scales(0);
     const Lds lds = values_at(vat);
     scores<1>(x, s[1], [&](int i) { weigh(s[0], scale, p[0], i, KP); });
+    if constexpr (S::SCALED) {
 #pragma unroll
-    for (int i = 0; i < kReadsAhead; ++i) v[i] = values(lds, i / DT, i % DT);
-    moderate(s[0], scale, p[0]);
-    __builtin_amdgcn_sched_barrier(0);
-    product<0>(lds, p[0], v, [&](int i) { weigh(s[1], scale, p[1], i, VP); });
-    moderate(s[1], scale, p[1]);
-    product<1>(lds, p[1], v, nothing);
+      for (int i = 0; i < kReadsAhead; ++i) v[i] = values(lds, i / DT, i % DT, power_at(scale, i / DT));
+      const Scale both[2] = {scale, scales(1)};
+      moderate(s[0], scale, p[0]);
+      __builtin_amdgcn_sched_barrier(0);
+      product<0>(lds, p[0], v, [&](int i) { weigh(s[1], both[1], p[1], i, VP); }, both);
+      moderate(s[1], both[1], p[1]);
+      product<1>(lds, p[1], v, nothing, both);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kReadsAhead; ++i) v[i] = values(lds, i / DT, i % DT);
+      moderate(s[0], scale, p[0]);
+      __builtin_amdgcn_sched_barrier(0);
+      product<0>(lds, p[0], v, [&](int i) { weigh(s[1], scale, p[1], i, VP); });
+      moderate(s[1], scale, p[1]);
+      product<1>(lds, p[1], v, nothing);
+    }
   }
   // Any other strip, from key `key0` on; holes(key): as for mask().  In this form for all strips, four prompts of 4096
   // tokens took 422 us instead of 413: the masks' registers are those of the loop above, too.
-  template <bool FINITE, typename H>
-  __device__ __forceinline__ void strip_seen(uint32_t kat, uint32_t vat, float scale, int key0, H holes) {
+  template <bool FINITE, typename F, typename H>
+  __device__ __forceinline__ void strip_seen(uint32_t kat, uint32_t vat, F scales, int key0, H holes) {
     const auto nothing = [](int) {};
     f16v s[2];
     Keys x = keys(kat);
@@ -826,13 +973,17 @@ struct Tile32 {
       if (n && !two) break;
       mask(s[n], key0 + 32 * n, holes(key0 + 32 * n));
       Weights p;
+      const Scale scale = scales(n);
       weigh(s[n], scale, p, 0, 1);
       moderate(s[n], scale, p);
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          W8 v = only_seen(values(lds, 2 * n + k, d), see.hi_max + 1 - (key0 + 32 * n + 16 * k + 8 * half));
+          const int count = see.hi_max + 1 - (key0 + 32 * n + 16 * k + 8 * half);
+          W8 v;
+          if constexpr (S::SCALED) v = only_seen(values(lds, 2 * n + k, d, power_at(scale, k)), count);
+          else v = only_seen(values(lds, 2 * n + k, d), count);
           if constexpr (FINITE) v = only_finite<W>(v);
           o[d] = mfma(v, p.w[k], o[d]);
         }
@@ -884,12 +1035,13 @@ struct Tile32 {
       for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
-          const f4 x = {o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
+          f4 x = {o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
+          if constexpr (S::SCALED) x *= power_of(ref);
           *(f4*)(p + 32 * d + 2 * i) = x;
         }
       return;
     }
-    const float inv = inverse(a.v_scale, sum, top == -INFINITY);  // a row that saw nothing has o = 0, too
+    const float inv = inverse(S::SCALED ? power_of(ref) : a.v_scale, sum, top == -INFINITY);  // a row that saw nothing has o = 0, too
     const int G = a.num_heads / a.num_kv_heads;
     T* p = (T*)a.out + (it.q0 + see.tok) * a.out_token_stride + (int64_t)(head * G + see.g) * a.out_head_stride + 4 * half;
     typedef T T4 __attribute__((ext_vector_type(4)));
@@ -906,7 +1058,7 @@ struct Tile32 {
 };
 
 template <typename S, int R>
-__device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it, int head, uint32_t lds, int* flag,
+__device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it, int head, uint32_t lds, int* flag, uint32_t scales,
                                             int64_t slot, float* parts, float* stats) {
   const int wave = uniform(threadIdx.x >> 6);
   Tile32<S> w;
@@ -918,7 +1070,7 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
 
   // A strip's loads in groups of 16 keys of K or V; every wave takes its share.
   Ahead<S, 2> ahead;
-  ahead.start(c, c.k, it.k0 + 16 * wave, S::ST, strips, it.k1);
+  ahead.start(c, c.k, it.k0 + 16 * wave, S::ST, strips, it.k1, it.seen);
   const uint64_t to_v = c.v - c.k;
   const auto dma_k = [&](int j) { return w.dma.of_k(j); };
   const auto dma_v = [&](int j) { return w.dma.of_v(j); };
@@ -926,10 +1078,25 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
     uint64_t b[2];
     uint32_t to;
   };
+  // Scales of 64 strips, twice: a strip's eight groups of eight keys, those of the lanes' halves apart.  The next 64 strips'
+  // are written R - 1 strips ahead, with a barrier in between.
+  const auto refilled = [&] {
+    const uint32_t at = scales + (ahead.base & 64) * kStripScales;
+    ahead.scales(c, [&](int) { return w.ref; }, [&](int strip, int group, f2 x) {
+      *(SCOOT_LDS f2*)(at + strip * kStripScales + group * (kStripScales / 2) + wave * 8) = x;
+    });
+  };
+  const auto scales_of = [&](int strip) {
+    const uint32_t at = scales + (strip & 127) * kStripScales + w.half * (kStripScales / 2);
+    return [at, &a](int n) {
+      if constexpr (S::SCALED) return *(const SCOOT_LDS f4*)(at + 16 * n);
+      else return a.score_scale;
+    };
+  };
   auto next = [&](int strip) {
     Next n;
     n.to = lds + (strip % R) * S::kStrip + wave * 16 * S::RB;
-    ahead.get(c, strip, n.b);
+    ahead.get(c, strip, n.b, refilled);
     return n;
   };
   auto part = [&](const Next& n, int i) {
@@ -950,6 +1117,10 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
   // The waves' first addresses tell of their entries.
   const bool holes = strips <= 64 ? any_wave<kWaves>(ahead.holes, flag) : any_holes<kWaves>(a, it, flag);
   settle();
+  if constexpr (S::SCALED) {
+    w.ref = largest_exponent(a, it, head, flag);
+    refilled();
+  }
   int u0, u1;
   w.see.whole(it, strips, S::ST, holes, u0, u1);
 
@@ -969,12 +1140,12 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
           turn(strip);
           const Next n = next(strip + R - 1);
           const uint32_t at = lds + (strip % R) * S::kStrip;
-          w.strip(at, at + kHalf, a.score_scale, [&](int i) { part(n, i); });
+          w.strip(at, at + kHalf, scales_of(strip), [&](int i) { part(n, i); });
         }
         for (; strip < u1; ++strip) {
           turn(strip);
           const uint32_t at = lds + (strip % R) * S::kStrip;
-          w.strip(at, at + kHalf, a.score_scale, [](int) {});
+          w.strip(at, at + kHalf, scales_of(strip), [](int) {});
         }
         __builtin_amdgcn_s_setprio(0);
       } else {
@@ -983,7 +1154,7 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
         const uint32_t at = lds + (strip % R) * S::kStrip;
         const int key0 = it.k0 + strip * S::ST;
         if (key0 <= w.see.hi_max)
-          w.template strip_seen<decltype(finite)::value>(at, at + kHalf, a.score_scale, key0,
+          w.template strip_seen<decltype(finite)::value>(at, at + kHalf, scales_of(strip), key0,
                                                          [&](int key) { return holes ? c.holes(key) : 0; });
         ++strip;
       }
@@ -991,8 +1162,12 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
   };
   pass(std::false_type{});
   if (any_wave<kWaves>(w.spoilt(), flag)) {
-    ahead.start(c, c.k, it.k0 + 16 * wave, S::ST, strips, it.k1);
+    ahead.start(c, c.k, it.k0 + 16 * wave, S::ST, strips, it.k1, it.seen);
     begin();
+    if constexpr (S::SCALED) {
+      settle();
+      refilled();
+    }
     pass(std::true_type{});
     w.add_lost(c, it.k0, u0 < u1 ? it.k0 + u0 * S::ST : it.k1);  // the strips that went through the mask
     if (u0 < u1) w.add_lost(c, it.k0 + u1 * S::ST, it.k1);
@@ -1021,6 +1196,7 @@ struct Tile16 {
   T8 q[KS];
   f4 o[DT];
   float m, l;
+  int ref = 0;  // as Tile32's, but it may grow
   int koff[KN];
   // LDS offsets of V's reads; for 8-bit heads of 256, which would have sixteen, the first one, of which the others differ
   // by some bits.
@@ -1089,13 +1265,14 @@ struct Tile16 {
     }
   }
 
-  // V^T: lane's element d = 16 dt + lane % 16 of the keys 8 quad .. + 7.
-  __device__ __forceinline__ W8 values(uint32_t lds, int dt) const {
+  // V^T: lane's element d = 16 dt + lane % 16 of the keys 8 quad .. + 7, times powers of two if there are any.
+  template <typename... By>
+  __device__ __forceinline__ W8 values(uint32_t lds, int dt, By... by) const {
     const int n = dt % Order::VM;
     const uint32_t at = lds + (kFewRegs ? here(voff[0]) ^ n * 16 * Order::U : voff[n % VN]) + (dt / Order::VM) * (Order::VM * 16 * Order::U);
     if constexpr (S::F8) {
       const i2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((SCOOT_LDS i2*)at);
-      return widen<_Float16>(v[0], v[1]);
+      return widen<_Float16>(v[0], v[1], by...);
     } else {
       union {
         s4 h[2];
@@ -1118,46 +1295,63 @@ struct Tile16 {
     }
   }
 
-  // As Tile32::weigh() and moderate().
-  __device__ __forceinline__ W8 weights(const f4 (&s)[2], float scale) {
+  // As Tile32::weigh() and moderate(); a lane's keys are of one block, the fraction of whose values' scale is f.
+  __device__ __forceinline__ W8 weights(const f4 (&s)[2], float scale, float f) {
     float add = 0.0f;
-    W8 w = eight_weights<W, false>([&](int i) { return s[i / 4][i % 4]; }, scale, m, 0.0f, add);
+    const auto score = [&](int i) { return s[i / 4][i % 4]; };
+    W8 w = eight_weights<W, false, S::SCALED>(score, scale, m, 0.0f, f, add);
     if (__builtin_amdgcn_ballot_w64(!(add <= kMost))) {
       float x = s[0][0];
 #pragma unroll
       for (int k = 1; k < 8; ++k) x = fmaxf(x, s[k / 4][k % 4]);
+      if constexpr (S::SCALED) x *= scale;
       auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
       x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
       sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-      x = below(fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])), scale);
+      if constexpr (S::SCALED) {
+        x = below(fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])), 1.0f);
+      } else {
+        x = below(fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])), scale);
+      }
       uint32_t over = !(add <= kMost);
       sw = __builtin_amdgcn_permlane32_swap(over, over, false, false);
       over = sw[0] | sw[1];
       sw = __builtin_amdgcn_permlane16_swap(over, over, false, false);
       const bool moves = (sw[0] | sw[1]) != 0;
-      const float up = moves && x > m ? x : m, f = __builtin_amdgcn_exp2f(m - up);
+      const float up = moves && x > m ? x : m, less = __builtin_amdgcn_exp2f(m - up);
       m = up;
-      l *= f;
+      l *= less;
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[d][i] *= f;
+        for (int i = 0; i < 4; ++i) o[d][i] *= less;
       add = 0.0f;
-      w = eight_weights<W, true>([&](int i) { return s[i / 4][i % 4]; }, scale, m, moves ? kLimit : INFINITY, add);
+      w = eight_weights<W, true, S::SCALED>(score, scale, m, moves ? kLimit : INFINITY, f, add);
     }
-    l += add;
+    l += S::SCALED ? add * __builtin_amdgcn_rcpf(f) : add;
     return w;
   }
 
-  __device__ __forceinline__ void product(uint32_t lds, W8 w) {
+  __device__ __forceinline__ void refer(int r) {
+    if (r <= ref) return;
+    const float f = to_reference(ref, r);
+    ref = r;
 #pragma unroll
-    for (int d = 0; d < DT; ++d) o[d] = mfma(values(lds, d), w, o[d]);
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[d][i] *= f;
   }
-  template <bool FINITE>
-  __device__ __forceinline__ void product_seen(uint32_t lds, W8 w, int key0) {
+
+  template <typename... By>
+  __device__ __forceinline__ void product(uint32_t lds, W8 w, By... by) {
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[d] = mfma(values(lds, d, by...), w, o[d]);
+  }
+  template <bool FINITE, typename... By>
+  __device__ __forceinline__ void product_seen(uint32_t lds, W8 w, int key0, By... by) {
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
-      W8 v = only_seen(values(lds, d), see.hi_max + 1 - (key0 + 8 * quad));
+      W8 v = only_seen(values(lds, d, by...), see.hi_max + 1 - (key0 + 8 * quad));
       if constexpr (FINITE) v = only_finite<W>(v);
       o[d] = mfma(v, w, o[d]);
     }
@@ -1198,7 +1392,7 @@ struct Tile16 {
 
 template <typename S, int W>
 __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, int row0, int head, uint32_t lds, char* smem,
-                                         float* ml, int* flag, int64_t slot_row, float* parts, float* stats) {
+                                         float* ml, int* flag, uint32_t scales, int64_t slot_row, float* parts, float* stats) {
   typedef typename S::T T;
   const int wave = uniform(threadIdx.x >> 6);
   Tile16<S> w;
@@ -1213,7 +1407,7 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
     uint64_t b[4];
   };
   Ahead<S, 4> ahead;  // its strips: every W-th one
-  ahead.start(c, c.k, it.k0 + 32 * wave, 32 * W, (strips - wave + W - 1) / W, it.k1);
+  ahead.start(c, c.k, it.k0 + 32 * wave, 32 * W, (strips - wave + W - 1) / W, it.k1, it.seen);
   const auto dma_k = [&](int j) { return w.dma.of_k(j); };
   const auto dma_v = [&](int j) { return w.dma.of_v(j); };
   auto load_k = [&](const Base& b) {
@@ -1226,10 +1420,21 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
     load16<S>(dma_v, vat + 16 * S::RB, to_v + b.b[2], to_v + b.b[3]);
   };
 
+  // Scales of the wave's next 64 strips: its own, so it waits for no other.
+  const uint32_t scale_at = scales + wave * kWaveScales;
+  const auto refilled = [&] {
+    const auto refer = [&](int top) {
+#pragma unroll
+      for (int o = 1; o < 64; o *= 2) top = max(top, __shfl_xor(top, o));
+      w.refer(uniform(top));
+      return w.ref;
+    };
+    ahead.scales(c, refer, [&](int strip, int group, f2 x) { *(SCOOT_LDS f2*)(scale_at + strip * 32 + group * 8) = x; });
+  };
   Base b;
   auto begin = [&] {
     if (wave >= strips) return;
-    ahead.get(c, 0, b.b);
+    ahead.get(c, 0, b.b, refilled);
     load_k(b);
     load_v(b);
   };
@@ -1239,6 +1444,10 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
   bool holes = ahead.holes;
   if (strips > 64 * W) holes = any_holes<W>(a, it, flag);
   settle();
+  if constexpr (S::SCALED) {
+    w.clear();
+    refilled();
+  }
   int u0, u1;  // strips seen whole by every row
   w.see.whole(it, strips, 32, holes, u0, u1);
 
@@ -1249,18 +1458,25 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
     const int key0 = it.k0 + strip * 32;
     wait_vm<2 * S::NJ>();  // the keys, not the values behind them
     f4 s[2];
+    f2 scale = {a.score_scale, 0.0f};
+    const int ref = w.ref;
+    if constexpr (S::SCALED) scale = *(const SCOOT_LDS f2*)(scale_at + (strip / W & 63) * 32 + w.quad * 8);
     w.scores(kat, s);
     wait_lds();
     if (more) {
-      ahead.get(c, strip / W + 1, b.b);
+      ahead.get(c, strip / W + 1, b.b, refilled);
       load_k(b);
     }
     if (kMasked) w.mask(s, key0, holes ? c.holes(key0) : 0);
-    const typename Tile16<S>::W8 p = w.weights(s, a.score_scale);
+    const typename Tile16<S>::W8 p = w.weights(s, scale.x, fraction(scale.y));
     if (more) wait_vm<2 * S::NJ>();
     else wait_vm<0>();
-    if (kMasked) w.template product_seen<decltype(finite)::value>(vat, p, key0);
-    else w.product(vat, p);
+    const auto product = [&](auto... by) {
+      if (kMasked) w.template product_seen<decltype(finite)::value>(vat, p, key0, by...);
+      else w.product(vat, p, by...);
+    };
+    if constexpr (S::SCALED) product(power(scale.y) * to_reference(ref, w.ref));
+    else product();
     wait_lds();
     if (more) load_v(b);
     strip += W;
@@ -1278,8 +1494,12 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
   };
   pass(std::false_type{});
   if (w.spoilt()) {
-    ahead.start(c, c.k, it.k0 + 32 * wave, 32 * W, (strips - wave + W - 1) / W, it.k1);
+    ahead.start(c, c.k, it.k0 + 32 * wave, 32 * W, (strips - wave + W - 1) / W, it.k1, it.seen);
     begin();
+    if constexpr (S::SCALED) {
+      settle();
+      refilled();
+    }
     pass(std::true_type{});
     for (strip = wave; strip < strips; strip += W)
       if (strip < u0 || strip >= u1) w.add_lost(c, it.k0 + strip * 32, min(it.k0 + strip * 32 + 32, it.k1));
@@ -1292,7 +1512,7 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
   constexpr int kRow = S::D + 4;  // floats of a row, off by 16 bytes so that rows start on different banks
   float* mine = (float*)smem + (wave * kFew + (w.lane & 15)) * kRow + 4 * w.quad;
 #pragma unroll
-  for (int d = 0; d < Tile16<S>::DT; ++d) *(f4*)(mine + 16 * d) = w.o[d];
+  for (int d = 0; d < Tile16<S>::DT; ++d) *(f4*)(mine + 16 * d) = S::SCALED ? w.o[d] * power_of(w.ref) : w.o[d];
   __syncthreads();
   const int G = a.num_heads / a.num_kv_heads;
   const int rows = min(kFew, it.rows - row0);
@@ -1342,6 +1562,10 @@ struct FewLds {
 template <typename S, int R, int W>
 constexpr int kFlagAt = R * S::kStrip > FewLds<S, W>::kEnd ? R * S::kStrip : FewLds<S, W>::kEnd;
 template <typename S, int R, int W>
+constexpr int kScalesAt = kFlagAt<S, R, W> + 4 * W;
+template <typename S, int R, int W>
+constexpr int kLdsEnd = kScalesAt<S, R, W> + (S::SCALED ? std::max(R > 0 ? 128 * kStripScales : 0, W * kWaveScales) : 0);
+template <typename S, int R, int W>
 __global__ __launch_bounds__(64 * W, (waves_per_simd(S::D, R))) void attention_kernel(KvAttnArgs a, Plan p, float* parts, float* stats) {
   extern __shared__ __attribute__((aligned(256))) char smem[];
   const uint32_t lds = (uint32_t)(uintptr_t)(SCOOT_LDS char*)smem;
@@ -1354,13 +1578,13 @@ __global__ __launch_bounds__(64 * W, (waves_per_simd(S::D, R))) void attention_k
   int* flag = (int*)(smem + kFlagAt<S, R, W>);
   if constexpr (R > 0) {
     if (it.shared) {
-      shared_tile<S, R>(a, it, (int)head, lds, flag, slot, parts, stats);
+      shared_tile<S, R>(a, it, (int)head, lds, flag, lds + kScalesAt<S, R, W>, slot, parts, stats);
       return;
     }
   }
   float* ml = (float*)(smem + FewLds<S, W>::kStats);
   for (int row0 = 0; row0 < it.rows; row0 += kFew)
-    few_rows<S, W>(a, it, row0, (int)head, lds, smem, ml, flag, slot * (R > 0 ? kTile : kFew), parts, stats);
+    few_rows<S, W>(a, it, row0, (int)head, lds, smem, ml, flag, lds + kScalesAt<S, R, W>, slot * (R > 0 ? kTile : kFew), parts, stats);
 }
 
 // Joins the parts of a tile's keys: one workgroup per key head and as many rows
@@ -1428,7 +1652,7 @@ int launch_kernel(const KvAttnArgs& a, const Plan& p, float* parts, float* stats
   const int rc = allow_full_lds((const void*)attention_kernel<S, R, W>, "kv attention");
   if (rc != SCOOT_OK) return rc;
   hipLaunchKernelGGL((attention_kernel<S, R, W>), dim3((unsigned)(p.items * p.splits * a.num_kv_heads)), dim3(64 * W),
-                     (kFlagAt<S, R, W> + 4 * W), stream, a, p, parts, stats);
+                     (kLdsEnd<S, R, W>), stream, a, p, parts, stats);
   return SCOOT_OK;
 }
 
@@ -1456,9 +1680,22 @@ int launch(const KvAttnArgs& a, const Plan& p, float* parts, float* stats, hipSt
   return SCOOT_OK;
 }
 
-// One per head dimension, each in a file of its own.
+// One per head dimension, each in a file of its own, and with scales of blocks in another.
 template <int D>
 int launch_dim(const KvAttnArgs& a, const Plan& p, scoot_kv_type type, bool f8, float* parts, float* stats, hipStream_t stream);
+template <int D>
+int launch_scaled(const KvAttnArgs& a, const Plan& p, scoot_kv_type type, float* parts, float* stats, hipStream_t stream);
+
+#define SCOOT_KV_ATTN_SCALED_DIM(D)                                                                                       \
+  namespace scoot {                                                                                                       \
+  namespace kvattn {                                                                                                      \
+  template <>                                                                                                             \
+  int launch_scaled<D>(const KvAttnArgs& a, const Plan& p, scoot_kv_type type, float* parts, float* stats, hipStream_t s) { \
+    return type == SCOOT_KV_F16 ? launch<Shape<_Float16, true, D, true>>(a, p, parts, stats, s)                           \
+                                : launch<Shape<__bf16, true, D, true>>(a, p, parts, stats, s);                            \
+  }                                                                                                                       \
+  }                                                                                                                       \
+  }
 
 #define SCOOT_KV_ATTN_DIM(D)                                                                                              \
   namespace scoot {                                                                                                       \
