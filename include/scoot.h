@@ -772,7 +772,8 @@ int scoot_rotate(const void* x, scoot_kv_type type, int64_t num_tokens, int num_
  * (num_heads > 0), turned into q_out, which may be q itself.  rotary_dim 0:
  * nothing is turned, positions and freqs are not used, and there are no
  * queries.  A token with a negative position is skipped whole, one whose slot
- * is outside the cache has its queries turned and nothing stored.
+ * is outside the cache has its queries turned and nothing stored.  k_scale and
+ * v_scale: from 2^-100 to 2^100.
  *
  * k_scales, v_scales (both or neither; an 8-bit cache): [num_blocks]
  * [num_kv_heads] scales of every block and head, in and out, in the place of

@@ -280,6 +280,8 @@ int scoot_kv_append(const void* q, int num_heads, int64_t q_token_stride, int64_
     return fail_static(SCOOT_ERR_INVALID_ARG, "kv append: k_scales and v_scales go together");
   if (k_scales && (cache_type != SCOOT_KV_F8 || k_scale != 1.0f || v_scale != 1.0f))
     return fail_static(SCOOT_ERR_INVALID_ARG, "kv append: scales of blocks need an 8-bit cache and no other scale");
+  if (!(k_scale >= 0x1p-100f && k_scale <= 0x1p100f && v_scale >= 0x1p-100f && v_scale <= 0x1p100f))
+    return fail_static(SCOOT_ERR_INVALID_ARG, "kv append: scales must be from 2^-100 to 2^100");
   if (k_scales && k_scales == v_scales) return fail_static(SCOOT_ERR_INVALID_ARG, "kv append: k_scales and v_scales must differ");
   if (num_tokens == 0) return SCOOT_OK;
   const bool stores = num_blocks > 0;  // a cache without blocks holds no tokens

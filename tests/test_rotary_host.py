@@ -81,7 +81,7 @@ def test_rotate_refuses(change, status):
     (dict(q_out=None), INVALID), (dict(k=None), INVALID), (dict(v=None), INVALID), (dict(slots=None), INVALID), (dict(positions=None), INVALID),
     (dict(freqs=None), INVALID), (dict(k_cache=None), INVALID), (dict(v_cache=P + 8), INVALID), (dict(k=P + 1), INVALID), (dict(q_out=P + 1), INVALID),
     (dict(slots=P + 4), INVALID), (dict(k_scale=2.0), INVALID), (dict(cache_type=2, k_scale=0.0), INVALID), (dict(cache_type=2, v_scale=NAN), INVALID),
-    (dict(F8, k_scales=None), INVALID), (dict(F8, v_scales=None), INVALID), (dict(F8, cache_type=1), INVALID), (dict(F8, k_scale=2.0), INVALID),
+    (dict(cache_type=2, k_scale=2.0 ** -101), INVALID), (dict(cache_type=2, v_scale=2.0 ** 101), INVALID), (dict(F8, k_scales=None), INVALID), (dict(F8, v_scales=None), INVALID), (dict(F8, cache_type=1), INVALID), (dict(F8, k_scale=2.0), INVALID),
     (dict(F8, k_scales=P + 2), INVALID), (dict(F8, v_scales=P), INVALID)], ids=str)
 def test_append_refuses(change, status):
     _refused(lib().scoot_kv_append, APPEND, status, **change)
