@@ -803,7 +803,8 @@ int scoot_kv_append(const void* q, int num_heads, int64_t q_token_stride, int64_
  * 2^-64 to 2^64 (a scale that is not makes results of the rows that see its
  * block undefined, and no others):
  *   out = sum_t softmax_t(scale * k_scales[b_t] * q . k_t) * v_scales[b_t] * v_t
- * The workspace is scoot_kv_attention_workspace's. */
+ * A power of two as the scale of values is exact; another one is off by up to
+ * 2^-24 of the row's largest score, as scores themselves are.  The workspace is scoot_kv_attention_workspace's. */
 int scoot_kv_attention_scaled(const void* q, scoot_kv_type type, int64_t num_tokens, int num_heads, int num_kv_heads,
                               int head_dim, int64_t q_token_stride, int64_t q_head_stride, const void* k_cache,
                               const void* v_cache, int64_t num_blocks, int block_size, const int32_t* block_table,

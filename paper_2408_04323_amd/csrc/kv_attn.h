@@ -39,12 +39,15 @@
 // block, so its scale a of the keys takes the place of the one scale in their
 // exponents.  The scale b of the values is 2^e f, 1 <= f < 2: the values are
 // widened to half precision times 2^(e - r), which the conversion does by the
-// way, with r the largest e so far; f goes to the weights before they are
-// rounded, and l adds the rounded weights over f.  So m, the weights and l are
-// those of one scale, whatever the scores; values lose nothing down to scales of
-// 2^-15 of the largest, and 2^-34 of the largest value below that.  A weight
-// costs one product more.  The scales of 64 strips at a time are fetched with
-// their addresses and wait in LDS.
+// way, with r near the largest e so far; log2 f goes into the exponents beside
+// m, and l adds the weights over f.  So m, the weights and l are those of one
+// scale, whatever the scores, and powers of two cost next to nothing; values
+// lose nothing down to 2^-15 of the reference, and 2^-25 of it below that.
+// Products of weights and f instead would be exact beside any score, too, and
+// cost 13% (one chunk over 30,000 keys, heads of 128: 516 us with one scale, 583).
+// The scales of 64 strips at a time go straight from memory into LDS, where
+// their addresses are made (through registers: 40 more, and a wave per SIMD less
+// for few rows of 64 dimensions).
 //
 // Registers decide the waves per SIMD: three for tiles of 64 dimensions, two for
 // 128, one for 192 and 256, where o and q take 144 and 192 of a lane's 512.  A
@@ -91,6 +94,11 @@ constexpr int kStripScales = 64;          // bytes of the scales of a tile's str
 constexpr int kWaveScales = 64 * 4 * 8;   // and of a wave's 64 strips
 
 constexpr float kLimit = 14.0f;              // of a weight's exponent where it moved: no other weight is above kMost
+
+// The scale of a block's scores, kept off 0 and infinity: -inf stays -inf, and 0 stays 0.
+__device__ __forceinline__ float key_scale(float score_scale, float k) {
+  return __builtin_fminf(__builtin_fmaxf(score_scale * k, 1.4e-45f), 3.4e38f);
+}
 
 constexpr int gcd256(int x) { return x % 256 == 0 ? 256 : x % 128 == 0 ? 128 : 64; }
 
@@ -189,6 +197,10 @@ __device__ __forceinline__ void load_lds(uint32_t to, uint64_t base, uint32_t of
 __device__ __forceinline__ void load_lds(uint32_t to, uint64_t addr) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(addr) : "memory", "m0");
 }
+// 64 lanes x 4 bytes, each from an address of its own.
+__device__ __forceinline__ void load_lds_dword(uint32_t to, uint64_t addr) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(addr) : "memory", "m0");
+}
 #pragma clang diagnostic pop
 
 // What a workgroup works on: rows of a request from row0 on (a tile's, or 16), one key
@@ -200,7 +212,6 @@ struct Item {
   int row0;         // first row of the tile
   int len;          // cached tokens that have table entries
   int k0, k1;       // keys of this workgroup; k0 is a multiple of 32
-  int seen;         // first key that any row of the tile sees
   int splits;       // parts that the tile's keys are in
   int split;
   int seq;
@@ -271,8 +282,8 @@ __device__ __forceinline__ bool find_item(const KvAttnArgs& a, const Plan& p, in
   // The tile's keys, and this split's part of them.
   const int64_t top = it.pos0 + last_row / G;
   const int end = (int)clamp64(top + 1, 0, it.len);
-  it.seen = a.window > 0 ? (int)clamp64(it.pos0 + it.row0 / G - a.window + 1, 0, end) : 0;
-  const int begin = it.seen & ~31;
+  int begin = 0;
+  if (a.window > 0) begin = (int)clamp64(it.pos0 + it.row0 / G - a.window + 1, 0, end) & ~31;
   const int parts = end > begin ? (int)(((int64_t)end - begin + p.part - 1) / p.part) : 1;
   it.splits = parts < splits ? parts : splits;
   it.split = split;
@@ -282,16 +293,15 @@ __device__ __forceinline__ bool find_item(const KvAttnArgs& a, const Plan& p, in
   return true;
 }
 
-// A scale b = 2^e f of values at the reference r, 2^(e - r) f (r with the bias of a float), and its two parts.
-__device__ __forceinline__ float referred(float b, int r) {
-  const uint32_t x = __float_as_uint(b);
-  return __uint_as_float((uint32_t)max((int)(x >> 23) - r + 127, 1) << 23 | (x & 0x7fffffu));
-}
+// A scale 2^e f of values, 1 <= f < 2, by its parts: e (with the bias of a float), f, and 2^(e - r) for a reference r.
+__device__ __forceinline__ int exponent(float b) { return (int)(__float_as_uint(b) >> 23); }
 __device__ __forceinline__ float fraction(float b) { return __uint_as_float((__float_as_uint(b) & 0x7fffffu) | 0x3f800000u); }
-__device__ __forceinline__ float power(float b) { return __uint_as_float(__float_as_uint(b) & 0x7f800000u); }
-// What a sum at the reference r is multiplied by for one at 2^0, and for one at a larger reference.
+__device__ __forceinline__ float power_at(float b, int r) { return __uint_as_float((uint32_t)max(exponent(b) - r + 127, 1) << 23); }
+// 2^r, and 2^(r - larger).
 __device__ __forceinline__ float power_of(int r) { return __uint_as_float((uint32_t)r << 23); }
 __device__ __forceinline__ float to_reference(int r, int larger) { return __uint_as_float((uint32_t)max(127 + r - larger, 0) << 23); }
+// The reference moves where an exponent is this far above it: 448 * 2^6 is still a number in half precision.
+constexpr int kAboveReference = 6;
 
 // Blocks of the cache, as scalars.
 template <typename S>
@@ -302,10 +312,8 @@ struct Cache {
   uint32_t block_bytes;  // of all heads; at most 1024 heads of 256 keys of 512 bytes
   uint32_t num_blocks;
   int shift, last;       // last entry of the row
-  const float* k_scales;  // of the head, num_kv_heads apart
-  const float* v_scales;
+  uint64_t k_scales, v_scales;  // of the head, every block's `heads` floats after the one before
   uint32_t heads;
-  float score_scale;
 
   __device__ __forceinline__ void setup(const KvAttnArgs& a, int seq, int head) {
     entries = a.block_table + (int64_t)seq * a.table_stride;
@@ -318,18 +326,10 @@ struct Cache {
     shift = a.block_shift;
     last = a.max_blocks - 1;
     if constexpr (S::SCALED) {
-      k_scales = a.k_scales + head;
-      v_scales = a.v_scales + head;
+      k_scales = (uint64_t)(a.k_scales + head);
+      v_scales = (uint64_t)(a.v_scales + head);
       heads = (uint32_t)a.num_kv_heads;
-      score_scale = a.score_scale;
     }
-  }
-  // What the scores of a block are multiplied by, and its values.  Of a block that no row sees, which may hold anything:
-  // numbers that keep 0 * inf out of what is masked, and do not count for the largest.  No memory's content gives others.
-  __device__ __forceinline__ f2 scales(float k, float v, bool seen) const {
-    const f2 r = {seen ? __builtin_fminf(__builtin_fmaxf(score_scale * k, 1.4e-45f), 3.4e38f) : 1.0f,
-                  seen && v > 0.0f && v < INFINITY ? v : 0x1p-126f};
-    return r;
   }
   // The entry of eight keys from `key` on (inside one block), for at().
   __device__ __forceinline__ uint32_t entry(int key) const {
@@ -354,16 +354,16 @@ struct Cache {
 // Addresses of a wave's next 64 strips, one strip per lane: N groups of eight
 // keys each, `stride` keys from strip to strip.  (By scalars, a strip would
 // cost some forty instructions, and a scalar load is waited for together with
-// the reads of LDS.)
-template <typename S, int N>
+// the reads of LDS.)  Scales go along, into LDS: [k, v][groups][64
+// strips], of every second 64 strips 64 kStripScales further on if
+// TWICE; they have arrived when the strips' own loads have.
+template <typename S, int N, bool TWICE>
 struct Ahead {
   uint32_t lo[N], hi[N];
   uint64_t from;  // keys or values
   int key0, stride, strips, base, end;
+  uint32_t scales;  // where in LDS the strips' scales go
   bool holes;     // some group below key `end` of the 64 strips has no block
-  float ks[S::SCALED ? N : 1], vs[S::SCALED ? N : 1];
-  int seen;       // first key that counts
-  int there;      // which groups of the lane's strip have a block
 
   __device__ __forceinline__ void fill(const Cache<S>& c, int strip) {
     base = strip;
@@ -384,38 +384,17 @@ struct Ahead {
       lo[j] = (uint32_t)at;
       hi[j] = (uint32_t)(at >> 32);
       if constexpr (S::SCALED) {
-        const bool real = e[j] < c.num_blocks;
-        const int64_t of = (int64_t)(real ? e[j] : 0) * c.heads;
-        there = (j ? there : 0) | (int)real << j;
-        ks[j] = c.k_scales[of];
-        vs[j] = c.v_scales[of];
+        const uint64_t of = (uint64_t)(e[j] < c.num_blocks ? e[j] : 0) * c.heads * 4;
+        const uint32_t to = scales + (TWICE ? (strip & 64) * kStripScales : 0) + j * 256;
+        load_lds_dword(to, c.k_scales + of);
+        load_lds_dword(to + (TWICE ? 32 : 16) * kStripScales, c.v_scales + of);
       }
     }
     holes = __builtin_amdgcn_ballot_w64(hole) != 0;
   }
-  // The scales that fill() fetched: put(strip of 64, group, scales); refer(the largest exponent of the values' scales) goes
-  // before, for the reference that they are put at.
-  template <typename F, typename G>
-  __device__ __forceinline__ void scales(const Cache<S>& c, F refer, G put) const {
-    const int lane = threadIdx.x & 63, strip = base + lane;
-    f2 x[N];
-    int top = 0;
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const int key = key0 + strip * stride + 8 * j;
-      x[j] = c.scales(ks[j], vs[j], strip < strips && key < end && key + 8 > seen && there >> j & 1);
-      top = max(top, (int)(__float_as_uint(x[j][1]) >> 23));
-    }
-    const int r = refer(top);
-#pragma unroll
-    for (int j = 0; j < N; ++j) {
-      x[j][1] = referred(x[j][1], r);
-      put(lane, j, x[j]);
-    }
-  }
-  __device__ __forceinline__ void start(const Cache<S>& c, uint64_t cache, int first, int keys, int n, int last, int from_key) {
+  __device__ __forceinline__ void start(const Cache<S>& c, uint64_t cache, int first, int keys, int n, int last, uint32_t to) {
     from = cache;
-    seen = from_key;
+    scales = to;
     key0 = first;
     stride = keys;
     strips = n;
@@ -424,15 +403,8 @@ struct Ahead {
     if (n > 0) fill(c, 0);
   }
   // The groups of a strip, which follows the last one asked for.
-  template <typename F>
-  __device__ __forceinline__ void get(const Cache<S>& c, int strip, uint64_t (&b)[N], F refilled) {
-    if (strip - base == 64) {
-      fill(c, strip);
-      if constexpr (S::SCALED) {
-        settle();
-        refilled();
-      }
-    }
+  __device__ __forceinline__ void get(const Cache<S>& c, int strip, uint64_t (&b)[N]) {
+    if (strip - base == 64) fill(c, strip);
 #pragma unroll
     for (int j = 0; j < N; ++j)
       b[j] = (uint32_t)__builtin_amdgcn_readlane((int)lo[j], strip - base) |
@@ -460,24 +432,6 @@ __device__ __forceinline__ bool any_holes(const KvAttnArgs& a, const Item& it, i
   for (int64_t e = (it.k0 >> a.block_shift) + threadIdx.x; (e << a.block_shift) < it.k1; e += 64 * W)
     h = h || (uint32_t)t[e] >= (uint32_t)a.num_blocks;
   return any_wave<W>(__builtin_amdgcn_ballot_w64(h) != 0, flag);
-}
-
-// The largest exponent of the values' scales of a tile's keys.
-__device__ __forceinline__ int largest_exponent(const KvAttnArgs& a, const Item& it, int head, int* flag) {
-  const int32_t* t = a.block_table + (int64_t)it.seq * a.table_stride;
-  int top = 1;
-  const int from = it.k0 > it.seen ? it.k0 : it.seen;
-  for (int64_t e = (from >> a.block_shift) + threadIdx.x; (e << a.block_shift) < it.k1; e += kThreads) {
-    const uint32_t block = (uint32_t)t[e];
-    const float v = block < (uint32_t)a.num_blocks ? a.v_scales[(int64_t)block * a.num_kv_heads + head] : 0.0f;
-    top = max(top, v > 0.0f && v < INFINITY ? (int)(__float_as_uint(v) >> 23) : 1);
-  }
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) top = max(top, __shfl_xor(top, o));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) flag[threadIdx.x >> 6] = top;
-  __syncthreads();
-  return uniform(max(max(flag[0], flag[1]), max(flag[2], flag[3])));
 }
 
 // Eight 8-bit floats as 16-bit ones, exact, times a power of two.
@@ -520,14 +474,14 @@ __device__ __forceinline__ float below(float s, float scale) {
 // Not above the limit; NaN stays.
 __device__ __forceinline__ float limited(float x, float limit) { return __builtin_elementwise_minimum(x, limit); }
 
-// Eight weights 2^(scale s - m) (SCALED: times f), rounded, and their sum added to l.
-template <typename W, bool LIMITED, bool SCALED, typename F>
-__device__ __forceinline__ typename Vec<W>::v8 eight_weights(F score, float scale, float m, float limit, float f, float& l) {
+// Eight weights 2^(scale s - m), rounded, and their sum added to l.
+template <typename W, bool LIMITED, typename F>
+__device__ __forceinline__ typename Vec<W>::v8 eight_weights(F score, float scale, float m, float limit, float& l) {
   typename Vec<W>::v8 r;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const float x = fmaf(score(i), scale, -m), w = __builtin_amdgcn_exp2f(LIMITED ? limited(x, limit) : x);
-    r[i] = (W)(SCALED ? w * f : w);
+    const float x = fmaf(score(i), scale, -m);
+    r[i] = (W)__builtin_amdgcn_exp2f(LIMITED ? limited(x, limit) : x);
   }
 #pragma unroll
   for (int i = 0; i < 8; i += 2) l = add_pair<W>(r, i, l);
@@ -622,7 +576,7 @@ __device__ __forceinline__ void load16(F off, uint32_t to, uint64_t b0, uint64_t
 // hi, and over the rows.  Positions grow with the rows.
 struct Sight {
   int tok, g;  // token and head of the lane's row
-  int hi, lo, hi_min, hi_max, lo_max;
+  int hi, lo, hi_min, hi_max, lo_max, lo_min;
 
   __device__ __forceinline__ void start(const KvAttnArgs& a, const Item& it, int row0, int r, int count) {
     const int G = a.num_heads / a.num_kv_heads;
@@ -637,7 +591,10 @@ struct Sight {
     hi_min = upto(it, first);
     hi_max = upto(it, last);
     lo_max = after(a, it, last);
+    lo_min = after(a, it, first);
   }
+  // Whether some row sees some of the eight keys from `key` on.
+  __device__ __forceinline__ bool any_of(int key) const { return key <= hi_max && key + 7 > lo_min; }
   static __device__ __forceinline__ int upto(const Item& it, int tok) { return (int)clamp64(it.pos0 + tok, -1, it.len - 1); }
   static __device__ __forceinline__ int after(const KvAttnArgs& a, const Item& it, int tok) {
     return a.window > 0 ? (int)clamp64(it.pos0 + tok - a.window, -1, 0x7fffffff) : -1;
@@ -708,7 +665,7 @@ struct Tile32 {
   T8 q[KS];
   f16v o[DT];
   float m, l;
-  int ref;  // o is at 2^-ref (with a float's bias); the same in all lanes
+  int ref = 0;  // what o is times is 2^ref (with a float's bias); the same in all lanes
   // LDS offsets of this lane's reads; with few registers the first ones, of which the others differ by some bits.
   static constexpr bool kFewRegs = S::D == 256;
   static constexpr int KN = kFewRegs ? 1 : Order::KM / 2, VM = kFewRegs ? 1 : VN;
@@ -842,22 +799,38 @@ struct Tile32 {
   // Weights of 32 keys.  No maximum is taken as long as the weights stay
   // moderate, which their sum tells; whether a row's m moves depends on that
   // row alone.  weigh() is the i-th of n parts of the work, moderate() its end.
-  struct Weights {
+  struct Less {
+    float less[2];  // log2 f - m of each block
+  };
+  struct NoLess {};
+  struct Weights : std::conditional<S::SCALED, Less, NoLess>::type {
     W8 w[2];
     float add[S::SCALED ? 2 : 1];  // of each block's keys, or of all
     __device__ __forceinline__ float all() const { return S::SCALED ? add[0] + add[S::SCALED] : add[0]; }
   };
   // What the scores of 32 keys are multiplied by: one number, or that and the values' scale of a lane's two blocks.
-  typedef typename std::conditional<S::SCALED, f4, float>::type Scale;
+  struct Scales {
+    f4 x;
+    bool two;  // the values' scales are powers of two, in all lanes
+    __device__ __forceinline__ float operator[](int i) const { return x[i]; }
+  };
+  typedef typename std::conditional<S::SCALED, Scales, float>::type Scale;
   template <bool LIMITED = false>
   __device__ __forceinline__ void weigh(const f16v& s, Scale scale, Weights& x, int i, int n, float limit = 0.0f) const {
     const int from = 2 * (8 * i / n), to = 2 * (8 * (i + 1) / n);
     if constexpr (S::SCALED) {
-      if (i == 0) x.add[0] = x.add[1] = 0.0f;
+      if (i == 0) {
+        x.add[0] = x.add[1] = 0.0f;
+        x.less[0] = x.less[1] = -m;
+        if (!scale.two) {
+          x.less[0] += __builtin_amdgcn_logf(fraction(scale[1]));
+          x.less[1] += __builtin_amdgcn_logf(fraction(scale[3]));
+        }
+      }
 #pragma unroll
       for (int j = from; j < to; ++j) {
-        const float e = fmaf(s[j], scale[j / 8 * 2], -m), w = __builtin_amdgcn_exp2f(LIMITED ? limited(e, limit) : e);
-        x.w[j / 8][j % 8] = (W)(w * fraction(scale[j / 8 * 2 + 1]));
+        const float e = fmaf(s[j], scale[j / 8 * 2], x.less[j / 8]);
+        x.w[j / 8][j % 8] = (W)__builtin_amdgcn_exp2f(LIMITED ? limited(e, limit) : e);
       }
 #pragma unroll
       for (int j = from; j < to; j += 2) x.add[j / 8] = add_pair<W>(x.w[j / 8], j % 8, x.add[j / 8]);
@@ -902,10 +875,13 @@ struct Tile32 {
       }
       weigh<true>(s, scale, w, 0, 1, moves ? kLimit : INFINITY);
     }
-    if constexpr (S::SCALED)
-      l += w.add[0] * __builtin_amdgcn_rcpf(fraction(scale[1])) + w.add[1] * __builtin_amdgcn_rcpf(fraction(scale[3]));
-    else
-      l += w.add[0];
+    if constexpr (S::SCALED) {
+      if (!scale.two) {
+        w.add[0] *= __builtin_amdgcn_rcpf(fraction(scale[1]));
+        w.add[1] *= __builtin_amdgcn_rcpf(fraction(scale[3]));
+      }
+    }
+    l += w.all();
   }
 
   template <int n, typename F, typename... Scales>
@@ -914,14 +890,28 @@ struct Tile32 {
     for (int j = 0; j < VP; ++j) {
       const int i = n * VP + j, next = i + kReadsAhead;
       o[j % DT] = mfma(v[i % kReadsAhead], w.w[j / DT], o[j % DT]);
-      if (next < 2 * VP) v[i % kReadsAhead] = values(lds, next / DT, next % DT, power_at(scale[next / VP], next / DT % 2)...);
+      if (next < 2 * VP) v[i % kReadsAhead] = values(lds, next / DT, next % DT, power_at(scale[next / VP][next / DT % 2 * 2 + 1], ref)...);
       between(j);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
-  // What the values of the lane's block k (of two) of 32 keys are multiplied by.
-  static __device__ __forceinline__ float power_at(Scale scale, int k) {
-    return power(k ? scale[3] : scale[1]);
+  // The values' scales of the lane's four blocks of a strip, before their first use: the reference moves if they are far
+  // above it.  Whether they are all powers of two, in all lanes.
+  __device__ __forceinline__ bool refer(float a, float b, float c, float d) {
+    const int e = max(max(exponent(a), exponent(b)), max(exponent(c), exponent(d)));
+    if (__builtin_amdgcn_ballot_w64(e > ref + kAboveReference)) {
+      const auto sw = __builtin_amdgcn_permlane32_swap(e, e, false, false);
+      const int r = uniform(max((int)sw[0], (int)sw[1]));
+      const float f = to_reference(ref, r);
+      ref = r;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] *= f;
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    return __builtin_amdgcn_ballot_w64(((__float_as_uint(a) | __float_as_uint(b) | __float_as_uint(c) | __float_as_uint(d)) & 0x7fffffu) != 0) == 0;
   }
   // A strip that every row sees whole.  Of the two halves of 64 keys the first one's weights are made between the
   // second one's scores, and the second one's between the first one's values; load(i), i < KP, the i-th part of a
@@ -940,7 +930,7 @@ struct Tile32 {
     scores<1>(x, s[1], [&](int i) { weigh(s[0], scale, p[0], i, KP); });
     if constexpr (S::SCALED) {
 #pragma unroll
-      for (int i = 0; i < kReadsAhead; ++i) v[i] = values(lds, i / DT, i % DT, power_at(scale, i / DT));
+      for (int i = 0; i < kReadsAhead; ++i) v[i] = values(lds, i / DT, i % DT, power_at(scale[i / DT * 2 + 1], ref));
       const Scale both[2] = {scale, scales(1)};
       moderate(s[0], scale, p[0]);
       __builtin_amdgcn_sched_barrier(0);
@@ -982,7 +972,7 @@ struct Tile32 {
         for (int d = 0; d < DT; ++d) {
           const int count = see.hi_max + 1 - (key0 + 32 * n + 16 * k + 8 * half);
           W8 v;
-          if constexpr (S::SCALED) v = only_seen(values(lds, 2 * n + k, d, power_at(scale, k)), count);
+          if constexpr (S::SCALED) v = only_seen(values(lds, 2 * n + k, d, power_at(scale[2 * k + 1], ref)), count);
           else v = only_seen(values(lds, 2 * n + k, d), count);
           if constexpr (FINITE) v = only_finite<W>(v);
           o[d] = mfma(v, p.w[k], o[d]);
@@ -1069,8 +1059,8 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
   const int strips = (it.k1 - it.k0 + S::ST - 1) / S::ST;
 
   // A strip's loads in groups of 16 keys of K or V; every wave takes its share.
-  Ahead<S, 2> ahead;
-  ahead.start(c, c.k, it.k0 + 16 * wave, S::ST, strips, it.k1, it.seen);
+  Ahead<S, 2, true> ahead;
+  ahead.start(c, c.k, it.k0 + 16 * wave, S::ST, strips, it.k1, scales + wave * 512);
   const uint64_t to_v = c.v - c.k;
   const auto dma_k = [&](int j) { return w.dma.of_k(j); };
   const auto dma_v = [&](int j) { return w.dma.of_v(j); };
@@ -1078,25 +1068,45 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
     uint64_t b[2];
     uint32_t to;
   };
-  // Scales of 64 strips, twice: a strip's eight groups of eight keys, those of the lanes' halves apart.  The next 64 strips'
-  // are written R - 1 strips ahead, with a barrier in between.
-  const auto refilled = [&] {
-    const uint32_t at = scales + (ahead.base & 64) * kStripScales;
-    ahead.scales(c, [&](int) { return w.ref; }, [&](int strip, int group, f2 x) {
-      *(SCOOT_LDS f2*)(at + strip * kStripScales + group * (kStripScales / 2) + wave * 8) = x;
-    });
+  // A strip's eight groups of eight keys lie in blocks, of which the lane's half needs the groups 0, 2, 4, 6 or 1, 3, 5, 7.
+  const auto scale_at = [&](int strip, int group) {
+    return scales + (strip & 64) * kStripScales + (strip & 63) * 4 + (2 * group + w.half) * 256;
   };
-  const auto scales_of = [&](int strip) {
-    const uint32_t at = scales + (strip & 127) * kStripScales + w.half * (kStripScales / 2);
-    return [at, &a](int n) {
-      if constexpr (S::SCALED) return *(const SCOOT_LDS f4*)(at + 16 * n);
-      else return a.score_scale;
+  // seen(group): whether some row sees the group.  A block that none sees may have any number for a scale.
+  const auto value_scale = [&](int strip, int group, auto seen) {
+    const float v = *(const SCOOT_LDS float*)(scale_at(strip, group) + 32 * kStripScales);
+    return seen(group) ? v : 0x1p-126f;
+  };
+  const auto scales_of = [&](int strip, auto seen, bool two) {
+    return [=, &a](int n) {
+      if constexpr (S::SCALED) {
+        typename Tile32<S>::Scale r;
+        r.two = two;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          r.x[2 * i] = key_scale(a.score_scale, *(const SCOOT_LDS float*)scale_at(strip, 2 * n + i));
+          r.x[2 * i + 1] = value_scale(strip, 2 * n + i, seen);
+        }
+        return r;
+      } else {
+        return a.score_scale;
+      }
     };
+  };
+  const auto refer = [&](int strip, auto seen) {
+    return w.refer(value_scale(strip, 0, seen), value_scale(strip, 1, seen), value_scale(strip, 2, seen), value_scale(strip, 3, seen));
+  };
+  const auto all_seen = [](int) { return true; };
+  // A strip that every row sees whole.
+  const auto whole = [&](int strip, uint32_t at, auto load) {
+    bool two = true;
+    if constexpr (S::SCALED) two = refer(strip, all_seen);
+    w.strip(at, at + kHalf, scales_of(strip, all_seen, two), load);
   };
   auto next = [&](int strip) {
     Next n;
     n.to = lds + (strip % R) * S::kStrip + wave * 16 * S::RB;
-    ahead.get(c, strip, n.b, refilled);
+    ahead.get(c, strip, n.b);
     return n;
   };
   auto part = [&](const Next& n, int i) {
@@ -1117,10 +1127,6 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
   // The waves' first addresses tell of their entries.
   const bool holes = strips <= 64 ? any_wave<kWaves>(ahead.holes, flag) : any_holes<kWaves>(a, it, flag);
   settle();
-  if constexpr (S::SCALED) {
-    w.ref = largest_exponent(a, it, head, flag);
-    refilled();
-  }
   int u0, u1;
   w.see.whole(it, strips, S::ST, holes, u0, u1);
 
@@ -1140,12 +1146,12 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
           turn(strip);
           const Next n = next(strip + R - 1);
           const uint32_t at = lds + (strip % R) * S::kStrip;
-          w.strip(at, at + kHalf, scales_of(strip), [&](int i) { part(n, i); });
+          whole(strip, at, [&](int i) { part(n, i); });
         }
         for (; strip < u1; ++strip) {
           turn(strip);
           const uint32_t at = lds + (strip % R) * S::kStrip;
-          w.strip(at, at + kHalf, scales_of(strip), [](int) {});
+          whole(strip, at, [](int) {});
         }
         __builtin_amdgcn_s_setprio(0);
       } else {
@@ -1153,21 +1159,24 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
         if (strip + R - 1 < strips) load(strip + R - 1);
         const uint32_t at = lds + (strip % R) * S::kStrip;
         const int key0 = it.k0 + strip * S::ST;
-        if (key0 <= w.see.hi_max)
-          w.template strip_seen<decltype(finite)::value>(at, at + kHalf, scales_of(strip), key0,
-                                                         [&](int key) { return holes ? c.holes(key) : 0; });
+        if (key0 <= w.see.hi_max) {
+          const auto holes_of = [&](int key) { return holes ? c.holes(key) : 0; };
+          int none = 0;  // the strip's groups that have no block
+          if constexpr (S::SCALED) none = holes_of(key0) | holes_of(key0 + 32) << 4;
+          const auto seen = [&, none](int group) {
+            return w.see.any_of(key0 + 16 * group + 8 * w.half) && !(none >> (2 * group + w.half) & 1);
+          };
+          if constexpr (S::SCALED) refer(strip, seen);
+          w.template strip_seen<decltype(finite)::value>(at, at + kHalf, scales_of(strip, seen, false), key0, holes_of);
+        }
         ++strip;
       }
     }
   };
   pass(std::false_type{});
   if (any_wave<kWaves>(w.spoilt(), flag)) {
-    ahead.start(c, c.k, it.k0 + 16 * wave, S::ST, strips, it.k1, it.seen);
+    ahead.start(c, c.k, it.k0 + 16 * wave, S::ST, strips, it.k1, scales + wave * 512);
     begin();
-    if constexpr (S::SCALED) {
-      settle();
-      refilled();
-    }
     pass(std::true_type{});
     w.add_lost(c, it.k0, u0 < u1 ? it.k0 + u0 * S::ST : it.k1);  // the strips that went through the mask
     if (u0 < u1) w.add_lost(c, it.k0 + u1 * S::ST, it.k1);
@@ -1196,7 +1205,7 @@ struct Tile16 {
   T8 q[KS];
   f4 o[DT];
   float m, l;
-  int ref = 0;  // as Tile32's, but it may grow
+  int ref = 0;  // as Tile32's
   int koff[KN];
   // LDS offsets of V's reads; for 8-bit heads of 256, which would have sixteen, the first one, of which the others differ
   // by some bits.
@@ -1298,8 +1307,9 @@ struct Tile16 {
   // As Tile32::weigh() and moderate(); a lane's keys are of one block, the fraction of whose values' scale is f.
   __device__ __forceinline__ W8 weights(const f4 (&s)[2], float scale, float f) {
     float add = 0.0f;
+    const float more = S::SCALED ? __builtin_amdgcn_logf(f) : 0.0f;
     const auto score = [&](int i) { return s[i / 4][i % 4]; };
-    W8 w = eight_weights<W, false, S::SCALED>(score, scale, m, 0.0f, f, add);
+    W8 w = eight_weights<W, false>(score, scale, S::SCALED ? m - more : m, 0.0f, add);
     if (__builtin_amdgcn_ballot_w64(!(add <= kMost))) {
       float x = s[0][0];
 #pragma unroll
@@ -1326,14 +1336,20 @@ struct Tile16 {
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[d][i] *= less;
       add = 0.0f;
-      w = eight_weights<W, true, S::SCALED>(score, scale, m, moves ? kLimit : INFINITY, f, add);
+      w = eight_weights<W, true>(score, scale, S::SCALED ? m - more : m, moves ? kLimit : INFINITY, add);
     }
     l += S::SCALED ? add * __builtin_amdgcn_rcpf(f) : add;
     return w;
   }
 
-  __device__ __forceinline__ void refer(int r) {
-    if (r <= ref) return;
+  // As Tile32's, for the scale of the values of the lane's keys.
+  __device__ __forceinline__ void refer(float v) {
+    if (__builtin_amdgcn_ballot_w64(exponent(v) > ref + kAboveReference) == 0) return;
+    int r = exponent(v);
+    auto sw = __builtin_amdgcn_permlane32_swap(r, r, false, false);
+    r = max((int)sw[0], (int)sw[1]);
+    sw = __builtin_amdgcn_permlane16_swap(r, r, false, false);
+    r = uniform(max((int)sw[0], (int)sw[1]));
     const float f = to_reference(ref, r);
     ref = r;
 #pragma unroll
@@ -1406,8 +1422,8 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
   struct Base {
     uint64_t b[4];
   };
-  Ahead<S, 4> ahead;  // its strips: every W-th one
-  ahead.start(c, c.k, it.k0 + 32 * wave, 32 * W, (strips - wave + W - 1) / W, it.k1, it.seen);
+  Ahead<S, 4, false> ahead;  // its strips: every W-th one
+  ahead.start(c, c.k, it.k0 + 32 * wave, 32 * W, (strips - wave + W - 1) / W, it.k1, scales + wave * kWaveScales);
   const auto dma_k = [&](int j) { return w.dma.of_k(j); };
   const auto dma_v = [&](int j) { return w.dma.of_v(j); };
   auto load_k = [&](const Base& b) {
@@ -1420,21 +1436,10 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
     load16<S>(dma_v, vat + 16 * S::RB, to_v + b.b[2], to_v + b.b[3]);
   };
 
-  // Scales of the wave's next 64 strips: its own, so it waits for no other.
-  const uint32_t scale_at = scales + wave * kWaveScales;
-  const auto refilled = [&] {
-    const auto refer = [&](int top) {
-#pragma unroll
-      for (int o = 1; o < 64; o *= 2) top = max(top, __shfl_xor(top, o));
-      w.refer(uniform(top));
-      return w.ref;
-    };
-    ahead.scales(c, refer, [&](int strip, int group, f2 x) { *(SCOOT_LDS f2*)(scale_at + strip * 32 + group * 8) = x; });
-  };
   Base b;
   auto begin = [&] {
     if (wave >= strips) return;
-    ahead.get(c, 0, b.b, refilled);
+    ahead.get(c, 0, b.b);
     load_k(b);
     load_v(b);
   };
@@ -1444,10 +1449,6 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
   bool holes = ahead.holes;
   if (strips > 64 * W) holes = any_holes<W>(a, it, flag);
   settle();
-  if constexpr (S::SCALED) {
-    w.clear();
-    refilled();
-  }
   int u0, u1;  // strips seen whole by every row
   w.see.whole(it, strips, 32, holes, u0, u1);
 
@@ -1456,26 +1457,34 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
     constexpr bool kMasked = decltype(masked)::value;
     const bool more = strip + W < strips;
     const int key0 = it.k0 + strip * 32;
+    int none = 0;  // groups that have no block
+    if constexpr (kMasked && S::SCALED) none = holes ? c.holes(key0) : 0;
     wait_vm<2 * S::NJ>();  // the keys, not the values behind them
     f4 s[2];
-    f2 scale = {a.score_scale, 0.0f};
-    const int ref = w.ref;
-    if constexpr (S::SCALED) scale = *(const SCOOT_LDS f2*)(scale_at + (strip / W & 63) * 32 + w.quad * 8);
+    float scale = a.score_scale, value = 1.0f;
+    if constexpr (S::SCALED) {
+      const uint32_t at = scales + wave * kWaveScales + w.quad * 256 + (strip / W & 63) * 4;
+      scale = key_scale(scale, *(const SCOOT_LDS float*)at);
+      value = *(const SCOOT_LDS float*)(at + 16 * kStripScales);
+      // A block that no row sees may have any number for a scale.
+      if (kMasked && !(w.see.any_of(key0 + 8 * w.quad) && !(none >> w.quad & 1))) value = 0x1p-126f;
+      w.refer(value);
+    }
     w.scores(kat, s);
     wait_lds();
     if (more) {
-      ahead.get(c, strip / W + 1, b.b, refilled);
+      ahead.get(c, strip / W + 1, b.b);
       load_k(b);
     }
     if (kMasked) w.mask(s, key0, holes ? c.holes(key0) : 0);
-    const typename Tile16<S>::W8 p = w.weights(s, scale.x, fraction(scale.y));
+    const typename Tile16<S>::W8 p = w.weights(s, scale, fraction(value));
     if (more) wait_vm<2 * S::NJ>();
     else wait_vm<0>();
     const auto product = [&](auto... by) {
       if (kMasked) w.template product_seen<decltype(finite)::value>(vat, p, key0, by...);
       else w.product(vat, p, by...);
     };
-    if constexpr (S::SCALED) product(power(scale.y) * to_reference(ref, w.ref));
+    if constexpr (S::SCALED) product(power_at(value, w.ref));
     else product();
     wait_lds();
     if (more) load_v(b);
@@ -1494,12 +1503,8 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
   };
   pass(std::false_type{});
   if (w.spoilt()) {
-    ahead.start(c, c.k, it.k0 + 32 * wave, 32 * W, (strips - wave + W - 1) / W, it.k1, it.seen);
+    ahead.start(c, c.k, it.k0 + 32 * wave, 32 * W, (strips - wave + W - 1) / W, it.k1, scales + wave * kWaveScales);
     begin();
-    if constexpr (S::SCALED) {
-      settle();
-      refilled();
-    }
     pass(std::true_type{});
     for (strip = wave; strip < strips; strip += W)
       if (strip < u0 || strip >= u1) w.add_lost(c, it.k0 + strip * 32, min(it.k0 + strip * 32 + 32, it.k1));

@@ -55,15 +55,17 @@ def _reference(c, s):
 
 
 def _bound(c, s, ref):
-    """The oracle's bound with what scales add: a score's scale is a product of two floats (2^-24 of the score, twice), a
-    value's fraction and its reciprocal are off by 2^-22 of the weight; values at less than 2^-15 of the largest scale are
-    off by at most 2^-25 * 2^e for the largest scale's exponent e, less than 2^-25 of the largest scale, as its weights are
-    (those below the normal range by 2^-25 of the largest times 448 of these)."""
+    """The oracle's bound with what scales add.  A score's scale is a product of two floats (2^-24 of the score, twice).  A
+    value's scale is 2^e f; log2 f goes into the weight's exponent beside m, which is log2(e) times the largest score, less 6:
+    rounded to 2^-24 of that, (1.45 reach + 8) 2^-24, times ln 2 of the weight; the logarithm itself and the reciprocal of f are
+    off by 2^-22: (3 * 2^-24 reach + 2^-21) in all.  Values at less than 2^-15 of the largest scale are off by at most
+    2^-25 * 2^6 * 2^e for the largest scale's exponent e (it may be up to 2^6 above the reference), less than 2^-25 of 448 times
+    the largest scale, and so are weights below the normal range."""
     out, spread, reach = ref
     vs = f64(s["vs"])
     top = 448.0 * max(float(vs[np.isfinite(vs) & (vs > 0) & (vs < 1e30)].max()), 1e-30)
     keys = max(a + n for a, n in c["lens"])
-    more = (2 * 2.0 ** -24 * reach[..., None] + 2.0 ** -22) * (spread + np.abs(out)) + 2.0 ** -25 * top
+    more = (3 * 2.0 ** -24 * reach[..., None] + 2.0 ** -21) * (spread + np.abs(out)) + 2.0 ** -25 * top
     return kv.attention_bound(out, spread, reach, keys, c["d"], BITS[c["kind"]], 11, top) + more
 
 
@@ -147,14 +149,14 @@ def test_blocks_of_zeros_count():
 
 @pytest.mark.parametrize("tokens,d,length", [(1, 64, 700), (4, 128, 5000), (40, 64, 300), (40, 256, 300), (40, 128, 4000)])
 def test_large_scores_have_a_softmax(tokens, d, length):
-    """Scores up to the largest float over blocks of unlike scales: every third key has the score x, the others 1.5 x (x
-    negative) or 0.5 x, so the result is the mean of every third value, up to the rounding of the weights (2^-11), of the
-    result (2^-8) and of sums in float; the fraction of a value's scale is a float's."""
+    """Scores up to the largest float over blocks of unlike scales, powers of two: every third key has the score x, the others
+    1.5 x (x negative) or 0.5 x, so the result is the mean of every third value, up to the rounding of the weights (2^-11), of
+    the result (2^-8) and of sums in float.  (Other scales' fractions are lost beside such scores, as the interface says.)"""
     say("scaled, large scores", tokens, d, length)
     blocks, kind = -(-length // 16), torch.bfloat16
     g = torch.Generator(device=DEV).manual_seed(1)
     codes = torch.randn(blocks, 1, 16, d, generator=g, device=DEV).mul_(50).clamp_(-448, 448).to(torch.float8_e4m3fn)
-    vs = torch.randn(blocks, 1, generator=g, device=DEV).mul_(2).exp2_()
+    vs = torch.randint(-5, 6, (blocks, 1), generator=g, device=DEV).float().exp2_()
     ks = torch.randint(-3, 4, (blocks, 1), generator=g, device=DEV).float().exp2_()
     third = torch.arange(blocks * 16, device=DEV) % 3 == 0
     v = (codes.double() * vs[:, :, None, None].double()).view(-1, d)
