@@ -39,15 +39,17 @@
 // block, so its scale a of the keys takes the place of the one scale in their
 // exponents.  The scale b of the values is 2^e f, 1 <= f < 2: the values are
 // widened to half precision times 2^(e - r), which the conversion does by the
-// way, with r near the largest e so far; log2 f goes into the exponents beside
-// m, and l adds the weights over f.  So m, the weights and l are those of one
-// scale, whatever the scores, and powers of two cost next to nothing; values
-// lose nothing down to 2^-15 of the reference, and 2^-25 of it below that.
-// Products of weights and f instead would be exact beside any score, too, and
-// cost 13% (one chunk over 30,000 keys, heads of 128: 516 us with one scale, 583).
+// way, with r the largest e so far (or near it); log2 f goes into the exponents
+// beside m, and l adds the weights over f.  So m, the weights and l are those of
+// one scale, whatever the scores, and a weight costs nothing more; values lose
+// nothing down to 2^-15 of the reference, and 2^-25 of it below that.  (Weights
+// times f instead would be exact beside any score for any f, not for powers of
+// two alone; a product per weight costs 13%.)
 // The scales of 64 strips at a time go straight from memory into LDS, where
 // their addresses are made (through registers: 40 more, and a wave per SIMD less
-// for few rows of 64 dimensions).
+// for few rows of 64 dimensions).  Tiles make of them, once for 64 strips, what
+// a strip takes as it is: made strip by strip, a chunk over 30,000 keys took 545
+// us (heads of 128) and 567 (192), so 515 and 486, with one scale 494 and 474.
 //
 // Registers decide the waves per SIMD: three for tiles of 64 dimensions, two for
 // 128, one for 192 and 256, where o and q take 144 and 192 of a lane's 512.  A
@@ -90,8 +92,9 @@ constexpr float kMost = 16384.0f;            // m moves once a lane's weights of
 constexpr float kBelow = 6.0f;               // to this much below their largest: half precision holds 64 as well as 1, and
                                              // weights down to 2^-30 of the largest, which counts where many keys are small
 
-constexpr int kStripScales = 64;          // bytes of the scales of a tile's strip,
-constexpr int kWaveScales = 64 * 4 * 8;   // and of a wave's 64 strips
+constexpr int kStripScales = 96;          // bytes of the scales of a tile's strip: of keys, of values, their logarithms;
+constexpr int kGroupScales = 256;         // of a group of eight keys, 64 strips;
+constexpr int kWaveScales = 64 * 4 * 8;   // of a wave's own 64 strips, without logarithms
 
 constexpr float kLimit = 14.0f;              // of a weight's exponent where it moved: no other weight is above kMost
 
@@ -385,9 +388,9 @@ struct Ahead {
       hi[j] = (uint32_t)(at >> 32);
       if constexpr (S::SCALED) {
         const uint64_t of = (uint64_t)(e[j] < c.num_blocks ? e[j] : 0) * c.heads * 4;
-        const uint32_t to = scales + (TWICE ? (strip & 64) * kStripScales : 0) + j * 256;
+        const uint32_t to = scales + (TWICE ? (strip & 64) * kStripScales : 0) + j * kGroupScales;
         load_lds_dword(to, c.k_scales + of);
-        load_lds_dword(to + (TWICE ? 32 : 16) * kStripScales, c.v_scales + of);
+        load_lds_dword(to + (TWICE ? 8 : 4) * kGroupScales, c.v_scales + of);
       }
     }
     holes = __builtin_amdgcn_ballot_w64(hole) != 0;
@@ -710,7 +713,9 @@ struct Tile32 {
   // `between`, that runs while the matrix unit is busy: left alone, the compiler
   // waits for each read and keeps products and weights apart.
   static constexpr int KR = S::F8 ? KS / 2 : KS;  // reads of K for 32 keys
-  static constexpr int kAheadK = KR < kReadsAhead ? KR : kReadsAhead;
+  // Fewer where scales take the registers (heads of 256: 409 us, 452 with four).
+  static constexpr int kAheadV = S::SCALED && S::D == 256 ? 2 : kReadsAhead;
+  static constexpr int kAheadK = KR < kAheadV ? KR : kAheadV;
   static constexpr int KP = KS;      // products per 32 keys: of the scores,
   static constexpr int VP = 2 * DT;  // and of the values
   typedef typename std::conditional<S::F8, i4, T8>::type Piece;
@@ -808,24 +813,16 @@ struct Tile32 {
     float add[S::SCALED ? 2 : 1];  // of each block's keys, or of all
     __device__ __forceinline__ float all() const { return S::SCALED ? add[0] + add[S::SCALED] : add[0]; }
   };
-  // What the scores of 32 keys are multiplied by: one number, or that and the values' scale of a lane's two blocks.
-  struct Scales {
-    f4 x;
-    bool two;  // the values' scales are powers of two, in all lanes
-    __device__ __forceinline__ float operator[](int i) const { return x[i]; }
-  };
-  typedef typename std::conditional<S::SCALED, Scales, float>::type Scale;
+  // What the scores of 32 keys are multiplied by: one number, or that and log2 f of the values' scale of a lane's two blocks.
+  typedef typename std::conditional<S::SCALED, f4, float>::type Scale;
   template <bool LIMITED = false>
   __device__ __forceinline__ void weigh(const f16v& s, Scale scale, Weights& x, int i, int n, float limit = 0.0f) const {
     const int from = 2 * (8 * i / n), to = 2 * (8 * (i + 1) / n);
     if constexpr (S::SCALED) {
       if (i == 0) {
         x.add[0] = x.add[1] = 0.0f;
-        x.less[0] = x.less[1] = -m;
-        if (!scale.two) {
-          x.less[0] += __builtin_amdgcn_logf(fraction(scale[1]));
-          x.less[1] += __builtin_amdgcn_logf(fraction(scale[3]));
-        }
+        x.less[0] = scale[1] - m;
+        x.less[1] = scale[3] - m;
       }
 #pragma unroll
       for (int j = from; j < to; ++j) {
@@ -875,71 +872,65 @@ struct Tile32 {
       }
       weigh<true>(s, scale, w, 0, 1, moves ? kLimit : INFINITY);
     }
-    if constexpr (S::SCALED) {
-      if (!scale.two) {
-        w.add[0] *= __builtin_amdgcn_rcpf(fraction(scale[1]));
-        w.add[1] *= __builtin_amdgcn_rcpf(fraction(scale[3]));
-      }
-    }
-    l += w.all();
+    if constexpr (S::SCALED) l += w.add[0] * __builtin_amdgcn_exp2f(-scale[1]) + w.add[1] * __builtin_amdgcn_exp2f(-scale[3]);
+    else l += w.add[0];
   }
 
-  template <int n, typename F, typename... Scales>
-  __device__ __forceinline__ void product(const Lds& lds, const Weights& w, W8 (&v)[kReadsAhead], F between, const Scales&... scale) {
+  template <int n, typename F, typename... B>
+  __device__ __forceinline__ void product(const Lds& lds, const Weights& w, W8 (&v)[kAheadV], F between, const B&... by) {
 #pragma unroll
     for (int j = 0; j < VP; ++j) {
-      const int i = n * VP + j, next = i + kReadsAhead;
-      o[j % DT] = mfma(v[i % kReadsAhead], w.w[j / DT], o[j % DT]);
-      if (next < 2 * VP) v[i % kReadsAhead] = values(lds, next / DT, next % DT, power_at(scale[next / VP][next / DT % 2 * 2 + 1], ref)...);
+      const int i = n * VP + j, next = i + kAheadV;
+      o[j % DT] = mfma(v[i % kAheadV], w.w[j / DT], o[j % DT]);
+      if (next < 2 * VP) v[i % kAheadV] = values(lds, next / DT, next % DT, by[next / DT]...);
       between(j);
       __builtin_amdgcn_sched_barrier(0);
     }
   }
-  // The values' scales of the lane's four blocks of a strip, before their first use: the reference moves if they are far
-  // above it.  Whether they are all powers of two, in all lanes.
-  __device__ __forceinline__ bool refer(float a, float b, float c, float d) {
-    const int e = max(max(exponent(a), exponent(b)), max(exponent(c), exponent(d)));
-    if (__builtin_amdgcn_ballot_w64(e > ref + kAboveReference)) {
-      const auto sw = __builtin_amdgcn_permlane32_swap(e, e, false, false);
-      const int r = uniform(max((int)sw[0], (int)sw[1]));
-      const float f = to_reference(ref, r);
-      ref = r;
+  // What o is times is 2^r from here on, if that is larger than before.
+  __device__ __forceinline__ void refer(int r) {
+    if (r <= ref) return;
+    const float f = to_reference(ref, r);
+    ref = r;
 #pragma unroll
-      for (int d = 0; d < DT; ++d) {
+    for (int d = 0; d < DT; ++d) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[d][i] *= f;
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      for (int i = 0; i < 16; ++i) o[d][i] *= f;
+      __builtin_amdgcn_sched_barrier(0);
     }
-    return __builtin_amdgcn_ballot_w64(((__float_as_uint(a) | __float_as_uint(b) | __float_as_uint(c) | __float_as_uint(d)) & 0x7fffffu) != 0) == 0;
   }
   // A strip that every row sees whole.  Of the two halves of 64 keys the first one's weights are made between the
   // second one's scores, and the second one's between the first one's values; load(i), i < KP, the i-th part of a
   // strip's loads, goes between the first one's scores.
-  // scales: of the strip's two halves, by their numbers.
+  // scales: one number, or those of the lane's four blocks.
   template <typename F, typename L>
   __device__ __forceinline__ void strip(uint32_t kat, uint32_t vat, F scales, L load) {
     const auto nothing = [](int) {};
     f16v s[2];
     Weights p[2];
-    W8 v[kReadsAhead];
+    W8 v[kAheadV];
     Keys x = keys(kat);
-    scores<0>(x, s[0], load);
-    const Scale scale = scales(0);
-    const Lds lds = values_at(vat);
-    scores<1>(x, s[1], [&](int i) { weigh(s[0], scale, p[0], i, KP); });
     if constexpr (S::SCALED) {
+      scores<0>(x, s[0], load);
+      const Scale first = {scales.key(0), scales.log(0), scales.key(1), scales.log(1)};
+      const float by[4] = {scales.power(0), scales.power(1), scales.power(2), scales.power(3)};
+      const Lds lds = values_at(vat);
+      scores<1>(x, s[1], [&](int i) { weigh(s[0], first, p[0], i, KP); });
 #pragma unroll
-      for (int i = 0; i < kReadsAhead; ++i) v[i] = values(lds, i / DT, i % DT, power_at(scale[i / DT * 2 + 1], ref));
-      const Scale both[2] = {scale, scales(1)};
-      moderate(s[0], scale, p[0]);
+      for (int i = 0; i < kAheadV; ++i) v[i] = values(lds, i / DT, i % DT, by[i / DT]);
+      const Scale second = {scales.key(2), scales.log(2), scales.key(3), scales.log(3)};
+      moderate(s[0], first, p[0]);
       __builtin_amdgcn_sched_barrier(0);
-      product<0>(lds, p[0], v, [&](int i) { weigh(s[1], both[1], p[1], i, VP); }, both);
-      moderate(s[1], both[1], p[1]);
-      product<1>(lds, p[1], v, nothing, both);
+      product<0>(lds, p[0], v, [&](int i) { weigh(s[1], second, p[1], i, VP); }, by);
+      moderate(s[1], second, p[1]);
+      product<1>(lds, p[1], v, nothing, by);
     } else {
+      scores<0>(x, s[0], load);
+      const float scale = scales;
+      const Lds lds = values_at(vat);
+      scores<1>(x, s[1], [&](int i) { weigh(s[0], scale, p[0], i, KP); });
 #pragma unroll
-      for (int i = 0; i < kReadsAhead; ++i) v[i] = values(lds, i / DT, i % DT);
+      for (int i = 0; i < kAheadV; ++i) v[i] = values(lds, i / DT, i % DT);
       moderate(s[0], scale, p[0]);
       __builtin_amdgcn_sched_barrier(0);
       product<0>(lds, p[0], v, [&](int i) { weigh(s[1], scale, p[1], i, VP); });
@@ -963,7 +954,9 @@ struct Tile32 {
       if (n && !two) break;
       mask(s[n], key0 + 32 * n, holes(key0 + 32 * n));
       Weights p;
-      const Scale scale = scales(n);
+      Scale scale;
+      if constexpr (S::SCALED) scale = f4{scales.key(2 * n), scales.log(2 * n), scales.key(2 * n + 1), scales.log(2 * n + 1)};
+      else scale = scales;
       weigh(s[n], scale, p, 0, 1);
       moderate(s[n], scale, p);
 #pragma unroll
@@ -972,7 +965,7 @@ struct Tile32 {
         for (int d = 0; d < DT; ++d) {
           const int count = see.hi_max + 1 - (key0 + 32 * n + 16 * k + 8 * half);
           W8 v;
-          if constexpr (S::SCALED) v = only_seen(values(lds, 2 * n + k, d, power_at(scale[2 * k + 1], ref)), count);
+          if constexpr (S::SCALED) v = only_seen(values(lds, 2 * n + k, d, scales.power(2 * n + k)), count);
           else v = only_seen(values(lds, 2 * n + k, d), count);
           if constexpr (FINITE) v = only_finite<W>(v);
           o[d] = mfma(v, p.w[k], o[d]);
@@ -1047,6 +1040,17 @@ struct Tile32 {
   }
 };
 
+// Scales of a strip's blocks in LDS, by the number of the lane's group of eight keys (of four).
+struct BlockScales {
+  uint32_t at;
+  __device__ __forceinline__ float get(int group, int kind) const {
+    return *(const SCOOT_LDS float*)(at + 2 * group * kGroupScales + kind * 8 * kGroupScales);
+  }
+  __device__ __forceinline__ float key(int group) const { return get(group, 0); }    // scores are multiplied by this,
+  __device__ __forceinline__ float power(int group) const { return get(group, 1); }  // values by this,
+  __device__ __forceinline__ float log(int group) const { return get(group, 2); }    // which leaves 2 to this
+};
+
 template <typename S, int R>
 __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it, int head, uint32_t lds, int* flag, uint32_t scales,
                                             int64_t slot, float* parts, float* stats) {
@@ -1060,7 +1064,7 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
 
   // A strip's loads in groups of 16 keys of K or V; every wave takes its share.
   Ahead<S, 2, true> ahead;
-  ahead.start(c, c.k, it.k0 + 16 * wave, S::ST, strips, it.k1, scales + wave * 512);
+  ahead.start(c, c.k, it.k0 + 16 * wave, S::ST, strips, it.k1, scales + wave * 2 * kGroupScales);
   const uint64_t to_v = c.v - c.k;
   const auto dma_k = [&](int j) { return w.dma.of_k(j); };
   const auto dma_v = [&](int j) { return w.dma.of_v(j); };
@@ -1068,41 +1072,14 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
     uint64_t b[2];
     uint32_t to;
   };
-  // A strip's eight groups of eight keys lie in blocks, of which the lane's half needs the groups 0, 2, 4, 6 or 1, 3, 5, 7.
-  const auto scale_at = [&](int strip, int group) {
-    return scales + (strip & 64) * kStripScales + (strip & 63) * 4 + (2 * group + w.half) * 256;
+  const auto scales_of = [&](int strip) {
+    if constexpr (S::SCALED)
+      return BlockScales{scales + (strip & 64) * kStripScales + (strip & 63) * 4 + w.half * kGroupScales};
+    else
+      return a.score_scale;
   };
-  // seen(group): whether some row sees the group.  A block that none sees may have any number for a scale.
-  const auto value_scale = [&](int strip, int group, auto seen) {
-    const float v = *(const SCOOT_LDS float*)(scale_at(strip, group) + 32 * kStripScales);
-    return seen(group) ? v : 0x1p-126f;
-  };
-  const auto scales_of = [&](int strip, auto seen, bool two) {
-    return [=, &a](int n) {
-      if constexpr (S::SCALED) {
-        typename Tile32<S>::Scale r;
-        r.two = two;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          r.x[2 * i] = key_scale(a.score_scale, *(const SCOOT_LDS float*)scale_at(strip, 2 * n + i));
-          r.x[2 * i + 1] = value_scale(strip, 2 * n + i, seen);
-        }
-        return r;
-      } else {
-        return a.score_scale;
-      }
-    };
-  };
-  const auto refer = [&](int strip, auto seen) {
-    return w.refer(value_scale(strip, 0, seen), value_scale(strip, 1, seen), value_scale(strip, 2, seen), value_scale(strip, 3, seen));
-  };
-  const auto all_seen = [](int) { return true; };
   // A strip that every row sees whole.
-  const auto whole = [&](int strip, uint32_t at, auto load) {
-    bool two = true;
-    if constexpr (S::SCALED) two = refer(strip, all_seen);
-    w.strip(at, at + kHalf, scales_of(strip, all_seen, two), load);
-  };
+  const auto whole = [&](int strip, uint32_t at, auto load) { w.strip(at, at + kHalf, scales_of(strip), load); };
   auto next = [&](int strip) {
     Next n;
     n.to = lds + (strip % R) * S::kStrip + wave * 16 * S::RB;
@@ -1130,6 +1107,39 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
   int u0, u1;
   w.see.whole(it, strips, S::ST, holes, u0, u1);
 
+  // Before the first of 64 strips: their scales have landed and become what the strips take, and the reference is up to
+  // them.  Every wave does that for the groups of eight keys whose scales it fetched, a lane for a strip.
+  const auto prepare = [&](int strip) {
+    const int seen = a.window > 0 ? (int)clamp64(it.pos0 + it.row0 / (a.num_heads / a.num_kv_heads) - a.window + 1, 0, it.k1) : 0;
+    const int mine = strip + (threadIdx.x & 63);
+    const uint32_t at = scales + (strip & 64) * kStripScales + 2 * wave * kGroupScales + (threadIdx.x & 63) * 4;
+    const auto in_lds = [&](int kind, int j) { return (SCOOT_LDS float*)(at + (8 * kind + j) * kGroupScales); };
+    wait_vm<0>();
+    float b[2];
+    int top = 0;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      // A block that no row sees may have any number for a scale, and does not count.
+      const int key = it.k0 + mine * S::ST + 16 * wave + 8 * j, e = key >> c.shift;
+      bool real = mine < strips && key < it.k1 && key + 8 > seen;
+      if (holes && real) real = (uint32_t)c.entries[e < c.last ? e : c.last] < c.num_blocks;
+      b[j] = real ? *in_lds(1, j) : 0x1p-126f;
+      top = max(top, exponent(b[j]));
+    }
+#pragma unroll
+    for (int i = 1; i < 64; i *= 2) top = max(top, __shfl_xor(top, i));
+    if ((threadIdx.x & 63) == 0) flag[wave] = top;
+    settle();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    w.refer(uniform(max(max(flag[0], flag[1]), max(flag[2], flag[3]))));
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      *in_lds(0, j) = key_scale(a.score_scale, *in_lds(0, j));
+      *in_lds(1, j) = power_at(b[j], w.ref);
+      *in_lds(2, j) = __builtin_amdgcn_logf(fraction(b[j]));
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  };
   auto turn = [&](int strip) {
     // This strip has landed, for every wave, and everyone is done with the one before, whose place the next load takes.
     if (R > 2 && strip + R - 2 < strips) wait_vm<(R - 2) * 2 * S::NJ>();
@@ -1140,15 +1150,19 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
     w.clear();
     int strip = 0;
     while (strip < strips) {
+      if constexpr (S::SCALED) {
+        if ((strip & 63) == 0) prepare(strip);
+      }
+      const int scaled = strip | 63;  // the last strip whose scales are there
       if (strip >= u0 && strip < u1) {
         __builtin_amdgcn_s_setprio(1);  // over waves that wait or mask: a late chunk of 64-dimensional heads 566 -> 559 us
-        for (; strip < min(u1, strips - (R - 1)); ++strip) {
+        for (; strip < min(u1, strips - (R - 1)) && (!S::SCALED || strip <= scaled); ++strip) {
           turn(strip);
           const Next n = next(strip + R - 1);
           const uint32_t at = lds + (strip % R) * S::kStrip;
           whole(strip, at, [&](int i) { part(n, i); });
         }
-        for (; strip < u1; ++strip) {
+        for (; strip < u1 && (!S::SCALED || strip <= scaled); ++strip) {
           turn(strip);
           const uint32_t at = lds + (strip % R) * S::kStrip;
           whole(strip, at, [](int) {});
@@ -1160,14 +1174,8 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
         const uint32_t at = lds + (strip % R) * S::kStrip;
         const int key0 = it.k0 + strip * S::ST;
         if (key0 <= w.see.hi_max) {
-          const auto holes_of = [&](int key) { return holes ? c.holes(key) : 0; };
-          int none = 0;  // the strip's groups that have no block
-          if constexpr (S::SCALED) none = holes_of(key0) | holes_of(key0 + 32) << 4;
-          const auto seen = [&, none](int group) {
-            return w.see.any_of(key0 + 16 * group + 8 * w.half) && !(none >> (2 * group + w.half) & 1);
-          };
-          if constexpr (S::SCALED) refer(strip, seen);
-          w.template strip_seen<decltype(finite)::value>(at, at + kHalf, scales_of(strip, seen, false), key0, holes_of);
+          w.template strip_seen<decltype(finite)::value>(at, at + kHalf, scales_of(strip), key0,
+                                                         [&](int key) { return holes ? c.holes(key) : 0; });
         }
         ++strip;
       }
@@ -1175,7 +1183,7 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
   };
   pass(std::false_type{});
   if (any_wave<kWaves>(w.spoilt(), flag)) {
-    ahead.start(c, c.k, it.k0 + 16 * wave, S::ST, strips, it.k1, scales + wave * 512);
+    ahead.start(c, c.k, it.k0 + 16 * wave, S::ST, strips, it.k1, scales + wave * 2 * kGroupScales);
     begin();
     pass(std::true_type{});
     w.add_lost(c, it.k0, u0 < u1 ? it.k0 + u0 * S::ST : it.k1);  // the strips that went through the mask
@@ -1461,16 +1469,16 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
     if constexpr (kMasked && S::SCALED) none = holes ? c.holes(key0) : 0;
     wait_vm<2 * S::NJ>();  // the keys, not the values behind them
     f4 s[2];
+    w.scores(kat, s);
     float scale = a.score_scale, value = 1.0f;
     if constexpr (S::SCALED) {
-      const uint32_t at = scales + wave * kWaveScales + w.quad * 256 + (strip / W & 63) * 4;
+      const uint32_t at = scales + wave * kWaveScales + w.quad * kGroupScales + (strip / W & 63) * 4;
       scale = key_scale(scale, *(const SCOOT_LDS float*)at);
-      value = *(const SCOOT_LDS float*)(at + 16 * kStripScales);
+      value = *(const SCOOT_LDS float*)(at + 4 * kGroupScales);
       // A block that no row sees may have any number for a scale.
       if (kMasked && !(w.see.any_of(key0 + 8 * w.quad) && !(none >> w.quad & 1))) value = 0x1p-126f;
       w.refer(value);
     }
-    w.scores(kat, s);
     wait_lds();
     if (more) {
       ahead.get(c, strip / W + 1, b.b);
