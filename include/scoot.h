@@ -800,8 +800,9 @@ int scoot_kv_append(const void* q, int num_heads, int64_t q_token_stride, int64_
 
 /* scoot_kv_attention over an 8-bit cache with a scale for every block and
  * head, k_scales and v_scales [num_blocks][num_kv_heads], positive and from
- * 2^-64 to 2^64 (a scale that is not makes results of the rows that see its
- * block undefined, and no others):
+ * 2^-64 to 2^64.  A scale that is not makes the results of the requests that
+ * see its block undefined for its head's queries; blocks that no query of a
+ * request sees may have anything:
  *   out = sum_t softmax_t(scale * k_scales[b_t] * q . k_t) * v_scales[b_t] * v_t
  * A power of two as the scale of values is exact; another one is off by up to
  * 2^-24 of the row's largest score, as scores themselves are.  The workspace is scoot_kv_attention_workspace's. */
