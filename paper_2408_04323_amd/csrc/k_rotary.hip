@@ -169,7 +169,9 @@ struct Unit {
       }
     }
   }
-  __device__ __forceinline__ void store_f8(uint8_t* row, const float (&y)[2][N], const Quotient& by) const {
+  // by: a value as it is stored, not above 448 but for less than half a step.
+  template <typename F>
+  __device__ __forceinline__ void store_f8(uint8_t* row, const float (&y)[2][N], F by) const {
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
       const int e = p ? e1 : e0;
@@ -182,6 +184,10 @@ struct Unit {
     }
   }
 };
+
+// i / pairs for rows below 600 and pairs up to 512: the quotient is off by less than 2^-22 of itself, and i + 1/2 is at least
+// 1 / (2 pairs) of a row away from the next one.
+__device__ __forceinline__ int row_of(int i, int pairs) { return (int)(((float)i + 0.5f) * __builtin_amdgcn_rcpf((float)pairs)); }
 
 constexpr int kThreads = 256;
 
@@ -239,8 +245,9 @@ __device__ __forceinline__ void rows_part(const KvAppendArgs& a, const Rows& w, 
     if (u0 == 0 && pairs) {
 #pragma unroll 1
       for (int i = tid; i < w.tokens * pairs; i += kThreads) {
-        const int64_t ti = first + i / pairs;
-        if (ti < a.num_tokens) cs[i] = turn_of((double)a.positions[ti] * a.freqs[i % pairs], a.magnitude, a.reverse);
+        const int row = row_of(i, pairs);
+        if (first + row < a.num_tokens)
+          cs[i] = turn_of((double)a.positions[first + row] * a.freqs[i - row * pairs], a.magnitude, a.reverse);
       }
       __syncthreads();
     }
@@ -355,25 +362,31 @@ __device__ __forceinline__ void store_heads(const KvAppendArgs& a, const Runs& w
   };
   typedef Unit<T, N, IL> U;
   const bool one = w.units <= w.lanes;
-  typename U::Two x = {};  // the last one is kept, and the first one stored
-  float top = 0.0f;
-  if (k.mine) {
+  float y[2][N] = {};  // the last ones are kept, and the first ones stored
+  const auto read = [&](const U& unit, int r) { turned(unit, unit.load(k.row + r * k.step), r, y); };
+  // The largest value, in magnitude, without NaN; without infinities, too, where there are any: these are limited when
+  // stored, and NaN is kept.
+  const auto largest = [&](auto finite) {
+    float top = 0.0f;
+    if (!k.mine) return top;
 #pragma unroll 1
     for (int r = r0; r < n; r += rows)
 #pragma unroll 1
       for (int u = u0; u < w.units; u += w.lanes) {
         const U unit(u, w.units, a.head_dim, a.turned);
-        x = unit.load(k.row + r * k.step);
-        float y[2][N];
-        turned(unit, x, r, y);
+        read(unit, r);
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-          const float p = __builtin_fabsf(y[0][j]), q = __builtin_fabsf(y[1][j]);
-          top = p < INFINITY ? fmaxf(top, p) : top;  // infinities are limited when stored, NaN is kept
-          top = unit.e1 >= 0 && q < INFINITY ? fmaxf(top, q) : top;
+        for (int i = 0; i < N; ++i) {
+          const float p = __builtin_fabsf(y[0][i]), q = unit.e1 >= 0 ? __builtin_fabsf(y[1][i]) : 0.0f;
+          if (decltype(finite)::value) top = fmaxf(top, fmaxf(p < INFINITY ? p : 0.0f, q < INFINITY ? q : 0.0f));
+          else top = fmaxf(top, fmaxf(p, q));
         }
       }
-  }
+    return top;
+  };
+  float top = largest(std::false_type{});
+  bool simple = top < INFINITY;  // none of the lane's values has to be limited
+  if (__builtin_amdgcn_ballot_w64(!simple)) top = largest(std::true_type{});
   for (int o = 1; o < span; o *= 2) top = fmaxf(top, __shfl_xor(top, o));
   if (team) {  // every wave has read the old scale before one writes the new one
     __syncthreads();
@@ -388,16 +401,20 @@ __device__ __forceinline__ void store_heads(const KvAppendArgs& a, const Runs& w
   if (!k.mine) return;
   if (in == 0) *k.scale = scale;
   if (grows) scale_again(k.to, (int64_t)begin * a.head_dim, old / scale, in, lanes);
+  // All values are within the scale, which is a power of two, as a rule: a product then.
+  simple = simple && (__float_as_uint(scale) & 0x7fffffu) == 0 && top <= 448.0f * scale;
+  const bool products = __builtin_amdgcn_ballot_w64(!simple) == 0;
+  const float inverse = 1.0f / scale;
   const Quotient quotient(scale);
 #pragma unroll 1
   for (int r = last; r >= 0; r -= rows)
 #pragma unroll 1
     for (int u = u0; u < w.units; u += w.lanes) {
       const U unit(u, w.units, a.head_dim, a.turned);
-      if (!one || r != last) x = unit.load(k.row + r * k.step);
-      float y[2][N];
-      turned(unit, x, r, y);
-      unit.store_f8(k.to + (a.slots[t + r] & (bs - 1)) * a.head_dim, y, quotient);
+      if (!one || r != last) read(unit, r);
+      uint8_t* to = k.to + (a.slots[t + r] & (bs - 1)) * a.head_dim;
+      if (products) unit.store_f8(to, y, [&](float x) { return x * inverse; });
+      else unit.store_f8(to, y, quotient);
     }
 }
 
@@ -462,8 +479,10 @@ __device__ __forceinline__ void runs_part(const KvAppendArgs& a, const Runs& w, 
       from = __builtin_ctzll(keys);
       const int to = end + __shfl(n, end);
 #pragma unroll 1
-      for (int i = threadIdx.x; i < (to - from) * pairs; i += kThreads)
-        cs[i] = turn_of((double)a.positions[first + from + i / pairs] * a.freqs[i % pairs], a.magnitude, false);
+      for (int i = threadIdx.x; i < (to - from) * pairs; i += kThreads) {
+        const int row = row_of(i, pairs);
+        cs[i] = turn_of((double)a.positions[first + from + row] * a.freqs[i - row * pairs], a.magnitude, false);
+      }
     }
     __syncthreads();
   }

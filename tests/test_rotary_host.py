@@ -98,6 +98,15 @@ def test_attention_with_scales_refuses():
     assert lib().scoot_kv_attention_scaled(*dict(a, num_tokens=0, k_scales=None).values()) == 0
 
 
+def test_the_kernels_way_to_divide_by_the_pairs():
+    """Row i / pairs as (i + 1/2) times a float reciprocal that may be off by one unit: the whole quotient for every number of
+    pairs and every row that a workgroup's cosines and sines have."""
+    for pairs in range(1, 513):
+        i = np.arange(300 * pairs)
+        for by in (np.nextafter(np.float32(1) / np.float32(pairs), np.float32(d)) for d in (0, 2)):
+            assert np.array_equal(((i.astype(np.float32) + np.float32(0.5)) * by).astype(np.int64), i // pairs), pairs
+
+
 def test_empty_calls_launch_nothing():
     assert lib().scoot_rotate(*dict(ROTATE, num_tokens=0).values()) == 0
     assert lib().scoot_kv_append(*dict(APPEND, num_tokens=0).values()) == 0
