@@ -759,7 +759,8 @@ int scoot_rotary_frequencies(int dim, double base, int scaling, double factor, d
  * and else does not overlap it.  Rows of tokens with a negative position are
  * not written.  reverse: the other way (the same magnitude), which is what the
  * gradient of x is of the gradient of out.
- * head_dim: a multiple of 8, at most 1024; rotary_dim even, 0 .. head_dim.
+ * head_dim: a multiple of 8, at most 1024; rotary_dim even, 0 .. head_dim; 0:
+ * positions and freqs are not used, and every row is copied.
  * Rows that start on 16 bytes, and rotary_dim a multiple of 16 (interleaved:
  * of 8), are faster.  Errors: INVALID_ARG, UNSUPPORTED, DEVICE, NO_MEMORY. */
 int scoot_rotate(const void* x, scoot_kv_type type, int64_t num_tokens, int num_heads, int head_dim, int64_t x_token_stride,
@@ -784,7 +785,7 @@ int scoot_rotate(const void* x, scoot_kv_type type, int64_t num_tokens, int num_
  * earlier values (its first new slot is not its first one) and that is no
  * smaller.  Where the scale grows, the earlier values (those before the first
  * new slot) are stored anew, times old / new scale; the scale of a block with
- * earlier values that is not positive and finite is replaced and they stay as
+ * earlier values that is not from 2^-64 to 2^64 is replaced and they stay as
  * they are.  Infinities are limited to 448 E, NaN is kept.  With scales, the
  * tokens of one block have to be rows in a row, with slots that ascend, as
  * scoot_kv_assign gives them; otherwise that block's values and scales are
@@ -805,7 +806,8 @@ int scoot_kv_append(const void* q, int num_heads, int64_t q_token_stride, int64_
  * request sees may have anything:
  *   out = sum_t softmax_t(scale * k_scales[b_t] * q . k_t) * v_scales[b_t] * v_t
  * A power of two as the scale of values is exact; another one is off by up to
- * 2^-24 of the row's largest score, as scores themselves are.  The workspace is scoot_kv_attention_workspace's. */
+ * 2^-24 of the row's largest score, as scores themselves are.  The workspace is
+ * scoot_kv_attention_workspace's. */
 int scoot_kv_attention_scaled(const void* q, scoot_kv_type type, int64_t num_tokens, int num_heads, int num_kv_heads,
                               int head_dim, int64_t q_token_stride, int64_t q_head_stride, const void* k_cache,
                               const void* v_cache, int64_t num_blocks, int block_size, const int32_t* block_table,

@@ -759,10 +759,16 @@ def _refuse_caches(k_cache, v_cache):
                (v_cache.dtype is k_cache.dtype and v_cache.shape == k_cache.shape, "v_cache must have k_cache's type and shape"))
 
 
+def _is_scales(t):
+    """A tensor that is no number: one of a single element is, but for two dimensions."""
+    import torch
+    return isinstance(t, torch.Tensor) and (t.numel() != 1 or t.dim() == 2)
+
+
 def _refuse_scales(k_scale, v_scale, k_cache):
     """Scales of every block and head, or numbers."""
     import torch
-    both = [isinstance(t, torch.Tensor) and t.dim() > 0 for t in (k_scale, v_scale)]
+    both = [_is_scales(t) for t in (k_scale, v_scale)]
     _kv_refuse((both[0] == both[1], "k_scale and v_scale must both be numbers or both be tensors"))
     if not all(both):
         return
@@ -977,7 +983,7 @@ def kv_append(k, v, positions, slots, k_cache, v_cache, rotary=None, k_scale=1.0
             if out is not None:
                 _refuse_vectors(out, "out", q.shape[1], dim)
                 _kv_refuse((out.dtype is q.dtype and out.shape == q.shape, "out must have q's type and shape"))
-        _refuse_mixed(k, **{n: t for n, t in (("k_scale", k_scale), ("v_scale", v_scale)) if hasattr(t, "device")})
+        _refuse_mixed(k, **{n: t for n, t in (("k_scale", k_scale), ("v_scale", v_scale)) if _is_scales(t)})
         raise ValueError("kv_append takes tensors")
     if q is None or out is not None or isinstance(got, int):
         if got:
@@ -1017,7 +1023,7 @@ def kv_attention(q, k_cache, v_cache, block_table, query_start, seq_len, max_new
         _refuse_mixed(q, k_cache=k_cache, v_cache=v_cache, seq_len=seq_len, query_start=query_start, block_table=block_table,
                       out=out, workspace=workspace)
         _refuse_scales(k_scale, v_scale, k_cache)
-        _refuse_mixed(q, **{n: t for n, t in (("k_scale", k_scale), ("v_scale", v_scale)) if hasattr(t, "device") and t.dim()})
+        _refuse_mixed(q, **{n: t for n, t in (("k_scale", k_scale), ("v_scale", v_scale)) if _is_scales(t)})
         if out is not None:
             _refuse_vectors(out, "out", q.shape[1], dim)
             _kv_refuse((out.dtype is q.dtype and out.shape == q.shape, "out must have q's type and shape"))

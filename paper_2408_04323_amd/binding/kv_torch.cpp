@@ -83,7 +83,12 @@ bool are_scales(PyObject* k, PyObject* v, const at::Tensor& cache) {
   }
   return type_of(cache) == kF8;
 }
-bool is_scales(PyObject* o) { return THPVariable_Check(o) && THPVariable_Unpack(o).dim() > 0; }
+// A tensor that is no number: one of a single element is, but for two dimensions.
+bool is_scales(PyObject* o) {
+  if (!THPVariable_Check(o)) return false;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  return t.numel() != 1 || t.dim() == 2;
+}
 
 bool with(const at::Tensor& t, std::initializer_list<const at::Tensor*> others) {
   for (const at::Tensor* o : others)

@@ -283,6 +283,22 @@ def test_append_agrees_with_rotate_and_write():
     assert torch.equal(q, turned[:, :8]) and torch.equal(a, b)
 
 
+def test_a_tensor_of_one_element_is_a_number():
+    """For the append and for the attention over what it stored."""
+    rng = np.random.default_rng(10)
+    x = dev(rng.standard_normal((20, 8, 64)), torch.bfloat16)
+    pos, slots = dev(np.arange(20), torch.int32), dev(np.arange(20), torch.int64)
+    table, start, length = dev([[0, 1]], torch.int32), dev([0, 20], torch.int32), dev([20], torch.int32)
+    got = []
+    for number in (0.25, np.float32(0.25), torch.tensor(0.25), torch.tensor([0.25])):
+        c = torch.zeros(2, 2, 2, 16, 64, dtype=torch.float8_e4m3fn, device=DEV)
+        q = S.kv_append(x[:, 4:6], x[:, 6:], pos, slots, c[0], c[1], rotary=S.rotary_create(64), k_scale=number, v_scale=number, q=x[:, :4])
+        out = S.kv_attention(q, c[0], c[1], table, start, length, 20, 20, k_scale=number, v_scale=number)
+        got.append((c.view(torch.uint8), out))
+    for c, out in got[1:]:
+        assert torch.equal(c, got[0][0]) and torch.equal(out, got[0][1])
+
+
 def test_no_tokens():
     z = torch.empty(0, 2, 64, dtype=torch.bfloat16, device=DEV)
     c = torch.zeros(2, 3, 2, 16, 64, dtype=torch.bfloat16, device=DEV)

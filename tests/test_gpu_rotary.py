@@ -99,6 +99,13 @@ def test_rows_of_negative_positions_stay():
     check(f64(out), f64(x), pos, f64_freqs(rot), 1.0, False, False, "f16")
 
 
+def test_nothing_to_turn_copies_every_row():
+    """Without pairs the positions are not looked at."""
+    x = dev(np.random.default_rng(4).standard_normal((5, 3, 40)), torch.bfloat16)
+    none = S.Rotary(torch.zeros(0, dtype=torch.float64, device=DEV))
+    assert torch.equal(S.rotate(x, dev([-1, 0, -7, 3, 2 ** 31 - 1], torch.int32), none), x)
+
+
 def f64_freqs(rot):
     return rot.freqs.cpu().numpy()
 

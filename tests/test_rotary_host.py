@@ -235,6 +235,16 @@ def test_attention_with_other_scales_is_refused(no_call, change, what):
         S.kv_attention(**t, max_new_len=2, max_seq_len=9, stream=0)
 
 
+@pytest.mark.parametrize("number", [np.float32(0.5), torch.tensor(0.5), torch.tensor([0.5])], ids=str)
+def test_numbers_of_other_kinds_are_no_scales_of_blocks(no_call, number):
+    """What is wrong is the output, and that is what the error says."""
+    with pytest.raises(ValueError, match="out must"):
+        _append(k_cache=_f8(), v_cache=_f8(), k_scale=number, v_scale=0.5, out=_half(3, 5, 64))
+    with pytest.raises(ValueError, match="out must"):
+        S.kv_attention(_half(3, 4, 64), _f8(), _f8(), _fake(2, 3), _fake(3), _fake(2), 2, 9, k_scale=number, v_scale=0.5, out=_half(3, 5, 64),
+                       workspace=_fake(4096, dtype=torch.uint8), stream=0)
+
+
 @pytest.mark.parametrize("stream", [0, 4096])
 def test_a_given_stream_and_host_tensors_are_refused(stream):
     x, f = torch.zeros(3, 2, 64, dtype=torch.bfloat16), torch.zeros(32, dtype=torch.float64)
