@@ -7,7 +7,9 @@ enable-chunked-prefill of the space in workloads/synth.py takes synthetic
 requests through kv_assign (blocks and slots), kv_write (keys and values into
 the cache) and kv_attention (prompt chunks and single tokens over the cache),
 and measures generated tokens per second and the 99th percentile of the step
-time.  A configuration whose step runs out of blocks counts as crashed, which
+time.  With --rotary the vectors are turned by their positions on the way, and
+with --cache f8 the cache holds 8-bit floats with a scale per block and head
+(kv_append in the place of kv_write).  A configuration whose step runs out of blocks counts as crashed, which
 the feasibility forest learns.  The other knobs do not act on one layer of one
 GPU and are searched along.
 
@@ -39,14 +41,20 @@ def requests(n, seed=0):
 
 
 class CacheStep:
-    """The cache of one layer and the requests that run in it."""
+    """The cache of one layer and the requests that run in it.  ``rotary``
+    turns queries and keys by their positions; a ``scaled`` cache holds 8-bit
+    floats with a scale per block and head."""
 
-    def __init__(self, block_size, cache_tokens, device="cuda"):
+    def __init__(self, block_size, cache_tokens, device="cuda", rotary=None, scaled=False):
         self.bs = int(block_size)
         blocks = cache_tokens // self.bs
         shape = (blocks, KV_HEADS, self.bs, DIM)
-        self.k_cache = torch.zeros(shape, dtype=torch.bfloat16, device=device)
-        self.v_cache = torch.zeros(shape, dtype=torch.bfloat16, device=device)
+        self.rotary, self.scaled = rotary, scaled
+        dtype = torch.float8_e4m3fn if scaled else torch.bfloat16
+        self.k_cache = torch.zeros(shape, dtype=dtype, device=device)
+        self.v_cache = torch.zeros(shape, dtype=dtype, device=device)
+        self.k_scale = torch.ones(shape[:2], device=device) if scaled else 1.0
+        self.v_scale = torch.ones(shape[:2], device=device) if scaled else 1.0
         self.free = torch.randperm(blocks, device=device).to(torch.int32)
         self.cols = -(-VLLM_MAX_MODEL_LEN // self.bs)
         self.table = torch.full((0, self.cols), -1, dtype=torch.int32, device=device)
@@ -71,10 +79,15 @@ class CacheStep:
         lens = torch.tensor([self.context, new], dtype=torch.int32).to(self.device)
         batch = scoot.kv_assign(lens[0], lens[1], self.table, self.free, self.bs, tokens)
         q, k, v = qkv[:tokens, :HEADS], qkv[:tokens, HEADS:HEADS + KV_HEADS], qkv[:tokens, HEADS + KV_HEADS:]
-        scoot.kv_write(k, v, batch.slots, self.k_cache, self.v_cache)
+        if self.rotary is None and not self.scaled:
+            scoot.kv_write(k, v, batch.slots, self.k_cache, self.v_cache)
+        else:
+            turned = scoot.kv_append(k, v, batch.positions, batch.slots, self.k_cache, self.v_cache, self.rotary, self.k_scale,
+                                     self.v_scale, q=None if self.rotary is None else q)
+            q = q if turned is None else turned
         self.context = [c + n for c, n in zip(self.context, new)]
         out = scoot.kv_attention(q, self.k_cache, self.v_cache, self.table, batch.query_start, batch.seq_len,
-                                 max_new_len=max(new), max_seq_len=max(self.context))
+                                 max_new_len=max(new), max_seq_len=max(self.context), k_scale=self.k_scale, v_scale=self.v_scale)
         self.free = self.free[taken:]
         return out
 
@@ -88,11 +101,11 @@ class CacheStep:
         self.context = [self.context[i] for i in keep]
 
 
-def evaluate(knobs, work, cache_tokens=1 << 16, device="cuda"):
+def evaluate(knobs, work, cache_tokens=1 << 16, device="cuda", **of_step):
     """(generated tokens per second, 99th percentile of the step time in
     seconds) of serving ``work`` under ``knobs``; None if the cache ran full."""
     budget, seats = int(knobs["max-num-batched-tokens"]), int(knobs["max-num-seqs"])
-    step = CacheStep(knobs["block-size"], cache_tokens, device)
+    step = CacheStep(knobs["block-size"], cache_tokens, device, **of_step)
     gen = torch.Generator(device=device).manual_seed(1)
     qkv = torch.randn(budget, HEADS + 2 * KV_HEADS, DIM, generator=gen, device=device).to(torch.bfloat16)
     waiting, running, times, made = list(work), [], [], 0  # running: [prompt tokens left, answer tokens left]
@@ -135,7 +148,7 @@ def evaluate(knobs, work, cache_tokens=1 << 16, device="cuda"):
     return made / sum(times), float(np.quantile(times, 0.99))
 
 
-def tune(rounds, parallel, n_requests=64, cache_tokens=1 << 16, pool=16384, say=print):
+def tune(rounds, parallel, n_requests=64, cache_tokens=1 << 16, pool=16384, say=print, **of_step):
     """Algorithm 1 with measured evaluations: (X, Y, valid, best row)."""
     sp = vllm_space()
     poly, vinit = sobol_table(sp["d"])
@@ -148,7 +161,7 @@ def tune(rounds, parallel, n_requests=64, cache_tokens=1 << 16, pool=16384, say=
         bad = False
         for i in range(len(x)):
             kn = {name: col[i] for name, col in knobs.items()}
-            got = evaluate(kn, work, cache_tokens)
+            got = evaluate(kn, work, cache_tokens, **of_step)
             bad = bad or got is None
             y = (0.0, 0.0) if got is None else (-got[0], got[1])
             X, Y, valid = np.vstack([X, x[i]]), np.vstack([Y, y]), np.append(valid, np.uint8(got is not None))
@@ -167,8 +180,11 @@ def main():
     ap.add_argument("--parallel", type=int, default=2)
     ap.add_argument("--requests", type=int, default=64)
     ap.add_argument("--cache-tokens", type=int, default=1 << 16)
+    ap.add_argument("--rotary", type=float, metavar="BASE", help="turn queries and keys by their positions")
+    ap.add_argument("--cache", choices=("bf16", "f8"), default="bf16")
     a = ap.parse_args()
-    X, Y, valid, best = tune(a.rounds, a.parallel, a.requests, a.cache_tokens)
+    rotary = None if a.rotary is None else scoot.rotary_create(DIM, base=a.rotary)
+    X, Y, valid, best = tune(a.rounds, a.parallel, a.requests, a.cache_tokens, rotary=rotary, scaled=a.cache == "f8")
     if best < 0:
         print("no configuration ran")
         return 1

@@ -1,5 +1,5 @@
 """A serving step with rotations and scales of blocks, as an engine runs it: slots, an append that turns queries and keys,
-attention over the cache in 8 bits.  Several steps, eagerly, on a stream of their own and captured; the example's step."""
+attention over the cache in 8 bits.  Several steps, eagerly, on a stream of their own and captured."""
 import numpy as np
 import pytest
 
