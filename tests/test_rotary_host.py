@@ -170,18 +170,18 @@ def _rotate(**change):
 
 
 @pytest.mark.parametrize("change,what", [
-    (dict(x=torch.zeros(3, 4, 64, dtype=torch.bfloat16)), "x must be a device tensor"), (dict(x=_fake(3, 4, 64, dtype=torch.float32)), "x must be float16"),
-    (dict(x=_half(3, 4, 128)[..., ::2]), "contiguous in its last"), (dict(x=_half(3, 64)), r"must be \(tokens"),
-    (dict(positions=_fake(4)), "positions must have 3"), (dict(positions=_fake(3, dtype=torch.int64)), "positions must be int32"),
-    (dict(positions=torch.zeros(3, dtype=torch.int32)), "positions must be a device"), (dict(positions=_fake(6)[::2]), "positions must be contiguous"),
-    (dict(positions=_fake(3, device="cuda:1")), "positions must be on the device"), (dict(rotary=None), "must be a Rotary"),
-    (dict(rotary=_rotary(33)), "more pairs than a head"), (dict(rotary=_rotary(dtype=torch.float32)), "float64"),
-    (dict(rotary=_rotary(device="cuda:1")), "freqs must be on the device"), (dict(rotary=S.Rotary([1.0])), "float64 device tensor"),
-    (dict(out=_half(3, 4, 32)), "out must be"), (dict(out=_half(2, 4, 64)), "out must have x's"), (dict(out=_half(3, 4, 64, device="cuda:1")), "out must be on the device"),
-    (dict(out=_fake(3, 4, 64, dtype=torch.float16)), "out must have x's")])
+    (lambda: dict(x=torch.zeros(3, 4, 64, dtype=torch.bfloat16)), "x must be a device tensor"), (lambda: dict(x=_fake(3, 4, 64, dtype=torch.float32)), "x must be float16"),
+    (lambda: dict(x=_half(3, 4, 128)[..., ::2]), "contiguous in its last"), (lambda: dict(x=_half(3, 64)), r"must be \(tokens"),
+    (lambda: dict(positions=_fake(4)), "positions must have 3"), (lambda: dict(positions=_fake(3, dtype=torch.int64)), "positions must be int32"),
+    (lambda: dict(positions=torch.zeros(3, dtype=torch.int32)), "positions must be a device"), (lambda: dict(positions=_fake(6)[::2]), "positions must be contiguous"),
+    (lambda: dict(positions=_fake(3, device="cuda:1")), "positions must be on the device"), (lambda: dict(rotary=None), "must be a Rotary"),
+    (lambda: dict(rotary=_rotary(33)), "more pairs than a head"), (lambda: dict(rotary=_rotary(dtype=torch.float32)), "float64"),
+    (lambda: dict(rotary=_rotary(device="cuda:1")), "freqs must be on the device"), (lambda: dict(rotary=S.Rotary([1.0])), "float64 device tensor"),
+    (lambda: dict(out=_half(3, 4, 32)), "out must be"), (lambda: dict(out=_half(2, 4, 64)), "out must have x's"), (lambda: dict(out=_half(3, 4, 64, device="cuda:1")), "out must be on the device"),
+    (lambda: dict(out=_fake(3, 4, 64, dtype=torch.float16)), "out must have x's")])
 def test_rotate_of_other_tensors_is_refused(no_call, change, what):
     with pytest.raises(ValueError, match=what):
-        _rotate(**change)
+        _rotate(**change())
 
 
 def _scales(*shape, **more):
@@ -199,22 +199,23 @@ def _append(**change):
     return S.kv_append(**t, stream=0)
 
 
-IN_8 = dict(k_cache=_f8(), v_cache=_f8(), k_scale=_scales(), v_scale=_scales())
+def _in_8():
+    return dict(k_cache=_f8(), v_cache=_f8(), k_scale=_scales(), v_scale=_scales())
 
 
 @pytest.mark.parametrize("change,what", [
-    (dict(k=_half(3, 3, 64)), "k must be"), (dict(v=_half(2, 2, 64)), "v must have"), (dict(slots=_fake(3)), "slots must be"),
-    (dict(slots=_fake(4, dtype=torch.int64)), "slots must have 3"), (dict(positions=None), "positions must be a device tensor"),
-    (dict(positions=_fake(2)), "positions must have 3"), (dict(rotary=_rotary(40)), "more pairs"), (dict(rotary="yes"), "must be a Rotary"),
-    (dict(rotary=None), "queries need a rotary"), (dict(q=None), "out needs queries"), (dict(q=_half(3, 4, 32)), "q must be"),
-    (dict(q=_half(2, 4, 64)), "q must have"), (dict(q=_fake(3, 4, 64, dtype=torch.float16)), "q must have"), (dict(out=_half(3, 5, 64)), "out must"),
-    (dict(k_scale=_scales(), v_scale=_scales()), "need a float8"), (dict(IN_8, v_scale=1.0), "both be numbers"),
-    (dict(IN_8, k_scale=_scales(4, 3)), "k_scale must be"), (dict(IN_8, v_scale=_scales(dtype=torch.float64)), "v_scale must be float32"),
-    (dict(IN_8, v_scale=_scales(2, 4).t()), "v_scale must be contiguous"), (dict(IN_8, k_scale=torch.ones(4, 2)), "k_scale must be a device"),
-    (dict(IN_8, k_scale=_scales(device="cuda:1")), "k_scale must be on the device")])
+    (lambda: dict(k=_half(3, 3, 64)), "k must be"), (lambda: dict(v=_half(2, 2, 64)), "v must have"), (lambda: dict(slots=_fake(3)), "slots must be"),
+    (lambda: dict(slots=_fake(4, dtype=torch.int64)), "slots must have 3"), (lambda: dict(positions=None), "positions must be a device tensor"),
+    (lambda: dict(positions=_fake(2)), "positions must have 3"), (lambda: dict(rotary=_rotary(40)), "more pairs"), (lambda: dict(rotary="yes"), "must be a Rotary"),
+    (lambda: dict(rotary=None), "queries need a rotary"), (lambda: dict(q=None), "out needs queries"), (lambda: dict(q=_half(3, 4, 32)), "q must be"),
+    (lambda: dict(q=_half(2, 4, 64)), "q must have"), (lambda: dict(q=_fake(3, 4, 64, dtype=torch.float16)), "q must have"), (lambda: dict(out=_half(3, 5, 64)), "out must"),
+    (lambda: dict(k_scale=_scales(), v_scale=_scales()), "need a float8"), (lambda: dict(_in_8(), v_scale=1.0), "both be numbers"),
+    (lambda: dict(_in_8(), k_scale=_scales(4, 3)), "k_scale must be"), (lambda: dict(_in_8(), v_scale=_scales(dtype=torch.float64)), "v_scale must be float32"),
+    (lambda: dict(_in_8(), v_scale=_scales(2, 4).t()), "v_scale must be contiguous"), (lambda: dict(_in_8(), k_scale=torch.ones(4, 2)), "k_scale must be a device"),
+    (lambda: dict(_in_8(), k_scale=_scales(device="cuda:1")), "k_scale must be on the device")])
 def test_append_of_other_tensors_is_refused(no_call, change, what):
     with pytest.raises(ValueError, match=what):
-        _append(**change)
+        _append(**change())
 
 
 @pytest.mark.parametrize("name", ["v", "positions", "slots", "k_cache", "v_cache", "q", "out"])
@@ -226,11 +227,11 @@ def test_append_across_devices_is_refused(no_call, name):
 
 
 @pytest.mark.parametrize("change,what", [
-    (dict(k_scale=_scales(4, 3)), "k_scale must be"), (dict(v_scale=_scales(dtype=torch.float16)), "v_scale must be float32"), (dict(v_scale=0.5), "both be numbers"),
-    (dict(v_scale=_scales(device="cuda:1")), "v_scale must be on the device"), (dict(k_cache=_half(4, 2, 16, 64), v_cache=_half(4, 2, 16, 64)), "need a float8")])
+    (lambda: dict(k_scale=_scales(4, 3)), "k_scale must be"), (lambda: dict(v_scale=_scales(dtype=torch.float16)), "v_scale must be float32"), (lambda: dict(v_scale=0.5), "both be numbers"),
+    (lambda: dict(v_scale=_scales(device="cuda:1")), "v_scale must be on the device"), (lambda: dict(k_cache=_half(4, 2, 16, 64), v_cache=_half(4, 2, 16, 64)), "need a float8")])
 def test_attention_with_other_scales_is_refused(no_call, change, what):
-    t = dict(q=_half(3, 4, 64), block_table=_fake(2, 3), query_start=_fake(3), seq_len=_fake(2), out=_half(3, 4, 64), workspace=_fake(4096, dtype=torch.uint8), **IN_8)
-    t.update(change)
+    t = dict(q=_half(3, 4, 64), block_table=_fake(2, 3), query_start=_fake(3), seq_len=_fake(2), out=_half(3, 4, 64), workspace=_fake(4096, dtype=torch.uint8), **_in_8())
+    t.update(change())
     with pytest.raises(ValueError, match=what):
         S.kv_attention(**t, max_new_len=2, max_seq_len=9, stream=0)
 
