@@ -895,8 +895,9 @@ def rotary_frequencies(dim, base=10000.0, scaling=None, factor=1.0, length=0, lo
     that turn less than ``low`` times."""
     if scaling not in ROTARY_SCALINGS:
         raise ValueError(f"scaling must be one of {list(ROTARY_SCALINGS)}")
-    freqs, magnitude = np.zeros(max(int(dim) // 2, 1), dtype=np.float64), C.c_double(0.0)
-    check(lib().scoot_rotary_frequencies(int(dim), float(base), ROTARY_SCALINGS[scaling], float(factor), float(length), float(low),
+    dim = max(-1, min(int(dim), 2048))  # from 1025 on the library refuses it
+    freqs, magnitude = np.zeros(max(dim // 2, 1), dtype=np.float64), C.c_double(0.0)
+    check(lib().scoot_rotary_frequencies(dim, float(base), ROTARY_SCALINGS[scaling], float(factor), float(length), float(low),
                                          float(high), freqs.ctypes.data_as(C.POINTER(C.c_double)), C.byref(magnitude)),
           "rotary_frequencies")
     return freqs, magnitude.value

@@ -45,6 +45,13 @@ def test_frequencies_refuse(change):
         S.rotary_frequencies(64, scaling="other")
 
 
+@pytest.mark.parametrize("dim", [-2 ** 40, -1, 0, 63, 1026, 2 ** 32 + 64, 2 ** 50])
+def test_sizes_that_are_none(dim):
+    """Sizes that pass 32 bits are not taken for what is left of them."""
+    with pytest.raises(S.ScootError, match="dim must be even"):
+        S.rotary_frequencies(dim)
+
+
 ROTATE = dict(x=P, type=1, num_tokens=4, num_heads=2, head_dim=64, x_token_stride=128, x_head_stride=64, positions=P, freqs=P, rotary_dim=64,
               interleaved=0, magnitude=1.0, reverse=0, out=P, out_token_stride=128, out_head_stride=64, stream=None)
 APPEND = dict(q=P, num_heads=4, q_token_stride=256, q_head_stride=64, q_out=P, q_out_token_stride=256, q_out_head_stride=64, k=P, v=P, type=1,
