@@ -67,6 +67,7 @@
 
 #include "kv.h"
 #include "kv_plan.h"
+#include "kv_waves.h"
 
 namespace scoot {
 namespace kvattn {
@@ -415,16 +416,16 @@ struct Ahead {
   }
 };
 
+struct Workgroup {
+  __device__ __forceinline__ void sync() const { __syncthreads(); }
+  __device__ __forceinline__ bool leads() const { return (threadIdx.x & 63) == 0; }
+  __device__ __forceinline__ int wave() const { return threadIdx.x >> 6; }
+};
+
 // Whether `x` holds in any of the workgroup's waves; `flag`: a word of LDS for each.
 template <int W>
 __device__ __forceinline__ bool any_wave(bool x, int* flag) {
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) flag[threadIdx.x >> 6] = x;
-  __syncthreads();
-  int any = 0;
-#pragma unroll
-  for (int w = 0; w < W; ++w) any |= flag[w];
-  return uniform(any) != 0;
+  return uniform(any_of_waves<W>(Workgroup{}, flag, x)) != 0;
 }
 
 // Whether any of the item's keys lies in an entry that names no block.
@@ -1128,10 +1129,8 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
     }
 #pragma unroll
     for (int i = 1; i < 64; i *= 2) top = max(top, __shfl_xor(top, i));
-    if ((threadIdx.x & 63) == 0) flag[wave] = top;
     settle();
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    w.refer(uniform(max(max(flag[0], flag[1]), max(flag[2], flag[3]))));
+    w.refer(uniform(most_of_waves<kWaves>(Workgroup{}, flag, top)));
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       *in_lds(0, j) = key_scale(a.score_scale, *in_lds(0, j));
