@@ -41,10 +41,20 @@
 // widened to half precision times 2^(e - r), which the conversion does by the
 // way, with r the largest e so far (or near it); log2 f goes into the exponents
 // beside m, and l adds the weights over f.  So m, the weights and l are those of
-// one scale, whatever the scores, and a weight costs nothing more; values lose
-// nothing down to 2^-15 of the reference, and 2^-25 of it below that.  (Weights
+// one scale, whatever the scores, and a weight costs nothing more.  (Weights
 // times f instead would be exact beside any score for any f, not for powers of
-// two alone; a product per weight costs 13%.)
+// two alone; a product per weight costs 13%.)  Half precision holds every code
+// times 2^(e - r) down to e - r = -15.  Where the blocks that a tile's rows see
+// (or a wave's, of few rows) are further apart, all its keys are done once more in
+// a wide form, in which no row's result depends on blocks that it does not see:
+// 2^e and f go into the weights, whose largest is 2^80 and which are two bfloat16
+// numbers, 16 bits with a float's exponents, so that products of weights down to
+// 2^-200 of the largest count; the codes are exact as they are, l takes weights
+// without scales, and there are two products and a second exponential: 48 requests
+// of up to 32,767 keys 299 -> 595 us, late chunks over 30,000 keys 339 -> 779 (heads of
+// 64), 525 -> 1015 (128).  That it is there costs the others registers: those late
+// chunks 0.5% and nothing, of 192 and 256 1.3% and 2.8%, single tokens over 1000 keys
+// 0.2 us of 10.7.
 // The scales of 64 strips at a time go straight from memory into LDS, where
 // their addresses are made (through registers: 40 more, and a wave per SIMD less
 // for few rows of 64 dimensions).  Tiles make of them, once for 64 strips, what
@@ -301,11 +311,16 @@ __device__ __forceinline__ bool find_item(const KvAttnArgs& a, const Plan& p, in
 __device__ __forceinline__ int exponent(float b) { return (int)(__float_as_uint(b) >> 23); }
 __device__ __forceinline__ float fraction(float b) { return __uint_as_float((__float_as_uint(b) & 0x7fffffu) | 0x3f800000u); }
 __device__ __forceinline__ float power_at(float b, int r) { return __uint_as_float((uint32_t)max(exponent(b) - r + 127, 1) << 23); }
-// 2^r, and 2^(r - larger).
-__device__ __forceinline__ float power_of(int r) { return __uint_as_float((uint32_t)r << 23); }
+// x 2^r, and 2^(r - larger).
+__device__ __forceinline__ float from_reference(float x, int r) { return __builtin_amdgcn_ldexpf(x, r - 127); }
 __device__ __forceinline__ float to_reference(int r, int larger) { return __uint_as_float((uint32_t)max(127 + r - larger, 0) << 23); }
 // The reference moves where an exponent is this far above it: 448 * 2^6 is still a number in half precision.
 constexpr int kAboveReference = 6;
+// Codes, which are multiples of 2^-9, are exact in half precision down to this far below it: its numbers are multiples of 2^-24.
+constexpr int kBelowReference = 15;
+// The wide form's largest weight: 2^31 keys of 448 times twice as much are a float, and what is 2^126 times as small is one too.
+constexpr float kWideTop = 80.0f;
+constexpr float kNothing = -1e30f;  // exponent of the wide form's weights before any
 
 // Blocks of the cache, as scalars.
 template <typename S>
@@ -492,6 +507,38 @@ __device__ __forceinline__ typename Vec<W>::v8 eight_weights(F score, float scal
   return r;
 }
 
+// What a part's sums are multiplied by for another m: 2^x.  With scales, the largest values may have weights of 2^-128 of the
+// others', and less, where 2^x is no float while the product is one.
+template <typename S>
+struct Factor {
+  float f;
+  int e = 0;
+  __device__ __forceinline__ explicit Factor(float x) {
+    if constexpr (S::SCALED) {
+      e = x < -120.0f ? -128 : 0;
+      x -= (float)e;
+    }
+    f = __builtin_amdgcn_exp2f(x);
+  }
+  __device__ __forceinline__ float operator()(float o) const {
+    if constexpr (S::SCALED) o = __builtin_amdgcn_ldexpf(o, e);  // small ones that this loses are nothing beside the others
+    return o * f;
+  }
+};
+
+// The wide form's m up to a largest score x, and `wide`, a whole number by which o's exponent is above m, up to the largest
+// exponent of a weight with its block's, most(m), which becomes kWideTop.  Returns what o is multiplied by.
+template <typename F>
+__device__ __forceinline__ float rise(float& m, float& l, float& wide, float x, F most) {
+  x = below(x, 1.0f);
+  const float up = x > m ? x : m, less = m - up;
+  m = up;
+  l *= __builtin_amdgcn_exp2f(less);
+  const float before = fmaxf(wide + less, kNothing);
+  wide = __builtin_floorf(fmaxf(before, most(up) - kWideTop));
+  return __builtin_amdgcn_exp2f(before - wide);
+}
+
 // Where some rows do not see some keys, 0 * inf must not arise.
 //
 // Eight keys' values without those past the first `seen`, which no row sees.
@@ -510,7 +557,7 @@ __device__ __forceinline__ V only_seen(V v, int seen) {
 // value is not finite spoils the others' sums; that shows in the end, and the
 // tile is done again with these values left out and added afterwards.
 template <typename W>
-__device__ __forceinline__ typename Vec<W>::v8 only_finite(typename Vec<W>::v8 v) {
+__device__ __forceinline__ typename Vec<W>::v8 only_finite(typename Vec<W>::v8 v, uint32_t& left_out) {
   constexpr uint32_t kExp = (std::is_same<W, _Float16>::value ? 0x7c00u : 0x7f80u) * 0x10001u;
   union {
     typename Vec<W>::v8 v;
@@ -522,8 +569,26 @@ __device__ __forceinline__ typename Vec<W>::v8 only_finite(typename Vec<W>::v8 v
     // A full exponent carries into the sign's place; from there all over its half.
     const uint32_t e = ((x.w[i] & kExp) + (0x80008000u - kExp)) & 0x80008000u;
     x.w[i] &= ~(e | (e - (e >> 15)));
+    left_out |= e;
   }
   return x.v;
+}
+template <typename W>
+__device__ __forceinline__ typename Vec<W>::v8 only_finite(typename Vec<W>::v8 v) {
+  uint32_t any = 0;
+  return only_finite<W>(v, any);
+}
+// Eight weights 2^(scale s - m) times a block's 2^more f, in two parts of eight bits each, and their sum without these added
+// to l.
+template <typename F>
+__device__ __forceinline__ void wide_weights(F score, float scale, float m, float more, float f, b8& high, b8& low, float& l) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float e = limited(fmaf(score(i), scale, -m), kLimit), x = __builtin_amdgcn_exp2f(e + more) * f;
+    l += __builtin_amdgcn_exp2f(e);
+    high[i] = (__bf16)x;
+    low[i] = (__bf16)(x - (float)high[i]);
+  }
 }
 
 // Memory offsets of a lane's loads of 16 keys: its pieces, as they lie in LDS.
@@ -669,7 +734,9 @@ struct Tile32 {
   T8 q[KS];
   f16v o[DT];
   float m, l;
-  int ref = 0;  // what o is times is 2^ref (with a float's bias); the same in all lanes
+  int ref = 0;  // what o is times is 2^ref (with a float's bias); the same in all lanes until the end
+  uint32_t lost = 0;  // not 0: strip_wide() has left values out
+  float wide;  // o of strip_wide() is times 2^-wide
   // LDS offsets of this lane's reads; with few registers the first ones, of which the others differ by some bits.
   static constexpr bool kFewRegs = S::D == 256;
   static constexpr int KN = kFewRegs ? 1 : Order::KM / 2, VM = kFewRegs ? 1 : VN;
@@ -771,12 +838,12 @@ struct Tile32 {
     return r;
   }
   // V^T: lane's element d = 32 dt + lane % 32 of the keys 16 ks + 8 half .. + 7, times powers of two if there are any.
-  template <typename... By>
-  __device__ __forceinline__ W8 values(const Lds& v, int ks, int dt, By... by) const {
+  template <typename R = W, typename... By>
+  __device__ __forceinline__ typename Vec<R>::v8 values(const Lds& v, int ks, int dt, By... by) const {
     const uint32_t at = v.at[dt % VN] + (dt / VN) * (VN * 16 * Order::U) + ks * 16 * S::RB;
     if constexpr (S::F8) {
       const i2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((SCOOT_LDS i2*)at);
-      return widen<_Float16>(v[0], v[1], by...);
+      return widen<R>(v[0], v[1], by...);
     } else {
       union {
         s4 h[2];
@@ -973,6 +1040,58 @@ struct Tile32 {
         }
     }
   }
+  // Any strip, in the form whose values and weights have a float's exponents; `whole`: every row sees all of it.
+  template <typename F, typename H>
+  __device__ __forceinline__ void strip_wide(uint32_t kat, uint32_t vat, F scales, int key0, bool whole, H holes) {
+    const auto nothing = [](int) {};
+    Keys x = keys(kat);
+    f16v s;
+    scores<0>(x, s, nothing);
+    half_wide<0>(s, vat, scales, key0, whole, holes);
+    if (key0 + 32 > see.hi_max) return;
+    scores<1>(x, s, nothing);
+    half_wide<1>(s, vat, scales, key0, whole, holes);
+  }
+  template <int n, typename F, typename H>
+  __device__ __forceinline__ void half_wide(f16v& s, uint32_t vat, F scales, int key0, bool whole, H holes) {
+    if (!whole) mask(s, key0 + 32 * n, holes(key0 + 32 * n));
+    raise(s, f4{scales.key(2 * n), scales.exponent(2 * n), scales.key(2 * n + 1), scales.exponent(2 * n + 1)});
+    const Lds lds = values_at(vat);
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      b8 high, low;
+      wide_weights([&](int i) { return s[8 * k + i]; }, scales.key(2 * n + k), m, scales.exponent(2 * n + k) - wide,
+                   scales.fraction(2 * n + k), high, low, l);
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        b8 v = values<__bf16>(lds, 2 * n + k, d);
+        if (!whole) v = only_finite<__bf16>(only_seen(v, see.hi_max + 1 - (key0 + 32 * n + 16 * k + 8 * half)), lost);
+        o[d] = mfma(v, high, o[d]);
+        o[d] = mfma(v, low, o[d]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  // m up to the largest of 32 scores, `wide` to the largest of their weights times the blocks' powers of two; `scale`: of the
+  // scores, and that power's exponent, of both blocks.
+  __device__ __forceinline__ void raise(const f16v& s, f4 scale) {
+    const auto both = [](float x) {
+      const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+      return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+    };
+    float x = s[0], y = s[8];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) x = fmaxf(x, s[i]), y = fmaxf(y, s[8 + i]);
+    const float f = rise(m, l, wide, both(fmaxf(x * scale[0], y * scale[2])), [&](float m) {
+      return both(fmaxf(limited(fmaf(x, scale[0], -m), kLimit) + scale[1], limited(fmaf(y, scale[2], -m), kLimit) + scale[3]));
+    });
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] *= f;
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
   __device__ __forceinline__ bool spoilt() const {
     bool x = false;
 #pragma unroll
@@ -1006,6 +1125,7 @@ struct Tile32 {
     return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
   }
 
+  __device__ __forceinline__ float result(int d, int i) const { return S::SCALED ? from_reference(o[d][i], ref) : o[d][i]; }
   // Result rows: into `out`, or unscaled into the workspace (row `at` on).
   __device__ __forceinline__ void store(const KvAttnArgs& a, const Item& it, int row0, int head, int64_t at, float* parts,
                                         float* stats) const {
@@ -1019,13 +1139,11 @@ struct Tile32 {
       for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int i = 0; i < 16; i += 4) {
-          f4 x = {o[d][i], o[d][i + 1], o[d][i + 2], o[d][i + 3]};
-          if constexpr (S::SCALED) x *= power_of(ref);
-          *(f4*)(p + 32 * d + 2 * i) = x;
+          *(f4*)(p + 32 * d + 2 * i) = f4{result(d, i), result(d, i + 1), result(d, i + 2), result(d, i + 3)};
         }
       return;
     }
-    const float inv = inverse(S::SCALED ? power_of(ref) : a.v_scale, sum, top == -INFINITY);  // a row that saw nothing has o = 0, too
+    const float inv = inverse(S::SCALED ? 1.0f : a.v_scale, sum, top == -INFINITY);  // a row that saw nothing has o = 0, too
     const int G = a.num_heads / a.num_kv_heads;
     T* p = (T*)a.out + (it.q0 + see.tok) * a.out_token_stride + (int64_t)(head * G + see.g) * a.out_head_stride + 4 * half;
     typedef T T4 __attribute__((ext_vector_type(4)));
@@ -1035,7 +1153,7 @@ struct Tile32 {
       for (int i = 0; i < 16; i += 4) {
         T4 x;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] = (T)(o[d][i + j] * inv);
+        for (int j = 0; j < 4; ++j) x[j] = (T)(result(d, i + j) * inv);
         *(T4*)(p + 32 * d + 2 * i) = x;
       }
   }
@@ -1049,7 +1167,9 @@ struct BlockScales {
   }
   __device__ __forceinline__ float key(int group) const { return get(group, 0); }    // scores are multiplied by this,
   __device__ __forceinline__ float power(int group) const { return get(group, 1); }  // values by this,
-  __device__ __forceinline__ float log(int group) const { return get(group, 2); }    // which leaves 2 to this
+  __device__ __forceinline__ float log(int group) const { return get(group, 2); }    // which leaves 2 to this,
+  __device__ __forceinline__ float exponent(int group) const { return get(group, 1); }  // or, in the wide form, the exponent
+  __device__ __forceinline__ float fraction(int group) const { return get(group, 2); }  // and the fraction of the values' scale
 };
 
 template <typename S, int R>
@@ -1109,15 +1229,18 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
   w.see.whole(it, strips, S::ST, holes, u0, u1);
 
   // Before the first of 64 strips: their scales have landed and become what the strips take, and the reference is up to
-  // them.  Every wave does that for the groups of eight keys whose scales it fetched, a lane for a strip.
-  const auto prepare = [&](int strip) {
+  // them.  Every wave does that for the groups of eight keys whose scales it fetched, a lane for a strip.  Not for a wide
+  // pass: false if the exponents of the tile are too far apart for half precision.
+  int least = 255;
+  const auto prepare = [&](int strip, auto wide) {
+    constexpr bool kWide = decltype(wide)::value;
     const int seen = a.window > 0 ? (int)clamp64(it.pos0 + it.row0 / (a.num_heads / a.num_kv_heads) - a.window + 1, 0, it.k1) : 0;
     const int mine = strip + (threadIdx.x & 63);
     const uint32_t at = scales + (strip & 64) * kStripScales + 2 * wave * kGroupScales + (threadIdx.x & 63) * 4;
     const auto in_lds = [&](int kind, int j) { return (SCOOT_LDS float*)(at + (8 * kind + j) * kGroupScales); };
     wait_vm<0>();
     float b[2];
-    int top = 0;
+    int all = 0;  // the largest exponent, and, in the upper half, 255 less the smallest one
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       // A block that no row sees may have any number for a scale, and does not count.
@@ -1125,19 +1248,25 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
       bool real = mine < strips && key < it.k1 && key + 8 > seen;
       if (holes && real) real = (uint32_t)c.entries[e < c.last ? e : c.last] < c.num_blocks;
       b[j] = real ? *in_lds(1, j) : 0x1p-126f;
-      top = max(top, exponent(b[j]));
+      if (real) all = most_of(all, exponent(b[j]) | max(255 - exponent(b[j]), 0) << 16);
     }
-#pragma unroll
-    for (int i = 1; i < 64; i *= 2) top = max(top, __shfl_xor(top, i));
     settle();
-    w.refer(uniform(most_of_waves<kWaves>(Workgroup{}, flag, top)));
+    if constexpr (!kWide) {
+#pragma unroll
+      for (int i = 1; i < 64; i *= 2) all = most_of(all, __shfl_xor(all, i));
+      all = uniform(most_of_waves<kWaves>(Workgroup{}, flag, all));
+      w.refer(all & 0xffff);
+      least = min(least, 255 - (all >> 16));
+      if (w.ref - least > kBelowReference) return false;
+    }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       *in_lds(0, j) = key_scale(a.score_scale, *in_lds(0, j));
-      *in_lds(1, j) = power_at(b[j], w.ref);
-      *in_lds(2, j) = __builtin_amdgcn_logf(fraction(b[j]));
+      *in_lds(1, j) = kWide ? (float)(exponent(b[j]) - 127) : power_at(b[j], w.ref);
+      *in_lds(2, j) = kWide ? fraction(b[j]) : __builtin_amdgcn_logf(fraction(b[j]));
     }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    return true;
   };
   auto turn = [&](int strip) {
     // This strip has landed, for every wave, and everyone is done with the one before, whose place the next load takes.
@@ -1145,15 +1274,29 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
     else wait_vm<0>();
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   };
-  auto pass = [&](auto finite) {
+  // Once more with values that are not finite left out, or, with scales, in the wide form: then `again` is true.
+  bool early = false;
+  auto pass = [&](auto again) {
+    constexpr bool kWide = S::SCALED && decltype(again)::value;
     w.clear();
     int strip = 0;
     while (strip < strips) {
       if constexpr (S::SCALED) {
-        if ((strip & 63) == 0) prepare(strip);
+        if ((strip & 63) == 0 && !prepare(strip, again)) {
+          early = true;
+          break;
+        }
       }
       const int scaled = strip | 63;  // the last strip whose scales are there
-      if (strip >= u0 && strip < u1) {
+      if constexpr (kWide) {
+        turn(strip);
+        if (strip + R - 1 < strips) load(strip + R - 1);
+        const uint32_t at = lds + (strip % R) * S::kStrip;
+        const int key0 = it.k0 + strip * S::ST;
+        if (key0 <= w.see.hi_max)
+          w.strip_wide(at, at + kHalf, scales_of(strip), key0, strip >= u0 && strip < u1, [&](int key) { return holes ? c.holes(key) : 0; });
+        ++strip;
+      } else if (strip >= u0 && strip < u1) {
         __builtin_amdgcn_s_setprio(1);  // over waves that wait or mask: a late chunk of 64-dimensional heads 566 -> 559 us
         for (; strip < min(u1, strips - (R - 1)) && (!S::SCALED || strip <= scaled); ++strip) {
           turn(strip);
@@ -1173,20 +1316,25 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
         const uint32_t at = lds + (strip % R) * S::kStrip;
         const int key0 = it.k0 + strip * S::ST;
         if (key0 <= w.see.hi_max) {
-          w.template strip_seen<decltype(finite)::value>(at, at + kHalf, scales_of(strip), key0,
-                                                         [&](int key) { return holes ? c.holes(key) : 0; });
+          w.template strip_seen<decltype(again)::value>(at, at + kHalf, scales_of(strip), key0,
+                                                        [&](int key) { return holes ? c.holes(key) : 0; });
         }
         ++strip;
       }
     }
   };
   pass(std::false_type{});
-  if (any_wave<kWaves>(w.spoilt(), flag)) {
+  if (any_wave<kWaves>(early || w.spoilt(), flag)) {
+    if constexpr (S::SCALED) wait_vm<0>();  // the loads of a pass that ended early
     ahead.start(c, c.k, it.k0 + 16 * wave, S::ST, strips, it.k1, scales + wave * 2 * kGroupScales);
+    w.wide = kNothing;
     begin();
     pass(std::true_type{});
-    w.add_lost(c, it.k0, u0 < u1 ? it.k0 + u0 * S::ST : it.k1);  // the strips that went through the mask
-    if (u0 < u1) w.add_lost(c, it.k0 + u1 * S::ST, it.k1);
+    if constexpr (S::SCALED) w.ref = 127 + (int)fmaxf(w.wide, -1000.0f);
+    if (!S::SCALED || __builtin_amdgcn_ballot_w64(w.lost != 0)) {
+      w.add_lost(c, it.k0, u0 < u1 ? it.k0 + u0 * S::ST : it.k1);  // the strips that went through the mask
+      if (u0 < u1) w.add_lost(c, it.k0 + u1 * S::ST, it.k1);
+    }
   }
   w.store(a, it, row0, head, slot * kTile + (row0 - it.row0), parts, stats);
 }
@@ -1213,6 +1361,9 @@ struct Tile16 {
   f4 o[DT];
   float m, l;
   int ref = 0;  // as Tile32's
+  uint32_t lost = 0;
+  float wide;
+  float least = INFINITY;  // scale of values that the lane has met
   int koff[KN];
   // LDS offsets of V's reads; for 8-bit heads of 256, which would have sixteen, the first one, of which the others differ
   // by some bits.
@@ -1282,13 +1433,13 @@ struct Tile16 {
   }
 
   // V^T: lane's element d = 16 dt + lane % 16 of the keys 8 quad .. + 7, times powers of two if there are any.
-  template <typename... By>
-  __device__ __forceinline__ W8 values(uint32_t lds, int dt, By... by) const {
+  template <typename R = W, typename... By>
+  __device__ __forceinline__ typename Vec<R>::v8 values(uint32_t lds, int dt, By... by) const {
     const int n = dt % Order::VM;
     const uint32_t at = lds + (kFewRegs ? here(voff[0]) ^ n * 16 * Order::U : voff[n % VN]) + (dt / Order::VM) * (Order::VM * 16 * Order::U);
     if constexpr (S::F8) {
       const i2 v = __builtin_amdgcn_ds_read_tr8_b64_v2i32((SCOOT_LDS i2*)at);
-      return widen<_Float16>(v[0], v[1], by...);
+      return widen<R>(v[0], v[1], by...);
     } else {
       union {
         s4 h[2];
@@ -1347,6 +1498,38 @@ struct Tile16 {
     }
     l += S::SCALED ? add * __builtin_amdgcn_rcpf(f) : add;
     return w;
+  }
+
+  // As Tile32's, with one block to a lane.
+  __device__ __forceinline__ void raise(const f4 (&s)[2], float scale, float exponent) {
+    const auto all = [](float x) {
+      auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+      x = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+      sw = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+      return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+    };
+    float x = s[0][0];
+#pragma unroll
+    for (int k = 1; k < 8; ++k) x = fmaxf(x, s[k / 4][k % 4]);
+    const float f = rise(m, l, wide, all(x * scale), [&](float m) { return all(limited(fmaf(x, scale, -m), kLimit) + exponent); });
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[d][i] *= f;
+  }
+  __device__ __forceinline__ void product_wide(uint32_t lds, const b8& high, const b8& low, int key0, bool whole) {
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+      b8 v = values<__bf16>(here(lds), d);
+      if (!whole) v = only_finite<__bf16>(only_seen(v, see.hi_max + 1 - (key0 + 8 * quad)), lost);
+      o[d] = mfma(v, high, o[d]);
+      o[d] = mfma(v, low, o[d]);
+      __builtin_amdgcn_sched_barrier(0);  // one after the other: this form must not cost the others registers
+    }
+  }
+  // Whether the wave's scales are too far apart for half precision.
+  __device__ __forceinline__ bool far_apart() const {
+    return S::SCALED && __builtin_amdgcn_ballot_w64(exponent(least) < ref - kBelowReference) != 0;
   }
 
   // As Tile32's, for the scale of the values of the lane's keys.
@@ -1460,8 +1643,8 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
   w.see.whole(it, strips, 32, holes, u0, u1);
 
   int strip;
-  auto step = [&](auto masked, auto finite) {
-    constexpr bool kMasked = decltype(masked)::value;
+  auto step = [&](auto masked, auto again) {
+    constexpr bool kMasked = decltype(masked)::value, kWide = S::SCALED && decltype(again)::value;
     const bool more = strip + W < strips;
     const int key0 = it.k0 + strip * 32;
     int none = 0;  // groups that have no block
@@ -1475,8 +1658,10 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
       scale = key_scale(scale, *(const SCOOT_LDS float*)at);
       value = *(const SCOOT_LDS float*)(at + 4 * kGroupScales);
       // A block that no row sees may have any number for a scale.
-      if (kMasked && !(w.see.any_of(key0 + 8 * w.quad) && !(none >> w.quad & 1))) value = 0x1p-126f;
-      w.refer(value);
+      const bool any = !kMasked || (w.see.any_of(key0 + 8 * w.quad) && !(none >> w.quad & 1));
+      if constexpr (!kWide) w.least = fminf(w.least, any ? value : INFINITY);
+      if (!any) value = 0x1p-126f;
+      if constexpr (!kWide) w.refer(value);
     }
     wait_lds();
     if (more) {
@@ -1484,36 +1669,50 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
       load_k(b);
     }
     if (kMasked) w.mask(s, key0, holes ? c.holes(key0) : 0);
-    const typename Tile16<S>::W8 p = w.weights(s, scale, fraction(value));
-    if (more) wait_vm<2 * S::NJ>();
-    else wait_vm<0>();
-    const auto product = [&](auto... by) {
-      if (kMasked) w.template product_seen<decltype(finite)::value>(vat, p, key0, by...);
-      else w.product(vat, p, by...);
+    const auto landed = [&] {
+      if (more) wait_vm<2 * S::NJ>();
+      else wait_vm<0>();
     };
-    if constexpr (S::SCALED) product(power_at(value, w.ref));
-    else product();
+    if constexpr (kWide) {
+      b8 high, low;
+      const float e = (float)(exponent(value) - 127);
+      w.raise(s, scale, e);
+      wide_weights([&](int i) { return s[i / 4][i % 4]; }, scale, w.m, e - w.wide, fraction(value), high, low, w.l);
+      landed();
+      w.product_wide(vat, high, low, key0, strip >= u0 && strip < u1);
+    } else {
+      const typename Tile16<S>::W8 p = w.weights(s, scale, fraction(value));
+      landed();
+      const auto product = [&](auto... by) {
+        if (kMasked) w.template product_seen<decltype(again)::value>(vat, p, key0, by...);
+        else w.product(vat, p, by...);
+      };
+      if constexpr (S::SCALED) product(power_at(value, w.ref));
+      else product();
+    }
     wait_lds();
     if (more) load_v(b);
     strip += W;
   };
-  auto pass = [&](auto finite) {
+  auto pass = [&](auto again) {
     w.clear();
     strip = wave;
     while (strip < strips) {
-      if (strip >= u0 && strip < u1) {
-        while (strip < u1) step(std::false_type{}, finite);
+      if (!(S::SCALED && decltype(again)::value) && strip >= u0 && strip < u1) {
+        while (strip < u1) step(std::false_type{}, again);
       } else {
-        step(std::true_type{}, finite);
+        step(std::true_type{}, again);
       }
     }
   };
   pass(std::false_type{});
-  if (w.spoilt()) {
+  if (w.spoilt() || w.far_apart()) {
     ahead.start(c, c.k, it.k0 + 32 * wave, 32 * W, (strips - wave + W - 1) / W, it.k1, scales + wave * kWaveScales);
+    w.wide = kNothing;
     begin();
     pass(std::true_type{});
-    for (strip = wave; strip < strips; strip += W)
+    if constexpr (S::SCALED) w.ref = 127 + (int)fmaxf(w.wide, -1000.0f);
+    for (strip = wave; strip < strips && (!S::SCALED || __builtin_amdgcn_ballot_w64(w.lost != 0)); strip += W)
       if (strip < u0 || strip >= u1) w.add_lost(c, it.k0 + strip * 32, min(it.k0 + strip * 32 + 32, it.k1));
   }
 
@@ -1524,7 +1723,13 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
   constexpr int kRow = S::D + 4;  // floats of a row, off by 16 bytes so that rows start on different banks
   float* mine = (float*)smem + (wave * kFew + (w.lane & 15)) * kRow + 4 * w.quad;
 #pragma unroll
-  for (int d = 0; d < Tile16<S>::DT; ++d) *(f4*)(mine + 16 * d) = S::SCALED ? w.o[d] * power_of(w.ref) : w.o[d];
+  for (int d = 0; d < Tile16<S>::DT; ++d) {
+    f4 x = w.o[d];
+    if constexpr (S::SCALED)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[j] = from_reference(x[j], w.ref);
+    *(f4*)(mine + 16 * d) = x;
+  }
   __syncthreads();
   const int G = a.num_heads / a.num_kv_heads;
   const int rows = min(kFew, it.rows - row0);
@@ -1536,11 +1741,11 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
     for (int v = 0; v < W; ++v) top = fmaxf(top, ml[(v * kFew + r) * 2]);
 #pragma unroll
     for (int v = 0; v < W; ++v) {
-      const float f = __builtin_amdgcn_exp2f(ml[(v * kFew + r) * 2] - top);
-      l += f * ml[(v * kFew + r) * 2 + 1];
+      const Factor<S> f(ml[(v * kFew + r) * 2] - top);
+      l += f(ml[(v * kFew + r) * 2 + 1]);
       const f4 x = *(const f4*)((const float*)smem + (v * kFew + r) * kRow + d);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] += f * x[j];
+      for (int j = 0; j < 4; ++j) o[j] += f(x[j]);
     }
     bool lost = false;
     if (l == 0.0f)
@@ -1636,17 +1841,17 @@ __global__ __launch_bounds__(kThreads) void join_kernel(KvAttnArgs a, Plan p, co
       up = fmaxf(up, ml[j].x);
       least = fminf(least, ml[j].x);
     }
-    const float f = __builtin_amdgcn_exp2f(top - up);
+    const Factor<S> f(top - up);
     top = up;
-    sum *= f;
+    sum = f(sum);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] *= f;
+    for (int i = 0; i < 4; ++i) o[i] = f(o[i]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float g = s0 + j < it.splits ? __builtin_amdgcn_exp2f(ml[j].x - up) : 0.0f;
-      sum += s0 + j < it.splits ? ml[j].y * g : 0.0f;
+      const Factor<S> g(ml[j].x - up);
+      sum += s0 + j < it.splits ? g(ml[j].y) : 0.0f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] += s0 + j < it.splits ? x[j][i] * g : 0.0f;
+      for (int i = 0; i < 4; ++i) o[i] += s0 + j < it.splits ? g(x[j][i]) : 0.0f;
     }
   }
   const float inv = inverse(a.v_scale, sum, least == -INFINITY);
