@@ -807,12 +807,11 @@ int scoot_kv_append(const void* q, int num_heads, int64_t q_token_stride, int64_
  *   out = sum_t softmax_t(scale * k_scales[b_t] * q . k_t) * v_scales[b_t] * v_t
  * Values stand for code * scale without another rounding, however far scales
  * are apart, and a row's result does not depend on the scales of blocks that it
- * does not see.  Weights are rounded to half precision (2^-11 of a weight, or
- * 2^-31 of the row's largest), or, where a request's blocks have scales of values
- * that are more than 2^15 apart, to 16 bits, products down to 2^-200 of the
- * largest among them; these requests take up to 2.4 times as long.  A power of two
- * as the scale of values is exact; another one is off by up to 2^-24 of the row's
- * largest score, as scores themselves are.  The workspace is
+ * does not see.  Weights are rounded to half precision (off by 1.2 * 2^-11 of a
+ * weight, or 2^-31 of the row's largest), or, where a request's blocks have scales
+ * of values that are more than 2^15 apart or scores pass 1400, to 16 bits, products
+ * down to 2^-200 of the largest among them; these requests take up to 2.4 times as
+ * long.  The workspace is
  * scoot_kv_attention_workspace's. */
 int scoot_kv_attention_scaled(const void* q, scoot_kv_type type, int64_t num_tokens, int num_heads, int num_kv_heads,
                               int head_dim, int64_t q_token_stride, int64_t q_head_stride, const void* k_cache,

@@ -41,11 +41,10 @@
 // widened to half precision times 2^(e - r), which the conversion does by the
 // way, with r the largest e so far (or near it); log2 f goes into the exponents
 // beside m, and l adds the weights over f.  So m, the weights and l are those of
-// one scale, whatever the scores, and a weight costs nothing more.  (Weights
-// times f instead would be exact beside any score for any f, not for powers of
-// two alone; a product per weight costs 13%.)  Half precision holds every code
-// times 2^(e - r) down to e - r = -15.  Where the blocks that a tile's rows see
-// (or a wave's, of few rows) are further apart, all its keys are done once more in
+// one scale, and a weight costs nothing more (a product per weight costs 13%).
+// Half precision holds every code times 2^(e - r) down to e - r = -15, and beside
+// m up to 2^11 log2 f is exact enough.  Where the blocks that a tile's rows see (or
+// a wave's, of few rows) are further apart or m is larger, its keys are done again in
 // a wide form, in which no row's result depends on blocks that it does not see:
 // 2^e and f go into the weights, whose largest is 2^80 and which are two bfloat16
 // numbers, 16 bits with a float's exponents, so that products of weights down to
@@ -436,6 +435,13 @@ struct Workgroup {
   __device__ __forceinline__ bool leads() const { return (threadIdx.x & 63) == 0; }
   __device__ __forceinline__ int wave() const { return threadIdx.x >> 6; }
 };
+
+// Whether rows of the wave have scores beside which a scale's logarithm is lost: log2 f is rounded with m, to 2^-24 of it, so
+// that from here on weights would be off by more than 2^-13.5, with large scores by f.  (The wide form keeps f apart.)
+template <typename S>
+__device__ __forceinline__ bool large_scores(float m) {
+  return S::SCALED && __builtin_amdgcn_ballot_w64(__builtin_fabsf(m) >= 2048.0f && m != kNoScore) != 0;
+}
 
 // Whether `x` holds in any of the workgroup's waves; `flag`: a word of LDS for each.
 template <int W>
@@ -1324,7 +1330,7 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
     }
   };
   pass(std::false_type{});
-  if (any_wave<kWaves>(early || w.spoilt(), flag)) {
+  if (any_wave<kWaves>(early || w.spoilt() || large_scores<S>(w.m), flag)) {
     if constexpr (S::SCALED) wait_vm<0>();  // the loads of a pass that ended early
     ahead.start(c, c.k, it.k0 + 16 * wave, S::ST, strips, it.k1, scales + wave * 2 * kGroupScales);
     w.wide = kNothing;
@@ -1706,7 +1712,7 @@ __device__ __forceinline__ void few_rows(const KvAttnArgs& a, const Item& it, in
     }
   };
   pass(std::false_type{});
-  if (w.spoilt() || w.far_apart()) {
+  if (w.spoilt() || w.far_apart() || large_scores<S>(w.m)) {
     ahead.start(c, c.k, it.k0 + 32 * wave, 32 * W, (strips - wave + W - 1) / W, it.k1, scales + wave * kWaveScales);
     w.wide = kNothing;
     begin();

@@ -189,3 +189,37 @@ def test_missing_blocks_and_any_scales_far_apart(lens, d, window, kind):
     ok = np.abs(ref[0]) + bound < (65504.0 if kind == "f16" else 3e38)
     assert ok[-1].all()
     _check(np.where(ok, got, 0), np.where(ok, ref[0], 0), np.where(ok, bound + 2.0 ** -25, 1))
+
+
+@pytest.mark.parametrize("tokens,d,length", [(1, 64, 700), (4, 128, 5000), (40, 64, 300), (40, 256, 300), (40, 128, 4000)])
+def test_fractions_of_scales_beside_large_scores(tokens, d, length):
+    """Values' scales that are no powers of two beside scores of any size: every third key has the same score x, the others
+    1.5 x (x negative) or 0.5 x, whose weights are below 2^-1000 of theirs or, for the smallest x, as the oracle's softmax says.
+    What is off: the weights' rounding (2^-11) and the logarithm of a scale (2^-21), the result's rounding (2^-8), sums in float,
+    and, with scores below 2^11, at which a scale's logarithm is added to them, 2^-13 of the weights."""
+    say("rows, fractions", tokens, d, length)
+    blocks = -(-length // 16)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    codes = torch.randn(blocks, 1, 16, d, generator=g, device=DEV).mul_(50).clamp_(-448, 448).to(torch.float8_e4m3fn)
+    vs = (torch.rand(blocks, 1, generator=g, device=DEV) * 4 - 2).exp2_()
+    ks = torch.randint(-3, 4, (blocks, 1), generator=g, device=DEV).float().exp2_()
+    third = torch.arange(blocks * 16, device=DEV) % 3 == 0
+    v = (codes.double() * vs[:, :, None, None].double()).view(-1, d)
+    mean = ((v * third[:, None]).cumsum(0) / third.cumsum(0)[:, None])[:length]
+    size_of = ((v.abs() * third[:, None]).cumsum(0) / third.cumsum(0)[:, None])[:length]
+    table = torch.arange(blocks, dtype=torch.int32, device=DEV)[None]
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    for size in (1.4e3, 1e4, 1e6, 2e7, 3e7, 1.1e8, 3e9, 1e15, 1e30, 1e37):
+        for sign in (-1.0, 1.0):
+            k = torch.zeros(blocks * 16, d, device=DEV)
+            k[:, 1] = 16.0 * torch.where(third, 1.0, 1.5 if sign < 0 else 0.5)
+            k = (k.view(blocks, 1, 16, d) / ks[:, :, None, None]).to(torch.float8_e4m3fn)
+            q = torch.zeros(tokens, 2, d, dtype=torch.bfloat16, device=DEV)
+            q[..., 1] = sign * min(size / 16, 3e36)
+            n = min(tokens, length)
+            scale = size / (float(q[0, 0, 1].abs()) * 16.0)
+            got = S.kv_attention(q, k, codes, table, i32(0, tokens), i32(length), tokens, length, scale=scale, k_scale=ks, v_scale=vs)
+            off = (got[tokens - n:].double() - mean[length - n:, None]).abs()
+            weights = 2 * (2.0 ** -11 + 2.0 ** -21 + (2.0 ** -13 if size < 2048 else 0.0)) + length * 2.0 ** -23
+            bound = 2.0 ** -8 * mean[length - n:, None].abs() + weights * size_of[length - n:, None] * 1.01
+            assert (off <= bound).all(), (size, sign, float((off / bound).max()))
