@@ -759,19 +759,23 @@ def _refuse_caches(k_cache, v_cache):
                (v_cache.dtype is k_cache.dtype and v_cache.shape == k_cache.shape, "v_cache must have k_cache's type and shape"))
 
 
-def _is_scales(t):
-    """A tensor that is no number: one of a single element is, but for two dimensions."""
+def _of_blocks(k_scale, v_scale, k_cache):
+    """Whether scales are meant to be of blocks: a tensor of one element is a number, unless the cache has one block and one
+    head and both are what its scales are."""
     import torch
-    return isinstance(t, torch.Tensor) and (t.numel() != 1 or t.dim() == 2)
+    tensors = [t for t in (k_scale, v_scale) if isinstance(t, torch.Tensor)]
+    if any(t.numel() != 1 for t in tensors):
+        return True
+    return (len(tensors) == 2 and all(t.dim() == 2 and t.is_cuda and t.dtype is torch.float32 for t in tensors)
+            and _kv_types[k_cache.dtype] == KV_F8 and tuple(k_cache.shape[:2]) == (1, 1))
 
 
 def _refuse_scales(k_scale, v_scale, k_cache):
     """Scales of every block and head, or numbers."""
     import torch
-    both = [_is_scales(t) for t in (k_scale, v_scale)]
-    _kv_refuse((both[0] == both[1], "k_scale and v_scale must both be numbers or both be tensors"))
-    if not all(both):
+    if not _of_blocks(k_scale, v_scale, k_cache):
         return
+    _kv_refuse((all(isinstance(t, torch.Tensor) for t in (k_scale, v_scale)), "k_scale and v_scale must both be numbers or both be tensors"))
     _kv_refuse((_kv_types[k_cache.dtype] == KV_F8, "scales of blocks need a float8_e4m3fn cache"))
     for t, name in ((k_scale, "k_scale"), (v_scale, "v_scale")):
         _kv_refuse((t.is_cuda, f"{name} must be a device tensor"), (t.dtype is torch.float32, f"{name} must be float32"),
@@ -984,7 +988,8 @@ def kv_append(k, v, positions, slots, k_cache, v_cache, rotary=None, k_scale=1.0
             if out is not None:
                 _refuse_vectors(out, "out", q.shape[1], dim)
                 _kv_refuse((out.dtype is q.dtype and out.shape == q.shape, "out must have q's type and shape"))
-        _refuse_mixed(k, **{n: t for n, t in (("k_scale", k_scale), ("v_scale", v_scale)) if _is_scales(t)})
+        if _of_blocks(k_scale, v_scale, k_cache):
+            _refuse_mixed(k, k_scale=k_scale, v_scale=v_scale)
         raise ValueError("kv_append takes tensors")
     if q is None or out is not None or isinstance(got, int):
         if got:
@@ -1001,10 +1006,11 @@ def kv_attention(q, k_cache, v_cache, block_table, query_start, seq_len, max_new
     query sees what stands up to its own position (the last ``window`` of
     these, if given).  ``max_new_len`` and ``max_seq_len``: the longest request
     of the step as the caller knows it; ``scale`` defaults to head_dim ** -0.5.
-    ``k_scale`` and ``v_scale``: numbers, or, over a float8_e4m3fn cache,
-    float32 tensors (blocks, kv_heads), a scale for every block and head as
-    kv_append keeps them (scoot_kv_attention_scaled).  A ``workspace`` (uint8, at least kv_attention_workspace's bytes) may be
-    kept between calls.  Returns ``out``, made if not given; no gradient is
+    ``k_scale`` and ``v_scale``: numbers (tensors of one element, too), or, over
+    a float8_e4m3fn cache, float32 tensors (blocks, kv_heads), a scale for every
+    block and head as kv_append keeps them (scoot_kv_attention_scaled).  A
+    ``workspace`` (uint8, at least kv_attention_workspace's bytes) may be kept
+    between calls.  Returns ``out``, made if not given; no gradient is
     defined over a cache that is written in place, and it has none."""
     _kv or _kv_setup()
     args = (q, k_cache, v_cache, block_table, query_start, seq_len, max_new_len, max_seq_len, scale, window, k_scale, v_scale,
@@ -1024,7 +1030,8 @@ def kv_attention(q, k_cache, v_cache, block_table, query_start, seq_len, max_new
         _refuse_mixed(q, k_cache=k_cache, v_cache=v_cache, seq_len=seq_len, query_start=query_start, block_table=block_table,
                       out=out, workspace=workspace)
         _refuse_scales(k_scale, v_scale, k_cache)
-        _refuse_mixed(q, **{n: t for n, t in (("k_scale", k_scale), ("v_scale", v_scale)) if _is_scales(t)})
+        if _of_blocks(k_scale, v_scale, k_cache):
+            _refuse_mixed(q, k_scale=k_scale, v_scale=v_scale)
         if out is not None:
             _refuse_vectors(out, "out", q.shape[1], dim)
             _kv_refuse((out.dtype is q.dtype and out.shape == q.shape, "out must have q's type and shape"))

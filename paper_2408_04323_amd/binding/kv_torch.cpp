@@ -83,11 +83,20 @@ bool are_scales(PyObject* k, PyObject* v, const at::Tensor& cache) {
   }
   return type_of(cache) == kF8;
 }
-// A tensor that is no number: one of a single element is, but for two dimensions.
-bool is_scales(PyObject* o) {
-  if (!THPVariable_Check(o)) return false;
-  const at::Tensor& t = THPVariable_Unpack(o);
-  return t.numel() != 1 || t.dim() == 2;
+// Whether scales are meant to be of blocks: a tensor of one element is a number, unless the cache has one block and one head and
+// both are what its scales are.
+bool of_blocks(PyObject* k, PyObject* v, const at::Tensor& cache) {
+  bool one = type_of(cache) == kF8 && cache.size(0) == 1 && cache.size(1) == 1;
+  for (PyObject* o : {k, v}) {
+    if (!THPVariable_Check(o)) {
+      one = false;
+      continue;
+    }
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (t.numel() != 1) return true;
+    one = one && t.dim() == 2 && t.is_cuda() && t.scalar_type() == at::kFloat;
+  }
+  return one;
 }
 
 bool with(const at::Tensor& t, std::initializer_list<const at::Tensor*> others) {
@@ -325,7 +334,7 @@ PyObject* append(PyObject*, PyObject* const* args, Py_ssize_t n) {
         Py_RETURN_NONE;
     }
   }
-  const bool scaled = is_scales(args[9]) || is_scales(args[10]);
+  const bool scaled = of_blocks(args[9], args[10], kc);
   if (scaled && !are_scales(args[9], args[10], kc)) Py_RETURN_NONE;
   double magnitude;
   int64_t interleaved;
@@ -374,7 +383,7 @@ PyObject* attention(PyObject*, PyObject* const* args, Py_ssize_t n) {
   int64_t max_new, max_seq, window;
   float scale = (float)(1.0 / std::sqrt((double)std::max<int64_t>(dim, 1))), ks = 1.0f, vs = 1.0f;
   void* stream;
-  const bool scaled = is_scales(args[10]) || is_scales(args[11]);
+  const bool scaled = of_blocks(args[10], args[11], kc);
   if (scaled && !are_scales(args[10], args[11], kc)) Py_RETURN_NONE;
   if (!get(args[6], max_new) || !get(args[7], max_seq) || (args[8] != Py_None && !get(args[8], scale)) || !get(args[9], window) ||
       (!scaled && (!get(args[10], ks) || !get(args[11], vs))) || !get_stream(args[14], q, stream))
