@@ -73,7 +73,9 @@ struct Quotient {
 // A thread's unit: two pieces of N elements of a vector (N = 8, or 1 where rows or pairs are not aligned to that), such
 // that pairs lie within the unit.  Neighbouring threads have neighbouring pieces, first and second ones, so that each load
 // and store takes whole lines: halves pair piece u with that half of the turned elements later, neighbours (of which a
-// piece of eight holds four) and elements that stay with that half of theirs later.
+// piece of eight holds four) and elements that stay with that half of theirs later.  Single elements take twice the time:
+// 8192 tokens of 32 heads of 96, 24 turned, as halves 34.8 us (2.9 TB/s), as neighbours, whose pairs are in pieces of eight,
+// 17.2 (5.8).
 template <typename T, int N, bool IL>
 struct Unit {
   typedef typename std::conditional<N == 8, typename Vec8<T>::type, T>::type Raw;
@@ -582,10 +584,20 @@ int append_launch(const KvAppendArgs& a, bool f8, hipStream_t s) {
   if (blocks) {
     p.runs.units = Unit<T, N, IL>::count(a.head_dim, a.turned);
     p.runs.lanes = std::min(64, power_of_two(p.runs.units));
+    // As many tokens as a block has, so that one workgroup has all of a block's heads at hand; 32 where workgroups abound and
+    // cosines are made for a block's tokens only once more: in us, with blocks of 8, 15 + 2 * 5 heads of 64, 8192 tokens 15.1
+    // (14.3 with 32), 16,384 26.2 (22.9), 32,767 48.4 (39.4); 32 + 2 * 8 of 128 37.3 (36.9), 90.9 (87.9), 175 (161); blocks of 16,
+    // 16 + 2 * 16 of 128 33.9 (35.0), 80.0 (80.0), 24,576 128 (133), 32,767 157 (157).  Eight with blocks of 32 take 1.5 times as
+    // long, and 32 with single tokens in blocks of 16 of one head 1.7 times.
     p.runs.tokens = a.num_tokens >= 32768 ? 32 : std::min(std::max(1 << a.block_shift, 8), 32);
     const auto bytes = [&] { return kTops + ((int64_t)p.runs.tokens + (1 << a.block_shift) - 1) * pairs * 8; };
     while (p.runs.tokens > 1 && bytes() > kLdsBytes) p.runs.tokens /= 2;
-    // Items of a chunk of single tokens, and of one of whole blocks, for the waves.
+    // Workgroups that share a chunk's heads: until there are 1024, but each with items for all waves, whose number depends on
+    // whether the chunk is single tokens or whole blocks: enough for either with few tokens, for both with many.  In us, with
+    // as many as either allows (and both): 15 + 2 * 5 heads of 64, blocks of 8, 64 tokens 5.9 (7.9), 1024 6.3 (8.3), 3000 8.3
+    // (9.8); 32 + 2 * 8 of 128, blocks of 16, 1024 9.1 (9.9), 2048 12.4 (11.0), 3000 16.8 (15.7); of 32, 1024 11.7 (12.6), 2048
+    // 17.8 (14.4), 3000 20.0 (15.9); single tokens, blocks of 32, 1024 8.6 (14.4), 2048 13.4 (15.8).  512, 1024, 2048
+    // workgroups: 2049 tokens into blocks of 8 17.7, 13.6, 13.4; 4096 19.9, 21.0, 23.5; 8192 of 15 + 2 * 5 heads 14.3, 14.7, 17.4.
     const int singles = p.runs.tokens * 2 * a.num_kv_heads * p.runs.lanes / kThreads;
     const int whole = std::max(1, p.runs.tokens >> a.block_shift) * 2 * a.num_kv_heads / (kThreads / 64);
     const int most = std::max(1, a.num_tokens <= 2048 ? std::max(singles, whole) : std::min(singles, whole));

@@ -52,7 +52,7 @@
 // without scales, and there are two products and a second exponential: 48 requests
 // of up to 32,767 keys 299 -> 595 us, late chunks over 30,000 keys 339 -> 779 (heads of
 // 64), 525 -> 1015 (128).  That it is there costs the others registers: those late
-// chunks 0.5% and nothing, of 192 and 256 1.3% and 2.8%, single tokens over 1000 keys
+// chunks up to 1% and nothing, of 192 and 256 up to 1.3% and 3.6%, single tokens over 1000 keys
 // 0.2 us of 10.7.
 // The scales of 64 strips at a time go straight from memory into LDS, where
 // their addresses are made (through registers: 40 more, and a wave per SIMD less
