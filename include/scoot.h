@@ -810,7 +810,7 @@ int scoot_kv_append(const void* q, int num_heads, int64_t q_token_stride, int64_
  * does not see.  Weights are rounded to half precision (off by 1.2 * 2^-11 of a
  * weight, or 2^-31 of the row's largest), or, where a request's blocks have scales
  * of values that are more than 2^15 apart or scores pass 1400, to 16 bits, products
- * down to 2^-200 of the largest among them; these requests take up to 2.4 times as
+ * down to 2^-200 of the largest among them; these requests take up to 2.8 times as
  * long.  The workspace is
  * scoot_kv_attention_workspace's. */
 int scoot_kv_attention_scaled(const void* q, scoot_kv_type type, int64_t num_tokens, int num_heads, int num_kv_heads,

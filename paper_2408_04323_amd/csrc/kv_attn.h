@@ -52,8 +52,7 @@
 // without scales, and there are two products and a second exponential: 48 requests
 // of up to 32,767 keys 299 -> 595 us, late chunks over 30,000 keys 339 -> 779 (heads of
 // 64), 525 -> 1015 (128).  That it is there costs the others registers: those late
-// chunks up to 1% and nothing, of 192 and 256 up to 1.3% and 3.6%, single tokens over 1000 keys
-// 0.2 us of 10.7.
+// chunks up to 1%, of 192 1.3%, of 256 0.9%, single tokens over 1000 keys 0.2 us of 10.7.
 // The scales of 64 strips at a time go straight from memory into LDS, where
 // their addresses are made (through registers: 40 more, and a wave per SIMD less
 // for few rows of 64 dimensions).  Tiles make of them, once for 64 strips, what
@@ -1236,7 +1235,9 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
 
   // Before the first of 64 strips: their scales have landed and become what the strips take, and the reference is up to
   // them.  Every wave does that for the groups of eight keys whose scales it fetched, a lane for a strip.  Not for a wide
-  // pass: false if the exponents of the tile are too far apart for half precision.
+  // pass: false if the exponents of the tile are too far apart for half precision.  The pass then ends there, but for heads
+  // of 256, whose registers that costs (late chunks over 30,000 keys 803 -> 826 us).
+  constexpr bool kEnds = S::D < 256;
   int least = 255;
   const auto prepare = [&](int strip, auto wide) {
     constexpr bool kWide = decltype(wide)::value;
@@ -1263,7 +1264,7 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
       all = uniform(most_of_waves<kWaves>(Workgroup{}, flag, all));
       w.refer(all & 0xffff);
       least = min(least, 255 - (all >> 16));
-      if (w.ref - least > kBelowReference) return false;
+      if (kEnds && w.ref - least > kBelowReference) return false;
     }
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -1272,7 +1273,7 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
       *in_lds(2, j) = kWide ? fraction(b[j]) : __builtin_amdgcn_logf(fraction(b[j]));
     }
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    return true;
+    return kWide || w.ref - least <= kBelowReference;
   };
   auto turn = [&](int strip) {
     // This strip has landed, for every wave, and everyone is done with the one before, whose place the next load takes.
@@ -1290,7 +1291,7 @@ __device__ __forceinline__ void shared_tile(const KvAttnArgs& a, const Item& it,
       if constexpr (S::SCALED) {
         if ((strip & 63) == 0 && !prepare(strip, again)) {
           early = true;
-          break;
+          if constexpr (kEnds) break;
         }
       }
       const int scaled = strip | 63;  // the last strip whose scales are there
